@@ -550,6 +550,95 @@ int32_t hb_meta_query_attn_project(int32_t S, int32_t L, int32_t D, int32_t H, i
                                    void *pre, void *residual_out_or_null, void *workspace, size_t workspace_bytes,
                                    void *stream);
 
+/*
+ * ---- 4-bit KV cache ----------------------------------------------------------------------------
+ * The paged cache of hb_tree_verify_attn and hb_kv_compact with K and V in 4 bits: 17/64 of bf16's bytes.
+ * A row (one position of one head) is D elements of E2M1 (sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6) in blocks of 32, each with a scale byte s worth 2^(s - 127); s = 255: the block is NaN.
+ *   codes   device uint8 [num_blocks, Hkv, page, D / 2]    byte i of a row: element 2i in the low half, 2i + 1 in the high
+ *   scales  device uint8 [num_blocks, Hkv, page, D / 32]
+ * for K and for V, 16-byte aligned.  D is a multiple of 32.  A block of 32 numbers is written under the smallest power of two
+ * s that brings its largest magnitude to 7 s or less (bytes 1 to 252), each rounded to the nearest element, ties to the even
+ * code, above 6 s to 6 s; a block that holds an infinity or NaN becomes NaN.  Reads give what the codes stand for,
+ * exact in bf16.
+ * Where a call takes weight (float32) and pos (int32), both device [B, Hkv, max_blocks_per_seq * page_size]: the attention
+ * weight that the position in a slot has gathered, and its position in the sequence.  After evictions the heads of a sequence
+ * hold different positions, all of them prefix_len[b]; seq_len[b] is the number of positions that there have been.
+ *
+ * hb_kv4_append: rows row_offset[b] .. row_offset[b+1] - 1 of k_rows and v_rows (a prompt, or part of one) to positions
+ * prefix_len[b], prefix_len[b] + 1, ... of sequence b; new_len[b] = prefix_len[b] + their number.
+ * hb_kv4_compact: the same for the nodes of an accepted path, as hb_kv_compact, out_slots included.
+ * Both set weight to 0 and pos to seq_len[b] + j (prefix_len[b] + j where seq_len is NULL) for row j of the call.
+ * Positions beyond max_blocks_per_seq * page_size are skipped; no other byte changes.
+ * hb_kv4_read: row r of sequence b (row_offset as above) = position first[b] + r - row_offset[b] as the cache holds it; zero
+ * where the table has no such position.
+ *   k_rows, v_rows  device [n_rows, Hkv, D]  desc->dtype      row_offset, first, seq_len  device int32
+ * seq_len, weight, pos, out_slots and new_len may be NULL.
+ * Uses desc->{dtype, batch, num_q_heads, num_kv_heads, head_dim, page_size, max_blocks_per_seq, num_blocks, total_nodes}.
+ * Errors: INVALID_ARG, UNSUPPORTED (also: D % 32, more rows than one launch takes), DEVICE.  Nothing to do is a success.
+ */
+int32_t hb_kv4_append(const hb_attn_desc *desc, int32_t n_rows, const void *k_rows, const void *v_rows, void *k_codes,
+                      void *k_scales, void *v_codes, void *v_scales, const int32_t *block_table, const int32_t *prefix_len,
+                      const int32_t *row_offset, const int32_t *seq_len_or_null, float *weight_or_null, int32_t *pos_or_null,
+                      int32_t *new_len_or_null, void *stream);
+
+int32_t hb_kv4_compact(const hb_attn_desc *desc, const void *k_tree, const void *v_tree, void *k_codes, void *k_scales,
+                       void *v_codes, void *v_scales, const int32_t *block_table, const int32_t *prefix_len,
+                       const int32_t *node_offset, const int32_t *accept_len, const int32_t *accept_path, int32_t max_path,
+                       const int32_t *seq_len_or_null, float *weight_or_null, int32_t *pos_or_null, int32_t *out_slots_or_null,
+                       int32_t *new_len_or_null, void *stream);
+
+int32_t hb_kv4_read(const hb_attn_desc *desc, int32_t n_rows, const void *k_codes, const void *k_scales, const void *v_codes,
+                    const void *v_scales, const int32_t *block_table, const int32_t *first, const int32_t *row_offset,
+                    void *k_rows, void *v_rows, void *stream);
+
+/*
+ * hb_tree_verify_attn with the prefix in a 4-bit cache; the nodes' own K and V (k_tree, v_tree) are as they are there, in
+ * desc->dtype.  Arguments, masks and errors as in hb_tree_verify_attn, and UNSUPPORTED for D % 32.
+ */
+int32_t hb_tree_verify_attn_kv4(const hb_attn_desc *desc, const void *q, const void *k_tree, const void *v_tree,
+                                const void *k_codes, const void *k_scales, const void *v_codes, const void *v_scales,
+                                const int32_t *block_table, const int32_t *prefix_len, const int32_t *node_offset,
+                                const int32_t *parent, void *out, float *lse_or_null, void *workspace, size_t workspace_bytes,
+                                void *stream);
+
+size_t hb_tree_verify_attn_kv4_workspace_bytes(const hb_attn_desc *desc);
+
+int32_t hb_tree_verify_attn_kv4_num_splits(const hb_attn_desc *desc);
+
+/*
+ * Attention weight that the cached positions received from committed nodes, added to what they have:
+ *   weight[b][g][p] = decay * weight[b][g][p] + sum over nodes i and query heads h of group g of
+ *                     exp(softmax_scale * <q[i,h], k_p> - lse[i,h])            for p < prefix_len[b]
+ * with q and lse as hb_tree_verify_attn_kv4 took and gave them.  Nodes: accept_path[b][0 .. accept_len[b] - 1]
+ * (accept_path device int32 [B, max_path], from hb_tree_accept), or all of a sequence's where both are NULL.  A sequence
+ * without such nodes keeps decay * weight.  Sums are in float32.
+ * Errors: INVALID_ARG (also: decay outside [0, 1]), UNSUPPORTED, DEVICE.
+ */
+int32_t hb_kv4_attn_weight(const hb_attn_desc *desc, const void *q, const void *k_codes, const void *k_scales,
+                           const int32_t *block_table, const int32_t *prefix_len, const int32_t *node_offset,
+                           const int32_t *accept_len_or_null, const int32_t *accept_path_or_null, int32_t max_path,
+                           const float *lse, float decay, float *weight, void *stream);
+
+/*
+ * Eviction: of the prefix_len[b] positions that head g of sequence b holds, new_len[b] = min(prefix_len[b], budget) stay:
+ * those with pos >= seq_len[b] - recent or pos < sinks (recent + sinks <= budget), then those of the largest weight, the
+ * lower slot among equals (NaN counts as -infinity).  What stays in a slot below new_len keeps it; the others, in the order of
+ * their slots, take the slots below new_len that come free, in order.
+ *   kept        device int32 [B, Hkv, budget]  the slot whose position is now in slot i, -1 for i >= new_len[b]
+ *   weight_out, pos_out  as weight and pos, which they may be: slots below new_len are written, no others
+ *   workspace   device, hb_kv4_evict_workspace_bytes(desc, budget) bytes, 256-byte aligned
+ * Pages behind new_len are free afterwards.  Pages must not be shared between sequences.  new_len may be NULL
+ * and must not overlap prefix_len.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, DEVICE.
+ */
+int32_t hb_kv4_evict(const hb_attn_desc *desc, int32_t budget, int32_t recent, int32_t sinks, void *k_codes, void *k_scales,
+                     void *v_codes, void *v_scales, const int32_t *block_table, const int32_t *prefix_len, const int32_t *seq_len,
+                     const float *weight, const int32_t *pos, float *weight_out, int32_t *pos_out, int32_t *kept,
+                     int32_t *new_len_or_null, void *workspace, size_t workspace_bytes, void *stream);
+
+size_t hb_kv4_evict_workspace_bytes(const hb_attn_desc *desc, int32_t budget);
+
 #ifdef __cplusplus
 }
 #endif

@@ -127,6 +127,24 @@ def _load():
     for call in (lib.hb_lmhead_accept, lib.hb_lmhead_accept_cleared):
         call.restype = i32
         call.argtypes = [C.POINTER(AttnDesc)] + [i32] * 3 + [p] * 5 + [i32] + [p] * 6 + [sz, i32, i32] + [p] * 9
+    lib.hb_kv4_append.restype = i32
+    lib.hb_kv4_append.argtypes = [C.POINTER(AttnDesc), i32] + [p] * 14
+    lib.hb_kv4_compact.restype = i32
+    lib.hb_kv4_compact.argtypes = [C.POINTER(AttnDesc)] + [p] * 11 + [i32] + [p] * 6
+    lib.hb_kv4_read.restype = i32
+    lib.hb_kv4_read.argtypes = [C.POINTER(AttnDesc), i32] + [p] * 10
+    lib.hb_tree_verify_attn_kv4.restype = i32
+    lib.hb_tree_verify_attn_kv4.argtypes = [C.POINTER(AttnDesc)] + [p] * 13 + [p, sz, p]
+    lib.hb_tree_verify_attn_kv4_workspace_bytes.restype = sz
+    lib.hb_tree_verify_attn_kv4_workspace_bytes.argtypes = [C.POINTER(AttnDesc)]
+    lib.hb_tree_verify_attn_kv4_num_splits.restype = i32
+    lib.hb_tree_verify_attn_kv4_num_splits.argtypes = [C.POINTER(AttnDesc)]
+    lib.hb_kv4_attn_weight.restype = i32
+    lib.hb_kv4_attn_weight.argtypes = [C.POINTER(AttnDesc)] + [p] * 8 + [i32, p, C.c_float, p, p]
+    lib.hb_kv4_evict.restype = i32
+    lib.hb_kv4_evict.argtypes = [C.POINTER(AttnDesc), i32, i32, i32] + [p] * 14 + [sz, p]
+    lib.hb_kv4_evict_workspace_bytes.restype = sz
+    lib.hb_kv4_evict_workspace_bytes.argtypes = [C.POINTER(AttnDesc), i32]
     return lib
 
 
@@ -492,3 +510,112 @@ def _lmhead_accept(call):
 hb_lmhead_accept = _lmhead_accept(lib.hb_lmhead_accept)
 # for keys that hb_tree_verify_attn_clearing has set to zero
 hb_lmhead_accept_cleared = _lmhead_accept(lib.hb_lmhead_accept_cleared)
+
+
+def _kv4_rows(desc: AttnDesc, k_rows, v_rows) -> int:
+    n = k_rows.shape[0]
+    if k_rows.shape != (n, desc.num_kv_heads, desc.head_dim) or v_rows.shape != k_rows.shape:
+        raise ValueError("rows must be [n, Hkv, D], K and V alike")
+    if _dtype_code(k_rows) != desc.dtype or v_rows.dtype != k_rows.dtype:
+        raise ValueError("rows must have the descriptor's dtype")
+    return n
+
+
+def _kv4_pool(desc: AttnDesc, *pool) -> None:
+    """Codes and scales in turn."""
+    if any(t.dtype != torch.uint8 for t in pool):
+        raise ValueError("codes and scales are uint8 tensors")
+    lead = (desc.num_blocks, desc.num_kv_heads, desc.page_size)
+    if any(t.shape != lead + (desc.head_dim // (32 if i % 2 else 2),) for i, t in enumerate(pool)):
+        raise ValueError("codes must be [num_blocks, Hkv, page, D / 2], scales [num_blocks, Hkv, page, D / 32]")
+
+
+def _kv4_slots(desc: AttnDesc, weight, pos) -> None:
+    shape = (desc.batch, desc.num_kv_heads, desc.max_blocks_per_seq * desc.page_size)
+    for t, dtype in ((weight, torch.float32), (pos, torch.int32)):
+        if t is not None and (t.dtype != dtype or t.shape != shape):
+            raise ValueError("weight (float32) and pos (int32) must be [B, Hkv, max_blocks * page]")
+
+
+def _kv4_ints(*tensors) -> None:
+    if any(t is not None and t.dtype != torch.int32 for t in tensors):
+        raise ValueError("lengths, offsets, positions, paths and tables are int32 tensors")
+
+
+def hb_kv4_append(desc: AttnDesc, k_rows, v_rows, k_codes, k_scales, v_codes, v_scales, block_table, prefix_len, row_offset,
+                  seq_len=None, weight=None, pos=None, new_len=None, stream=None) -> None:
+    n = _kv4_rows(desc, k_rows, v_rows)
+    _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
+    _kv4_slots(desc, weight, pos)
+    _kv4_ints(block_table, prefix_len, row_offset, seq_len, new_len)
+    _check(lib.hb_kv4_append(C.byref(desc), n, _ptr(k_rows), _ptr(v_rows), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes),
+                             _ptr(v_scales), _ptr(block_table), _ptr(prefix_len), _ptr(row_offset), _ptr(seq_len), _ptr(weight),
+                             _ptr(pos), _ptr(new_len), _stream(stream)))
+
+
+def hb_kv4_compact(desc: AttnDesc, k_tree, v_tree, k_codes, k_scales, v_codes, v_scales, block_table, prefix_len, node_offset,
+                   accept_len, accept_path, max_path: int, seq_len=None, weight=None, pos=None, out_slots=None, new_len=None,
+                   stream=None) -> None:
+    if _kv4_rows(desc, k_tree, v_tree) != desc.total_nodes:
+        raise ValueError("rows must be [total_nodes, Hkv, D]")
+    _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
+    _kv4_slots(desc, weight, pos)
+    _kv4_ints(block_table, prefix_len, node_offset, accept_len, accept_path, seq_len, out_slots, new_len)
+    _check(lib.hb_kv4_compact(C.byref(desc), _ptr(k_tree), _ptr(v_tree), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes),
+                              _ptr(v_scales), _ptr(block_table), _ptr(prefix_len), _ptr(node_offset), _ptr(accept_len),
+                              _ptr(accept_path), max_path, _ptr(seq_len), _ptr(weight), _ptr(pos), _ptr(out_slots),
+                              _ptr(new_len), _stream(stream)))
+
+
+def hb_kv4_read(desc: AttnDesc, k_codes, k_scales, v_codes, v_scales, block_table, first, row_offset, k_rows, v_rows,
+                stream=None) -> None:
+    n = _kv4_rows(desc, k_rows, v_rows)
+    _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
+    _kv4_ints(block_table, first, row_offset)
+    _check(lib.hb_kv4_read(C.byref(desc), n, _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(block_table),
+                           _ptr(first), _ptr(row_offset), _ptr(k_rows), _ptr(v_rows), _stream(stream)))
+
+
+def hb_tree_verify_attn_kv4_workspace_bytes(desc: AttnDesc) -> int:
+    return int(lib.hb_tree_verify_attn_kv4_workspace_bytes(C.byref(desc)))
+
+
+def hb_tree_verify_attn_kv4_num_splits(desc: AttnDesc) -> int:
+    return int(lib.hb_tree_verify_attn_kv4_num_splits(C.byref(desc)))
+
+
+def hb_tree_verify_attn_kv4(desc: AttnDesc, q, k_tree, v_tree, k_codes, k_scales, v_codes, v_scales, block_table, prefix_len,
+                            node_offset, parent, out, lse=None, workspace=None, stream=None) -> None:
+    _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(lib.hb_tree_verify_attn_kv4(C.byref(desc), _ptr(q), _ptr(k_tree), _ptr(v_tree), _ptr(k_codes), _ptr(k_scales),
+                                       _ptr(v_codes), _ptr(v_scales), _ptr(block_table), _ptr(prefix_len), _ptr(node_offset),
+                                       _ptr(parent), _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def hb_kv4_attn_weight(desc: AttnDesc, q, k_codes, k_scales, block_table, prefix_len, node_offset, accept_len, accept_path,
+                       max_path: int, lse, decay: float, weight, stream=None) -> None:
+    _kv4_pool(desc, k_codes, k_scales)
+    _kv4_slots(desc, weight, None)
+    _kv4_ints(block_table, prefix_len, node_offset, accept_len, accept_path)
+    _check(lib.hb_kv4_attn_weight(C.byref(desc), _ptr(q), _ptr(k_codes), _ptr(k_scales), _ptr(block_table), _ptr(prefix_len),
+                                  _ptr(node_offset), _ptr(accept_len), _ptr(accept_path), max_path, _ptr(lse), decay,
+                                  _ptr(weight), _stream(stream)))
+
+
+def hb_kv4_evict_workspace_bytes(desc: AttnDesc, budget: int) -> int:
+    return int(lib.hb_kv4_evict_workspace_bytes(C.byref(desc), budget))
+
+
+def hb_kv4_evict(desc: AttnDesc, budget: int, recent: int, sinks: int, k_codes, k_scales, v_codes, v_scales, block_table,
+                 prefix_len, seq_len, weight, pos, weight_out, pos_out, kept, new_len, workspace, stream=None) -> None:
+    _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
+    _kv4_slots(desc, weight, pos)
+    _kv4_slots(desc, weight_out, pos_out)
+    _kv4_ints(block_table, prefix_len, seq_len, kept, new_len)
+    if kept.shape != (desc.batch, desc.num_kv_heads, budget):
+        raise ValueError("kept must be [B, Hkv, budget]")
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(lib.hb_kv4_evict(C.byref(desc), budget, recent, sinks, _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales),
+                            _ptr(block_table), _ptr(prefix_len), _ptr(seq_len), _ptr(weight), _ptr(pos), _ptr(weight_out),
+                            _ptr(pos_out), _ptr(kept), _ptr(new_len), _ptr(workspace), ws_bytes, _stream(stream)))

@@ -77,6 +77,8 @@ static int32_t check_shape(const hb_attn_desc *d) {
   return HB_OK;
 }
 
+int32_t check_attn_desc(const hb_attn_desc *d) { return check_shape(d); }
+
 int32_t make_attn_plan(const hb_attn_desc *d, AttnPlan *plan) {
   int32_t rc = check_shape(d);
   if (rc) return rc;

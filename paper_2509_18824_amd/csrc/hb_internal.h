@@ -227,6 +227,36 @@ struct TailArgs {
 };
 hipError_t launch_verify_tail(const hb_attn_desc &d, TailArgs t, hipStream_t s);
 
+// ---- 4-bit cache (kv4_*.hip) ---------------------------------------------------------------
+struct Kv4Pool;
+int32_t check_attn_desc(const hb_attn_desc *d);  // the fields that every call over a paged cache reads
+struct Kv4AppendArgs {
+  hb_attn_desc d;
+  int32_t rows;      // destination rows: of all sequences, or max_path for each
+  int32_t src_rows;  // rows of k and v
+  int32_t max_path;
+  const void *k, *v;
+  uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+  const int32_t *block_table, *prefix_len, *row_offset, *accept_len, *accept_path, *seq_len;  // the last three may be null
+  float *weight;      // may be null, as all below
+  int32_t *pos, *out_slots, *new_len;
+};
+hipError_t launch_kv4_append(const Kv4AppendArgs &a, hipStream_t s);
+hipError_t launch_kv4_read(const hb_attn_desc &d, int32_t rows, const Kv4Pool &k, const Kv4Pool &v, const int32_t *block_table,
+                           const int32_t *first, const int32_t *row_offset, void *k_rows, void *v_rows, hipStream_t s);
+struct Kv4EvictArgs {
+  hb_attn_desc d;
+  int32_t budget, recent, sinks;
+  uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+  const int32_t *block_table, *prefix_len, *seq_len;
+  const float *weight;
+  const int32_t *pos;
+  float *weight_out;
+  int32_t *pos_out, *kept, *new_len;
+  int32_t *moves, *counts;  // workspace: [unit][2][budget], [unit]
+};
+hipError_t launch_kv4_evict(const Kv4EvictArgs &a, hipStream_t s);
+
 // ---- argmax key: (order-preserving float bits << 32) | (0xffffffff - index) ---------------
 // max over keys = largest value, lowest index among equal values.  NaN is mapped to -inf.
 __device__ inline unsigned long long argmax_key(float v, uint32_t idx) {

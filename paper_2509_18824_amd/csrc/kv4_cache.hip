@@ -1,0 +1,294 @@
+// Rows into and out of the 4-bit cache, and the eviction of positions from it.
+#include "kv4.h"
+
+namespace hb {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// eight elements of a row as float32
+__device__ inline void load8(const float *p, float (&x)[8]) {
+  const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] = a[e];
+    x[4 + e] = b[e];
+  }
+}
+__device__ inline void load8(const bf16_t *p, float (&x)[8]) {
+  const u32x4 a = *(const u32x4 *)p;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[2 * e] = __uint_as_float(a[e] << 16);
+    x[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
+  }
+}
+__device__ inline void store8(float *p, const float (&x)[8]) {
+  *(f32x4 *)p = (f32x4){x[0], x[1], x[2], x[3]};
+  *(f32x4 *)(p + 4) = (f32x4){x[4], x[5], x[6], x[7]};
+}
+__device__ inline void store8(bf16_t *p, const float (&x)[8]) {
+  *(u32x4 *)p = (u32x4){pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+}
+
+// Quantises rows into the pages.  A thread takes eight elements, four threads a block of 32: its largest
+// magnitude is two exchanges away.  Threads run over the pieces of a head's row, then over rows, then over heads:
+// neighbouring rows of a head are neighbours in a page.  PATH: the rows that a path names, max_path to a sequence.
+template <typename T, bool PATH>
+__global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
+  const hb_attn_desc &d = a.d;
+  const long gid = (long)blockIdx.x * 256 + threadIdx.x;
+  if (blockIdx.y == 0) {
+    for (long b = gid; a.new_len && b < d.batch; b += (long)gridDim.x * 256) {
+      int n = PATH ? a.accept_len[b] : a.row_offset[b + 1] - a.row_offset[b];
+      n = n < 0 ? 0 : PATH && n > a.max_path ? a.max_path : n;
+      const int L = a.prefix_len[b];
+      a.new_len[b] = (L < 0 ? 0 : L) + n;
+    }
+  }
+  const int pieces = d.head_dim / 8;
+  const int piece = (int)(gid % pieces);
+  const long item = gid / pieces;
+  if (item >= (long)a.rows * d.num_kv_heads) return;  // pieces is a multiple of four: a block's threads leave together
+  const int r = (int)(item % a.rows), h = (int)(item / a.rows);
+  int b, j, src = r;
+  bool live;
+  if (PATH) {
+    b = r / a.max_path;
+    j = r - b * a.max_path;
+    live = j < a.accept_len[b];
+    const int n0 = a.row_offset[b], n = a.row_offset[b + 1] - n0;
+    int node = live ? a.accept_path[(size_t)b * a.max_path + j] : 0;
+    node = node < 0 ? 0 : (node >= n ? n - 1 : node);
+    src = n0 + node;
+    src = src < 0 ? 0 : (src >= a.src_rows ? a.src_rows - 1 : src);
+  } else {
+    b = kv4_sequence(a.row_offset, d.batch, r);
+    j = r - a.row_offset[b];
+    live = j >= 0 && r < a.row_offset[b + 1];
+  }
+  int L = a.prefix_len[b];
+  L = L < 0 ? 0 : L;
+  const long p = (long)L + j;
+  const bool in_table = live && p < (long)d.max_blocks_per_seq * d.page_size;
+  if (PATH && a.out_slots && h == 0 && piece == 0 && blockIdx.y == 0) {
+    int slot = -1;
+    if (in_table) {
+      const size_t row = kv4_row(d, a.block_table, b, 0, (int)p);
+      slot = (int)(row / ((size_t)d.num_kv_heads * d.page_size)) * d.page_size + (int)(row % d.page_size);
+    }
+    a.out_slots[r] = slot;
+  }
+  if (!in_table) return;
+  const size_t row = kv4_row(d, a.block_table, b, h, (int)p);
+  const T *x_at = (const T *)(blockIdx.y ? a.v : a.k) + ((size_t)src * d.num_kv_heads + h) * d.head_dim + piece * 8;
+  float x[8];
+  load8(x_at, x);
+  uint32_t top = 0;  // magnitudes compare as their bits do, and what is not finite is above the rest
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+  const uint32_t s = kv4_scale_of(top);
+  uint32_t codes = 0;  // to the nearest, ties to even; above 6: 6
+  if (s != kKv4NaN) {
+    const float scale = kv4_scale(s);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], scale, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], scale, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], scale, 3);
+  }
+  uint8_t *to = blockIdx.y ? a.v_codes : a.k_codes, *to_scale = blockIdx.y ? a.v_scales : a.k_scales;
+  *(uint32_t *)(to + row * (d.head_dim / 2) + piece * 4) = codes;
+  if (piece % 4 == 0) to_scale[row * (d.head_dim / kKv4Block) + piece / 4] = (uint8_t)s;
+  if (blockIdx.y == 0 && piece == 0) {
+    const size_t at = ((size_t)b * d.num_kv_heads + h) * d.max_blocks_per_seq * d.page_size + p;
+    if (a.weight) a.weight[at] = 0.f;
+    if (a.pos) a.pos[at] = (a.seq_len ? a.seq_len[b] : L) + j;
+  }
+}
+
+// The other way: rows as the cache holds them; positions that the table does not cover read as zero.
+template <typename T>
+__global__ __launch_bounds__(256) void kv4_read_kernel(hb_attn_desc d, int rows, Kv4Pool kp, Kv4Pool vp,
+                                                       const int32_t *__restrict__ block_table, const int32_t *__restrict__ first,
+                                                       const int32_t *__restrict__ row_offset, T *__restrict__ k, T *__restrict__ v) {
+  const long gid = (long)blockIdx.x * 256 + threadIdx.x;
+  const int pieces = d.head_dim / 8;
+  const int piece = (int)(gid % pieces);
+  const long item = gid / pieces;
+  if (item >= (long)rows * d.num_kv_heads) return;
+  const int r = (int)(item % rows), h = (int)(item / rows);
+  const int b = kv4_sequence(row_offset, d.batch, r);
+  const long p = (long)first[b] + r - row_offset[b];
+  const Kv4Pool &from = blockIdx.y ? vp : kp;
+  float x[8] = {};
+  if (p >= 0 && p < (long)d.max_blocks_per_seq * d.page_size) {
+    const size_t row = kv4_row(d, block_table, b, h, (int)p);
+    const uint32_t c = *(const uint32_t *)(from.codes + row * (d.head_dim / 2) + piece * 4);
+    const float s = kv4_scale(from.scales[row * (d.head_dim / kKv4Block) + piece / 4]);
+    const kv4_f32x2 p0 = kv4_pair<0>(c, s), p1 = kv4_pair<1>(c, s), p2 = kv4_pair<2>(c, s), p3 = kv4_pair<3>(c, s);
+    x[0] = p0[0], x[1] = p0[1], x[2] = p1[0], x[3] = p1[1], x[4] = p2[0], x[5] = p2[1], x[6] = p3[0], x[7] = p3[1];
+  }
+  store8((blockIdx.y ? v : k) + ((size_t)r * d.num_kv_heads + h) * d.head_dim + piece * 8, x);
+}
+
+// ---- eviction ------------------------------------------------------------------------------------------
+// order-preserving bits of a weight; not a number counts as the least, protected positions as the greatest
+__device__ inline uint32_t weight_key(float w, bool safe) {
+  if (safe) w = __builtin_huge_valf();
+  if (!(w == w)) w = -__builtin_huge_valf();
+  if (w == 0.f) w = 0.f;  // -0 weighs what 0 does
+  const uint32_t u = __float_as_uint(w);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+constexpr int kSelectThreads = 1024;
+
+// number of set flags in front of this thread's in the workgroup, and their total
+__device__ inline int block_rank(bool flag, int *waves, int &total) {
+  const unsigned long long m = __ballot(flag);
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  __syncthreads();
+  if (lane == 0) waves[w] = __popcll(m);
+  __syncthreads();
+  int before = 0;
+  total = 0;
+  for (int i = 0; i < kSelectThreads / 64; ++i) {
+    before += i < w ? waves[i] : 0;
+    total += waves[i];
+  }
+  return before + __popcll(m & ((1ull << lane) - 1ull));
+}
+
+// One workgroup per (sequence, head): which positions stay.  The least key that stays is found digit by digit
+// (8 bits, a histogram each); of the positions that have just this key the first ones stay.  Kept positions in front of the
+// new length stay in their slot; the others are listed, and so are the slots that come free in front of it.
+__global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs a) {
+  const hb_attn_desc &d = a.d;
+  __shared__ int hist[256], waves[kSelectThreads / 64];
+  __shared__ uint32_t s_prefix;
+  __shared__ int s_need;
+  const int tid = threadIdx.x, b = blockIdx.x / d.num_kv_heads;
+  const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
+  const int L = kv4_length(d, a.prefix_len, b), stays = L < a.budget ? L : a.budget;
+  const float *w = a.weight + (size_t)blockIdx.x * cap;
+  const int32_t *pos = a.pos + (size_t)blockIdx.x * cap;
+  const int recent_from = a.seq_len[b] - a.recent;
+  auto key = [&](int s) { return weight_key(w[s], pos[s] >= recent_from || pos[s] < a.sinks); };
+  if (tid == 0 && blockIdx.x % d.num_kv_heads == 0 && a.new_len) a.new_len[b] = stays;
+  uint32_t prefix = 0;
+  int need = stays;
+  if (stays < L && stays > 0) {
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      if (tid < 256) hist[tid] = 0;
+      __syncthreads();
+      for (int s = tid; s < L; s += kSelectThreads) {
+        const uint32_t k = key(s);
+        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+      }
+      __syncthreads();
+      if (tid == 0) {
+        int digit = 255, left = need;
+        while (digit > 0 && hist[digit] < left) left -= hist[digit--];
+        s_prefix = prefix | ((uint32_t)digit << shift);
+        s_need = left;
+      }
+      __syncthreads();
+      prefix = s_prefix;
+      need = s_need;
+    }
+  }
+  int32_t *kept = a.kept + (size_t)blockIdx.x * a.budget;
+  int32_t *from = a.moves + (size_t)blockIdx.x * 2 * a.budget, *to = from + a.budget;
+  int ties = 0, free_slots = 0, above = 0;
+  for (int s0 = 0; s0 < L; s0 += kSelectThreads) {
+    const int s = s0 + tid;
+    const uint32_t k = s < L ? key(s) : 0;
+    const bool all = stays == L, in = s < L && stays > 0;
+    const bool tie = in && !all && k == prefix;
+    int total;
+    const int rank = ties + block_rank(tie, waves, total);
+    ties += total;
+    const bool stay = in && (all || k > prefix || (tie && rank < need));
+    const bool frees = s < stays && !stay, moves = s >= stays && stay;
+    const int fr = free_slots + block_rank(frees, waves, total);
+    free_slots += total;
+    const int mr = above + block_rank(moves, waves, total);
+    above += total;
+    if (frees) to[fr] = s;
+    if (moves) from[mr] = s;
+    if (s < stays && stay) {
+      kept[s] = s;
+      a.weight_out[(size_t)blockIdx.x * cap + s] = w[s];
+      a.pos_out[(size_t)blockIdx.x * cap + s] = pos[s];
+    }
+  }
+  for (int s = stays + tid; s < a.budget; s += kSelectThreads) kept[s] = -1;
+  if (tid == 0) a.counts[blockIdx.x] = above;
+}
+
+// A row of K and V to the slot that came free for it: `lanes` lanes a move
+__global__ __launch_bounds__(256) void kv4_move_kernel(Kv4EvictArgs a) {
+  const hb_attn_desc &d = a.d;
+  const int i = (int)blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int unit = blockIdx.y, b = unit / d.num_kv_heads, h = unit % d.num_kv_heads;
+  if (i >= a.counts[unit]) return;
+  const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
+  const int32_t *moves = a.moves + (size_t)unit * 2 * a.budget;
+  const int src = moves[i], dst = moves[a.budget + i];
+  const size_t s = kv4_row(d, a.block_table, b, h, src), t = kv4_row(d, a.block_table, b, h, dst);
+  const int words = d.head_dim / 8, bytes = d.head_dim / kKv4Block;  // words of codes, scale bytes
+  if (lane < words) {
+    ((uint32_t *)a.k_codes)[t * words + lane] = ((const uint32_t *)a.k_codes)[s * words + lane];
+    ((uint32_t *)a.v_codes)[t * words + lane] = ((const uint32_t *)a.v_codes)[s * words + lane];
+  } else if (lane < words + bytes) {
+    a.k_scales[t * bytes + lane - words] = a.k_scales[s * bytes + lane - words];
+    a.v_scales[t * bytes + lane - words] = a.v_scales[s * bytes + lane - words];
+  }
+  if (lane == 63) {
+    a.kept[(size_t)unit * a.budget + dst] = src;
+    a.weight_out[unit * cap + dst] = a.weight[unit * cap + src];
+    a.pos_out[unit * cap + dst] = a.pos[unit * cap + src];
+  }
+}
+
+}  // namespace
+
+hipError_t launch_kv4_append(const Kv4AppendArgs &a, hipStream_t s) {
+  const long threads = (long)a.rows * a.d.num_kv_heads * (a.d.head_dim / 8);
+  const dim3 grid((unsigned)(threads ? (threads + 255) / 256 : 1), 2);
+  const bool path = a.accept_path != nullptr;
+  if (a.d.dtype == HB_F32) {
+    if (path) kv4_append_kernel<float, true><<<grid, 256, 0, s>>>(a);
+    else kv4_append_kernel<float, false><<<grid, 256, 0, s>>>(a);
+  } else {
+    if (path) kv4_append_kernel<bf16_t, true><<<grid, 256, 0, s>>>(a);
+    else kv4_append_kernel<bf16_t, false><<<grid, 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_read(const hb_attn_desc &d, int32_t rows, const Kv4Pool &k, const Kv4Pool &v, const int32_t *block_table,
+                           const int32_t *first, const int32_t *row_offset, void *k_rows, void *v_rows, hipStream_t s) {
+  const long threads = (long)rows * d.num_kv_heads * (d.head_dim / 8);
+  const dim3 grid((unsigned)((threads + 255) / 256), 2);
+  if (d.dtype == HB_F32)
+    kv4_read_kernel<float><<<grid, 256, 0, s>>>(d, rows, k, v, block_table, first, row_offset, (float *)k_rows, (float *)v_rows);
+  else
+    kv4_read_kernel<bf16_t><<<grid, 256, 0, s>>>(d, rows, k, v, block_table, first, row_offset, (bf16_t *)k_rows, (bf16_t *)v_rows);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_evict(const Kv4EvictArgs &a, hipStream_t s) {
+  const int units = a.d.batch * a.d.num_kv_heads;
+  kv4_select_kernel<<<units, kSelectThreads, 0, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  kv4_move_kernel<<<dim3((unsigned)((a.budget + 3) / 4), (unsigned)units), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace hb

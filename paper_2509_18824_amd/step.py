@@ -6,7 +6,7 @@ library.  ``VerifyStep`` chains the calls of one verification step on the curren
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -220,6 +220,20 @@ def kv_compact(desc, dev: DeviceInputs, accept_len, accept_path):
     hb.hb_kv_compact(desc, dev.k_tree, dev.v_tree, dev.k_pool, dev.v_pool, dev.block_table, dev.prefix_len,
                      dev.node_offset, accept_len, accept_path, max_path, out_slots, new_len)
     return out_slots, new_len
+
+
+class Kv4Pool(NamedTuple):
+    """One layer's 4-bit cache: codes [num_blocks, Hkv, page, D / 2] and scales [num_blocks, Hkv, page, D / 32] of K and V."""
+
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+
+
+def kv4_pool(num_blocks: int, Hkv: int, page: int, D: int, device="cuda") -> Kv4Pool:
+    u8 = lambda n: torch.empty((num_blocks, Hkv, page, n), dtype=torch.uint8, device=device)
+    return Kv4Pool(u8(D // 2), u8(D // 32), u8(D // 2), u8(D // 32))
 
 
 class VerifyStep:
