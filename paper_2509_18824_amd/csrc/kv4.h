@@ -28,6 +28,18 @@ struct Kv4AttnArgs {
   void *out;
   float *lse, *part_o, *part_ml;
 };
+// How the matrix-core kernel cuts the prefixes, from what the host knows
+struct Kv4Plan {
+  int32_t row_groups;   // workgroups that share a chunk's query rows
+  int32_t grain;        // keys that a chunk's length is a multiple of
+  int32_t target;       // chunks per kv head, over all sequences
+  int32_t splits;       // chunks of a sequence, at most: slots of part_o and part_ml
+  uint32_t page_magic;  // ceil(2^32 / (page_size / 16)), 0 where that is one
+};
+bool kv4_attn_supports(const hb_attn_desc &d);
+void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan);
+hipError_t launch_kv4_attn(const Kv4AttnArgs &a, const Kv4Plan &plan, hipStream_t s);
+
 hipError_t launch_kv4_attn_scalar(const Kv4AttnArgs &a, hipStream_t s);
 hipError_t launch_kv4_merge(const Kv4AttnArgs &a, hipStream_t s);
 

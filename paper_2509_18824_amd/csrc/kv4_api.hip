@@ -47,30 +47,39 @@ static int64_t span_of(const hb_attn_desc *d) {
   return d->max_prefix_len_hint > 0 && d->max_prefix_len_hint < cap ? d->max_prefix_len_hint : cap;
 }
 
-struct Kv4Plan {
-  int32_t splits, chunk;
+struct AttnCut {
+  bool mfma;
+  Kv4Plan plan;            // the matrix-core kernel's
+  int32_t splits, chunk;   // slots of a row's partial results; the scalar kernel's chunk length
   size_t ml_offset, bytes;
 };
 
-static int32_t make_kv4_plan(const hb_attn_desc *d, Kv4Plan *plan) {
+static int32_t make_cut(const hb_attn_desc *d, AttnCut *cut) {
   int32_t rc = check_kv4(d);
   if (rc) return rc;
-  if (d->algo == HB_ATTN_MFMA) return fail(HB_ERR_UNSUPPORTED, "HB_ATTN_MFMA: no such kernel for the 4-bit cache");
-  const int64_t rows = (int64_t)d->total_nodes * d->num_q_heads;
-  const int64_t span = span_of(d);
-  int64_t splits = d->num_splits;
-  if (splits == 0) {
-    splits = rows > 0 ? (2048 + rows - 1) / rows : 1;
-    if (splits > (span + 255) / 256) splits = (span + 255) / 256;
+  const bool can = kv4_attn_supports(*d);
+  if (d->algo == HB_ATTN_MFMA && !can)
+    return fail(HB_ERR_UNSUPPORTED, "HB_ATTN_MFMA over the 4-bit cache needs bf16, head_dim 64 or 128, page_size a multiple of 16 up to "
+                "1024, a positive softmax_scale and Hq/Hkv <= 512");
+  cut->mfma = can && d->algo != HB_ATTN_SCALAR;
+  const int64_t rows = (int64_t)d->total_nodes * d->num_q_heads, span = span_of(d);
+  if (cut->mfma) {
+    kv4_attn_plan(*d, span, &cut->plan);
+    cut->splits = cut->plan.splits;
+  } else {
+    int64_t splits = d->num_splits;
+    if (splits == 0) {
+      splits = rows > 0 ? (2048 + rows - 1) / rows : 1;
+      if (splits > (span + 255) / 256) splits = (span + 255) / 256;
+    }
+    if (splits > 1024) splits = 1024;
+    int64_t chunk = (span + splits - 1) / splits;
+    chunk = (chunk + 63) / 64 * 64;
+    cut->splits = (int32_t)((span + chunk - 1) / chunk);
+    cut->chunk = (int32_t)chunk;
   }
-  if (splits > 1024) splits = 1024;
-  int64_t chunk = (span + splits - 1) / splits;
-  chunk = (chunk + 63) / 64 * 64;
-  splits = (span + chunk - 1) / chunk;
-  plan->splits = (int32_t)splits;
-  plan->chunk = (int32_t)chunk;
-  plan->ml_offset = splits > 1 ? round_up((size_t)rows * splits * d->head_dim * 4, 256) : 0;
-  plan->bytes = splits > 1 ? plan->ml_offset + round_up((size_t)rows * splits * 8, 256) : 0;
+  cut->ml_offset = cut->splits > 1 ? round_up((size_t)rows * cut->splits * d->head_dim * 4, 256) : 0;
+  cut->bytes = cut->splits > 1 ? cut->ml_offset + round_up((size_t)rows * cut->splits * 8, 256) : 0;
   return HB_OK;
 }
 
@@ -135,13 +144,13 @@ int32_t hb_kv4_read(const hb_attn_desc *desc, int32_t n_rows, const void *k_code
 }
 
 size_t hb_tree_verify_attn_kv4_workspace_bytes(const hb_attn_desc *desc) {
-  Kv4Plan plan;
-  return make_kv4_plan(desc, &plan) ? 0 : plan.bytes;
+  AttnCut cut;
+  return make_cut(desc, &cut) ? 0 : cut.bytes;
 }
 
 int32_t hb_tree_verify_attn_kv4_num_splits(const hb_attn_desc *desc) {
-  Kv4Plan plan;
-  return make_kv4_plan(desc, &plan) ? 0 : plan.splits;
+  AttnCut cut;
+  return make_cut(desc, &cut) ? 0 : cut.splits;
 }
 
 int32_t hb_tree_verify_attn_kv4(const hb_attn_desc *desc, const void *q, const void *k_tree, const void *v_tree,
@@ -149,8 +158,8 @@ int32_t hb_tree_verify_attn_kv4(const hb_attn_desc *desc, const void *q, const v
                                 const int32_t *block_table, const int32_t *prefix_len, const int32_t *node_offset,
                                 const int32_t *parent, void *out, float *lse, void *workspace, size_t workspace_bytes,
                                 void *stream) {
-  Kv4Plan plan;
-  int32_t rc = make_kv4_plan(desc, &plan);
+  AttnCut cut;
+  int32_t rc = make_cut(desc, &cut);
   if (rc) return rc;
   if (desc->batch == 0 || desc->total_nodes == 0) return HB_OK;
   if ((rc = check_pool(k_codes, k_scales, v_codes, v_scales))) return rc;
@@ -158,16 +167,20 @@ int32_t hb_tree_verify_attn_kv4(const hb_attn_desc *desc, const void *q, const v
     return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
   if (misaligned(q, 16) || misaligned(k_tree, 16) || misaligned(v_tree, 16) || misaligned(out, 16))
     return fail(HB_ERR_INVALID_ARG, "q, k_tree, v_tree and out must be 16-byte aligned");
-  if (plan.bytes) {
-    if (!workspace || workspace_bytes < plan.bytes)
-      return fail(HB_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", plan.bytes, workspace ? workspace_bytes : (size_t)0);
+  if (cut.bytes) {
+    if (!workspace || workspace_bytes < cut.bytes)
+      return fail(HB_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", cut.bytes, workspace ? workspace_bytes : (size_t)0);
     if (misaligned(workspace, 256)) return fail(HB_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   }
-  Kv4AttnArgs a = {*desc, plan.splits, plan.chunk, q, k_tree, v_tree, {(const uint8_t *)k_codes, (const uint8_t *)k_scales},
+  Kv4AttnArgs a = {*desc, cut.splits, cut.chunk, q, k_tree, v_tree, {(const uint8_t *)k_codes, (const uint8_t *)k_scales},
                    {(const uint8_t *)v_codes, (const uint8_t *)v_scales}, block_table, prefix_len, node_offset, parent, out, lse,
-                   (float *)workspace, (float *)((char *)workspace + plan.ml_offset)};
+                   (float *)workspace, (float *)((char *)workspace + cut.ml_offset)};
+  if (cut.mfma) {
+    HB_HIP_TRY(launch_kv4_attn(a, cut.plan, (hipStream_t)stream));
+    return HB_OK;
+  }
   HB_HIP_TRY(launch_kv4_attn_scalar(a, (hipStream_t)stream));
-  if (plan.splits > 1) HB_HIP_TRY(launch_kv4_merge(a, (hipStream_t)stream));
+  if (cut.splits > 1) HB_HIP_TRY(launch_kv4_merge(a, (hipStream_t)stream));
   return HB_OK;
 }
 
