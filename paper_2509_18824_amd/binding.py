@@ -512,34 +512,38 @@ hb_lmhead_accept = _lmhead_accept(lib.hb_lmhead_accept)
 hb_lmhead_accept_cleared = _lmhead_accept(lib.hb_lmhead_accept_cleared)
 
 
+# (sizes rather than shapes: a call's checks cost microseconds)
 def _kv4_rows(desc: AttnDesc, k_rows, v_rows) -> int:
-    n = k_rows.shape[0]
-    if k_rows.shape != (n, desc.num_kv_heads, desc.head_dim) or v_rows.shape != k_rows.shape:
+    n, row = k_rows.shape[0], desc.num_kv_heads * desc.head_dim
+    if k_rows.numel() != n * row or v_rows.numel() != n * row:
         raise ValueError("rows must be [n, Hkv, D], K and V alike")
     if _dtype_code(k_rows) != desc.dtype or v_rows.dtype != k_rows.dtype:
         raise ValueError("rows must have the descriptor's dtype")
     return n
 
 
-def _kv4_pool(desc: AttnDesc, *pool) -> None:
-    """Codes and scales in turn."""
-    if any(t.dtype != torch.uint8 for t in pool):
-        raise ValueError("codes and scales are uint8 tensors")
-    lead = (desc.num_blocks, desc.num_kv_heads, desc.page_size)
-    if any(t.shape != lead + (desc.head_dim // (32 if i % 2 else 2),) for i, t in enumerate(pool)):
-        raise ValueError("codes must be [num_blocks, Hkv, page, D / 2], scales [num_blocks, Hkv, page, D / 32]")
+_u8 = torch.uint8
+
+
+def _kv4_pool(desc: AttnDesc, k_codes, k_scales, v_codes=None, v_scales=None) -> None:
+    n = desc.num_blocks * desc.num_kv_heads * desc.page_size * (desc.head_dim // 32)  # blocks of 32: 16 bytes and one
+    if (k_codes.dtype is not _u8 or k_scales.dtype is not _u8 or k_codes.numel() != 16 * n or k_scales.numel() != n
+            or v_codes is not None and (v_codes.dtype is not _u8 or v_scales.dtype is not _u8 or v_codes.numel() != 16 * n
+                                        or v_scales.numel() != n)):
+        raise ValueError("codes must be uint8 [num_blocks, Hkv, page, D / 2], scales uint8 [num_blocks, Hkv, page, D / 32]")
 
 
 def _kv4_slots(desc: AttnDesc, weight, pos) -> None:
-    shape = (desc.batch, desc.num_kv_heads, desc.max_blocks_per_seq * desc.page_size)
-    for t, dtype in ((weight, torch.float32), (pos, torch.int32)):
-        if t is not None and (t.dtype != dtype or t.shape != shape):
-            raise ValueError("weight (float32) and pos (int32) must be [B, Hkv, max_blocks * page]")
+    n = desc.batch * desc.num_kv_heads * desc.max_blocks_per_seq * desc.page_size
+    if (weight is not None and (weight.dtype is not torch.float32 or weight.numel() != n)
+            or pos is not None and (pos.dtype is not torch.int32 or pos.numel() != n)):
+        raise ValueError("weight (float32) and pos (int32) must be [B, Hkv, max_blocks * page]")
 
 
 def _kv4_ints(*tensors) -> None:
-    if any(t is not None and t.dtype != torch.int32 for t in tensors):
-        raise ValueError("lengths, offsets, positions, paths and tables are int32 tensors")
+    for t in tensors:
+        if t is not None and t.dtype is not torch.int32:
+            raise ValueError("lengths, offsets, positions, paths and tables are int32 tensors")
 
 
 def hb_kv4_append(desc: AttnDesc, k_rows, v_rows, k_codes, k_scales, v_codes, v_scales, block_table, prefix_len, row_offset,
@@ -556,7 +560,7 @@ def hb_kv4_append(desc: AttnDesc, k_rows, v_rows, k_codes, k_scales, v_codes, v_
 def hb_kv4_compact(desc: AttnDesc, k_tree, v_tree, k_codes, k_scales, v_codes, v_scales, block_table, prefix_len, node_offset,
                    accept_len, accept_path, max_path: int, seq_len=None, weight=None, pos=None, out_slots=None, new_len=None,
                    stream=None) -> None:
-    if _kv4_rows(desc, k_tree, v_tree) != desc.total_nodes:
+    if _kv4_rows(desc, k_tree, v_tree) < desc.total_nodes:
         raise ValueError("rows must be [total_nodes, Hkv, D]")
     _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
     _kv4_slots(desc, weight, pos)
@@ -587,6 +591,11 @@ def hb_tree_verify_attn_kv4_num_splits(desc: AttnDesc) -> int:
 def hb_tree_verify_attn_kv4(desc: AttnDesc, q, k_tree, v_tree, k_codes, k_scales, v_codes, v_scales, block_table, prefix_len,
                             node_offset, parent, out, lse=None, workspace=None, stream=None) -> None:
     _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
+    rows = desc.total_nodes * desc.num_q_heads
+    if q.numel() < rows * desc.head_dim or out.numel() < rows * desc.head_dim or _dtype_code(q) != desc.dtype or out.dtype is not q.dtype:
+        raise ValueError("q and out must be [total_nodes, Hq, D] in the descriptor's dtype")
+    if _kv4_rows(desc, k_tree, v_tree) < desc.total_nodes or lse is not None and (lse.numel() < rows or lse.dtype is not torch.float32):
+        raise ValueError("k_tree and v_tree must be [total_nodes, Hkv, D], lse float32 [total_nodes, Hq]")
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(lib.hb_tree_verify_attn_kv4(C.byref(desc), _ptr(q), _ptr(k_tree), _ptr(v_tree), _ptr(k_codes), _ptr(k_scales),
                                        _ptr(v_codes), _ptr(v_scales), _ptr(block_table), _ptr(prefix_len), _ptr(node_offset),
@@ -613,7 +622,7 @@ def hb_kv4_evict(desc: AttnDesc, budget: int, recent: int, sinks: int, k_codes, 
     _kv4_slots(desc, weight, pos)
     _kv4_slots(desc, weight_out, pos_out)
     _kv4_ints(block_table, prefix_len, seq_len, kept, new_len)
-    if kept.shape != (desc.batch, desc.num_kv_heads, budget):
+    if kept.numel() != desc.batch * desc.num_kv_heads * budget:
         raise ValueError("kept must be [B, Hkv, budget]")
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(lib.hb_kv4_evict(C.byref(desc), budget, recent, sinks, _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales),

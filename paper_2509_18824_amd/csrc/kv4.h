@@ -53,7 +53,9 @@ struct Kv4WeightArgs {
   const float *lse;
   float *weight;
 };
-hipError_t launch_kv4_weight(const Kv4WeightArgs &a, int32_t longest, hipStream_t s);
+hipError_t launch_kv4_weight_scalar(const Kv4WeightArgs &a, int32_t longest, hipStream_t s);
+bool kv4_weight_supports(const hb_attn_desc &d);
+hipError_t launch_kv4_weight_mfma(const Kv4WeightArgs &a, int32_t longest, hipStream_t s);
 
 __device__ inline float kv4_scale(uint32_t s) {
   return __uint_as_float(s == kKv4NaN ? 0x7fc00000u : s == 0 ? 0x00400000u : s << 23);

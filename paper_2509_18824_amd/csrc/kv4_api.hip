@@ -200,7 +200,10 @@ int32_t hb_kv4_attn_weight(const hb_attn_desc *desc, const void *q, const void *
     return fail(HB_ERR_INVALID_ARG, "q, codes and scales must be 16-byte aligned");
   Kv4WeightArgs a = {*desc, max_path, decay, q, {(const uint8_t *)k_codes, (const uint8_t *)k_scales}, block_table, prefix_len,
                      node_offset, accept_len, accept_path, lse, weight};
-  HB_HIP_TRY(launch_kv4_weight(a, (int32_t)span_of(desc), (hipStream_t)stream));
+  if (desc->algo != HB_ATTN_SCALAR && kv4_weight_supports(*desc))
+    HB_HIP_TRY(launch_kv4_weight_mfma(a, (int32_t)span_of(desc), (hipStream_t)stream));
+  else
+    HB_HIP_TRY(launch_kv4_weight_scalar(a, (int32_t)span_of(desc), (hipStream_t)stream));
   return HB_OK;
 }
 

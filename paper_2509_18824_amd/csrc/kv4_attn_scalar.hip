@@ -1,4 +1,4 @@
-// Attention over the 4-bit cache in 32-bit arithmetic, for every type, head size and page size: one workgroup per
+// Attention and attention weights over the 4-bit cache in 32-bit arithmetic, for every type, head size and page size: one workgroup per
 // (node, query head, chunk of the prefix); the wavefronts deal out blocks of 64 keys.  A lane takes one key of a block
 // for the scores and two elements of the head (or four) for the values.  The merge of the chunks' partial results serves the
 // matrix-core kernel too.
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
 
 // Attention weight that every cached position received: a lane takes one position, a wavefront 64 of them.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void kv4_weight_kernel(Kv4WeightArgs a) {
+__global__ __launch_bounds__(kThreads) void kv4_weight_scalar_kernel(Kv4WeightArgs a) {
   const hb_attn_desc &d = a.d;
   __shared__ float q[256];
   const int tid = threadIdx.x, h = blockIdx.y % d.num_kv_heads, b = blockIdx.y / d.num_kv_heads, G = d.num_q_heads / d.num_kv_heads;
@@ -234,10 +234,10 @@ hipError_t launch_kv4_merge(const Kv4AttnArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_kv4_weight(const Kv4WeightArgs &a, int32_t longest, hipStream_t s) {
+hipError_t launch_kv4_weight_scalar(const Kv4WeightArgs &a, int32_t longest, hipStream_t s) {
   const dim3 grid((unsigned)((longest + kThreads - 1) / kThreads), (unsigned)(a.d.batch * a.d.num_kv_heads));
-  if (a.d.dtype == HB_F32) kv4_weight_kernel<float><<<grid, kThreads, 0, s>>>(a);
-  else kv4_weight_kernel<bf16_t><<<grid, kThreads, 0, s>>>(a);
+  if (a.d.dtype == HB_F32) kv4_weight_scalar_kernel<float><<<grid, kThreads, 0, s>>>(a);
+  else kv4_weight_scalar_kernel<bf16_t><<<grid, kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -146,111 +146,234 @@ __device__ inline uint32_t weight_key(float w, bool safe) {
 }
 
 constexpr int kSelectThreads = 1024;
+constexpr int kSelectWaves = kSelectThreads / 64;
+constexpr int kRounds = 8;                               // of four slots to a thread
+constexpr int kSlab = kSelectThreads * 4 * kRounds;      // 32768 slots
+constexpr int kBins = 2048;                              // digits of 11, 11 and 10 bits
 
-// number of set flags in front of this thread's in the workgroup, and their total
-__device__ inline int block_rank(bool flag, int *waves, int &total) {
-  const unsigned long long m = __ballot(flag);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  __syncthreads();
-  if (lane == 0) waves[w] = __popcll(m);
-  __syncthreads();
-  int before = 0;
-  total = 0;
-  for (int i = 0; i < kSelectThreads / 64; ++i) {
-    before += i < w ? waves[i] : 0;
-    total += waves[i];
+// the keys of a thread's slots of a slab: slots slab + 4096 round + 4 tid + 0 .. 3.  Slots past the length get key 0, which
+// no slot in front of it has.
+struct Keys {
+  uint32_t k[kRounds][4];
+};
+
+__device__ inline void load_keys(const float *w, const int32_t *pos, int slab, int L, int recent_from, int sinks, Keys &keys) {
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int s = slab + (r * kSelectThreads + (int)threadIdx.x) * 4;
+    if (slab + r * kSelectThreads * 4 < L) {  // uniform
+      // the row's capacity is a multiple of the page size: slots one by one where that is no multiple of four
+      float x[4];
+      int32_t p[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = s + e < L ? w[s + e] : 0.f;
+        p[e] = s + e < L ? pos[s + e] : 0;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) keys.k[r][e] = s + e < L ? weight_key(x[e], p[e] >= recent_from || p[e] < sinks) : 0u;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) keys.k[r][e] = 0u;
+    }
   }
-  return before + __popcll(m & ((1ull << lane) - 1ull));
 }
 
-// One workgroup per (sequence, head): which positions stay.  The least key that stays is found digit by digit
-// (8 bits, a histogram each); of the positions that have just this key the first ones stay.  Kept positions in front of the
-// new length stay in their slot; the others are listed, and so are the slots that come free in front of it.
+// Ranks in slot order of a slab's flags, two kinds at once: `n[r]` of a thread's round r holds their numbers (low and high half), and
+// becomes the number in front of the thread's first slot.  `total` counts the slab's.  A round's sum stays below 2^16.
+__device__ inline void slab_ranks(uint32_t (&n)[kRounds], uint32_t (*sums)[kSelectWaves], int (&total)[2]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t up[kRounds];
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) up[r] = n[r];
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      const uint32_t y = (uint32_t)__shfl_up((int)up[r], o, 64);
+      up[r] += lane >= o ? y : 0u;
+    }
+  __syncthreads();
+  if (lane == 63)
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) sums[r][wave] = up[r];
+  __syncthreads();
+  // every wavefront sums the (round, wavefront) totals in order: lane l those of round l / 8, wavefronts 2 (l % 8) and the next
+  uint32_t a = sums[lane >> 3][(lane & 7) * 2], b = sums[lane >> 3][(lane & 7) * 2 + 1];
+  int lo = (int)((a & 0xffffu) + (b & 0xffffu)), hi = (int)((a >> 16) + (b >> 16));
+  const int lo0 = lo, hi0 = hi;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(lo, o, 64), y = __shfl_up(hi, o, 64);
+    lo += lane >= o ? x : 0;
+    hi += lane >= o ? y : 0;
+  }
+  total[0] = __shfl(lo, 63, 64);
+  total[1] = __shfl(hi, 63, 64);
+  const int lo_before = lo - lo0, hi_before = hi - hi0;
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int at = r * 8 + (wave >> 1);
+    const uint32_t odd = (wave & 1) ? sums[r][wave & ~1] : 0u;
+    const int x = __shfl(lo_before, at, 64) + (int)(odd & 0xffffu) + (int)((up[r] - n[r]) & 0xffffu);
+    const int y = __shfl(hi_before, at, 64) + (int)(odd >> 16) + (int)((up[r] - n[r]) >> 16);
+    n[r] = (uint32_t)x | ((uint32_t)y << 16);  // both at most 32768, and only then is there no other
+  }
+}
+
+// One workgroup per (sequence, head): which positions stay.  The least key that stays is found digit by digit (11 bits, a
+// histogram each: the eight of the exponent alone would send most weights to a few counters); of the positions that have just this
+// key the first ones stay.  Kept positions in front of the new length stay in their slot; the others are listed, and so are the
+// slots that come free in front of it.
+// What bounds it is one CU's way to a row of weights and positions, and the steps in a row.  Up to 32768 slots their keys stay in
+// registers; longer rows are read again for every digit.
 __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs a) {
   const hb_attn_desc &d = a.d;
-  __shared__ int hist[256], waves[kSelectThreads / 64];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_need;
-  const int tid = threadIdx.x, b = blockIdx.x / d.num_kv_heads;
+  __shared__ int hist[kBins], s_sum[kSelectWaves];
+  __shared__ uint32_t sums[kRounds][kSelectWaves];
+  __shared__ int s_digit, s_need;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x / d.num_kv_heads;
   const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
   const int L = kv4_length(d, a.prefix_len, b), stays = L < a.budget ? L : a.budget;
   const float *w = a.weight + (size_t)blockIdx.x * cap;
   const int32_t *pos = a.pos + (size_t)blockIdx.x * cap;
   const int recent_from = a.seq_len[b] - a.recent;
-  auto key = [&](int s) { return weight_key(w[s], pos[s] >= recent_from || pos[s] < a.sinks); };
   if (tid == 0 && blockIdx.x % d.num_kv_heads == 0 && a.new_len) a.new_len[b] = stays;
-  uint32_t prefix = 0;
-  int need = stays;
-  if (stays < L && stays > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
+  const int slabs = (L + kSlab - 1) / kSlab;
+  Keys keys;
+  if (slabs == 1) load_keys(w, pos, 0, L, recent_from, a.sinks, keys);
+  uint32_t least = 0;  // the least key that stays, as far as it is known
+  int need = stays;    // positions with that key that stay
+  if (stays < L) {
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
+      for (int i = tid; i < bins; i += kSelectThreads) hist[i] = 0;
       __syncthreads();
-      for (int s = tid; s < L; s += kSelectThreads) {
-        const uint32_t k = key(s);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+      for (int slab = 0; slab < slabs; ++slab) {
+        if (slabs > 1) load_keys(w, pos, slab * kSlab, L, recent_from, a.sinks, keys);
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t k = keys.k[r][e];
+            const bool in = k != 0 && (pass == 0 || (k >> (pass == 1 ? 21 : 10)) == (least >> (pass == 1 ? 21 : 10)));
+            if (in) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1);
+          }
       }
       __syncthreads();
-      if (tid == 0) {
-        int digit = 255, left = need;
-        while (digit > 0 && hist[digit] < left) left -= hist[digit--];
-        s_prefix = prefix | ((uint32_t)digit << shift);
-        s_need = left;
+      // a thread's two counters, the largest digits first: the digit is where their running sum passes `need`
+      const int top = bins - 1 - 2 * tid;
+      const int c0 = top > 0 ? hist[top] : 0, c1 = top > 0 ? hist[top - 1] : 0;
+      int up = c0 + c1;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(up, o, 64);
+        up += lane >= o ? y : 0;
+      }
+      if (lane == 63) s_sum[wave] = up;
+      __syncthreads();
+      int before = up - c0 - c1;
+      for (int i = 0; i < wave; ++i) before += s_sum[i];
+      if (before < need && before + c0 + c1 >= need) {  // one thread
+        const bool first = before + c0 >= need;
+        s_digit = first ? top : top - 1;
+        s_need = need - before - (first ? 0 : c0);
       }
       __syncthreads();
-      prefix = s_prefix;
+      least |= (uint32_t)s_digit << shift;
       need = s_need;
+      __syncthreads();
     }
   }
   int32_t *kept = a.kept + (size_t)blockIdx.x * a.budget;
   int32_t *from = a.moves + (size_t)blockIdx.x * 2 * a.budget, *to = from + a.budget;
-  int ties = 0, free_slots = 0, above = 0;
-  for (int s0 = 0; s0 < L; s0 += kSelectThreads) {
-    const int s = s0 + tid;
-    const uint32_t k = s < L ? key(s) : 0;
-    const bool all = stays == L, in = s < L && stays > 0;
-    const bool tie = in && !all && k == prefix;
-    int total;
-    const int rank = ties + block_rank(tie, waves, total);
-    ties += total;
-    const bool stay = in && (all || k > prefix || (tie && rank < need));
-    const bool frees = s < stays && !stay, moves = s >= stays && stay;
-    const int fr = free_slots + block_rank(frees, waves, total);
-    free_slots += total;
-    const int mr = above + block_rank(moves, waves, total);
-    above += total;
-    if (frees) to[fr] = s;
-    if (moves) from[mr] = s;
-    if (s < stays && stay) {
-      kept[s] = s;
-      a.weight_out[(size_t)blockIdx.x * cap + s] = w[s];
-      a.pos_out[(size_t)blockIdx.x * cap + s] = pos[s];
+  int ties = 0, freed = 0, above = 0;
+  for (int slab = 0; slab < slabs; ++slab) {
+    if (slabs > 1) load_keys(w, pos, slab * kSlab, L, recent_from, a.sinks, keys);
+    uint32_t n[kRounds];
+    int total[2] = {0, 0};
+    // ranks among the positions that have the least key
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      n[r] = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) n[r] += keys.k[r][e] == least ? 1u : 0u;
     }
+    if (stays < L) slab_ranks(n, sums, total);
+    uint32_t stay = 0;  // bit 4 r + e
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      int rank = ties + (int)(n[r] & 0xffffu);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t k = keys.k[r][e];
+        const bool tie = k == least;
+        if (k != 0 && (stays == L || k > least || (tie && rank < need))) stay |= 1u << (4 * r + e);
+        rank += tie ? 1 : 0;
+      }
+    }
+    ties += total[0];
+    // ranks among the slots that come free (low half) and the positions that leave theirs (high half)
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      n[r] = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int s = slab * kSlab + (r * kSelectThreads + tid) * 4 + e;
+        const bool in = (stay >> (4 * r + e)) & 1;
+        n[r] += s < stays ? (in ? 0u : 1u) : (in ? 0x10000u : 0u);
+      }
+    }
+    if (stays < L) slab_ranks(n, sums, total);
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      int f = freed + (int)(n[r] & 0xffffu), m = above + (int)(n[r] >> 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int s = slab * kSlab + (r * kSelectThreads + tid) * 4 + e;
+        const bool in = (stay >> (4 * r + e)) & 1;
+        if (s < stays) {
+          if (in) {
+            kept[s] = s;
+            a.weight_out[(size_t)blockIdx.x * cap + s] = w[s];
+            a.pos_out[(size_t)blockIdx.x * cap + s] = pos[s];
+          } else {
+            to[f++] = s;
+          }
+        } else if (in) {
+          from[m++] = s;
+        }
+      }
+    }
+    freed += total[0];
+    above += total[1];
   }
   for (int s = stays + tid; s < a.budget; s += kSelectThreads) kept[s] = -1;
-  if (tid == 0) a.counts[blockIdx.x] = above;
+  if (tid == 0) a.counts[blockIdx.x] = stays < L ? above : 0;
 }
 
-// A row of K and V to the slot that came free for it: `lanes` lanes a move
+// Rows of K and V to the slots that came free for them: a lane takes a block of K or V (16 bytes and a scale), 2 D / 32 lanes a
+// move, so that a wavefront has several in flight.
 __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4EvictArgs a) {
   const hb_attn_desc &d = a.d;
-  const int i = (int)blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int unit = blockIdx.y, b = unit / d.num_kv_heads, h = unit % d.num_kv_heads;
-  if (i >= a.counts[unit]) return;
+  const int blocks = d.head_dim / kKv4Block, lanes = 2 * blocks, each = 64 / lanes;
+  const int lane = threadIdx.x & 63, part = lane % lanes, unit = blockIdx.y;
+  const int i = ((int)blockIdx.x * 4 + (threadIdx.x >> 6)) * each + lane / lanes;
+  if (lane >= each * lanes || i >= a.counts[unit]) return;
+  const int b = unit / d.num_kv_heads, h = unit % d.num_kv_heads;
   const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
   const int32_t *moves = a.moves + (size_t)unit * 2 * a.budget;
   const int src = moves[i], dst = moves[a.budget + i];
   const size_t s = kv4_row(d, a.block_table, b, h, src), t = kv4_row(d, a.block_table, b, h, dst);
-  const int words = d.head_dim / 8, bytes = d.head_dim / kKv4Block;  // words of codes, scale bytes
-  if (lane < words) {
-    ((uint32_t *)a.k_codes)[t * words + lane] = ((const uint32_t *)a.k_codes)[s * words + lane];
-    ((uint32_t *)a.v_codes)[t * words + lane] = ((const uint32_t *)a.v_codes)[s * words + lane];
-  } else if (lane < words + bytes) {
-    a.k_scales[t * bytes + lane - words] = a.k_scales[s * bytes + lane - words];
-    a.v_scales[t * bytes + lane - words] = a.v_scales[s * bytes + lane - words];
-  }
-  if (lane == 63) {
+  const bool value = part >= blocks;
+  const int blk = value ? part - blocks : part;
+  uint8_t *codes = value ? a.v_codes : a.k_codes, *scales = value ? a.v_scales : a.k_scales;
+  ((u32x4 *)codes)[t * blocks + blk] = ((const u32x4 *)codes)[s * blocks + blk];
+  scales[t * blocks + blk] = scales[s * blocks + blk];
+  if (part == 0) {
     a.kept[(size_t)unit * a.budget + dst] = src;
     a.weight_out[unit * cap + dst] = a.weight[unit * cap + src];
+  } else if (part == 1) {
     a.pos_out[unit * cap + dst] = a.pos[unit * cap + src];
   }
 }
@@ -287,7 +410,8 @@ hipError_t launch_kv4_evict(const Kv4EvictArgs &a, hipStream_t s) {
   kv4_select_kernel<<<units, kSelectThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  kv4_move_kernel<<<dim3((unsigned)((a.budget + 3) / 4), (unsigned)units), 256, 0, s>>>(a);
+  const int each = 4 * (64 / (2 * (a.d.head_dim / kKv4Block)));  // moves of a workgroup
+  kv4_move_kernel<<<dim3((unsigned)((a.budget + each - 1) / each), (unsigned)units), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
