@@ -253,9 +253,12 @@ struct Kv4EvictArgs {
   const int32_t *pos;
   float *weight_out;
   int32_t *pos_out, *kept, *new_len;
-  int32_t *moves, *counts;  // workspace: [unit][2][budget], [unit]
+  // workspace, per (sequence, head): positions that move, the last first, and the slots that they move to [2][budget]; their number; the
+  // least key that stays and how many that have it do; in front of every 256 slots, how many have a greater key and how many this
+  int32_t *moves, *counts, *least, *parts;
+  int32_t parts_each;
 };
-hipError_t launch_kv4_evict(const Kv4EvictArgs &a, hipStream_t s);
+hipError_t launch_kv4_evict(const Kv4EvictArgs &a, int64_t longest, hipStream_t s);  // longest: no prefix is longer
 
 // ---- argmax key: (order-preserving float bits << 32) | (0xffffffff - index) ---------------
 // max over keys = largest value, lowest index among equal values.  NaN is mapped to -inf.

@@ -207,13 +207,24 @@ int32_t hb_kv4_attn_weight(const hb_attn_desc *desc, const void *q, const void *
   return HB_OK;
 }
 
-static size_t evict_list_bytes(const hb_attn_desc *d, int32_t budget) {
-  return round_up((size_t)d->batch * d->num_kv_heads * 2 * budget * 4, 256);
+struct EvictLayout {
+  int64_t parts;
+  size_t counts, least, parts_at, bytes;
+};
+static EvictLayout evict_layout(const hb_attn_desc *d, int32_t budget) {
+  const size_t units = (size_t)d->batch * d->num_kv_heads;
+  EvictLayout e;
+  e.parts = ((int64_t)d->page_size * d->max_blocks_per_seq + 255) / 256;
+  e.counts = round_up(units * 2 * budget * 4, 256);
+  e.least = e.counts + round_up(units * 4, 256);
+  e.parts_at = e.least + round_up(units * 8, 256);
+  e.bytes = e.parts_at + round_up(units * e.parts * 8, 256);
+  return e;
 }
 
 size_t hb_kv4_evict_workspace_bytes(const hb_attn_desc *desc, int32_t budget) {
   if (check_kv4_cache(desc) || budget <= 0 || desc->batch == 0) return 0;
-  return evict_list_bytes(desc, budget) + round_up((size_t)desc->batch * desc->num_kv_heads * 4, 256);
+  return evict_layout(desc, budget).bytes;
 }
 
 int32_t hb_kv4_evict(const hb_attn_desc *desc, int32_t budget, int32_t recent, int32_t sinks, void *k_codes, void *k_scales,
@@ -229,14 +240,16 @@ int32_t hb_kv4_evict(const hb_attn_desc *desc, int32_t budget, int32_t recent, i
   if ((rc = check_pool(k_codes, k_scales, v_codes, v_scales))) return rc;
   if (!block_table || !prefix_len || !seq_len || !weight || !pos || !weight_out || !pos_out || !kept)
     return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
-  const size_t need = hb_kv4_evict_workspace_bytes(desc, budget);
+  const EvictLayout at = evict_layout(desc, budget);
+  const size_t need = at.bytes;
   if (!workspace || workspace_bytes < need)
     return fail(HB_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
   if (misaligned(workspace, 256)) return fail(HB_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   Kv4EvictArgs a = {*desc, budget, recent, sinks, (uint8_t *)k_codes, (uint8_t *)k_scales, (uint8_t *)v_codes, (uint8_t *)v_scales,
                     block_table, prefix_len, seq_len, weight, pos, weight_out, pos_out, kept, new_len, (int32_t *)workspace,
-                    (int32_t *)((char *)workspace + evict_list_bytes(desc, budget))};
-  HB_HIP_TRY(launch_kv4_evict(a, (hipStream_t)stream));
+                    (int32_t *)((char *)workspace + at.counts), (int32_t *)((char *)workspace + at.least),
+                    (int32_t *)((char *)workspace + at.parts_at), (int32_t)at.parts};
+  HB_HIP_TRY(launch_kv4_evict(a, span_of(desc), (hipStream_t)stream));
   return HB_OK;
 }
 

@@ -148,89 +148,60 @@ __device__ inline uint32_t weight_key(float w, bool safe) {
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / 64;
 constexpr int kRounds = 8;                               // of four slots to a thread
+constexpr int kPart = 256;                               // slots that a wavefront takes in a round
 constexpr int kSlab = kSelectThreads * 4 * kRounds;      // 32768 slots
 constexpr int kBins = 2048;                              // digits of 11, 11 and 10 bits
 
-// the keys of a thread's slots of a slab: slots slab + 4096 round + 4 tid + 0 .. 3.  Slots past the length get key 0, which
-// no slot in front of it has.
-struct Keys {
-  uint32_t k[kRounds][4];
-};
-
-__device__ inline void load_keys(const float *w, const int32_t *pos, int slab, int L, int recent_from, int sinks, Keys &keys) {
+// keys of four slots from s on; a slot past the length gets key 0, which no slot in front of it has
+__device__ inline void load_keys(const float *w, const int32_t *pos, int s, int L, bool vec, int recent_from, int sinks,
+                                 uint32_t (&key)[4], f32x4 &x, int32_t (&p)[4]) {
+  typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+  x = (f32x4){0.f, 0.f, 0.f, 0.f};
+  i32x4 y = {0, 0, 0, 0};
+  if (vec && s + 3 < L) {
+    x = *(const f32x4 *)(w + s);
+    y = *(const i32x4 *)(pos + s);
+  } else {
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int s = slab + (r * kSelectThreads + (int)threadIdx.x) * 4;
-    if (slab + r * kSelectThreads * 4 < L) {  // uniform
-      // the row's capacity is a multiple of the page size: slots one by one where that is no multiple of four
-      float x[4];
-      int32_t p[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] = s + e < L ? w[s + e] : 0.f;
-        p[e] = s + e < L ? pos[s + e] : 0;
+    for (int e = 0; e < 4; ++e)
+      if (s + e < L) {
+        x[e] = w[s + e];
+        y[e] = pos[s + e];
       }
+  }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) keys.k[r][e] = s + e < L ? weight_key(x[e], p[e] >= recent_from || p[e] < sinks) : 0u;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) keys.k[r][e] = 0u;
-    }
+  for (int e = 0; e < 4; ++e) {
+    p[e] = y[e];
+    key[e] = s + e < L ? weight_key(x[e], y[e] >= recent_from || y[e] < sinks) : 0u;
   }
 }
 
-// Ranks in slot order of a slab's flags, two kinds at once: `n[r]` of a thread's round r holds their numbers (low and high half), and
-// becomes the number in front of the thread's first slot.  `total` counts the slab's.  A round's sum stays below 2^16.
-__device__ inline void slab_ranks(uint32_t (&n)[kRounds], uint32_t (*sums)[kSelectWaves], int (&total)[2]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t up[kRounds];
+// number of the wavefront's slots in front of this lane's first one that a flag of theirs is set for: flag e of a lane is slot
+// 4 lane + e; and of all
+__device__ inline int lanes_before(const unsigned long long (&m)[4]) {
+  int n = 0;
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) up[r] = n[r];
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1)
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      const uint32_t y = (uint32_t)__shfl_up((int)up[r], o, 64);
-      up[r] += lane >= o ? y : 0u;
-    }
-  __syncthreads();
-  if (lane == 63)
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) sums[r][wave] = up[r];
-  __syncthreads();
-  // every wavefront sums the (round, wavefront) totals in order: lane l those of round l / 8, wavefronts 2 (l % 8) and the next
-  uint32_t a = sums[lane >> 3][(lane & 7) * 2], b = sums[lane >> 3][(lane & 7) * 2 + 1];
-  int lo = (int)((a & 0xffffu) + (b & 0xffffu)), hi = (int)((a >> 16) + (b >> 16));
-  const int lo0 = lo, hi0 = hi;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int x = __shfl_up(lo, o, 64), y = __shfl_up(hi, o, 64);
-    lo += lane >= o ? x : 0;
-    hi += lane >= o ? y : 0;
-  }
-  total[0] = __shfl(lo, 63, 64);
-  total[1] = __shfl(hi, 63, 64);
-  const int lo_before = lo - lo0, hi_before = hi - hi0;
-#pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int at = r * 8 + (wave >> 1);
-    const uint32_t odd = (wave & 1) ? sums[r][wave & ~1] : 0u;
-    const int x = __shfl(lo_before, at, 64) + (int)(odd & 0xffffu) + (int)((up[r] - n[r]) & 0xffffu);
-    const int y = __shfl(hi_before, at, 64) + (int)(odd >> 16) + (int)((up[r] - n[r]) >> 16);
-    n[r] = (uint32_t)x | ((uint32_t)y << 16);  // both at most 32768, and only then is there no other
-  }
+  for (int e = 0; e < 4; ++e) n += __builtin_amdgcn_mbcnt_hi((uint32_t)(m[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m[e], 0));
+  return n;
+}
+__device__ inline int all_of(const unsigned long long (&m)[4]) {
+  return __popcll(m[0]) + __popcll(m[1]) + __popcll(m[2]) + __popcll(m[3]);
 }
 
-// One workgroup per (sequence, head): which positions stay.  The least key that stays is found digit by digit (11 bits, a
-// histogram each: the eight of the exponent alone would send most weights to a few counters); of the positions that have just this
-// key the first ones stay.  Kept positions in front of the new length stay in their slot; the others are listed, and so are the
-// slots that come free in front of it.
-// What bounds it is one CU's way to a row of weights and positions, and the steps in a row.  Up to 32768 slots their keys stay in
-// registers; longer rows are read again for every digit.
+// slots in which vectors of four may be loaded
+__device__ inline bool in_fours(const Kv4EvictArgs &a, size_t cap) {
+  return cap % 4 == 0 && (((uintptr_t)a.weight | (uintptr_t)a.pos) & 15) == 0;
+}
+
+// One workgroup per (sequence, head) finds the least key that stays, digit by digit (11 bits, a histogram each: the exponent's eight
+// alone would send most weights to a few counters), how many of the positions that have it stay (the first ones do), and how
+// many stay in front of every 256 slots.  A CU's vector instructions bound it (32768 slots: 32 keys to a thread), so
+// what can be done by more CUs is left to the next launch.  Up to 32768 slots their keys stay in registers; longer rows are
+// read again for every digit.
 __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs a) {
   const hb_attn_desc &d = a.d;
   __shared__ int hist[kBins], s_sum[kSelectWaves];
-  __shared__ uint32_t sums[kRounds][kSelectWaves];
+  __shared__ int s_above[kRounds * kSelectWaves], s_ties[kRounds * kSelectWaves];
   __shared__ int s_digit, s_need;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x / d.num_kv_heads;
   const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
@@ -238,27 +209,44 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs
   const float *w = a.weight + (size_t)blockIdx.x * cap;
   const int32_t *pos = a.pos + (size_t)blockIdx.x * cap;
   const int recent_from = a.seq_len[b] - a.recent;
-  if (tid == 0 && blockIdx.x % d.num_kv_heads == 0 && a.new_len) a.new_len[b] = stays;
+  const bool vec = in_fours(a, cap);
+  if (tid == 0) {
+    if (blockIdx.x % d.num_kv_heads == 0 && a.new_len) a.new_len[b] = stays;
+    if (stays == L) a.counts[blockIdx.x] = 0;  // else the next launch counts
+  }
   const int slabs = (L + kSlab - 1) / kSlab;
-  Keys keys;
-  if (slabs == 1) load_keys(w, pos, 0, L, recent_from, a.sinks, keys);
+  uint32_t keys[kRounds][4];
+  auto load = [&](int slab) {
+    f32x4 x;
+    int32_t p[4];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      const int s = slab * kSlab + r * kSelectThreads * 4;
+      keys[r][0] = keys[r][1] = keys[r][2] = keys[r][3] = 0;
+      if (s < L) load_keys(w, pos, s + tid * 4, L, vec, recent_from, a.sinks, keys[r], x, p);  // uniform
+    }
+  };
+  if (slabs == 1) load(0);
   uint32_t least = 0;  // the least key that stays, as far as it is known
-  int need = stays;    // positions with that key that stay
+  int need = 0;        // positions with that key that stay
   if (stays < L) {
+    need = stays;
     for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048, known = pass == 2 ? 10 : 21;
       for (int i = tid; i < bins; i += kSelectThreads) hist[i] = 0;
       __syncthreads();
       for (int slab = 0; slab < slabs; ++slab) {
-        if (slabs > 1) load_keys(w, pos, slab * kSlab, L, recent_from, a.sinks, keys);
+        if (slabs > 1) load(slab);
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r)
+        for (int r = 0; r < kRounds; ++r) {
+          if (slab * kSlab + r * kSelectThreads * 4 >= L) break;  // uniform
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const uint32_t k = keys.k[r][e];
-            const bool in = k != 0 && (pass == 0 || (k >> (pass == 1 ? 21 : 10)) == (least >> (pass == 1 ? 21 : 10)));
-            if (in) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1);
+            const uint32_t k = keys[r][e];
+            // (the slots past the length fall into counter 0, which is above every position's digit: never reached)
+            if (pass == 0 || ((k ^ least) >> known) == 0) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1);
           }
+        }
       }
       __syncthreads();
       // a thread's two counters, the largest digits first: the digit is where their running sum passes `need`
@@ -285,71 +273,115 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs
       __syncthreads();
     }
   }
-  int32_t *kept = a.kept + (size_t)blockIdx.x * a.budget;
-  int32_t *from = a.moves + (size_t)blockIdx.x * 2 * a.budget, *to = from + a.budget;
-  int ties = 0, freed = 0, above = 0;
-  for (int slab = 0; slab < slabs; ++slab) {
-    if (slabs > 1) load_keys(w, pos, slab * kSlab, L, recent_from, a.sinks, keys);
-    uint32_t n[kRounds];
-    int total[2] = {0, 0};
-    // ranks among the positions that have the least key
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      n[r] = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) n[r] += keys.k[r][e] == least ? 1u : 0u;
-    }
-    if (stays < L) slab_ranks(n, sums, total);
-    uint32_t stay = 0;  // bit 4 r + e
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      int rank = ties + (int)(n[r] & 0xffffu);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t k = keys.k[r][e];
-        const bool tie = k == least;
-        if (k != 0 && (stays == L || k > least || (tie && rank < need))) stay |= 1u << (4 * r + e);
-        rank += tie ? 1 : 0;
-      }
-    }
-    ties += total[0];
-    // ranks among the slots that come free (low half) and the positions that leave theirs (high half)
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      n[r] = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int s = slab * kSlab + (r * kSelectThreads + tid) * 4 + e;
-        const bool in = (stay >> (4 * r + e)) & 1;
-        n[r] += s < stays ? (in ? 0u : 1u) : (in ? 0x10000u : 0u);
-      }
-    }
-    if (stays < L) slab_ranks(n, sums, total);
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      int f = freed + (int)(n[r] & 0xffffu), m = above + (int)(n[r] >> 16);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int s = slab * kSlab + (r * kSelectThreads + tid) * 4 + e;
-        const bool in = (stay >> (4 * r + e)) & 1;
-        if (s < stays) {
-          if (in) {
-            kept[s] = s;
-            a.weight_out[(size_t)blockIdx.x * cap + s] = w[s];
-            a.pos_out[(size_t)blockIdx.x * cap + s] = pos[s];
-          } else {
-            to[f++] = s;
-          }
-        } else if (in) {
-          from[m++] = s;
-        }
-      }
-    }
-    freed += total[0];
-    above += total[1];
+  if (tid == 0) {
+    a.least[blockIdx.x * 2] = (int32_t)least;
+    a.least[blockIdx.x * 2 + 1] = need;
   }
-  for (int s = stays + tid; s < a.budget; s += kSelectThreads) kept[s] = -1;
-  if (tid == 0) a.counts[blockIdx.x] = stays < L ? above : 0;
+  int32_t *parts = a.parts + (size_t)blockIdx.x * a.parts_each * 2;
+  int above = 0, ties = 0;  // in front of the slab
+  for (int slab = 0; slab < slabs; ++slab) {
+    if (slabs > 1) load(slab);
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      unsigned long long ma[4], mt[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        ma[e] = __ballot(keys[r][e] > least);
+        mt[e] = __ballot(keys[r][e] == least && least != 0);
+      }
+      if (lane == 0) {
+        s_above[r * kSelectWaves + wave] = all_of(ma);
+        s_ties[r * kSelectWaves + wave] = all_of(mt);
+      }
+    }
+    __syncthreads();
+    if (wave < 2) {  // 64 parts each, on the line of the slab's 128
+      const int i = wave * 64 + lane;
+      int x = s_above[i], y = s_ties[i];
+      int head_x = 0, head_y = 0;
+      if (wave == 1)
+        for (int q = 0; q < 64; ++q) {
+          head_x += s_above[q];
+          head_y += s_ties[q];
+        }
+      const int x0 = x, y0 = y;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(x, o, 64), v = __shfl_up(y, o, 64);
+        x += lane >= o ? u : 0;
+        y += lane >= o ? v : 0;
+      }
+      const int part = slab * (kSlab / kPart) + i;
+      if (part < a.parts_each) {
+        parts[part * 2] = above + head_x + x - x0;
+        parts[part * 2 + 1] = ties + head_y + y - y0;
+      }
+      if (i == 127) {
+        s_sum[0] = above + head_x + x;
+        s_sum[1] = ties + head_y + y;
+      }
+    }
+    __syncthreads();
+    above = s_sum[0];
+    ties = s_sum[1];
+    __syncthreads();
+  }
+}
+
+// What stays where, 256 slots to a wavefront: kept positions in front of the new length stay in their slot; the others are
+// listed from the last one on, the slots that come free from the first.
+__global__ __launch_bounds__(256) void kv4_list_kernel(Kv4EvictArgs a) {
+  const hb_attn_desc &d = a.d;
+  const int lane = threadIdx.x & 63, unit = blockIdx.y, b = unit / d.num_kv_heads;
+  const int part = blockIdx.x * 4 + (threadIdx.x >> 6), s0 = part * kPart;
+  const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
+  const int L = kv4_length(d, a.prefix_len, b), stays = L < a.budget ? L : a.budget;
+  int32_t *kept = a.kept + (size_t)unit * a.budget;
+  for (long s = stays + s0 + lane; s < (long)stays + s0 + kPart && s < a.budget; s += 64) kept[s] = -1;
+  // (budgets beyond the row: the last workgroup's part goes on to their end)
+  if (part == (int)gridDim.x * 4 - 1)
+    for (long s = (long)stays + s0 + kPart + lane; s < a.budget; s += 64) kept[s] = -1;
+  if (s0 >= L) return;
+  const int32_t *before = a.parts + ((size_t)unit * a.parts_each + part) * 2;
+  const uint32_t least = (uint32_t)a.least[unit * 2];
+  const int need = a.least[unit * 2 + 1], above = before[0], ties = before[1];
+  const float *w = a.weight + unit * cap;
+  const int32_t *pos = a.pos + unit * cap;
+  uint32_t key[4];
+  f32x4 x;
+  int32_t p[4];
+  const int s = s0 + lane * 4;
+  load_keys(w, pos, s, L, in_fours(a, cap), a.seq_len[b] - a.recent, a.sinks, key, x, p);
+  unsigned long long m[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) m[e] = __ballot(key[e] == least && least != 0);
+  int tie = ties + lanes_before(m);
+  bool stay[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bool t = key[e] == least && least != 0;
+    stay[e] = key[e] > least || (t && tie < need);
+    tie += t ? 1 : 0;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) m[e] = __ballot(stay[e]);
+  int n = above + min(ties, need) + lanes_before(m);  // that stay in front of slot s + e
+  int32_t *from = a.moves + (size_t)unit * 2 * a.budget, *to = from + a.budget;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int at = s + e;
+    if (at == stays && at < L) a.counts[unit] = stays - n;
+    if (stay[e] && at < stays) {
+      kept[at] = at;
+      a.weight_out[unit * cap + at] = x[e];
+      a.pos_out[unit * cap + at] = p[e];
+    } else if (stay[e]) {
+      from[stays - 1 - n] = at;
+    } else if (at < stays) {
+      to[at - n] = at;
+    }
+    n += stay[e] ? 1 : 0;
+  }
 }
 
 // Rows of K and V to the slots that came free for them: a lane takes a block of K or V (16 bytes and a scale), 2 D / 32 lanes a
@@ -359,11 +391,12 @@ __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4EvictArgs a) {
   const int blocks = d.head_dim / kKv4Block, lanes = 2 * blocks, each = 64 / lanes;
   const int lane = threadIdx.x & 63, part = lane % lanes, unit = blockIdx.y;
   const int i = ((int)blockIdx.x * 4 + (threadIdx.x >> 6)) * each + lane / lanes;
-  if (lane >= each * lanes || i >= a.counts[unit]) return;
+  const int count = a.counts[unit];
+  if (lane >= each * lanes || i >= count) return;
   const int b = unit / d.num_kv_heads, h = unit % d.num_kv_heads;
   const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
   const int32_t *moves = a.moves + (size_t)unit * 2 * a.budget;
-  const int src = moves[i], dst = moves[a.budget + i];
+  const int src = moves[count - 1 - i], dst = moves[a.budget + i];
   const size_t s = kv4_row(d, a.block_table, b, h, src), t = kv4_row(d, a.block_table, b, h, dst);
   const bool value = part >= blocks;
   const int blk = value ? part - blocks : part;
@@ -405,10 +438,14 @@ hipError_t launch_kv4_read(const hb_attn_desc &d, int32_t rows, const Kv4Pool &k
   return hipGetLastError();
 }
 
-hipError_t launch_kv4_evict(const Kv4EvictArgs &a, hipStream_t s) {
+hipError_t launch_kv4_evict(const Kv4EvictArgs &a, int64_t longest, hipStream_t s) {
   const int units = a.d.batch * a.d.num_kv_heads;
   kv4_select_kernel<<<units, kSelectThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t most = (int64_t)a.d.max_blocks_per_seq * a.d.page_size, span = most < longest ? most : longest;
+  kv4_list_kernel<<<dim3((unsigned)((span + 4 * kPart - 1) / (4 * kPart)), (unsigned)units), 256, 0, s>>>(a);
+  e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int each = 4 * (64 / (2 * (a.d.head_dim / kKv4Block)));  // moves of a workgroup
   kv4_move_kernel<<<dim3((unsigned)((a.budget + each - 1) / each), (unsigned)units), 256, 0, s>>>(a);
