@@ -257,8 +257,9 @@ struct Kv4EvictArgs {
   // least key that stays and how many that have it do; in front of every 256 slots, how many have a greater key and how many this
   int32_t *moves, *counts, *least, *parts;
   int32_t parts_each;
+  int32_t longest;  // no prefix is longer
 };
-hipError_t launch_kv4_evict(const Kv4EvictArgs &a, int64_t longest, hipStream_t s);  // longest: no prefix is longer
+hipError_t launch_kv4_evict(const Kv4EvictArgs &a, hipStream_t s);
 
 // ---- argmax key: (order-preserving float bits << 32) | (0xffffffff - index) ---------------
 // max over keys = largest value, lowest index among equal values.  NaN is mapped to -inf.

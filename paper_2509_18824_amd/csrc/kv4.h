@@ -33,6 +33,7 @@ struct Kv4Plan {
   int32_t row_groups;   // workgroups that share a chunk's query rows
   int32_t grain;        // keys that a chunk's length is a multiple of
   int32_t target;       // chunks per kv head, over all sequences
+  int32_t over;         // of these, what is left for sequences' last chunks, which are short
   int32_t splits;       // chunks of a sequence, at most: slots of part_o and part_ml
   uint32_t page_magic;  // ceil(2^32 / (page_size / 16)), 0 where that is one
 };

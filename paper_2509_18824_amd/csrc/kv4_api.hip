@@ -248,8 +248,8 @@ int32_t hb_kv4_evict(const hb_attn_desc *desc, int32_t budget, int32_t recent, i
   Kv4EvictArgs a = {*desc, budget, recent, sinks, (uint8_t *)k_codes, (uint8_t *)k_scales, (uint8_t *)v_codes, (uint8_t *)v_scales,
                     block_table, prefix_len, seq_len, weight, pos, weight_out, pos_out, kept, new_len, (int32_t *)workspace,
                     (int32_t *)((char *)workspace + at.counts), (int32_t *)((char *)workspace + at.least),
-                    (int32_t *)((char *)workspace + at.parts_at), (int32_t)at.parts};
-  HB_HIP_TRY(launch_kv4_evict(a, span_of(desc), (hipStream_t)stream));
+                    (int32_t *)((char *)workspace + at.parts_at), (int32_t)at.parts, (int32_t)span_of(desc)};
+  HB_HIP_TRY(launch_kv4_evict(a, (hipStream_t)stream));
   return HB_OK;
 }
 

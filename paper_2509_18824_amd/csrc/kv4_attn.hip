@@ -19,6 +19,9 @@
 // Chunks are cut on the device from the lengths (kv4_plan below), so that about as many workgroups start as the host planned
 // for, whatever the lengths are.
 #include "kv4.h"
+#include "wave_ops.h"
+
+#include <type_traits>
 
 namespace hb {
 
@@ -36,6 +39,7 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int swap2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStep = 32;  // keys
+constexpr int kWaves = 4;  // of a workgroup
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;  // log2 units a score may exceed its row's reference
@@ -122,68 +126,93 @@ struct Tile {
   uint32_t ks[2], vs[2];
 };
 
-// Where the workgroup's chunk lies
+// Where the workgroup's chunk lies, and the sequence's nodes
 struct Chunk {
-  int b, c, chunks, L, begin, end;
+  int b, c, chunks, L, begin, end, n0, n;
 };
 
-// Chunks of all sequences on one line: as many as `target`, each of the same number of steps (a multiple of `grain`) and no
-// sequence in more than `slots`; a sequence without a prefix has one too, for its tree.  Returns the chunk's length in keys.  Every
-// workgroup finds it by itself from the lengths; lane i holds a sequence.
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-  return x;
-}
-__device__ __forceinline__ int wave_most(int x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o, 64));
-  return x;
-}
-__device__ int kv4_chunk_length(const hb_attn_desc &d, const int32_t *__restrict__ prefix_len, const Kv4Plan &plan) {
-  const int lane = threadIdx.x & 63;
-  int steps = 0, longest = 0;
-  for (int b = lane; b < d.batch; b += 64) {
-    const int L = kv4_length(d, prefix_len, b), n = (L + plan.grain - 1) / plan.grain;
-    steps += n;
-    longest = max(longest, n);
-  }
-  steps = wave_sum(steps);
-  longest = wave_most(longest);
-  int len = (steps + plan.target - 1) / plan.target;
+__device__ __forceinline__ int kv4_chunks(int L, int len) { return L > 0 ? (L + len - 1) / len : 1; }
+
+// Chunks of all sequences on one line: as many as `target`, each of the same length (a multiple of `grain` keys) and no
+// sequence in more than `splits`; a sequence without a prefix has one too, for its tree.  Every workgroup finds the length by
+// itself from the sequences' lengths, a sequence to a lane.
+__device__ __forceinline__ int chunk_length(int grains, int longest, const Kv4Plan &plan) {
+  const int target = plan.target - plan.over;
+  int len = (grains + target - 1) / target;
   const int least = (longest + plan.splits - 1) / plan.splits;
   len = len < least ? least : len;
   return (len < 1 ? 1 : len) * plan.grain;
 }
-__device__ __forceinline__ int kv4_chunks(int L, int len) { return L > 0 ? (L + len - 1) / len : 1; }
+__device__ __forceinline__ int grains_of(int L, const Kv4Plan &plan) { return (L + plan.grain - 1) / plan.grain; }
+__device__ int chunk_length(const hb_attn_desc &d, const int32_t *__restrict__ prefix_len, const Kv4Plan &plan) {
+  int grains = 0, longest = 0;
+  for (int b0 = 0; b0 < d.batch; b0 += 64) {
+    const int b = b0 + (threadIdx.x & 63), n = b < d.batch ? grains_of(kv4_length(d, prefix_len, b), plan) : 0;
+    grains += sum_lanes(n);
+    longest = max(longest, max_lanes(n));
+  }
+  return chunk_length(grains, longest, plan);
+}
 
-// the chunk with index `unit` on the line
-__device__ bool kv4_find(const hb_attn_desc &d, const int32_t *__restrict__ prefix_len, int len, int unit, Chunk &c) {
+// the chunk with index `unit` on the line; false behind its end
+__device__ __forceinline__ bool find_chunk(const Kv4AttnArgs &a, const Kv4Plan &plan, int unit, Chunk &c) {
+  const hb_attn_desc &d = a.d;
   const int lane = threadIdx.x & 63;
+  // up to 64 sequences: lengths and offsets in one go
+  int L = 0, n0 = 0, n1 = 0, len;
+  if (lane < d.batch) {
+    L = kv4_length(d, a.prefix_len, lane);
+    n0 = a.node_offset[lane];
+    n1 = a.node_offset[lane + 1];
+  }
+  if (d.batch <= 64) {
+    const int n = grains_of(L, plan);
+    len = chunk_length(sum_lanes(n), max_lanes(n), plan);
+  } else {
+    len = chunk_length(d, a.prefix_len, plan);
+  }
   int before = 0;
   for (int b0 = 0; b0 < d.batch; b0 += 64) {
-    const int b = b0 + lane, L = b < d.batch ? kv4_length(d, prefix_len, b) : 0;
-    const int n = b < d.batch ? kv4_chunks(L, len) : 0;
-    int up = n;  // inclusive sum over the lanes
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(up, o, 64);
-      up += lane >= o ? y : 0;
+    const int b = b0 + lane;
+    if (b0) {
+      L = b < d.batch ? kv4_length(d, a.prefix_len, b) : 0;
+      n0 = b < d.batch ? a.node_offset[b] : 0;
+      n1 = b < d.batch ? a.node_offset[b + 1] : 0;
     }
+    const int n = b < d.batch ? kv4_chunks(L, len) : 0;
+    const int up = scan_lanes(n);
     const unsigned long long behind = __ballot(before + up > unit);
     if (behind) {
       const int who = __builtin_ctzll(behind);
       c.b = b0 + who;
-      c.L = __builtin_amdgcn_readfirstlane(__shfl(L, who, 64));
-      c.chunks = __builtin_amdgcn_readfirstlane(__shfl(n, who, 64));
-      c.c = unit - before - __builtin_amdgcn_readfirstlane(__shfl(up - n, who, 64));
+      c.L = __builtin_amdgcn_readlane(L, who);
+      c.chunks = __builtin_amdgcn_readlane(n, who);
+      c.c = unit - before - __builtin_amdgcn_readlane(up - n, who);
       c.begin = c.c * len;
       c.end = min(c.L, c.begin + len);
+      c.n0 = __builtin_amdgcn_readlane(n0, who);
+      c.n = __builtin_amdgcn_readlane(n1, who) - c.n0;
+      c.n = c.n < 0 ? 0 : c.n > d.max_nodes_per_tree ? d.max_nodes_per_tree : c.n;
+      if (c.n0 < 0 || c.n0 + c.n > d.total_nodes) c.n = 0;  // malformed offsets: touch nothing
       return true;
     }
     before += __builtin_amdgcn_readlane(up, 63);
   }
   return false;
+}
+
+// Nodes on the path of node `lane`, by doubling: a node's mask and the ancestor that it does not hold yet
+__device__ __forceinline__ unsigned long long path_of(int par, int lane, int n) {
+  unsigned long long path = lane < n ? 1ull << lane : 0ull;
+  int up = lane < n && par < lane ? par : -1;
+  for (int i = 0; i < 6 && __any(up >= 0); ++i) {
+    const int from = up < 0 ? 0 : up;
+    const unsigned long long p = ((unsigned long long)(uint32_t)__shfl((int)(path >> 32), from, 64) << 32) | (uint32_t)__shfl((int)path, from, 64);
+    const int next = __shfl(up, from, 64);
+    path |= up < 0 ? 0ull : p;
+    up = up < 0 ? -1 : next;
+  }
+  return path;
 }
 
 template <int TPW, int DB>
@@ -302,7 +331,8 @@ __device__ __forceinline__ void put_values(unsigned char *lv, int key, int kg, c
 }
 
 template <int TPW, int DB, int W>
-__global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4Plan plan) {
+__global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4Plan plan,
+                                                                       const int32_t *__restrict__ block_table) {
   constexpr int D = 32 * DB, kRow = 64 * DB;
   const hb_attn_desc &d = a.d;
   // values: 32 keys to a wavefront; at the end a tile's sums of all wavefronts; then references and sums
@@ -315,12 +345,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   const int rg = slot % plan.row_groups, unit = (slot / plan.row_groups) * 8 + (id & 7);
   const int g = unit % d.num_kv_heads, G = d.num_q_heads / d.num_kv_heads;
   Chunk ch;
-  const int len = kv4_chunk_length(d, a.prefix_len, plan);
-  if (!kv4_find(d, a.prefix_len, len, unit / d.num_kv_heads, ch)) return;
-  const int n0 = a.node_offset[ch.b];
-  int n = a.node_offset[ch.b + 1] - n0;
-  n = n < 0 ? 0 : n > d.max_nodes_per_tree ? d.max_nodes_per_tree : n;
-  if (n0 < 0 || n0 + n > d.total_nodes) n = 0;  // malformed offsets: touch nothing
+  if (!find_chunk(a, plan, unit / d.num_kv_heads, ch)) return;
+  const int n0 = ch.n0, n = ch.n;
   const int R = n * G, tile0 = rg * TPW;
   if (tile0 * 16 >= R) return;
   const size_t row_base = (size_t)n0 * d.num_q_heads + (size_t)g * G;
@@ -328,6 +354,51 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
     const int node = small_div(row, G);
     return row_base + (size_t)node * d.num_q_heads + (row - node * G);
   };
+
+  // The prefix: the codes of a step, and the pages of the step behind the one that was asked for last.  Steps past the chunk's
+  // end ask for its last keys again.
+  const int steps = ch.end > ch.begin ? (ch.end - ch.begin + kStep - 1) / kStep : 0;
+  // (a parameter of its own, which nothing that is written can be: then its entries come by scalar loads.  By vector loads
+  // each wait for one is a wait for all codes on their way)
+  const int32_t *table = block_table + (size_t)ch.b * d.max_blocks_per_seq;
+  const int first16 = ch.begin >> 4, last16 = (ch.end - 1) >> 4;
+  size_t next[2];  // rows of a pool: where the step's two halves begin
+  auto find = [&](int step) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at16 = min(first16 + 2 * step + h, last16);  // 16 keys lie in one page
+      const int page = plan.page_magic ? (int)__umulhi((uint32_t)at16, plan.page_magic) : at16;
+      int blk = table[page];
+      blk = blk < 0 ? 0 : (blk >= d.num_blocks ? d.num_blocks - 1 : blk);
+      next[h] = ((size_t)blk * d.num_kv_heads + g) * d.page_size + (at16 * 16 - page * d.page_size);
+    }
+  };
+  auto load = [&](int step, Tile &x) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const size_t codes = next[h] * (D / 2), scales = next[h] * DB;
+      if (DB == 4 || kg < DB) {
+        x.k[h] = *(const u32x4 *)(a.kp.codes + codes + j * (D / 2) + kg * 16);
+        x.v[h] = *(const u32x4 *)(a.vp.codes + codes + j * (D / 2) + kg * 16);
+        x.ks[h] = *(a.kp.scales + scales + j * DB + kg);
+        x.vs[h] = *(a.vp.scales + scales + j * DB + kg);
+      }
+    }
+    find(step + W);
+  };
+  Tile x, y;
+  if (DB < 4) {  // lanes without a block
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      x.k[h] = y.k[h] = x.v[h] = y.v[h] = (u32x4){0u, 0u, 0u, 0u};
+      x.ks[h] = y.ks[h] = x.vs[h] = y.vs[h] = 127;
+    }
+  }
+  if (wave < steps) {
+    find(wave);
+    load(wave, x);
+    load(wave + W, y);
+  }
 
   Rows<TPW, DB> w;
 #pragma unroll
@@ -356,20 +427,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   // ---- the nodes' own keys: 32 to a wavefront, chunk 0 only ------------------------------------------
   if (ch.c == 0 && wave < (n + 31) / 32) {
     const int first = 32 * wave;
-    // node `first + i` is seen by the rows whose path it lies on; lane i walks node i's path
-    unsigned long long path = 0;
-    {
-      const int par = lane < n ? a.parent[n0 + lane] : -1;
-      path = lane < n ? 1ull << lane : 0ull;
-      int x = lane < n ? lane : -1;
-      for (int guard = 0; guard < 64; ++guard) {
-        const int px = __shfl(par, x < 0 ? 0 : x, 64);
-        const bool up = x >= 0 && px >= 0 && px < x;
-        if (!__any(up)) break;
-        if (up) path |= 1ull << px;
-        x = up ? px : -1;
-      }
-    }
+    // node `first + i` is seen by the rows whose path it lies on; lane i holds node i's
+    const unsigned long long path = path_of(lane < n ? a.parent[n0 + lane] : -1, lane, n);
     const uint32_t mine = (uint32_t)(path >> first);
     f32x4 sc[TPW][2];
     bf16x8 ak[2][DB];
@@ -416,73 +475,57 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   }
 
   // ---- the prefix -------------------------------------------------------------------------------------
-  const int steps = ch.end > ch.begin ? (ch.end - ch.begin + kStep - 1) / kStep : 0;
-  if (wave < steps) {
-    const int32_t *table = a.block_table + (size_t)ch.b * d.max_blocks_per_seq;
-    const int last16 = (ch.end - 1) >> 4;
-    // 16 keys to a lane's row of blocks: keys p0 + j, which lie in one page
-    auto load_half = [&](int at16, u32x4 &k, u32x4 &v, uint32_t &ks, uint32_t &vs) {
-      at16 = min(at16, last16);
-      const int page = plan.page_magic ? (int)__umulhi((uint32_t)at16, plan.page_magic) : at16;
-      int blk = table[page];
-      blk = blk < 0 ? 0 : (blk >= d.num_blocks ? d.num_blocks - 1 : blk);
-      const size_t row = ((size_t)blk * d.num_kv_heads + g) * d.page_size + (at16 * 16 - page * d.page_size);
-      const size_t codes = row * (D / 2), scales = row * DB;
-      const bool there = DB == 4 || kg < DB;
-      k = v = (u32x4){0u, 0u, 0u, 0u};
-      ks = vs = 127;
-      if (there) {
-        k = *(const u32x4 *)(a.kp.codes + codes + j * (D / 2) + kg * 16);
-        v = *(const u32x4 *)(a.vp.codes + codes + j * (D / 2) + kg * 16);
-        ks = *(a.kp.scales + scales + j * DB + kg);
-        vs = *(a.vp.scales + scales + j * DB + kg);
-      }
-    };
-    auto load = [&](int step, Tile &x) {
-      const int at16 = (ch.begin >> 4) + 2 * step;
+  // left: keys of the step, 32 of them unless it is the sequence's last
+  auto attend = [&](auto tail, int step, Tile &x, int left) {
+    constexpr bool kTail = decltype(tail)::value;
+    f32x4 sc[TPW][2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) load_half(at16 + h, x.k[h], x.v[h], x.ks[h], x.vs[h]);
-    };
-    auto attend = [&](int step, Tile &x) {
-      const int left = ch.end - (ch.begin + step * kStep);  // keys of this step and behind it
-      f32x4 sc[TPW][2];
+    for (int t = 0; t < TPW; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const i32x8 ak = {(int)x.k[h][0], (int)x.k[h][1], (int)x.k[h][2], (int)x.k[h][3], 0, 0, 0, 0};
+        sc[t][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ak, w.q[t].lo, (f32x4){0.f, 0.f, 0.f, 0.f}, 4, 0, 0, (int)x.ks[h], 0, w.q[t].lo_scale);
+        sc[t][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ak, w.q[t].hi, sc[t][h], 4, 0, 0, (int)x.ks[h], 0, w.q[t].hi_scale);
+      }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4 c = x.v[h];
+      uint32_t s = x.vs[h];
+      if (kTail) {  // whatever lies behind the end: its weight is 0, and must not make that 0 * NaN
+        const bool there = 16 * h + j < left;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = there ? c[e] : 0u;
+        s = there ? s : 127u;
+      }
+      if (DB == 4 || kg < DB) put_values<DB>(lv, 16 * h + j, kg, c, s);
+    }
+    if (kTail) {
 #pragma unroll
       for (int t = 0; t < TPW; ++t)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const i32x8 ak = {(int)x.k[h][0], (int)x.k[h][1], (int)x.k[h][2], (int)x.k[h][3], 0, 0, 0, 0};
-          sc[t][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ak, w.q[t].lo, (f32x4){0.f, 0.f, 0.f, 0.f}, 4, 0, 0, (int)x.ks[h], 0, w.q[t].lo_scale);
-          sc[t][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ak, w.q[t].hi, sc[t][h], 4, 0, 0, (int)x.ks[h], 0, w.q[t].hi_scale);
-        }
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int key = 16 * h + j;
-        const bool there = key < left;
-        u32x4 c = x.v[h];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] = there ? c[e] : 0u;
-        if (DB == 4 || kg < DB) put_values<DB>(lv, key, kg, c, there ? x.vs[h] : 127u);
-      }
+          for (int r = 0; r < 4; ++r) sc[t][h][r] = 16 * h + 4 * kg + r < left ? sc[t][h][r] : kNegInf;
+    } else {
       load(step + 2 * W, x);
-      if (left < kStep) {  // uniform
-#pragma unroll
-        for (int t = 0; t < TPW; ++t)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) sc[t][h][r] = 16 * h + 4 * kg + r < left ? sc[t][h][r] : kNegInf;
-      }
-      f32x8 p[TPW];
-      weigh<TPW, DB>(w, sc, c1, p);
-      weigh_values<TPW, DB>(w, lv, j, kg, p, left < kStep);
-    };
-    Tile x, y;
-    load(wave, x);
-    load(wave + W, y);
-    for (int step = wave; step < steps; step += 2 * W) {
-      attend(step, x);
-      if (step + W < steps) attend(step + W, y);
     }
+    f32x8 p[TPW];
+    weigh<TPW, DB>(w, sc, c1, p);
+    weigh_values<TPW, DB>(w, lv, j, kg, p, kTail);
+  };
+  if (wave < steps) {
+    const int whole = (ch.end - ch.begin) / kStep;
+    int step = wave;
+    for (; step + W < whole; step += 2 * W) {
+      attend(std::false_type(), step, x, kStep);
+      attend(std::false_type(), step + W, y, kStep);
+    }
+    if (step < whole) {
+      attend(std::false_type(), step, x, kStep);
+      step += W;
+      x = y;
+    }
+    if (step < steps) attend(std::true_type(), step, x, ch.end - ch.begin - step * kStep);
   }
 
   // ---- join the wavefronts' results --------------------------------------------------------------------
@@ -535,11 +578,11 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   }
 }
 
-// Rows of sequences that were cut: the chunks' results joined (log2 units).  Four rows of 128 to a workgroup; a row's
-// threads hold four elements each.
+// Rows of sequences that were cut: the chunks' results joined (log2 units).  A row's threads hold four elements each; results
+// are asked for eight chunks at a time.
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a, Kv4Plan plan) {
   const int D = a.d.head_dim, tpr = D / 4;
-  const int len = kv4_chunk_length(a.d, a.prefix_len, plan);
+  const int len = chunk_length(a.d, a.prefix_len, plan);
   const long gid = (long)blockIdx.x * 256 + threadIdx.x;
   const int row = (int)(gid / tpr), piece = (int)(gid - (long)row * tpr);
   if (row >= a.d.total_nodes * a.d.num_q_heads) return;
@@ -551,13 +594,31 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a, Kv4Plan pl
   const kv4_f32x2 *ml = (const kv4_f32x2 *)a.part_ml + (size_t)row * plan.splits;
   const f32x4 *po = (const f32x4 *)a.part_o + (size_t)row * plan.splits * tpr + piece;
   float m = kNegInf, l = 0.f;
-  for (int c = 0; c < chunks; ++c) m = fmaxf(m, ml[c][0]);
-  const float ref = m == kNegInf ? 0.f : m;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int c = 0; c < chunks; ++c) {
-    const float w = fast_exp2(ml[c][0] - ref);
-    l = fmaf(ml[c][1], w, l);
-    o += po[(size_t)c * tpr] * w;
+  for (int c0 = 0; c0 < chunks; c0 += 8) {
+    kv4_f32x2 x[8];
+    f32x4 y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int c = min(c0 + i, chunks - 1);
+      x[i] = ml[c];
+      y[i] = po[(size_t)c * tpr];
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i][0]);
+    const float ref = top == kNegInf ? 0.f : top, corr = fast_exp2(m - ref);
+    m = top;
+    l *= corr;
+    o *= corr;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (c0 + i < chunks) {
+        const float w = fast_exp2(x[i][0] - ref);
+        l = fmaf(x[i][1], w, l);
+        o += y[i] * w;
+      }
+    }
   }
   const float inv = 1.f / l;
   *(u32x2 *)((bf16_t *)a.out + (size_t)row * D + piece * 4) = (u32x2){pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
@@ -567,7 +628,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a, Kv4Plan pl
 template <int TPW, int DB, int W>
 hipError_t launch(const Kv4AttnArgs &a, const Kv4Plan &plan, hipStream_t s) {
   const long units = ((long)plan.target + a.d.batch) * a.d.num_kv_heads;  // chunks on the line, at most
-  kv4_attn_kernel<TPW, DB, W><<<(unsigned)((units + 7) / 8 * 8 * plan.row_groups), 64 * W, 0, s>>>(a, plan);
+  kv4_attn_kernel<TPW, DB, W><<<(unsigned)((units + 7) / 8 * 8 * plan.row_groups), 64 * W, 0, s>>>(a, plan, a.block_table);
   return hipGetLastError();
 }
 
@@ -584,7 +645,7 @@ static int tiles_of(const hb_attn_desc &d) { return (d.num_q_heads / d.num_kv_he
 void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
   const int tiles = tiles_of(d), tpw = tiles > 1 ? 2 : 1;
   plan->row_groups = (tiles + tpw - 1) / tpw;
-  plan->grain = 8 * kStep;
+  plan->grain = kWaves * kStep;
   int64_t target = 512 / ((int64_t)d.num_kv_heads * plan->row_groups);
   target = target < 1 ? 1 : target;
   int64_t splits = d.num_splits ? d.num_splits : target;
@@ -593,6 +654,7 @@ void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
   splits = splits < 1 ? 1 : splits > 1024 ? 1024 : splits;
   plan->target = (int32_t)(d.num_splits ? (int64_t)d.num_splits * d.batch > 1 << 16 ? 1 << 16 : d.num_splits * d.batch : target);
   plan->target = plan->target < 1 ? 1 : plan->target;
+  plan->over = !d.num_splits && plan->target > 2 * d.batch ? d.batch : 0;
   plan->splits = (int32_t)splits;
   const int page16 = d.page_size / 16;
   plan->page_magic = page16 == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + page16 - 1) / page16);
@@ -601,8 +663,8 @@ void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
 hipError_t launch_kv4_attn(const Kv4AttnArgs &a, const Kv4Plan &plan, hipStream_t s) {
   const bool wide = tiles_of(a.d) > 1;
   hipError_t e;
-  if (a.d.head_dim == 128) e = wide ? launch<2, 4, 8>(a, plan, s) : launch<1, 4, 8>(a, plan, s);
-  else e = wide ? launch<2, 2, 8>(a, plan, s) : launch<1, 2, 8>(a, plan, s);
+  if (a.d.head_dim == 128) e = wide ? launch<2, 4, kWaves>(a, plan, s) : launch<1, 4, kWaves>(a, plan, s);
+  else e = wide ? launch<2, 2, kWaves>(a, plan, s) : launch<1, 2, kWaves>(a, plan, s);
   if (e != hipSuccess || plan.splits == 1) return e;
   const long threads = (long)a.d.total_nodes * a.d.num_q_heads * (a.d.head_dim / 4);
   kv4_join_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(a, plan);

@@ -205,7 +205,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs
   __shared__ int s_digit, s_need;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x / d.num_kv_heads;
   const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
-  const int L = kv4_length(d, a.prefix_len, b), stays = L < a.budget ? L : a.budget;
+  const int L = min(kv4_length(d, a.prefix_len, b), a.longest), stays = L < a.budget ? L : a.budget;
   const float *w = a.weight + (size_t)blockIdx.x * cap;
   const int32_t *pos = a.pos + (size_t)blockIdx.x * cap;
   const int recent_from = a.seq_len[b] - a.recent;
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(256) void kv4_list_kernel(Kv4EvictArgs a) {
   const int lane = threadIdx.x & 63, unit = blockIdx.y, b = unit / d.num_kv_heads;
   const int part = blockIdx.x * 4 + (threadIdx.x >> 6), s0 = part * kPart;
   const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
-  const int L = kv4_length(d, a.prefix_len, b), stays = L < a.budget ? L : a.budget;
+  const int L = min(kv4_length(d, a.prefix_len, b), a.longest), stays = L < a.budget ? L : a.budget;
   int32_t *kept = a.kept + (size_t)unit * a.budget;
   for (long s = stays + s0 + lane; s < (long)stays + s0 + kPart && s < a.budget; s += 64) kept[s] = -1;
   // (budgets beyond the row: the last workgroup's part goes on to their end)
@@ -438,13 +438,12 @@ hipError_t launch_kv4_read(const hb_attn_desc &d, int32_t rows, const Kv4Pool &k
   return hipGetLastError();
 }
 
-hipError_t launch_kv4_evict(const Kv4EvictArgs &a, int64_t longest, hipStream_t s) {
+hipError_t launch_kv4_evict(const Kv4EvictArgs &a, hipStream_t s) {
   const int units = a.d.batch * a.d.num_kv_heads;
   kv4_select_kernel<<<units, kSelectThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t most = (int64_t)a.d.max_blocks_per_seq * a.d.page_size, span = most < longest ? most : longest;
-  kv4_list_kernel<<<dim3((unsigned)((span + 4 * kPart - 1) / (4 * kPart)), (unsigned)units), 256, 0, s>>>(a);
+  kv4_list_kernel<<<dim3((unsigned)((a.longest + 4 * kPart - 1) / (4 * kPart)), (unsigned)units), 256, 0, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int each = 4 * (64 / (2 * (a.d.head_dim / kKv4Block)));  // moves of a workgroup
