@@ -27,14 +27,17 @@ struct Kv4AttnArgs {
   const int32_t *block_table, *prefix_len, *node_offset, *parent;
   void *out;
   float *lse, *part_o, *part_ml;
+  int32_t *cut;  // the matrix-core kernels' chunk length, or null where they do not cut
 };
 // How the matrix-core kernel cuts the prefixes, from what the host knows
 struct Kv4Plan {
-  int32_t row_groups;   // workgroups that share a chunk's query rows
+  int32_t row_groups;   // workgroups that share a chunk's query rows, at most
   int32_t grain;        // keys that a chunk's length is a multiple of
-  int32_t target;       // chunks per kv head, over all sequences
-  int32_t over;         // of these, what is left for sequences' last chunks, which are short
+  int32_t group_rows;   // query rows of a row group
+  int32_t target;       // workgroups per kv head, over all sequences
+  int32_t fit;          // not more than these, if longer chunks can do it
   int32_t splits;       // chunks of a sequence, at most: slots of part_o and part_ml
+  int32_t grid;         // workgroups that are started
   uint32_t page_magic;  // ceil(2^32 / (page_size / 16)), 0 where that is one
 };
 bool kv4_attn_supports(const hb_attn_desc &d);

@@ -51,7 +51,7 @@ struct AttnCut {
   bool mfma;
   Kv4Plan plan;            // the matrix-core kernel's
   int32_t splits, chunk;   // slots of a row's partial results; the scalar kernel's chunk length
-  size_t ml_offset, bytes;
+  size_t ml_offset, cut_offset, bytes;
 };
 
 static int32_t make_cut(const hb_attn_desc *d, AttnCut *cut) {
@@ -79,7 +79,8 @@ static int32_t make_cut(const hb_attn_desc *d, AttnCut *cut) {
     cut->chunk = (int32_t)chunk;
   }
   cut->ml_offset = cut->splits > 1 ? round_up((size_t)rows * cut->splits * d->head_dim * 4, 256) : 0;
-  cut->bytes = cut->splits > 1 ? cut->ml_offset + round_up((size_t)rows * cut->splits * 8, 256) : 0;
+  cut->cut_offset = cut->splits > 1 ? cut->ml_offset + round_up((size_t)rows * cut->splits * 8, 256) : 0;
+  cut->bytes = cut->splits > 1 ? cut->cut_offset + 256 : 0;
   return HB_OK;
 }
 
@@ -174,7 +175,8 @@ int32_t hb_tree_verify_attn_kv4(const hb_attn_desc *desc, const void *q, const v
   }
   Kv4AttnArgs a = {*desc, cut.splits, cut.chunk, q, k_tree, v_tree, {(const uint8_t *)k_codes, (const uint8_t *)k_scales},
                    {(const uint8_t *)v_codes, (const uint8_t *)v_scales}, block_table, prefix_len, node_offset, parent, out, lse,
-                   (float *)workspace, (float *)((char *)workspace + cut.ml_offset)};
+                   (float *)workspace, (float *)((char *)workspace + cut.ml_offset),
+                   cut.bytes ? (int32_t *)((char *)workspace + cut.cut_offset) : nullptr};
   if (cut.mfma) {
     HB_HIP_TRY(launch_kv4_attn(a, cut.plan, (hipStream_t)stream));
     return HB_OK;

@@ -40,9 +40,11 @@ typedef unsigned int swap2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStep = 32;  // keys
 constexpr int kWaves = 4;  // of a workgroup
+constexpr int kSharing = 4;  // of one whose wavefronts share keys
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kSlack = 8.f;  // log2 units a score may exceed its row's reference
+constexpr float kMostSum = 4096.f;  // of eight weights against their row's reference
+constexpr float kSlack = 8.f;       // log2 units: a largest score that is no further above the reference leaves it where it is
 constexpr float kNegInf = -__builtin_huge_valf();
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -126,74 +128,128 @@ struct Tile {
   uint32_t ks[2], vs[2];
 };
 
-// Where the workgroup's chunk lies, and the sequence's nodes
-struct Chunk {
-  int b, c, chunks, L, begin, end, n0, n;
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((kv4_f32x2){a, b}, bf16x2));
+}
+
+// Pages of a chunk's keys, 64 times 16 keys to the registers of a wavefront (lane l: the l-th 16) and the next 64 on their way.
+// Asked for one by one, by scalar loads, they would be waited for with the LDS reads of every step.
+struct Pages {
+  const int32_t *table;
+  int blocks, last16, first16, now, ahead;
+  uint32_t magic;
+
+  __device__ __forceinline__ int ask(int from) const {
+    const int at16 = min(from + (int)(threadIdx.x & 63), last16);
+    return table[magic ? (int)__umulhi((uint32_t)at16, magic) : at16];
+  }
+  __device__ __forceinline__ void begin(const hb_attn_desc &d, const int32_t *row, int at16, int last, uint32_t page_magic) {
+    table = row;
+    blocks = d.num_blocks;
+    last16 = last;
+    first16 = at16;
+    magic = page_magic;
+    now = ask(at16);
+    ahead = ask(at16 + 64);
+    asm volatile("" : "+v"(now));  // waited for here: where it is used next would be a wait for the codes asked for in between
+  }
+  // where in a pool the rows of the keys 16 at16 .. 16 at16 + 15 of head g begin; at16 never goes back by more than it has come
+  // on since the last 64 were left (a chunk's last keys, asked for again, are in the 64 that are there)
+  __device__ __forceinline__ size_t row(const hb_attn_desc &d, int at16, int g) {
+    at16 = min(at16, last16);
+    if (at16 - first16 >= 64) {  // uniform
+      first16 += 64;
+      now = ahead;
+      asm volatile("" : "+v"(now));
+      ahead = ask(first16 + 64);
+    }
+    int blk = __builtin_amdgcn_readlane(now, at16 - first16);
+    blk = blk < 0 ? 0 : (blk >= blocks ? blocks - 1 : blk);
+    const int page = magic ? (int)__umulhi((uint32_t)at16, magic) : at16;
+    return ((size_t)blk * d.num_kv_heads + g) * d.page_size + (at16 * 16 - page * d.page_size);
+  }
+};
+
+// What a workgroup works on: row group rg of the keys [begin, end) of head g of sequence b (chunk c of `chunks`), and the
+// sequence's nodes
+struct Piece {
+  int b, c, chunks, g, rg, groups, L, begin, end, n0, n;
 };
 
 __device__ __forceinline__ int kv4_chunks(int L, int len) { return L > 0 ? (L + len - 1) / len : 1; }
-
-// Chunks of all sequences on one line: as many as `target`, each of the same length (a multiple of `grain` keys) and no
-// sequence in more than `splits`; a sequence without a prefix has one too, for its tree.  Every workgroup finds the length by
-// itself from the sequences' lengths, a sequence to a lane.
-__device__ __forceinline__ int chunk_length(int grains, int longest, const Kv4Plan &plan) {
-  const int target = plan.target - plan.over;
-  int len = (grains + target - 1) / target;
-  const int least = (longest + plan.splits - 1) / plan.splits;
-  len = len < least ? least : len;
-  return (len < 1 ? 1 : len) * plan.grain;
-}
 __device__ __forceinline__ int grains_of(int L, const Kv4Plan &plan) { return (L + plan.grain - 1) / plan.grain; }
-__device__ int chunk_length(const hb_attn_desc &d, const int32_t *__restrict__ prefix_len, const Kv4Plan &plan) {
-  int grains = 0, longest = 0;
-  for (int b0 = 0; b0 < d.batch; b0 += 64) {
-    const int b = b0 + (threadIdx.x & 63), n = b < d.batch ? grains_of(kv4_length(d, prefix_len, b), plan) : 0;
-    grains += sum_lanes(n);
-    longest = max(longest, max_lanes(n));
-  }
-  return chunk_length(grains, longest, plan);
+__device__ __forceinline__ int nodes_of(const hb_attn_desc &d, int n0, int n1) {
+  const int n = n1 - n0 < 0 ? 0 : n1 - n0 > d.max_nodes_per_tree ? d.max_nodes_per_tree : n1 - n0;
+  return n0 < 0 || n0 + n > d.total_nodes ? 0 : n;  // malformed offsets: touch nothing
+}
+// row groups of a sequence with n nodes
+__device__ __forceinline__ int groups_of(const hb_attn_desc &d, int n, const Kv4Plan &plan) {
+  const int rows = n * (d.num_q_heads / d.num_kv_heads);
+  return (rows + plan.group_rows - 1) / plan.group_rows;
 }
 
-// the chunk with index `unit` on the line; false behind its end
-__device__ __forceinline__ bool find_chunk(const Kv4AttnArgs &a, const Kv4Plan &plan, int unit, Chunk &c) {
+// The workgroups' pieces.  Every sequence is cut into chunks of one length, a multiple of `grain` keys, the shortest with which
+// about `target` workgroups a kv head (a chunk has one for each of the sequence's row groups) and no sequence in more than
+// `splits` chunks come out; a sequence without a prefix has one chunk, for its tree.  Every workgroup finds this out from the
+// lengths, a sequence to a lane, and then which piece is its own.  Row groups of a chunk are neighbours, so are the heads,
+// and neighbours are on one XCD (workgroup ids go round the eight): they read the same keys, or the same lines of scales.
+// What is left over without a piece are the last ids: holes in between would leave the CUs of one shader engine idle.
+__device__ __forceinline__ bool find_piece(const Kv4AttnArgs &a, const Kv4Plan &plan, Piece &c) {
   const hb_attn_desc &d = a.d;
   const int lane = threadIdx.x & 63;
-  // up to 64 sequences: lengths and offsets in one go
-  int L = 0, n0 = 0, n1 = 0, len;
-  if (lane < d.batch) {
-    L = kv4_length(d, a.prefix_len, lane);
-    n0 = a.node_offset[lane];
-    n1 = a.node_offset[lane + 1];
-  }
-  if (d.batch <= 64) {
-    const int n = grains_of(L, plan);
-    len = chunk_length(sum_lanes(n), max_lanes(n), plan);
-  } else {
-    len = chunk_length(d, a.prefix_len, plan);
-  }
-  int before = 0;
+  int L = 0, n0 = 0, n1 = 0;  // of sequence b0 + lane
+  auto ask = [&](int b) {
+    const bool there = b < d.batch;
+    L = there ? kv4_length(d, a.prefix_len, b) : 0;
+    n0 = there ? a.node_offset[b] : 0;
+    n1 = there ? a.node_offset[b + 1] : 0;
+  };
+  int work = 0, longest = 0;  // grains, as often as there are row groups; of a sequence
   for (int b0 = 0; b0 < d.batch; b0 += 64) {
-    const int b = b0 + lane;
-    if (b0) {
-      L = b < d.batch ? kv4_length(d, a.prefix_len, b) : 0;
-      n0 = b < d.batch ? a.node_offset[b] : 0;
-      n1 = b < d.batch ? a.node_offset[b + 1] : 0;
+    ask(b0 + lane);
+    const int n = grains_of(L, plan);
+    work += sum_lanes(n * groups_of(d, nodes_of(d, n0, n1), plan));
+    longest = max(longest, max_lanes(n));
+  }
+  int len = max(max((work + plan.target - 1) / plan.target, (longest + plan.splits - 1) / plan.splits), 1);
+  int total = 0;  // workgroups of a kv head
+  for (;;) {
+    total = 0;
+    for (int b0 = 0; b0 < d.batch; b0 += 64) {
+      if (d.batch > 64) ask(b0 + lane);
+      total += sum_lanes(kv4_chunks(L, len * plan.grain) * groups_of(d, nodes_of(d, n0, n1), plan));
     }
-    const int n = b < d.batch ? kv4_chunks(L, len) : 0;
-    const int up = scan_lanes(n);
-    const unsigned long long behind = __ballot(before + up > unit);
+    // short last chunks make more of them than were asked for: longer ones, unless there are too many sequences for that
+    if (total <= plan.target || len >= longest || !plan.fit) break;
+    len += (len + 15) / 16;
+  }
+  len *= plan.grain;
+  const int each = (total * d.num_kv_heads + 7) / 8;  // of an XCD
+  const int id = blockIdx.x, slot = id >> 3, index = (id & 7) * each + slot;
+  if (a.cut && id == 0 && threadIdx.x == 0) *a.cut = len;  // for the launch that joins the chunks
+  if (slot >= each || index >= total * d.num_kv_heads) return false;
+  int before = 0;
+  const int at = index / d.num_kv_heads;
+  for (int b0 = 0; b0 < d.batch; b0 += 64) {
+    if (d.batch > 64) ask(b0 + lane);
+    const int chunks = kv4_chunks(L, len), groups = groups_of(d, nodes_of(d, n0, n1), plan);
+    const int up = scan_lanes(chunks * groups);
+    const unsigned long long behind = __ballot(before + up > at);
     if (behind) {
       const int who = __builtin_ctzll(behind);
       c.b = b0 + who;
       c.L = __builtin_amdgcn_readlane(L, who);
-      c.chunks = __builtin_amdgcn_readlane(n, who);
-      c.c = unit - before - __builtin_amdgcn_readlane(up - n, who);
+      c.chunks = __builtin_amdgcn_readlane(chunks, who);
+      c.groups = __builtin_amdgcn_readlane(groups, who);
+      int rest = index - (before + __builtin_amdgcn_readlane(up - chunks * groups, who)) * d.num_kv_heads;
+      c.rg = rest % c.groups;
+      rest /= c.groups;
+      c.g = rest % d.num_kv_heads;
+      c.c = rest / d.num_kv_heads;
       c.begin = c.c * len;
       c.end = min(c.L, c.begin + len);
       c.n0 = __builtin_amdgcn_readlane(n0, who);
-      c.n = __builtin_amdgcn_readlane(n1, who) - c.n0;
-      c.n = c.n < 0 ? 0 : c.n > d.max_nodes_per_tree ? d.max_nodes_per_tree : c.n;
-      if (c.n0 < 0 || c.n0 + c.n > d.total_nodes) c.n = 0;  // malformed offsets: touch nothing
+      c.n = nodes_of(d, c.n0, __builtin_amdgcn_readlane(n1, who));
       return true;
     }
     before += __builtin_amdgcn_readlane(up, 63);
@@ -221,29 +277,57 @@ struct Rows {
   f32x4 o[TPW][2 * DB];  // O^T: lane (j, kg) holds d = 16 dt + 4 kg + r of row j
   f32x4 lr[TPW];         // row sums of the rounded weights (every element), which is what the values are weighed with
   float l[TPW];          // of the weights as they are, the lane's own keys: a log-sum-exp of few keys would show their rounding
-  float m[TPW], ref[TPW], limit[TPW];  // reference exponent (log2 units), the same or 0 where there is none yet, largest score that keeps it
+  float m[TPW], ref[TPW], limit[TPW];  // reference exponent (log2 units), the same or 0 where there is none yet, largest sum of weights that keeps it
 };
 
-// softmax weights of a step's scores, after moving the reference of rows that need it
+// Scores of 32 keys.  The smaller pieces first, all of them: a sum's second product waits for its first.
+template <int TPW>
+__device__ __forceinline__ void score_tiles(const u32x4 (&k)[2], const int (&ks)[2], const QTile (&q)[TPW], f32x4 (&sc)[TPW][2]) {
+  i32x8 ak[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) ak[h] = (i32x8){(int)k[h][0], (int)k[h][1], (int)k[h][2], (int)k[h][3], 0, 0, 0, 0};
+#pragma unroll
+  for (int t = 0; t < TPW; ++t)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      sc[t][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ak[h], q[t].lo, (f32x4){0.f, 0.f, 0.f, 0.f}, 4, 0, 0, ks[h], 0, q[t].lo_scale);
+#pragma unroll
+  for (int t = 0; t < TPW; ++t)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      sc[t][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ak[h], q[t].hi, sc[t][h], 4, 0, 0, ks[h], 0, q[t].hi_scale);
+}
+
+// Softmax weights of a step's scores.  A row's reference is the largest score of the first step it sees, and moves when the
+// weights of a lane's eight keys against it sum to more than 2^12 (or to no number): then one of them is 2^9 or more, and
+// the reference becomes the row's largest score of the step.  Their sum is needed anyway, so that the common case takes no
+// maximum at all.
 template <int TPW, int DB>
 __device__ __forceinline__ void weigh(Rows<TPW, DB> &w, const f32x4 (&sc)[TPW][2], float c1, f32x8 (&p)[TPW]) {
-  float lm[TPW];
+  float sum[TPW];
+  auto weights = [&] {
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) p[t][r] = fast_exp2(fmaf(sc[t][r >> 2][r & 3], c1, -w.ref[t]));
+      sum[t] = ((p[t][0] + p[t][1]) + (p[t][2] + p[t][3])) + ((p[t][4] + p[t][5]) + (p[t][6] + p[t][7]));
+    }
+  };
+  weights();
   bool need = false;
 #pragma unroll
-  for (int t = 0; t < TPW; ++t) {
-    lm[t] = fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), sc[t][0][2]), sc[t][0][3]), sc[t][1][0]), sc[t][1][1]), sc[t][1][2]), sc[t][1][3]);
-    need |= !(lm[t] <= w.limit[t]);
-  }
+  for (int t = 0; t < TPW; ++t) need |= !(sum[t] <= w.limit[t]);
   if (__any(need)) {
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int t = 0; t < TPW; ++t) {
-      const float mx = group_max(lm[t]) * c1;
+      const float lm = fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), sc[t][0][2]), sc[t][0][3]), sc[t][1][0]), sc[t][1][1]), sc[t][1][2]), sc[t][1][3]);
+      const float mx = group_max(lm) * c1;  // c1 > 0
       const float old = w.m[t] == kNegInf ? mx : w.m[t];
       const bool grow = mx > old + kSlack;
       w.m[t] = grow ? mx : old;
       w.ref[t] = w.m[t] == kNegInf ? 0.f : w.m[t];
-      w.limit[t] = w.m[t] == kNegInf ? kNegInf : (w.m[t] + kSlack) / c1;
+      w.limit[t] = w.m[t] == kNegInf ? -1.f : kMostSum;
       if (__any(grow)) {
         const float alpha = grow ? fast_exp2(old - mx) : 1.f;
         w.l[t] *= alpha;
@@ -256,37 +340,37 @@ __device__ __forceinline__ void weigh(Rows<TPW, DB> &w, const f32x4 (&sc)[TPW][2
         }
       }
     }
+    weights();
   }
 #pragma unroll
-  for (int t = 0; t < TPW; ++t) {
-#pragma unroll
-    for (int r = 0; r < 8; ++r) p[t][r] = fast_exp2(fmaf(sc[t][r >> 2][r & 3], c1, -w.ref[t]));
-    w.l[t] += ((p[t][0] + p[t][1]) + (p[t][2] + p[t][3])) + ((p[t][4] + p[t][5]) + (p[t][6] + p[t][7]));
-  }
+  for (int t = 0; t < TPW; ++t) w.l[t] += sum[t];
 }
 
-// O^T += V^T P^T, and the row sums (an all-ones operand), with the step's values in `lv` as [key][d] bf16.  Lane (s, kg) of
-// a 16-lane group addresses 8 bytes of key 16 h + 4 kg + s / 4 at d = 16 dt + 4 (s % 4); the transposing read hands lane j the
-// four keys 16 h + 4 kg + 0 .. 3 at d = 16 dt + j, the order that the score accumulators have.
-template <int TPW, int DB>
-__device__ __forceinline__ void accumulate(Rows<TPW, DB> &w, const unsigned char *lv, int j, int kg, const bf16x8 (&pb)[TPW]) {
+// V^T of a step, from its values in LDS as [key][d] bf16.  Lane (s, kg) of a 16-lane group addresses 8 bytes of key
+// 16 h + 4 kg + s / 4 at d = 16 dt + 4 (s % 4); the transposing read hands lane j the four keys 16 h + 4 kg + 0 .. 3 at
+// d = 16 dt + j, the order that the score accumulators have.
+template <int DB>
+__device__ __forceinline__ void read_values(const unsigned char *lv, int j, int kg, bf16x8 (&av)[2 * DB]) {
   constexpr int kRow = 64 * DB;  // bytes of a key's row
-  // (no vector additions, and no sum over the lane groups: every row of the product is the sum)
-  const bf16x8 ones = {(__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f};
-#pragma unroll
-  for (int t = 0; t < TPW; ++t) {
-    w.lr[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[t], w.lr[t], 0, 0, 0);
-    asm volatile("" : "+v"(w.lr[t]));
-  }
   const int key = 4 * kg + (j >> 2);
   const int piece = (j >> 1) & 1, half = 8 * (j & 1), x = v_swz(key) & (4 * DB - 1);
-  bf16x8 av[2 * DB];
 #pragma unroll
   for (int dt = 0; dt < 2 * DB; ++dt) {
     const unsigned char *p = lv + key * kRow + (((2 * dt + piece) ^ x) * 16) + half;
     bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr)(p));
     bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr)(p + 16 * kRow));
     av[dt] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+}
+
+// O^T += V^T P^T, and the row sums (an all-ones operand: no vector additions, and no sum over the lane groups)
+template <int TPW, int DB>
+__device__ __forceinline__ void accumulate(Rows<TPW, DB> &w, const bf16x8 (&av)[2 * DB], const bf16x8 (&pb)[TPW]) {
+  const bf16x8 ones = {(__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+  for (int t = 0; t < TPW; ++t) {
+    w.lr[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[t], w.lr[t], 0, 0, 0);
+    asm volatile("" : "+v"(w.lr[t]));
   }
 #pragma unroll
   for (int dt = 0; dt < 2 * DB; ++dt)
@@ -301,16 +385,17 @@ __device__ __forceinline__ void accumulate(Rows<TPW, DB> &w, const unsigned char
 // 2^-9 average out; a row of few keys, the nodes' own and a short prefix, would show them.
 template <int TPW, int DB>
 __device__ __forceinline__ void weigh_values(Rows<TPW, DB> &w, const unsigned char *lv, int j, int kg, const f32x8 (&p)[TPW], bool fine) {
-  bf16x8 pb[TPW];
+  bf16x8 pb[TPW], av[2 * DB];
 #pragma unroll
   for (int t = 0; t < TPW; ++t) pb[t] = __builtin_convertvector(p[t], bf16x8);
+  read_values<DB>(lv, j, kg, av);
   if (fine) {
     bf16x8 rest[TPW];
 #pragma unroll
     for (int t = 0; t < TPW; ++t) rest[t] = __builtin_convertvector(p[t] - __builtin_convertvector(pb[t], f32x8), bf16x8);
-    accumulate<TPW, DB>(w, lv, j, kg, rest);
+    accumulate<TPW, DB>(w, av, rest);
   }
-  accumulate<TPW, DB>(w, lv, j, kg, pb);
+  accumulate<TPW, DB>(w, av, pb);
 }
 
 // A key's block of 32 values, widened, into its row in LDS
@@ -331,8 +416,7 @@ __device__ __forceinline__ void put_values(unsigned char *lv, int key, int kg, c
 }
 
 template <int TPW, int DB, int W>
-__global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4Plan plan,
-                                                                       const int32_t *__restrict__ block_table) {
+__global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4Plan plan) {
   constexpr int D = 32 * DB, kRow = 64 * DB;
   const hb_attn_desc &d = a.d;
   // values: 32 keys to a wavefront; at the end a tile's sums of all wavefronts; then references and sums
@@ -340,15 +424,9 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   __shared__ float s_m[W][TPW * 16], s_l[W][TPW * 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 15, kg = lane >> 4;
-  // row groups of a chunk are neighbours on one XCD (workgroup ids go round the eight): they read the same keys
-  const int id = blockIdx.x, slot = id >> 3;
-  const int rg = slot % plan.row_groups, unit = (slot / plan.row_groups) * 8 + (id & 7);
-  const int g = unit % d.num_kv_heads, G = d.num_q_heads / d.num_kv_heads;
-  Chunk ch;
-  if (!find_chunk(a, plan, unit / d.num_kv_heads, ch)) return;
-  const int n0 = ch.n0, n = ch.n;
-  const int R = n * G, tile0 = rg * TPW;
-  if (tile0 * 16 >= R) return;
+  Piece ch;
+  if (!find_piece(a, plan, ch)) return;
+  const int g = ch.g, G = d.num_q_heads / d.num_kv_heads, n0 = ch.n0, n = ch.n, R = n * G, tile0 = ch.rg * TPW;
   const size_t row_base = (size_t)n0 * d.num_q_heads + (size_t)g * G;
   auto row_at = [&](int row) {  // of a row of this head, among all rows
     const int node = small_div(row, G);
@@ -358,20 +436,12 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   // The prefix: the codes of a step, and the pages of the step behind the one that was asked for last.  Steps past the chunk's
   // end ask for its last keys again.
   const int steps = ch.end > ch.begin ? (ch.end - ch.begin + kStep - 1) / kStep : 0;
-  // (a parameter of its own, which nothing that is written can be: then its entries come by scalar loads.  By vector loads
-  // each wait for one is a wait for all codes on their way)
-  const int32_t *table = block_table + (size_t)ch.b * d.max_blocks_per_seq;
   const int first16 = ch.begin >> 4, last16 = (ch.end - 1) >> 4;
-  size_t next[2];  // rows of a pool: where the step's two halves begin
+  Pages pages;
+  size_t next[2];  // where the step's two halves begin
   auto find = [&](int step) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int at16 = min(first16 + 2 * step + h, last16);  // 16 keys lie in one page
-      const int page = plan.page_magic ? (int)__umulhi((uint32_t)at16, plan.page_magic) : at16;
-      int blk = table[page];
-      blk = blk < 0 ? 0 : (blk >= d.num_blocks ? d.num_blocks - 1 : blk);
-      next[h] = ((size_t)blk * d.num_kv_heads + g) * d.page_size + (at16 * 16 - page * d.page_size);
-    }
+    for (int h = 0; h < 2; ++h) next[h] = pages.row(d, first16 + 2 * step + h, g);
   };
   auto load = [&](int step, Tile &x) {
 #pragma unroll
@@ -395,6 +465,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
     }
   }
   if (wave < steps) {
+    pages.begin(d, a.block_table + (size_t)ch.b * d.max_blocks_per_seq, first16, last16, plan.page_magic);
     find(wave);
     load(wave, x);
     load(wave + W, y);
@@ -411,8 +482,9 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
       if (DB == 4) x[2] = src[8 + 2 * kg], x[3] = src[8 + 2 * kg + 1];
     }
     split_rows<DB>(x, w.q[t]);
-    w.m[t] = w.limit[t] = kNegInf;
+    w.m[t] = kNegInf;
     w.ref[t] = 0.f;
+    w.limit[t] = -1.f;
     w.l[t] = 0.f;
     w.lr[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -479,14 +551,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   auto attend = [&](auto tail, int step, Tile &x, int left) {
     constexpr bool kTail = decltype(tail)::value;
     f32x4 sc[TPW][2];
-#pragma unroll
-    for (int t = 0; t < TPW; ++t)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const i32x8 ak = {(int)x.k[h][0], (int)x.k[h][1], (int)x.k[h][2], (int)x.k[h][3], 0, 0, 0, 0};
-        sc[t][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ak, w.q[t].lo, (f32x4){0.f, 0.f, 0.f, 0.f}, 4, 0, 0, (int)x.ks[h], 0, w.q[t].lo_scale);
-        sc[t][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ak, w.q[t].hi, sc[t][h], 4, 0, 0, (int)x.ks[h], 0, w.q[t].hi_scale);
-      }
+    const int ks[2] = {(int)x.ks[0], (int)x.ks[1]};
+    score_tiles<TPW>(x.k, ks, w.q, sc);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       u32x4 c = x.v[h];
@@ -561,7 +627,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
       if (row < R) {
         if (ch.chunks == 1) {
           const float inv = 1.f / l;
-          *(u32x2 *)((bf16_t *)a.out + rr * D + 16 * dt + 4 * kg) = (u32x2){pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+          *(u32x2 *)((bf16_t *)a.out + rr * D + 16 * dt + 4 * kg) = (u32x2){pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
         } else {
           *(f32x4 *)(a.part_o + (rr * plan.splits + ch.c) * D + 16 * dt + 4 * kg) = o;
         }
@@ -578,11 +644,287 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   }
 }
 
+// ---- many rows ------------------------------------------------------------------------------------------
+// The same products where a (sequence, kv head) has many query rows (60 nodes of 7 heads: 27 tiles): the W wavefronts of a
+// workgroup have up to two tiles of rows each and share 64 keys at a time, whose values are widened into LDS once for all.  The
+// keys' codes lie there as they are; a wavefront's operand of 16 keys is one contiguous kilobyte.
+// The loop over 32-key blocks is skewed by one: the matrix core gets a block's V^T P^T and the next one's scores in one go, and
+// the vector work that follows has its scores already.  A thread asks for its share of a tile (16 bytes of keys and of
+// values, two scales) two tiles ahead and puts it in LDS one tile ahead, while the matrix core has that work.  Two stages of
+// LDS: what a barrier lets in has been written by everybody, and what it lets be overwritten has been read.
+template <int DB, int W>
+__global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4Plan plan) {
+  constexpr int D = 32 * DB, kRow = 64 * DB, TPW = 2, kTile = 64, kThreads = 64 * W;
+  constexpr int kPieces = kTile * DB, kShare = (kPieces + kThreads - 1) / kThreads;  // 16-byte pieces of a tile; of a thread
+  constexpr int kStage = kTile * (kRow + 16 * DB + DB);
+  const hb_attn_desc &d = a.d;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[2 * kStage];  // [values 64 x kRow | key codes 64 x D / 2 | key scales]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int j = lane & 15, kg = lane >> 4;
+  Piece ch;
+  if (!find_piece(a, plan, ch)) return;
+  const int g = ch.g, G = d.num_q_heads / d.num_kv_heads, n0 = ch.n0, n = ch.n, R = n * G;
+  // full groups and a last one that is not: wavefronts without rows only help to bring the keys, which leaves the CU to others
+  const int tiles = (R + 15) >> 4, tile_lo = ch.rg * TPW * W, tile_hi = min(tiles, tile_lo + TPW * W);
+  const size_t row_base = (size_t)n0 * d.num_q_heads + (size_t)g * G;
+  auto row_at = [&](int row) {
+    const int node = small_div(row, G);
+    return row_base + (size_t)node * d.num_q_heads + (row - node * G);
+  };
+  // tile t of this wavefront, and the rows of it that there are
+  auto tile_of = [&](int t) { return tile_lo + TPW * wave + t; };
+  const bool busy = tile_of(0) < tile_hi;
+  auto row_of = [&](int t) { return tile_of(t) < tile_hi ? tile_of(t) * 16 + j : R; };
+
+  // ---- a thread's share of a tile: piece i of 64 keys x DB blocks -----------------------------------
+  struct Share {
+    u32x4 k[kShare], v[kShare];
+    uint32_t ks[kShare], vs[kShare];
+  };
+  const int keys = ch.end > ch.begin ? ch.end - ch.begin : 0, n_tiles = (keys + kTile - 1) / kTile;
+  const int first16 = ch.begin >> 4, last16 = (ch.end - 1) >> 4;
+  constexpr int kWave16 = 64 / DB / 16;  // 16s of keys in a wavefront's pieces
+  static_assert(kWave16 == 1 || kWave16 == 2, "a wavefront takes 16 or 32 keys");
+  Pages pages;
+  size_t next[kShare][kWave16];
+  auto find = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < kShare; ++i)
+#pragma unroll
+      for (int q = 0; q < kWave16; ++q) next[i][q] = pages.row(d, first16 + tile * 4 + (wave + i * W) * kWave16 + q, g);
+  };
+  auto load = [&](int tile, Share &x) {
+#pragma unroll
+    for (int i = 0; i < kShare; ++i) {
+      if (kShare * kThreads > kPieces && i * kThreads + tid >= kPieces) continue;
+      const int key = lane / DB;
+      const size_t row = (kWave16 == 2 && key >= 16 ? next[i][kWave16 - 1] : next[i][0]) + (key & 15);
+      x.k[i] = *(const u32x4 *)(a.kp.codes + row * (D / 2) + lane % DB * 16);
+      x.v[i] = *(const u32x4 *)(a.vp.codes + row * (D / 2) + lane % DB * 16);
+      x.ks[i] = a.kp.scales[row * DB + lane % DB];
+      x.vs[i] = a.vp.scales[row * DB + lane % DB];
+    }
+    find(tile + 1);
+  };
+  auto put = [&](int tile, auto stage, const Share &x) {  // stage: tile & 1, known to the compiler
+    unsigned char *st = smem + decltype(stage)::value * kStage;
+    const int left = keys - tile * kTile;
+#pragma unroll
+    for (int i = 0; i < kShare; ++i) {
+      const int piece = i * kThreads + tid, key = piece / DB, blk = piece % DB;
+      if (kShare * kThreads > kPieces && piece >= kPieces) continue;
+      u32x4 c = x.v[i];
+      uint32_t s = x.vs[i];
+      if (left < kTile) {  // uniform: past the end, whatever it is, its weight is 0 and must not make that 0 * NaN
+        asm volatile("" ::: "memory");
+        const bool there = key < left;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = there ? c[e] : 0u;
+        s = there ? s : 127u;
+      }
+      put_values<DB>(st, key, blk, c, s);
+      *(u32x4 *)(st + kTile * kRow + piece * 16) = x.k[i];
+      st[kTile * (kRow + 16 * DB) + piece] = (unsigned char)x.ks[i];
+    }
+  };
+
+  Share x, y;
+  if (n_tiles > 0) {
+    pages.begin(d, a.block_table + (size_t)ch.b * d.max_blocks_per_seq, first16, last16, plan.page_magic);
+    find(0);
+    load(0, x);
+    load(1, y);
+  }
+
+  Rows<TPW, DB> w;
+#pragma unroll
+  for (int t = 0; t < TPW; ++t) {
+    const int row = row_of(t);
+    u32x4 q[4] = {};
+    if (row < R) {
+      const u32x4 *src = (const u32x4 *)a.q + row_at(row) * (D / 8);
+      q[0] = src[2 * kg], q[1] = src[2 * kg + 1];
+      if (DB == 4) q[2] = src[8 + 2 * kg], q[3] = src[8 + 2 * kg + 1];
+    }
+    split_rows<DB>(q, w.q[t]);
+    w.m[t] = kNegInf;
+    w.ref[t] = 0.f;
+    w.limit[t] = -1.f;
+    w.l[t] = 0.f;
+    w.lr[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int dt = 0; dt < 2 * DB; ++dt) {
+      w.o[t][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      asm volatile("" : "+v"(w.o[t][dt]));
+    }
+  }
+  const float c1 = d.softmax_scale * kLog2e;
+
+  // ---- the nodes' own keys, chunk 0 only: values in the second stage, keys straight from memory -----
+  if (ch.c == 0) {
+    unsigned char *lv = smem + kStage;
+    for (int i = tid; i < kTile * 2 * DB * 2; i += kThreads) {
+      const int key = i / (4 * DB), piece = i % (4 * DB);
+      u32x4 v = {0u, 0u, 0u, 0u};
+      if (key < n) {
+        v = ((const u32x4 *)a.v_tree)[((size_t)(n0 + key) * d.num_kv_heads + g) * (D / 8) + piece];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = finite_or_zero_bf16x2(v[e]);
+      }
+      *(u32x4 *)(lv + key * kRow + ((piece ^ (v_swz(key) & (4 * DB - 1))) * 16)) = v;
+    }
+    const unsigned long long path = path_of(lane < n ? a.parent[n0 + lane] : -1, lane, n);
+    __syncthreads();
+    for (int blk = 0; blk < 2; ++blk) {
+      if (32 * blk >= n || !busy) break;
+      const uint32_t mine = (uint32_t)(path >> (32 * blk));
+      f32x4 sc[TPW][2];
+#pragma unroll
+      for (int t = 0; t < TPW; ++t) sc[t][0] = sc[t][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < DB; ++ks) {
+        bf16x8 ak[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          ak[h] = __builtin_bit_cast(bf16x8, ((const u32x4 *)a.k_tree)[((size_t)(n0 + min(32 * blk + 16 * h + j, n - 1)) * d.num_kv_heads + g) * (D / 8) + 4 * ks + kg]);
+#pragma unroll
+        for (int t = 0; t < TPW; ++t) {
+          const bf16x8 qf = __builtin_bit_cast(bf16x8, ((const u32x4 *)a.q)[row_at(min(row_of(t), R - 1)) * (D / 8) + 4 * ks + kg]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) sc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ak[h], qf, sc[t][h], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < TPW; ++t) {
+        const int row = row_of(t);
+        const uint32_t allow = (uint32_t)__shfl((int)mine, row < R ? small_div(row, G) : 0, 64) >> (4 * kg);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[t][h][r] = ((allow >> (16 * h + r)) & 1u) ? sc[t][h][r] : kNegInf;
+      }
+      f32x8 p[TPW];
+      weigh<TPW, DB>(w, sc, c1, p);
+      weigh_values<TPW, DB>(w, lv + 32 * blk * kRow, j, kg, p, true);
+    }
+  }
+
+  // ---- the prefix --------------------------------------------------------------------------------------
+  if (n_tiles > 0) {
+    f32x4 sc[TPW][2];
+    bf16x8 av[2 * DB];
+    u32x4 kc[2];  // a block's keys
+    int ks[2];
+    auto read_keys = [&](auto stage, int blk) {
+      const unsigned char *at = smem + decltype(stage)::value * kStage + kTile * kRow;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int key = 32 * blk + 16 * h + j;
+        kc[h] = (u32x4){0u, 0u, 0u, 0u};
+        ks[h] = 127;
+        if (DB == 4 || kg < DB) {
+          kc[h] = *(const u32x4 *)(at + (key * DB + kg) * 16);
+          ks[h] = at[kTile * 16 * DB + key * DB + kg];
+        }
+      }
+    };
+    auto scores = [&] { score_tiles<TPW>(kc, ks, w.q, sc); };
+    // softmax of the scores that there are; the values of their block are asked for first
+    auto vector_work = [&](int tile, auto stage, int blk, f32x8 (&p)[TPW]) {
+      read_values<DB>(smem + decltype(stage)::value * kStage + 32 * blk * kRow, j, kg, av);
+      const int left = keys - tile * kTile - 32 * blk;
+      if (left < 32) {  // uniform
+        asm volatile("" ::: "memory");  // a branch, not selects in every pass
+#pragma unroll
+        for (int t = 0; t < TPW; ++t)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sc[t][h][r] = 16 * h + 4 * kg + r < left ? sc[t][h][r] : kNegInf;
+      }
+      weigh<TPW, DB>(w, sc, c1, p);
+      if (left < 32) {  // few keys or many, a sequence's last ones may be all that it has: see weigh_values
+        bf16x8 rest[TPW];
+#pragma unroll
+        for (int t = 0; t < TPW; ++t) rest[t] = __builtin_convertvector(p[t] - __builtin_convertvector(__builtin_convertvector(p[t], bf16x8), f32x8), bf16x8);
+        accumulate<TPW, DB>(w, av, rest);
+      }
+    };
+    auto values = [&](const f32x8 (&p)[TPW]) {
+      bf16x8 pb[TPW];
+#pragma unroll
+      for (int t = 0; t < TPW; ++t) pb[t] = __builtin_convertvector(p[t], bf16x8);
+      accumulate<TPW, DB>(w, av, pb);
+    };
+    // Barrier without the fence of __syncthreads(), which would wait for every load in flight: what has to be done in front of
+    // it are reads and writes of LDS
+    auto barrier = [] {
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+      asm volatile("s_barrier" ::: "memory");
+    };
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    put(0, even, x);
+    load(2, x);
+    barrier();  // tile 0 is there, and the nodes' values have been read
+    if (busy) {
+      read_keys(even, 0);
+      scores();
+    }
+    auto one_tile = [&](int i, auto stage, auto other, Share &share) {
+      f32x8 p[TPW];
+      put(i + 1, other, share);  // (behind the last tile: its keys once more, which nobody reads)
+      load(i + 3, share);
+      if (busy) {
+        vector_work(i, stage, 0, p);
+        read_keys(stage, 1);
+        values(p);
+        scores();
+        vector_work(i, stage, 1, p);
+      }
+      barrier();
+      if (busy) {
+        read_keys(other, 0);
+        values(p);
+        scores();
+      }
+    };
+    for (int i = 0; i < n_tiles; i += 2) {
+      one_tile(i, even, odd, y);
+      if (i + 1 < n_tiles) one_tile(i + 1, odd, even, x);
+    }
+  }
+
+  // ---- write out: lane (j, kg) holds O[row j][16 dt + 4 kg + r] ----------------------------------------
+#pragma unroll
+  for (int t = 0; t < TPW; ++t) {
+    const int row = row_of(t);
+    const float l = group_sum(w.l[t]);
+    if (row >= R) continue;
+    const size_t rr = row_at(row);
+    const float scale = w.lr[t][0] > 0.f ? l / w.lr[t][0] : 1.f;  // values weighed as the sum that they are divided by
+    if (ch.chunks == 1) {
+      const float inv = scale / l;
+#pragma unroll
+      for (int dt = 0; dt < 2 * DB; ++dt) {
+        const f32x4 o = w.o[t][dt] * inv;
+        *(u32x2 *)((bf16_t *)a.out + rr * D + 16 * dt + 4 * kg) = (u32x2){pack2(o[0], o[1]), pack2(o[2], o[3])};
+      }
+      if (a.lse && kg == 0) a.lse[rr] = (w.m[t] + log2f(l)) * kLn2;
+    } else {
+      float *po = a.part_o + (rr * plan.splits + ch.c) * D;
+#pragma unroll
+      for (int dt = 0; dt < 2 * DB; ++dt) *(f32x4 *)(po + 16 * dt + 4 * kg) = w.o[t][dt] * scale;
+      if (kg == 0) *(kv4_f32x2 *)(a.part_ml + (rr * plan.splits + ch.c) * 2) = (kv4_f32x2){w.m[t], l};
+    }
+  }
+}
+
 // Rows of sequences that were cut: the chunks' results joined (log2 units).  A row's threads hold four elements each; results
 // are asked for eight chunks at a time.
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a, Kv4Plan plan) {
   const int D = a.d.head_dim, tpr = D / 4;
-  const int len = chunk_length(a.d, a.prefix_len, plan);
+  const int len = *a.cut;
   const long gid = (long)blockIdx.x * 256 + threadIdx.x;
   const int row = (int)(gid / tpr), piece = (int)(gid - (long)row * tpr);
   if (row >= a.d.total_nodes * a.d.num_q_heads) return;
@@ -621,18 +963,26 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a, Kv4Plan pl
     }
   }
   const float inv = 1.f / l;
-  *(u32x2 *)((bf16_t *)a.out + (size_t)row * D + piece * 4) = (u32x2){pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+  *(u32x2 *)((bf16_t *)a.out + (size_t)row * D + piece * 4) = (u32x2){pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
   if (a.lse && piece == 0) a.lse[row] = (m + log2f(l)) * kLn2;
 }
 
 template <int TPW, int DB, int W>
 hipError_t launch(const Kv4AttnArgs &a, const Kv4Plan &plan, hipStream_t s) {
-  const long units = ((long)plan.target + a.d.batch) * a.d.num_kv_heads;  // chunks on the line, at most
-  kv4_attn_kernel<TPW, DB, W><<<(unsigned)((units + 7) / 8 * 8 * plan.row_groups), 64 * W, 0, s>>>(a, plan, a.block_table);
+  kv4_attn_kernel<TPW, DB, W><<<(unsigned)plan.grid, 64 * W, 0, s>>>(a, plan);
+  return hipGetLastError();
+}
+
+template <int DB, int W>
+hipError_t launch_rows(const Kv4AttnArgs &a, const Kv4Plan &plan, hipStream_t s) {
+  kv4_rows_kernel<DB, W><<<(unsigned)plan.grid, 64 * W, 0, s>>>(a, plan);
   return hipGetLastError();
 }
 
 }  // namespace
+
+// Rows of (sequence, kv head) from which on wavefronts share the keys: four tiles and less, each wavefront has keys of its own
+static bool shares_keys(const hb_attn_desc &d) { return d.num_q_heads / d.num_kv_heads * d.max_nodes_per_tree > 64; }
 
 bool kv4_attn_supports(const hb_attn_desc &d) {
   return d.dtype == HB_BF16 && (d.head_dim == 64 || d.head_dim == 128) && d.page_size % 16 == 0 && d.page_size <= 1024 &&
@@ -643,18 +993,22 @@ static int tiles_of(const hb_attn_desc &d) { return (d.num_q_heads / d.num_kv_he
 
 // Chunks are planned for some 512 workgroups
 void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
-  const int tiles = tiles_of(d), tpw = tiles > 1 ? 2 : 1;
-  plan->row_groups = (tiles + tpw - 1) / tpw;
+  const int tiles = tiles_of(d), group = shares_keys(d) ? 2 * kSharing : tiles > 1 ? 2 : 1;
+  plan->row_groups = (tiles + group - 1) / group;  // at most
+  plan->group_rows = 16 * group;
   plan->grain = kWaves * kStep;
-  int64_t target = 512 / ((int64_t)d.num_kv_heads * plan->row_groups);
+  int64_t target = 512 / d.num_kv_heads;  // workgroups of a kv head
   target = target < 1 ? 1 : target;
   int64_t splits = d.num_splits ? d.num_splits : target;
   const int64_t most = (span + plan->grain - 1) / plan->grain;
   splits = splits > most ? most : splits;
   splits = splits < 1 ? 1 : splits > 1024 ? 1024 : splits;
-  plan->target = (int32_t)(d.num_splits ? (int64_t)d.num_splits * d.batch > 1 << 16 ? 1 << 16 : d.num_splits * d.batch : target);
-  plan->target = plan->target < 1 ? 1 : plan->target;
-  plan->over = !d.num_splits && plan->target > 2 * d.batch ? d.batch : 0;
+  if (d.num_splits) target = (int64_t)d.num_splits * d.batch * plan->row_groups;
+  plan->target = (int32_t)(target < 1 ? 1 : target > 1 << 18 ? 1 << 18 : target);
+  // each sequence's last chunk may be one more than its share of the target
+  const int64_t ends = (int64_t)d.batch * plan->row_groups, most_wg = (plan->target + ends) * d.num_kv_heads;
+  plan->fit = d.num_splits == 0 && d.batch <= 64 && ends < plan->target;
+  plan->grid = (int32_t)((most_wg + 7) / 8 * 8);
   plan->splits = (int32_t)splits;
   const int page16 = d.page_size / 16;
   plan->page_magic = page16 == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + page16 - 1) / page16);
@@ -663,7 +1017,8 @@ void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
 hipError_t launch_kv4_attn(const Kv4AttnArgs &a, const Kv4Plan &plan, hipStream_t s) {
   const bool wide = tiles_of(a.d) > 1;
   hipError_t e;
-  if (a.d.head_dim == 128) e = wide ? launch<2, 4, kWaves>(a, plan, s) : launch<1, 4, kWaves>(a, plan, s);
+  if (shares_keys(a.d)) e = a.d.head_dim == 128 ? launch_rows<4, kSharing>(a, plan, s) : launch_rows<2, kSharing>(a, plan, s);
+  else if (a.d.head_dim == 128) e = wide ? launch<2, 4, kWaves>(a, plan, s) : launch<1, 4, kWaves>(a, plan, s);
   else e = wide ? launch<2, 2, kWaves>(a, plan, s) : launch<1, 2, kWaves>(a, plan, s);
   if (e != hipSuccess || plan.splits == 1) return e;
   const long threads = (long)a.d.total_nodes * a.d.num_q_heads * (a.d.head_dim / 4);
