@@ -1,5 +1,6 @@
 // Rows into and out of the 4-bit cache, and the eviction of positions from it.
 #include "kv4.h"
+#include "wave_ops.h"
 
 namespace hb {
 
@@ -48,13 +49,15 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
       a.new_len[b] = (L < 0 ? 0 : L) + n;
     }
   }
-  const int pieces = d.head_dim / 8;
-  const int piece = (int)(gid % pieces);
-  const long item = gid / pieces;
-  if (item >= (long)a.rows * d.num_kv_heads) return;  // pieces is a multiple of four: a block's threads leave together
-  const int r = (int)(item % a.rows), h = (int)(item / a.rows);
+  // pieces is a multiple of four: a block's threads leave together.  (32 bits hold what a launch may have)
+  const unsigned pieces = d.head_dim / 8, item = (unsigned)gid / pieces;
+  const int piece = (int)((unsigned)gid - item * pieces);
+  if (gid >= (long)a.rows * d.num_kv_heads * pieces) return;
+  const int h = (int)(item / (unsigned)a.rows), r = (int)(item - (unsigned)h * (unsigned)a.rows);
   int b, j, src = r;
   bool live;
+  float x[8];
+  if (!PATH) load8((const T *)(blockIdx.y ? a.v : a.k) + ((size_t)r * d.num_kv_heads + h) * d.head_dim + piece * 8, x);
   if (PATH) {
     b = r / a.max_path;
     j = r - b * a.max_path;
@@ -83,9 +86,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   }
   if (!in_table) return;
   const size_t row = kv4_row(d, a.block_table, b, h, (int)p);
-  const T *x_at = (const T *)(blockIdx.y ? a.v : a.k) + ((size_t)src * d.num_kv_heads + h) * d.head_dim + piece * 8;
-  float x[8];
-  load8(x_at, x);
+  if (PATH) load8((const T *)(blockIdx.y ? a.v : a.k) + ((size_t)src * d.num_kv_heads + h) * d.head_dim + piece * 8, x);
   uint32_t top = 0;  // magnitudes compare as their bits do, and what is not finite is above the rest
 #pragma unroll
   for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
@@ -116,11 +117,10 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(hb_attn_desc d, int rows,
                                                        const int32_t *__restrict__ block_table, const int32_t *__restrict__ first,
                                                        const int32_t *__restrict__ row_offset, T *__restrict__ k, T *__restrict__ v) {
   const long gid = (long)blockIdx.x * 256 + threadIdx.x;
-  const int pieces = d.head_dim / 8;
-  const int piece = (int)(gid % pieces);
-  const long item = gid / pieces;
-  if (item >= (long)rows * d.num_kv_heads) return;
-  const int r = (int)(item % rows), h = (int)(item / rows);
+  const unsigned pieces = d.head_dim / 8, item = (unsigned)gid / pieces;
+  const int piece = (int)((unsigned)gid - item * pieces);
+  if (gid >= (long)rows * d.num_kv_heads * pieces) return;
+  const int h = (int)(item / (unsigned)rows), r = (int)(item - (unsigned)h * (unsigned)rows);
   const int b = kv4_sequence(row_offset, d.batch, r);
   const long p = (long)first[b] + r - row_offset[b];
   const Kv4Pool &from = blockIdx.y ? vp : kp;
@@ -151,6 +151,7 @@ constexpr int kRounds = 8;                               // of four slots to a t
 constexpr int kPart = 256;                               // slots that a wavefront takes in a round
 constexpr int kSlab = kSelectThreads * 4 * kRounds;      // 32768 slots
 constexpr int kBins = 2048;                              // digits of 11, 11 and 10 bits
+constexpr int kCopies = 4;                               // of a histogram, for a quarter of the lanes each: weights share few digits
 
 // keys of four slots from s on; a slot past the length gets key 0, which no slot in front of it has
 __device__ inline void load_keys(const float *w, const int32_t *pos, int s, int L, bool vec, int recent_from, int sinks,
@@ -200,10 +201,10 @@ __device__ inline bool in_fours(const Kv4EvictArgs &a, size_t cap) {
 // read again for every digit.
 __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs a) {
   const hb_attn_desc &d = a.d;
-  __shared__ int hist[kBins], s_sum[kSelectWaves];
+  __shared__ int hist[kCopies * kBins], s_sum[kSelectWaves];
   __shared__ int s_above[kRounds * kSelectWaves], s_ties[kRounds * kSelectWaves];
   __shared__ int s_digit, s_need;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x / d.num_kv_heads;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x / d.num_kv_heads;
   const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
   const int L = min(kv4_length(d, a.prefix_len, b), a.longest), stays = L < a.budget ? L : a.budget;
   const float *w = a.weight + (size_t)blockIdx.x * cap;
@@ -233,7 +234,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs
     need = stays;
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048, known = pass == 2 ? 10 : 21;
-      for (int i = tid; i < bins; i += kSelectThreads) hist[i] = 0;
+      for (int i = tid; i < kCopies * bins; i += kSelectThreads) hist[i] = 0;
       __syncthreads();
       for (int slab = 0; slab < slabs; ++slab) {
         if (slabs > 1) load(slab);
@@ -244,24 +245,26 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs
           for (int e = 0; e < 4; ++e) {
             const uint32_t k = keys[r][e];
             // (the slots past the length fall into counter 0, which is above every position's digit: never reached)
-            if (pass == 0 || ((k ^ least) >> known) == 0) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1);
+            if (pass == 0 || ((k ^ least) >> known) == 0) atomicAdd(&hist[((k >> shift) & (bins - 1)) * kCopies + (lane & (kCopies - 1))], 1);
           }
         }
       }
       __syncthreads();
       // a thread's two counters, the largest digits first: the digit is where their running sum passes `need`
       const int top = bins - 1 - 2 * tid;
-      const int c0 = top > 0 ? hist[top] : 0, c1 = top > 0 ? hist[top - 1] : 0;
-      int up = c0 + c1;
+      int c0 = 0, c1 = 0;
+      if (top > 0) {
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(up, o, 64);
-        up += lane >= o ? y : 0;
+        for (int i = 0; i < kCopies; ++i) {
+          c0 += hist[top * kCopies + i];
+          c1 += hist[(top - 1) * kCopies + i];
+        }
       }
+      const int up = scan_lanes(c0 + c1);
       if (lane == 63) s_sum[wave] = up;
       __syncthreads();
-      int before = up - c0 - c1;
-      for (int i = 0; i < wave; ++i) before += s_sum[i];
+      const int waves = scan_lanes(lane < kSelectWaves ? s_sum[lane] : 0);
+      const int before = up - c0 - c1 + (wave ? __builtin_amdgcn_readlane(waves, wave - 1) : 0);
       if (before < need && before + c0 + c1 >= need) {  // one thread
         const bool first = before + c0 >= need;
         s_digit = first ? top : top - 1;
@@ -295,30 +298,21 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs
       }
     }
     __syncthreads();
-    if (wave < 2) {  // 64 parts each, on the line of the slab's 128
-      const int i = wave * 64 + lane;
-      int x = s_above[i], y = s_ties[i];
-      int head_x = 0, head_y = 0;
-      if (wave == 1)
-        for (int q = 0; q < 64; ++q) {
-          head_x += s_above[q];
-          head_y += s_ties[q];
-        }
-      const int x0 = x, y0 = y;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(x, o, 64), v = __shfl_up(y, o, 64);
-        x += lane >= o ? u : 0;
-        y += lane >= o ? v : 0;
-      }
-      const int part = slab * (kSlab / kPart) + i;
+    if (wave == 0) {  // two of the slab's 128 parts to a lane
+      const int x0 = s_above[2 * lane], x1 = s_above[2 * lane + 1], y0 = s_ties[2 * lane], y1 = s_ties[2 * lane + 1];
+      const int x = above + scan_lanes(x0 + x1), y = ties + scan_lanes(y0 + y1);
+      const int part = slab * (kSlab / kPart) + 2 * lane;
       if (part < a.parts_each) {
-        parts[part * 2] = above + head_x + x - x0;
-        parts[part * 2 + 1] = ties + head_y + y - y0;
+        parts[part * 2] = x - x0 - x1;
+        parts[part * 2 + 1] = y - y0 - y1;
       }
-      if (i == 127) {
-        s_sum[0] = above + head_x + x;
-        s_sum[1] = ties + head_y + y;
+      if (part + 1 < a.parts_each) {
+        parts[part * 2 + 2] = x - x1;
+        parts[part * 2 + 3] = y - y1;
+      }
+      if (lane == 63) {
+        s_sum[0] = x;
+        s_sum[1] = y;
       }
     }
     __syncthreads();

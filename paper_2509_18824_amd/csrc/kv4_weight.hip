@@ -49,89 +49,124 @@ __device__ __forceinline__ void pieces_of(const float *p, u32x4 (&x)[3]) {
 }
 
 template <typename T, int DB>
-__global__ __launch_bounds__(64 * kWaves) void kv4_weight_kernel(Kv4WeightArgs a, uint32_t page_magic, int keys_each) {
+__global__ __launch_bounds__(64 * kWaves) void kv4_weight_kernel(Kv4WeightArgs a, uint32_t page_magic, int rounds) {
   constexpr int P = sizeof(T) == 4 ? 3 : 1, kRows = sizeof(T) == 4 ? 32 : 64, D = 32 * DB;
   const hb_attn_desc &d = a.d;
   // 16-byte pieces [row][piece of bf16][d / 8], the last index XORed with the row so that 16 rows' reads spread over the banks
   __shared__ u32x4 s_q[kRows * P * 4 * DB];
   __shared__ float s_lse[kRows];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, j = lane & 15, kg = lane >> 4;
+  __shared__ int s_path[64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, kg = lane >> 4;
   const int h = blockIdx.y % d.num_kv_heads, b = blockIdx.y / d.num_kv_heads, G = d.num_q_heads / d.num_kv_heads;
-  const int L = kv4_length(d, a.prefix_len, b), begin = blockIdx.x * keys_each;
+  // a wavefront's keys: 64 in each round, the first at k0; what has to be known first is asked for in one go
+  const int begin = blockIdx.x * rounds * kWaves * kKeys, k0 = begin + wave * kKeys;
+  const int cap16 = d.max_blocks_per_seq * (d.page_size / 16);
+  const int32_t *table = a.block_table + (size_t)b * d.max_blocks_per_seq;
+  // lane 4 r + t: the page of the t-th 16 keys of round r
+  const int at16 = min((k0 >> 4) + (lane >> 2) * (kWaves * 4) + (lane & 3), cap16 - 1);
+  int pages = table[page_magic ? (int)__umulhi((uint32_t)at16, page_magic) : at16];
+  const int n0 = a.node_offset[b], n1 = a.node_offset[b + 1], accepted = a.accept_path ? a.accept_len[b] : 0;
+  const bool short_path = a.accept_path && a.max_path <= 64;
+  if (short_path && tid < a.max_path) s_path[tid] = a.accept_path[(size_t)b * a.max_path + tid];
+  const int L = kv4_length(d, a.prefix_len, b);
   if (begin >= L) return;
-  const int end = min(L, begin + keys_each);
-  const int n0 = a.node_offset[b];
-  int n = a.node_offset[b + 1] - n0;
-  n = n < 0 || n0 < 0 || n0 + n > d.total_nodes ? 0 : n;
-  int nodes = a.accept_path ? a.accept_len[b] : n;
+  const int end = min(L, begin + rounds * kWaves * kKeys);
+  const int n = n1 - n0 < 0 || n0 < 0 || n1 > d.total_nodes ? 0 : n1 - n0;
+  int nodes = a.accept_path ? accepted : n;
   nodes = nodes < 0 || n == 0 ? 0 : a.accept_path && nodes > a.max_path ? a.max_path : nodes;
   const int rows = nodes * G;
   const float c1 = d.softmax_scale * kLog2e;
   float *weight = a.weight + ((size_t)b * d.num_kv_heads + h) * d.max_blocks_per_seq * d.page_size;
-  const int32_t *table = a.block_table + (size_t)b * d.max_blocks_per_seq;
+  pages = pages < 0 ? 0 : (pages >= d.num_blocks ? d.num_blocks - 1 : pages);
 
-  // rows r0 .. r0 + kRows - 1 into LDS; past the last: zeros that weigh nothing
-  auto stage = [&](int r0) {
-    const int there = min(kRows, (rows - r0 + 15) / 16 * 16);
-    for (int i = tid; i < there * 4 * DB; i += 64 * kWaves) {
-      const int r = i / (4 * DB), piece = i % (4 * DB), row = r0 + r;
-      u32x4 x[P] = {};
-      if (row < rows) {
-        int node = row / G;
-        const int hg = row - node * G;
-        if (a.accept_path) node = a.accept_path[(size_t)b * a.max_path + node];
-        node = node < 0 ? 0 : node >= n ? n - 1 : node;
-        const size_t at = (size_t)(n0 + node) * d.num_q_heads + h * G + hg;
-        pieces_of((const T *)a.q + at * D + piece * 8, x);
-        if (piece == 0) s_lse[r] = a.lse[at] * kLog2e;
-      } else if (piece == 0) {
-        s_lse[r] = __builtin_huge_valf();
-      }
+  struct Keys {
+    u32x4 k[4];
+    uint32_t scale[4];
+    float old[4];
+  };
+  auto load = [&](int round, Keys &x) {
+    const int first = k0 + round * kWaves * kKeys;
 #pragma unroll
-      for (int p = 0; p < P; ++p) s_q[(r * P + p) * 4 * DB + (piece ^ (r & (4 * DB - 1)))] = x[p];
+    for (int t = 0; t < 4; ++t) {
+      x.k[t] = (u32x4){0u, 0u, 0u, 0u};
+      x.scale[t] = 127;
+      x.old[t] = 0.f;
+      if (first + 16 * t < end) {  // uniform
+        const int at = (first >> 4) + t, page = page_magic ? (int)__umulhi((uint32_t)at, page_magic) : at;
+        const int blk = __builtin_amdgcn_readlane(pages, 4 * round + t);
+        const size_t row = ((size_t)blk * d.num_kv_heads + h) * d.page_size + (at * 16 - page * d.page_size) + j;
+        if (DB == 4 || kg < DB) {
+          x.k[t] = *(const u32x4 *)(a.kp.codes + row * (D / 2) + kg * 16);
+          x.scale[t] = a.kp.scales[row * DB + kg];
+        }
+        if (first + 16 * t + j < end) x.old[t] = weight[first + 16 * t + j];
+      }
     }
   };
 
+  // rows r0 .. r0 + kRows - 1 into LDS, a thread's pieces of them asked for in one go; past the last: zeros that weigh nothing
+  auto stage = [&](int r0) {
+    constexpr int kItems = kRows * 4 * DB / (64 * kWaves);
+    const int there = min(kRows, (rows - r0 + 15) / 16 * 16);
+    u32x4 x[kItems][P];
+    float lse[kItems];
+#pragma unroll
+    for (int q = 0; q < kItems; ++q) {
+      const int i = tid + q * 64 * kWaves, piece = i % (4 * DB), row = r0 + i / (4 * DB);
+#pragma unroll
+      for (int p = 0; p < P; ++p) x[q][p] = (u32x4){0u, 0u, 0u, 0u};
+      lse[q] = __builtin_huge_valf();
+      if (row < rows) {
+        // row / G for both below 2^22: the quotient of the reciprocal is at most one off
+        int node = (int)((float)row * __builtin_amdgcn_rcpf((float)G));
+        node += (node + 1) * G <= row ? 1 : 0;
+        node -= node * G > row ? 1 : 0;
+        const int hg = row - node * G;
+        if (a.accept_path) node = short_path ? s_path[node] : a.accept_path[(size_t)b * a.max_path + node];
+        node = node < 0 ? 0 : node >= n ? n - 1 : node;
+        const size_t at = (size_t)(n0 + node) * d.num_q_heads + h * G + hg;
+        pieces_of((const T *)a.q + at * D + piece * 8, x[q]);
+        if (piece == 0) lse[q] = a.lse[at] * kLog2e;
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kItems; ++q) {
+      const int i = tid + q * 64 * kWaves, piece = i % (4 * DB), r = i / (4 * DB);
+      if (r >= there) continue;
+      if (piece == 0) s_lse[r] = lse[q];
+#pragma unroll
+      for (int p = 0; p < P; ++p) s_q[(r * P + p) * 4 * DB + (piece ^ (r & (4 * DB - 1)))] = x[q][p];
+    }
+  };
+
+  Keys x;
+  load(0, x);
   const bool one_batch = rows <= kRows;
+  __syncthreads();  // the path
   if (one_batch) {
     stage(0);
     __syncthreads();
   }
   // every wavefront goes round as often as the others: there are barriers inside where rows come in batches
-  for (int k0 = begin + wave * kKeys; k0 - wave * kKeys < end; k0 += kWaves * kKeys) {
-    u32x4 k[4] = {};
-    uint32_t scale[4] = {127, 127, 127, 127};
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int at16 = (k0 >> 4) + t;
-      if (at16 * 16 < end) {  // uniform
-        const int page = page_magic ? (int)__umulhi((uint32_t)at16, page_magic) : at16;
-        int blk = table[page];
-        blk = blk < 0 ? 0 : (blk >= d.num_blocks ? d.num_blocks - 1 : blk);
-        const size_t row = ((size_t)blk * d.num_kv_heads + h) * d.page_size + (at16 * 16 - page * d.page_size) + j;
-        if (DB == 4 || kg < DB) {
-          k[t] = *(const u32x4 *)(a.kp.codes + row * (D / 2) + kg * 16);
-          scale[t] = a.kp.scales[row * DB + kg];
-        }
-      }
-    }
+  for (int round = 0; begin + round * kWaves * kKeys < end; ++round) {
+    const int first = k0 + round * kWaves * kKeys;
     float old[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) old[t] = k0 + 16 * t + j < end ? weight[k0 + 16 * t + j] : 0.f;
     bf16x8 bk[4][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const float s = __uint_as_float(scale[t] << 23);
+      old[t] = x.old[t];
+      const float s = __uint_as_float(x.scale[t] << 23);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         u32x4 y;
-        y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(k[t][i], s, 0));
-        y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(k[t][i], s, 1));
-        y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(k[t][i], s, 2));
-        y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(k[t][i], s, 3));
+        y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 0));
+        y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 1));
+        y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 2));
+        y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 3));
         bk[t][i] = __builtin_bit_cast(bf16x8, y);
       }
     }
+    load(round + 1, x);  // on its way during the products
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     for (int r0 = 0; r0 < rows; r0 += kRows) {
       if (!one_batch) {
@@ -164,7 +199,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_weight_kernel(Kv4WeightArgs a
     for (int t = 0; t < 4; ++t) {
       const float all = group_sum(sum[t]);
       // lane group t writes the t-th 16 keys
-      if (kg == t && k0 + 16 * t + j < end) weight[k0 + 16 * t + j] = fmaf(old[t], a.decay, all);
+      if (kg == t && first + 16 * t + j < end) weight[first + 16 * t + j] = fmaf(old[t], a.decay, all);
     }
   }
 }
@@ -181,16 +216,16 @@ hipError_t launch_kv4_weight_mfma(const Kv4WeightArgs &a, int32_t longest, hipSt
   const int64_t units = (int64_t)a.d.batch * a.d.num_kv_heads;
   // 256 keys to a workgroup, more where that gives more than four workgroups a CU: their queries are staged once
   int64_t rounds = units * longest / (256 * 1024);
-  rounds = rounds < 1 ? 1 : rounds > 8 ? 8 : rounds;
+  rounds = rounds < 1 ? 1 : rounds > 8 ? 8 : rounds;  // a wavefront holds the pages of sixteen rounds
   const int keys = (int)rounds * kWaves * kKeys;
   const dim3 grid((unsigned)((longest + keys - 1) / keys), (unsigned)units);
   const bool f32 = a.d.dtype == HB_F32;
   if (a.d.head_dim == 128) {
-    if (f32) kv4_weight_kernel<float, 4><<<grid, 64 * kWaves, 0, s>>>(a, magic, keys);
-    else kv4_weight_kernel<bf16_t, 4><<<grid, 64 * kWaves, 0, s>>>(a, magic, keys);
+    if (f32) kv4_weight_kernel<float, 4><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds);
+    else kv4_weight_kernel<bf16_t, 4><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds);
   } else {
-    if (f32) kv4_weight_kernel<float, 2><<<grid, 64 * kWaves, 0, s>>>(a, magic, keys);
-    else kv4_weight_kernel<bf16_t, 2><<<grid, 64 * kWaves, 0, s>>>(a, magic, keys);
+    if (f32) kv4_weight_kernel<float, 2><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds);
+    else kv4_weight_kernel<bf16_t, 2><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds);
   }
   return hipGetLastError();
 }
