@@ -269,6 +269,60 @@ class VerifyStep:
                                     dev.prefix_len, self.out_slots, self.new_len)
 
 
+class Kv4VerifyStep:
+    """Verification steps of one layer over a 4-bit cache that is kept within a budget.
+
+    ``run`` enqueues one step: attention over the cache and the nodes' own keys, LM head and acceptance, the attention weight
+    that the cached positions received from the accepted nodes, and the append of these nodes.  ``advance`` makes the step's
+    lengths the next one's; ``evict`` cuts every head's positions back to ``budget`` (the last ``recent`` and the first
+    ``sinks`` ones stay).  A program calls it when lengths come near the pages that the table maps, between steps.  ``dev.k_pool``
+    and ``dev.v_pool`` are not used; ``dev.prefix_len`` is advanced in place."""
+
+    def __init__(self, desc: hb.AttnDesc, dev: DeviceInputs, pool: Kv4Pool, weight: torch.Tensor, draft_ids: torch.Tensor,
+                 max_path: int, budget: int, recent: int = 0, sinks: int = 0, decay: float = 1.0, seq_len=None):
+        self.desc, self.dev, self.pool, self.weight, self.draft_ids, self.max_path = desc, dev, pool, weight, draft_ids, max_path
+        self.budget, self.recent, self.sinks, self.decay = budget, recent, sinks, decay
+        d, B, T = dev.q.device, desc.batch, desc.total_nodes
+        i32 = lambda *shape: torch.empty(shape, dtype=torch.int32, device=d)
+        slots = (B, desc.num_kv_heads, desc.max_blocks_per_seq * desc.page_size)
+        self.seq_len = dev.prefix_len.clone() if seq_len is None else seq_len
+        # what is cached already has no weight yet, and is where it was written
+        self.slot_weight = torch.zeros(slots, dtype=torch.float32, device=d)
+        self.slot_pos = torch.arange(slots[2], dtype=torch.int32, device=d).expand(slots).contiguous()
+        self.out = torch.empty_like(dev.q)
+        self.lse = torch.empty(dev.q.shape[:2], dtype=torch.float32, device=d)
+        self.ws_attn = alloc_workspace(hb.hb_tree_verify_attn_kv4_workspace_bytes(desc), d)
+        self.ws_lm = alloc_workspace(max(8, hb.hb_lmhead_argmax_workspace_bytes(T)), d)
+        self.ws_evict = alloc_workspace(hb.hb_kv4_evict_workspace_bytes(desc, budget), d)
+        self.target_ids, self.accept_len, self.bonus = i32(T), i32(B), i32(B)
+        self.accept_path, self.out_tokens, self.out_slots = i32(B, max_path), i32(B, max_path), i32(B, max_path)
+        self.new_len, self.kept = i32(B), i32(B, desc.num_kv_heads, budget)
+
+    def run(self):
+        dev, desc = self.dev, self.desc
+        hb.hb_tree_verify_attn_kv4(desc, dev.q, dev.k_tree, dev.v_tree, *self.pool, dev.block_table, dev.prefix_len,
+                                   dev.node_offset, dev.parent, self.out, self.lse, self.ws_attn)
+        hb.hb_lmhead_accept(desc, self.out.view(self.out.shape[0], -1), self.weight, self.draft_ids, dev.node_offset, dev.parent,
+                            self.max_path, self.target_ids, self.accept_len, self.accept_path, self.out_tokens, self.bonus,
+                            self.ws_lm)
+        hb.hb_kv4_attn_weight(desc, dev.q, self.pool.k_codes, self.pool.k_scales, dev.block_table, dev.prefix_len,
+                              dev.node_offset, self.accept_len, self.accept_path, self.max_path, self.lse, self.decay,
+                              self.slot_weight)
+        hb.hb_kv4_compact(desc, dev.k_tree, dev.v_tree, *self.pool, dev.block_table, dev.prefix_len, dev.node_offset,
+                          self.accept_len, self.accept_path, self.max_path, self.seq_len, self.slot_weight, self.slot_pos,
+                          self.out_slots, self.new_len)
+
+    def advance(self):
+        self.dev.prefix_len.copy_(self.new_len)
+        self.seq_len.add_(self.accept_len)
+
+    def evict(self):
+        dev = self.dev
+        hb.hb_kv4_evict(self.desc, self.budget, self.recent, self.sinks, *self.pool, dev.block_table, dev.prefix_len, self.seq_len,
+                        self.slot_weight, self.slot_pos, self.slot_weight, self.slot_pos, self.kept, self.new_len, self.ws_evict)
+        dev.prefix_len.copy_(self.new_len)
+
+
 class VerifyLayerStack:
     """Buffers and call chain of one verification step through ``n_layers`` decoder layers, then
     LM head with argmax, acceptance, and the append of the accepted nodes' K/V to every layer's
