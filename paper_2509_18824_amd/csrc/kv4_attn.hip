@@ -40,6 +40,7 @@ typedef unsigned int swap2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStep = 32;  // keys
 constexpr int kWaves = 4;  // of a workgroup
+constexpr int kGrain = kWaves * kStep;  // keys that a chunk's length is a multiple of
 constexpr int kSharing = 4;  // of one whose wavefronts share keys
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -176,16 +177,17 @@ struct Piece {
   int b, c, chunks, g, rg, groups, L, begin, end, n0, n;
 };
 
-__device__ __forceinline__ int kv4_chunks(int L, int len) { return L > 0 ? (L + len - 1) / len : 1; }
-__device__ __forceinline__ int grains_of(int L, const Kv4Plan &plan) { return (L + plan.grain - 1) / plan.grain; }
+__device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
+// chunks of a sequence of `grains` grains, len grains long
+__device__ __forceinline__ int chunks_of(int grains, int len) { return grains > 0 ? div_up(grains, len) : 1; }
+__device__ __forceinline__ int grains_of(int L) { return (L + kGrain - 1) / kGrain; }
 __device__ __forceinline__ int nodes_of(const hb_attn_desc &d, int n0, int n1) {
   const int n = n1 - n0 < 0 ? 0 : n1 - n0 > d.max_nodes_per_tree ? d.max_nodes_per_tree : n1 - n0;
   return n0 < 0 || n0 + n > d.total_nodes ? 0 : n;  // malformed offsets: touch nothing
 }
 // row groups of a sequence with n nodes
-__device__ __forceinline__ int groups_of(const hb_attn_desc &d, int n, const Kv4Plan &plan) {
-  const int rows = n * (d.num_q_heads / d.num_kv_heads);
-  return (rows + plan.group_rows - 1) / plan.group_rows;
+__device__ __forceinline__ int groups_of(int n, const Kv4Plan &plan) {
+  return (n * plan.heads + (1 << plan.group_shift) - 1) >> plan.group_shift;
 }
 
 // The workgroups' pieces.  Every sequence is cut into chunks of one length, a multiple of `grain` keys, the shortest with which
@@ -207,23 +209,22 @@ __device__ __forceinline__ bool find_piece(const Kv4AttnArgs &a, const Kv4Plan &
   int work = 0, longest = 0;  // grains, as often as there are row groups; of a sequence
   for (int b0 = 0; b0 < d.batch; b0 += 64) {
     ask(b0 + lane);
-    const int n = grains_of(L, plan);
-    work += sum_lanes(n * groups_of(d, nodes_of(d, n0, n1), plan));
+    const int n = grains_of(L);
+    work += sum_lanes(n * groups_of(nodes_of(d, n0, n1), plan));
     longest = max(longest, max_lanes(n));
   }
-  int len = max(max((work + plan.target - 1) / plan.target, (longest + plan.splits - 1) / plan.splits), 1);
+  int len = max(max(div_up(work, plan.target), div_up(longest, plan.splits)), 1);  // in grains
   int total = 0;  // workgroups of a kv head
   for (;;) {
     total = 0;
     for (int b0 = 0; b0 < d.batch; b0 += 64) {
       if (d.batch > 64) ask(b0 + lane);
-      total += sum_lanes(kv4_chunks(L, len * plan.grain) * groups_of(d, nodes_of(d, n0, n1), plan));
+      total += sum_lanes(chunks_of(grains_of(L), len) * groups_of(nodes_of(d, n0, n1), plan));
     }
     // short last chunks make more of them than were asked for: longer ones, unless there are too many sequences for that
     if (total <= plan.target || len >= longest || !plan.fit) break;
     len += (len + 15) / 16;
   }
-  len *= plan.grain;
   const int each = (total * d.num_kv_heads + 7) / 8;  // of an XCD
   const int id = blockIdx.x, slot = id >> 3, index = (id & 7) * each + slot;
   if (a.cut && id == 0 && threadIdx.x == 0) *a.cut = len;  // for the launch that joins the chunks
@@ -232,7 +233,7 @@ __device__ __forceinline__ bool find_piece(const Kv4AttnArgs &a, const Kv4Plan &
   const int at = index / d.num_kv_heads;
   for (int b0 = 0; b0 < d.batch; b0 += 64) {
     if (d.batch > 64) ask(b0 + lane);
-    const int chunks = kv4_chunks(L, len), groups = groups_of(d, nodes_of(d, n0, n1), plan);
+    const int chunks = chunks_of(grains_of(L), len), groups = groups_of(nodes_of(d, n0, n1), plan);
     const int up = scan_lanes(chunks * groups);
     const unsigned long long behind = __ballot(before + up > at);
     if (behind) {
@@ -246,8 +247,8 @@ __device__ __forceinline__ bool find_piece(const Kv4AttnArgs &a, const Kv4Plan &
       rest /= c.groups;
       c.g = rest % d.num_kv_heads;
       c.c = rest / d.num_kv_heads;
-      c.begin = c.c * len;
-      c.end = min(c.L, c.begin + len);
+      c.begin = c.c * len * kGrain;
+      c.end = min(c.L, c.begin + len * kGrain);
       c.n0 = __builtin_amdgcn_readlane(n0, who);
       c.n = nodes_of(d, c.n0, __builtin_amdgcn_readlane(n1, who));
       return true;
@@ -426,7 +427,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   const int j = lane & 15, kg = lane >> 4;
   Piece ch;
   if (!find_piece(a, plan, ch)) return;
-  const int g = ch.g, G = d.num_q_heads / d.num_kv_heads, n0 = ch.n0, n = ch.n, R = n * G, tile0 = ch.rg * TPW;
+  const int g = ch.g, G = plan.heads, n0 = ch.n0, n = ch.n, R = n * G, tile0 = ch.rg * TPW;
   const size_t row_base = (size_t)n0 * d.num_q_heads + (size_t)g * G;
   auto row_at = [&](int row) {  // of a row of this head, among all rows
     const int node = small_div(row, G);
@@ -663,7 +664,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
   const int j = lane & 15, kg = lane >> 4;
   Piece ch;
   if (!find_piece(a, plan, ch)) return;
-  const int g = ch.g, G = d.num_q_heads / d.num_kv_heads, n0 = ch.n0, n = ch.n, R = n * G;
+  const int g = ch.g, G = plan.heads, n0 = ch.n0, n = ch.n, R = n * G;
   // full groups and a last one that is not: wavefronts without rows only help to bring the keys, which leaves the CU to others
   const int tiles = (R + 15) >> 4, tile_lo = ch.rg * TPW * W, tile_hi = min(tiles, tile_lo + TPW * W);
   const size_t row_base = (size_t)n0 * d.num_q_heads + (size_t)g * G;
@@ -931,7 +932,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a, Kv4Plan pl
   const int node = row / a.d.num_q_heads, b = kv4_sequence(a.node_offset, a.d.batch, node);
   const int first = a.node_offset[b], n = min(a.node_offset[b + 1] - first, a.d.max_nodes_per_tree);
   if (node < first || node >= first + n || first + n > a.d.total_nodes) return;
-  const int chunks = kv4_chunks(kv4_length(a.d, a.prefix_len, b), len);
+  const int chunks = chunks_of(grains_of(kv4_length(a.d, a.prefix_len, b)), len);
   if (chunks == 1) return;
   const kv4_f32x2 *ml = (const kv4_f32x2 *)a.part_ml + (size_t)row * plan.splits;
   const f32x4 *po = (const f32x4 *)a.part_o + (size_t)row * plan.splits * tpr + piece;
@@ -984,27 +985,34 @@ hipError_t launch_rows(const Kv4AttnArgs &a, const Kv4Plan &plan, hipStream_t s)
 // Rows of (sequence, kv head) from which on wavefronts share the keys: four tiles and less, each wavefront has keys of its own
 static bool shares_keys(const hb_attn_desc &d) { return d.num_q_heads / d.num_kv_heads * d.max_nodes_per_tree > 64; }
 
+static int tiles_of(const hb_attn_desc &d) { return (d.num_q_heads / d.num_kv_heads * d.max_nodes_per_tree + 15) / 16; }
+constexpr int64_t kMostGroups = 1 << 22;  // workgroups
+
 bool kv4_attn_supports(const hb_attn_desc &d) {
+  // what the workgroups count with 32 bits: pieces, and grains times row groups
+  const int64_t ends = (int64_t)d.batch * ((tiles_of(d) + 1) / 2 + 1);
+  if (ends * d.num_kv_heads > kMostGroups || ends * (((int64_t)d.page_size * d.max_blocks_per_seq) / kGrain + 1) > 1 << 30) return false;
   return d.dtype == HB_BF16 && (d.head_dim == 64 || d.head_dim == 128) && d.page_size % 16 == 0 && d.page_size <= 1024 &&
          d.softmax_scale > 0.f && d.softmax_scale < 1e30f && d.num_q_heads / d.num_kv_heads <= 512;
 }
 
-static int tiles_of(const hb_attn_desc &d) { return (d.num_q_heads / d.num_kv_heads * d.max_nodes_per_tree + 15) / 16; }
 
 // Chunks are planned for some 512 workgroups
 void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
   const int tiles = tiles_of(d), group = shares_keys(d) ? 2 * kSharing : tiles > 1 ? 2 : 1;
   plan->row_groups = (tiles + group - 1) / group;  // at most
-  plan->group_rows = 16 * group;
-  plan->grain = kWaves * kStep;
+  plan->group_shift = group == 1 ? 4 : group == 2 ? 5 : 7;
+  static_assert(2 * kSharing == 8, "128 rows to a workgroup whose wavefronts share keys");
+  plan->heads = d.num_q_heads / d.num_kv_heads;
   int64_t target = 512 / d.num_kv_heads;  // workgroups of a kv head
   target = target < 1 ? 1 : target;
   int64_t splits = d.num_splits ? d.num_splits : target;
-  const int64_t most = (span + plan->grain - 1) / plan->grain;
+  const int64_t most = (span + kGrain - 1) / kGrain;
   splits = splits > most ? most : splits;
   splits = splits < 1 ? 1 : splits > 1024 ? 1024 : splits;
   if (d.num_splits) target = (int64_t)d.num_splits * d.batch * plan->row_groups;
-  plan->target = (int32_t)(target < 1 ? 1 : target > 1 << 18 ? 1 << 18 : target);
+  const int64_t room = kMostGroups / d.num_kv_heads;
+  plan->target = (int32_t)(target < 1 ? 1 : target > room ? room : target);
   // each sequence's last chunk may be one more than its share of the target
   const int64_t ends = (int64_t)d.batch * plan->row_groups, most_wg = (plan->target + ends) * d.num_kv_heads;
   plan->fit = d.num_splits == 0 && d.batch <= 64 && ends < plan->target;

@@ -10,6 +10,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
+constexpr int kRowsInFlight = 16;  // of values
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -96,16 +97,34 @@ __global__ __launch_bounds__(kThreads) void kv4_attn_scalar_kernel(Kv4AttnArgs a
     const bool there = p < end;
     const size_t row = there ? kv4_row(d, a.block_table, b, g, p) : 0;
     const float w = block_weight(st, there ? dot_row(d, a.kp, row, q) : 0.f, there);
-    for (int i = 0; i < min(64, end - k0); ++i) {
-      const float pi = __shfl(w, i, 64);
-      const size_t vr = ((size_t)(uint32_t)__shfl((int)(row >> 32), i, 64) << 32) | (uint32_t)__shfl((int)row, i, 64);
+    // values, kRowsInFlight rows asked for before the first is used; a key past the end weighs nothing and reads the block's
+    // first row, whose values are zeroed
+    const int keys = min(64, end - k0);
+    for (int i0 = 0; i0 < keys; i0 += kRowsInFlight) {
+      uint32_t v[kRowsInFlight][2], vs[kRowsInFlight][2];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int byte = lane + 64 * e;  // elements 2 byte, 2 byte + 1
-        if (byte < D / 2) {
-          const kv4_f32x2 v = kv4_pair<0>(a.vp.codes[vr * (D / 2) + byte], kv4_scale(a.vp.scales[vr * (D / kKv4Block) + byte / 16]));
-          st.acc[2 * e] = fmaf(pi, v[0], st.acc[2 * e]);
-          st.acc[2 * e + 1] = fmaf(pi, v[1], st.acc[2 * e + 1]);
+      for (int i = 0; i < kRowsInFlight; ++i) {
+        const int from = i0 + i < keys ? i0 + i : 0;
+        const size_t vr = ((size_t)(uint32_t)__shfl((int)(row >> 32), from, 64) << 32) | (uint32_t)__shfl((int)row, from, 64);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int byte = lane + 64 * e;  // elements 2 byte, 2 byte + 1
+          v[i][e] = 0;
+          vs[i][e] = 127;
+          if (byte < D / 2 && i0 + i < keys) {
+            v[i][e] = a.vp.codes[vr * (D / 2) + byte];
+            vs[i][e] = a.vp.scales[vr * (D / kKv4Block) + byte / 16];
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kRowsInFlight; ++i) {
+        const float pi = __shfl(w, i0 + i, 64);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const kv4_f32x2 x = kv4_pair<0>(v[i][e], kv4_scale(vs[i][e]));
+          st.acc[2 * e] = fmaf(pi, x[0], st.acc[2 * e]);
+          st.acc[2 * e + 1] = fmaf(pi, x[1], st.acc[2 * e + 1]);
         }
       }
     }
@@ -115,6 +134,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attn_scalar_kernel(Kv4AttnArgs a
     float s = 0.f;
     if (there) {
       const T *k = (const T *)a.k_tree + ((size_t)(n0 + lane) * d.num_kv_heads + g) * D;
+#pragma unroll 16
       for (int i = 0; i < D; ++i) s = fmaf(load_f32(k + i), q[i], s);
     }
     const float w = block_weight(st, s, there);
