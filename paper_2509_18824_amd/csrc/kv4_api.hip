@@ -59,7 +59,7 @@ static int32_t make_cut(const hb_attn_desc *d, AttnCut *cut) {
   if (rc) return rc;
   const bool can = kv4_attn_supports(*d);
   if (d->algo == HB_ATTN_MFMA && !can)
-    return fail(HB_ERR_UNSUPPORTED, "HB_ATTN_MFMA over the 4-bit cache needs bf16, head_dim 64 or 128, page_size a multiple of 16 up to "
+    return fail(HB_ERR_UNSUPPORTED, "HB_ATTN_MFMA over the 4-bit cache needs head_dim 64 or 128, page_size a multiple of 16 up to "
                 "1024, a positive softmax_scale and Hq/Hkv <= 512");
   cut->mfma = can && d->algo != HB_ATTN_SCALAR;
   const int64_t rows = (int64_t)d->total_nodes * d->num_q_heads, span = span_of(d);

@@ -1,4 +1,4 @@
-// Attention over the 4-bit cache on the matrix cores of gfx950 (bf16, heads of 64 and 128, pages of a multiple of 16).
+// Attention over the 4-bit cache on the matrix cores of gfx950 (heads of 64 and 128, pages of a multiple of 16).
 //
 // Formulation (transposed, so that no score crosses lanes on its way into the second product):
 //   S^T = K Q^T     v_mfma_scale_f32_16x16x128_f8f6f4: A = 16 cached keys as they lie in memory, 4 bits and a scale byte for
@@ -132,6 +132,9 @@ struct Tile {
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((kv4_f32x2){a, b}, bf16x2));
 }
+
+__device__ __forceinline__ void store4(bf16_t *p, f32x4 v) { *(u32x2 *)p = (u32x2){pack2(v[0], v[1]), pack2(v[2], v[3])}; }
+__device__ __forceinline__ void store4(float *p, f32x4 v) { *(f32x4 *)p = v; }
 
 // Pages of a chunk's keys, 64 times 16 keys to the registers of a wavefront (lane l: the l-th 16) and the next 64 on their way.
 // Asked for one by one, by scalar loads, they would be waited for with the LDS reads of every step.
@@ -281,6 +284,47 @@ struct Rows {
   float m[TPW], ref[TPW], limit[TPW];  // reference exponent (log2 units), the same or 0 where there is none yet, largest sum of weights that keeps it
 };
 
+// ---- float32 ----------------------------------------------------------------------------------------
+// Queries, weights and the nodes' own keys and values are taken as three bf16 pieces of eight bits each, which is all of a
+// float32; cached keys are widened to bf16, which is exact.  A product of two such numbers keeps the six products of pieces that
+// matter to 2^-24, the smallest first.
+__device__ __forceinline__ void pieces_of(const f32x8 &x, bf16x8 (&p)[3]) {
+  f32x8 rest = x;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    p[i] = __builtin_convertvector(rest, bf16x8);
+    rest -= __builtin_convertvector(p[i], f32x8);
+  }
+}
+__device__ __forceinline__ f32x8 load_f32x8(const float *at) {
+  const f32x4 a = *(const f32x4 *)at, b = *(const f32x4 *)(at + 4);
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// lane (j, kg) of the i-th operand of a row: d = 32 kg + 8 i + 0 .. 7, as a cached key's block lies
+template <int DB>
+__device__ __forceinline__ void row_pieces(const float *row, bool there, int kg, bf16x8 (&p)[3][4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f32x8 x = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (there && (DB == 4 || kg < DB)) x = load_f32x8(row + 32 * kg + 8 * i);
+    bf16x8 y[3];
+    pieces_of(x, y);
+    p[0][i] = y[0], p[1][i] = y[1], p[2][i] = y[2];
+  }
+}
+__device__ __forceinline__ void widen_key(const u32x4 &codes, uint32_t scale, bf16x8 (&k)[4]) {
+  const float s = __uint_as_float(scale << 23);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    u32x4 y;
+    y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 0));
+    y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 1));
+    y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 2));
+    y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 3));
+    k[i] = __builtin_bit_cast(bf16x8, y);
+  }
+}
+
 // Scores of 32 keys.  The smaller pieces first, all of them: a sum's second product waits for its first.
 template <int TPW>
 __device__ __forceinline__ void score_tiles(const u32x4 (&k)[2], const int (&ks)[2], const QTile (&q)[TPW], f32x4 (&sc)[TPW][2]) {
@@ -416,9 +460,11 @@ __device__ __forceinline__ void put_values(unsigned char *lv, int key, int kg, c
   }
 }
 
-template <int TPW, int DB, int W>
+template <typename T, int TPW, int DB, int W>
 __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4Plan plan) {
   constexpr int D = 32 * DB, kRow = 64 * DB;
+  constexpr bool F32 = sizeof(T) == 4;
+  static_assert(!F32 || TPW == 1, "float32: one tile of rows");
   const hb_attn_desc &d = a.d;
   // values: 32 keys to a wavefront; at the end a tile's sums of all wavefronts; then references and sums
   __shared__ __attribute__((aligned(16))) unsigned char smem[W * (kStep * kRow > 64 * 16 * 2 * DB ? kStep * kRow : 64 * 16 * 2 * DB)];
@@ -473,16 +519,21 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   }
 
   Rows<TPW, DB> w;
+  bf16x8 q32[3][4];  // float32: the rows' pieces
 #pragma unroll
   for (int t = 0; t < TPW; ++t) {
     const int row = (tile0 + t) * 16 + j;
-    u32x4 x[4] = {};
-    if (row < R) {
-      const u32x4 *src = (const u32x4 *)a.q + row_at(row) * (D / 8);
-      x[0] = src[2 * kg], x[1] = src[2 * kg + 1];
-      if (DB == 4) x[2] = src[8 + 2 * kg], x[3] = src[8 + 2 * kg + 1];
+    if constexpr (F32) {
+      row_pieces<DB>((const float *)a.q + row_at(min(row, R - 1)) * D, row < R, kg, q32);
+    } else {
+      u32x4 x[4] = {};
+      if (row < R) {
+        const u32x4 *src = (const u32x4 *)a.q + row_at(row) * (D / 8);
+        x[0] = src[2 * kg], x[1] = src[2 * kg + 1];
+        if (DB == 4) x[2] = src[8 + 2 * kg], x[3] = src[8 + 2 * kg + 1];
+      }
+      split_rows<DB>(x, w.q[t]);
     }
-    split_rows<DB>(x, w.q[t]);
     w.m[t] = kNegInf;
     w.ref[t] = 0.f;
     w.limit[t] = -1.f;
@@ -504,47 +555,99 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
     const unsigned long long path = path_of(lane < n ? a.parent[n0 + lane] : -1, lane, n);
     const uint32_t mine = (uint32_t)(path >> first);
     f32x4 sc[TPW][2];
-    bf16x8 ak[2][DB];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int node = min(first + 16 * h + j, n - 1);
-      const u32x4 *src = (const u32x4 *)a.k_tree + ((size_t)(n0 + node) * d.num_kv_heads + g) * (D / 8);
-#pragma unroll
-      for (int ks = 0; ks < DB; ++ks) ak[h][ks] = __builtin_bit_cast(bf16x8, src[4 * ks + kg]);
-    }
-#pragma unroll
-    for (int t = 0; t < TPW; ++t) {
+    auto mask = [&](int t) {
       const int row = (tile0 + t) * 16 + j;
-      const u32x4 *src = (const u32x4 *)a.q + row_at(min(row, R - 1)) * (D / 8);
-      sc[t][0] = sc[t][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ks = 0; ks < DB; ++ks) {
-        const bf16x8 qf = __builtin_bit_cast(bf16x8, src[4 * ks + kg]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) sc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ak[h][ks], qf, sc[t][h], 0, 0, 0);
-      }
       const uint32_t allow = (uint32_t)__shfl((int)mine, row < R ? small_div(row, G) : 0, 64) >> (4 * kg);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r) sc[t][h][r] = ((allow >> (16 * h + r)) & 1u) ? sc[t][h][r] : kNegInf;
-    }
-    // values: a node off a row's path weighs 0, and must not make that 0 * NaN
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int key = 16 * h + j, node = first + key;
-      const u32x4 *src = (const u32x4 *)a.v_tree + ((size_t)(n0 + min(node, n - 1)) * d.num_kv_heads + g) * (D / 8);
-#pragma unroll
-      for (int i = 0; i < DB; ++i) {
-        u32x4 x = src[DB * kg + i];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = node < n ? finite_or_zero_bf16x2(x[e]) : 0u;
-        *(u32x4 *)(lv + key * kRow + (((DB * kg + i) ^ (v_swz(key) & (4 * DB - 1))) * 16)) = x;
-      }
-    }
+    };
+    auto piece_at = [&](int key, int piece) { return (u32x4 *)(lv + key * kRow + ((piece ^ (v_swz(key) & (4 * DB - 1))) * 16)); };
     f32x8 p[TPW];
-    weigh<TPW, DB>(w, sc, c1, p);
-    weigh_values<TPW, DB>(w, lv, j, kg, p, true);
+    if constexpr (F32) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        bf16x8 k[3][4];
+        row_pieces<DB>((const float *)a.k_tree + ((size_t)(n0 + min(first + 16 * h + j, n - 1)) * d.num_kv_heads + g) * D, true, kg, k);
+        sc[0][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+          for (int b = 0; b <= sum; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[0][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b][i], q32[sum - b][i], sc[0][h], 0, 0, 0);
+      }
+      mask(0);
+      weigh<TPW, DB>(w, sc, c1, p);
+      bf16x8 weight[3];
+      pieces_of(p[0], weight);
+      // the values a piece at a time; a node off a row's path weighs 0, and must not make that 0 * NaN
+#pragma unroll
+      for (int b = 2; b >= 0; --b) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int key = 16 * h + j, node = first + key;
+          const float *row = (const float *)a.v_tree + ((size_t)(n0 + min(node, n - 1)) * d.num_kv_heads + g) * D;
+#pragma unroll
+          for (int i = 0; i < DB; ++i) {
+            f32x8 x = load_f32x8(row + (DB * kg + i) * 8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = node < n && (__float_as_uint(x[e]) & 0x7f800000u) != 0x7f800000u ? x[e] : 0.f;
+            bf16x8 y[3];
+            pieces_of(x, y);
+            *piece_at(key, DB * kg + i) = __builtin_bit_cast(u32x4, y[b]);
+          }
+        }
+        bf16x8 av[2 * DB];
+        read_values<DB>(lv, j, kg, av);
+        // (the sums of the weights are those that the largest pieces of the values are weighed with)
+        const f32x4 lr = w.lr[0];
+#pragma unroll
+        for (int e = 2 - b; e >= 0; --e) {
+          const bf16x8 one[1] = {weight[e]};
+          accumulate<TPW, DB>(w, av, one);
+        }
+        if (b) w.lr[0] = lr;
+      }
+    } else {
+      bf16x8 ak[2][DB];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int node = min(first + 16 * h + j, n - 1);
+        const u32x4 *src = (const u32x4 *)a.k_tree + ((size_t)(n0 + node) * d.num_kv_heads + g) * (D / 8);
+#pragma unroll
+        for (int ks = 0; ks < DB; ++ks) ak[h][ks] = __builtin_bit_cast(bf16x8, src[4 * ks + kg]);
+      }
+#pragma unroll
+      for (int t = 0; t < TPW; ++t) {
+        const int row = (tile0 + t) * 16 + j;
+        const u32x4 *src = (const u32x4 *)a.q + row_at(min(row, R - 1)) * (D / 8);
+        sc[t][0] = sc[t][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < DB; ++ks) {
+          const bf16x8 qf = __builtin_bit_cast(bf16x8, src[4 * ks + kg]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) sc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ak[h][ks], qf, sc[t][h], 0, 0, 0);
+        }
+        mask(t);
+      }
+      // values: a node off a row's path weighs 0, and must not make that 0 * NaN
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int key = 16 * h + j, node = first + key;
+        const u32x4 *src = (const u32x4 *)a.v_tree + ((size_t)(n0 + min(node, n - 1)) * d.num_kv_heads + g) * (D / 8);
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+          u32x4 x = src[DB * kg + i];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = node < n ? finite_or_zero_bf16x2(x[e]) : 0u;
+          *piece_at(key, DB * kg + i) = x;
+        }
+      }
+      weigh<TPW, DB>(w, sc, c1, p);
+      weigh_values<TPW, DB>(w, lv, j, kg, p, true);
+    }
   }
 
   // ---- the prefix -------------------------------------------------------------------------------------
@@ -552,8 +655,21 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   auto attend = [&](auto tail, int step, Tile &x, int left) {
     constexpr bool kTail = decltype(tail)::value;
     f32x4 sc[TPW][2];
-    const int ks[2] = {(int)x.ks[0], (int)x.ks[1]};
-    score_tiles<TPW>(x.k, ks, w.q, sc);
+    if constexpr (F32) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        bf16x8 k[4];
+        widen_key(x.k[h], x.ks[h], k);
+        sc[0][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int b = 2; b >= 0; --b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[0][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i], q32[b][i], sc[0][h], 0, 0, 0);
+      }
+    } else {
+      const int ks[2] = {(int)x.ks[0], (int)x.ks[1]};
+      score_tiles<TPW>(x.k, ks, w.q, sc);
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       u32x4 c = x.v[h];
@@ -578,7 +694,18 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
     }
     f32x8 p[TPW];
     weigh<TPW, DB>(w, sc, c1, p);
-    weigh_values<TPW, DB>(w, lv, j, kg, p, kTail);
+    if constexpr (F32) {
+      bf16x8 weight[3], av[2 * DB];
+      pieces_of(p[0], weight);
+      read_values<DB>(lv, j, kg, av);
+#pragma unroll
+      for (int b = 2; b >= 0; --b) {
+        const bf16x8 one[1] = {weight[b]};
+        accumulate<TPW, DB>(w, av, one);
+      }
+    } else {
+      weigh_values<TPW, DB>(w, lv, j, kg, p, kTail);
+    }
   };
   if (wave < steps) {
     const int whole = (ch.end - ch.begin) / kStep;
@@ -627,8 +754,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
       for (int i = 0; i < W; ++i) o += all[(dt * W + i) * 64 + lane];
       if (row < R) {
         if (ch.chunks == 1) {
-          const float inv = 1.f / l;
-          *(u32x2 *)((bf16_t *)a.out + rr * D + 16 * dt + 4 * kg) = (u32x2){pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
+          store4((T *)a.out + rr * D + 16 * dt + 4 * kg, o * (1.f / l));
         } else {
           *(f32x4 *)(a.part_o + (rr * plan.splits + ch.c) * D + 16 * dt + 4 * kg) = o;
         }
@@ -907,10 +1033,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
     if (ch.chunks == 1) {
       const float inv = scale / l;
 #pragma unroll
-      for (int dt = 0; dt < 2 * DB; ++dt) {
-        const f32x4 o = w.o[t][dt] * inv;
-        *(u32x2 *)((bf16_t *)a.out + rr * D + 16 * dt + 4 * kg) = (u32x2){pack2(o[0], o[1]), pack2(o[2], o[3])};
-      }
+      for (int dt = 0; dt < 2 * DB; ++dt)
+        store4((bf16_t *)a.out + rr * D + 16 * dt + 4 * kg, w.o[t][dt] * inv);
       if (a.lse && kg == 0) a.lse[rr] = (w.m[t] + log2f(l)) * kLn2;
     } else {
       float *po = a.part_o + (rr * plan.splits + ch.c) * D;
@@ -923,6 +1047,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
 
 // Rows of sequences that were cut: the chunks' results joined (log2 units).  A row's threads hold four elements each; results
 // are asked for eight chunks at a time.
+template <typename T>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a, Kv4Plan plan) {
   const int D = a.d.head_dim, tpr = D / 4;
   const int len = *a.cut;
@@ -963,14 +1088,13 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a, Kv4Plan pl
       }
     }
   }
-  const float inv = 1.f / l;
-  *(u32x2 *)((bf16_t *)a.out + (size_t)row * D + piece * 4) = (u32x2){pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
+  store4((T *)a.out + (size_t)row * D + piece * 4, o * (1.f / l));
   if (a.lse && piece == 0) a.lse[row] = (m + log2f(l)) * kLn2;
 }
 
-template <int TPW, int DB, int W>
+template <typename T, int TPW, int DB>
 hipError_t launch(const Kv4AttnArgs &a, const Kv4Plan &plan, hipStream_t s) {
-  kv4_attn_kernel<TPW, DB, W><<<(unsigned)plan.grid, 64 * W, 0, s>>>(a, plan);
+  kv4_attn_kernel<T, TPW, DB, kWaves><<<(unsigned)plan.grid, 64 * kWaves, 0, s>>>(a, plan);
   return hipGetLastError();
 }
 
@@ -990,16 +1114,16 @@ constexpr int64_t kMostGroups = 1 << 22;  // workgroups
 
 bool kv4_attn_supports(const hb_attn_desc &d) {
   // what the workgroups count with 32 bits: pieces, and grains times row groups
-  const int64_t ends = (int64_t)d.batch * ((tiles_of(d) + 1) / 2 + 1);
+  const int64_t ends = (int64_t)d.batch * tiles_of(d);
   if (ends * d.num_kv_heads > kMostGroups || ends * (((int64_t)d.page_size * d.max_blocks_per_seq) / kGrain + 1) > 1 << 30) return false;
-  return d.dtype == HB_BF16 && (d.head_dim == 64 || d.head_dim == 128) && d.page_size % 16 == 0 && d.page_size <= 1024 &&
+  return (d.head_dim == 64 || d.head_dim == 128) && d.page_size % 16 == 0 && d.page_size <= 1024 &&
          d.softmax_scale > 0.f && d.softmax_scale < 1e30f && d.num_q_heads / d.num_kv_heads <= 512;
 }
 
 
 // Chunks are planned for some 512 workgroups
 void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
-  const int tiles = tiles_of(d), group = shares_keys(d) ? 2 * kSharing : tiles > 1 ? 2 : 1;
+  const int tiles = tiles_of(d), group = d.dtype == HB_F32 ? 1 : shares_keys(d) ? 2 * kSharing : tiles > 1 ? 2 : 1;
   plan->row_groups = (tiles + group - 1) / group;  // at most
   plan->group_shift = group == 1 ? 4 : group == 2 ? 5 : 7;
   static_assert(2 * kSharing == 8, "128 rows to a workgroup whose wavefronts share keys");
@@ -1023,14 +1147,17 @@ void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
 }
 
 hipError_t launch_kv4_attn(const Kv4AttnArgs &a, const Kv4Plan &plan, hipStream_t s) {
-  const bool wide = tiles_of(a.d) > 1;
+  const bool f32 = a.d.dtype == HB_F32, wide = tiles_of(a.d) > 1, whole = a.d.head_dim == 128;
   hipError_t e;
-  if (shares_keys(a.d)) e = a.d.head_dim == 128 ? launch_rows<4, kSharing>(a, plan, s) : launch_rows<2, kSharing>(a, plan, s);
-  else if (a.d.head_dim == 128) e = wide ? launch<2, 4, kWaves>(a, plan, s) : launch<1, 4, kWaves>(a, plan, s);
-  else e = wide ? launch<2, 2, kWaves>(a, plan, s) : launch<1, 2, kWaves>(a, plan, s);
+  if (f32) e = whole ? launch<float, 1, 4>(a, plan, s) : launch<float, 1, 2>(a, plan, s);
+  else if (shares_keys(a.d)) e = whole ? launch_rows<4, kSharing>(a, plan, s) : launch_rows<2, kSharing>(a, plan, s);
+  else if (wide) e = whole ? launch<bf16_t, 2, 4>(a, plan, s) : launch<bf16_t, 2, 2>(a, plan, s);
+  else e = whole ? launch<bf16_t, 1, 4>(a, plan, s) : launch<bf16_t, 1, 2>(a, plan, s);
   if (e != hipSuccess || plan.splits == 1) return e;
   const long threads = (long)a.d.total_nodes * a.d.num_q_heads * (a.d.head_dim / 4);
-  kv4_join_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(a, plan);
+  const unsigned grid = (unsigned)((threads + 255) / 256);
+  if (f32) kv4_join_kernel<float><<<grid, 256, 0, s>>>(a, plan);
+  else kv4_join_kernel<bf16_t><<<grid, 256, 0, s>>>(a, plan);
   return hipGetLastError();
 }
 
