@@ -1,20 +1,18 @@
 // Attention over the 4-bit cache on the matrix cores of gfx950 (heads of 64 and 128, pages of a multiple of 16).
 //
 // Formulation (transposed, so that no score crosses lanes on its way into the second product):
-//   S^T = K Q^T     v_mfma_scale_f32_16x16x128_f8f6f4: A = 16 cached keys as they lie in memory, 4 bits and a scale byte for
-//                   every 32 elements (a lane holds one block: 16 bytes); B = 16 query rows in 8 bits, twice
-//   O^T = V^T P^T   v_mfma_f32_16x16x32_bf16: A = V^T (16 d x 32 keys), values widened to bf16, which is exact
-// A query row is cut in two 8-bit pieces: q = 2^(E-7) (hi + lo / 16), E the exponent of the row's largest element, hi and lo
-// E4M3.  Eight significant bits are two times four, so the pieces are q exactly, except for elements below 2^-14 of the largest
-// (what is lost lies below 2^-22 of it).  Two such products take 2.4 times a bf16 product of a quarter of the length, and
-// keys are never unpacked.  The matrix core drops what lies some 2^-15 below the largest product of a sum: scores are off by
-// 5e-6 of their spread (root of the mean square, N(0, 1) data), where bf16 probabilities are off by 2e-3.
+//   S^T = K Q^T     v_mfma_f32_16x16x32_bf16: A = 16 cached keys (16 keys x 32 d), B = 16 query rows
+//   O^T = V^T P^T   the same: A = V^T (16 d x 32 keys), B = P^T
+// A block of 32 cached numbers is widened to bf16 by one instruction for two of them, scale included, and exactly: scores are
+// those of a bf16 cache.  (The matrix cores also take the codes as they are, against 8-bit pieces of the queries: two pieces
+// of a 128-long product cost the same 64 clocks as the four bf16 products, and what the hardware drops of such a sum, 5e-6
+// of a score's spread, shows in the log-sum-exp.)
 // Probabilities are rounded to bf16 for the second product, sums are kept in 32 bits.
 //
 // A wavefront takes 32 keys at a time of its own and TPW tiles of 16 query rows (row = node * G + head of the group); the
 // wavefronts of a workgroup take turns on the steps of a chunk of the prefix and join their results in LDS at its end.  Nobody
-// waits for anybody in between: a step's codes go from memory to registers two steps ahead, keys to the matrix core as they
-// are, values through 8 KB of LDS of the wavefront's own, where a transposing read turns them.
+// waits for anybody in between: a step's codes go from memory to registers two steps ahead, keys from there to the matrix core,
+// values through 8 KB of LDS of the wavefront's own, where a transposing read turns them.
 //
 // Chunks are cut on the device from the lengths (kv4_plan below), so that about as many workgroups start as the host planned
 // for, whatever the lengths are.
@@ -78,49 +76,30 @@ __device__ __forceinline__ uint32_t finite_or_zero_bf16x2(uint32_t w) {
   return lo | hi;
 }
 
-// 16 query rows as the B operand: lane (j, kg) holds d = 16 kg + 0 .. 15 and 64 + 16 kg + 0 .. 15 of row j
-struct QTile {
-  i32x8 hi, lo;
-  int hi_scale, lo_scale;
-};
-
+// A row as operand of the scores' products: lane (j, kg) of the i-th holds d = 32 kg + 8 i + 0 .. 7 of row j, which is how a cached
+// key's block kg lies.  (Heads of 64: lanes without a block hold zeros.)
 template <int DB>
-__device__ __forceinline__ void split_rows(const u32x4 (&x)[4], QTile &q) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 2 * (DB / 2); ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) top = max(top, max((x[i][e] << 16) & 0x7fffffffu, x[i][e] & 0x7fff0000u));
-  top = __float_as_uint(group_max(__uint_as_float(top > 0x7f800000u ? 0x7f800000u : top)));
-  const bool fine = top < 0x7f800000u;
-  int E = (int)(top >> 23) - 127;
-  E = E < -115 ? -115 : E;
-  const float unit = __uint_as_float((uint32_t)(127 + 7 - (fine ? E : 0)) << 23);  // 2^(7 - E)
+__device__ __forceinline__ void row_operand(const u32x4 *row, bool there, int kg, bf16x8 (&x)[4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    // words 2 i and 2 i + 1 of the operand: eight elements
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      int hi = 0, lo = 0;
-      if (i < 2 * (DB / 2)) {
-        float a[4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          a[2 * e] = __uint_as_float(x[i][2 * w + e] << 16) * unit;
-          a[2 * e + 1] = __uint_as_float(x[i][2 * w + e] & 0xffff0000u) * unit;
-        }
-        hi = __builtin_amdgcn_cvt_pk_fp8_f32(a[0], a[1], hi, false);
-        hi = __builtin_amdgcn_cvt_pk_fp8_f32(a[2], a[3], hi, true);
-        const kv4_f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), c = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-        lo = __builtin_amdgcn_cvt_pk_fp8_f32((a[0] - b[0]) * 16.f, (a[1] - b[1]) * 16.f, lo, false);
-        lo = __builtin_amdgcn_cvt_pk_fp8_f32((a[2] - c[0]) * 16.f, (a[3] - c[1]) * 16.f, lo, true);
-      }
-      q.hi[2 * i + w] = fine ? hi : 0x7f7f7f7f;  // NaN
-      q.lo[2 * i + w] = fine ? lo : 0;
-    }
+    u32x4 y = {0u, 0u, 0u, 0u};
+    if (there && (DB == 4 || kg < DB)) y = row[4 * kg + i];
+    x[i] = __builtin_bit_cast(bf16x8, y);
   }
-  q.hi_scale = E + 120;
-  q.lo_scale = E + 116;
+}
+
+// a block of 32 codes as the same operand
+__device__ __forceinline__ u32x4 widen8(uint32_t codes, float scale) {
+  u32x4 y;
+  y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+  y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+  y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+  y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+  return y;
+}
+__device__ __forceinline__ void widen_key(const u32x4 &codes, uint32_t scale, bf16x8 (&k)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) k[i] = __builtin_bit_cast(bf16x8, widen8(codes[i], __uint_as_float(scale << 23)));
 }
 
 // What a wavefront holds of 32 keys: lane (j, kg) the block kg of keys j and 16 + j
@@ -277,7 +256,7 @@ __device__ __forceinline__ unsigned long long path_of(int par, int lane, int n) 
 
 template <int TPW, int DB>
 struct Rows {
-  QTile q[TPW];
+  bf16x8 q[TPW][4];
   f32x4 o[TPW][2 * DB];  // O^T: lane (j, kg) holds d = 16 dt + 4 kg + r of row j
   f32x4 lr[TPW];         // row sums of the rounded weights (every element), which is what the values are weighed with
   float l[TPW];          // of the weights as they are, the lane's own keys: a log-sum-exp of few keys would show their rounding
@@ -312,35 +291,14 @@ __device__ __forceinline__ void row_pieces(const float *row, bool there, int kg,
     p[0][i] = y[0], p[1][i] = y[1], p[2][i] = y[2];
   }
 }
-__device__ __forceinline__ void widen_key(const u32x4 &codes, uint32_t scale, bf16x8 (&k)[4]) {
-  const float s = __uint_as_float(scale << 23);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    u32x4 y;
-    y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 0));
-    y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 1));
-    y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 2));
-    y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 3));
-    k[i] = __builtin_bit_cast(bf16x8, y);
-  }
-}
-
-// Scores of 32 keys.  The smaller pieces first, all of them: a sum's second product waits for its first.
+// Scores of 16 keys
 template <int TPW>
-__device__ __forceinline__ void score_tiles(const u32x4 (&k)[2], const int (&ks)[2], const QTile (&q)[TPW], f32x4 (&sc)[TPW][2]) {
-  i32x8 ak[2];
+__device__ __forceinline__ void score_tiles(const bf16x8 (&k)[4], const bf16x8 (&q)[TPW][4], int h, f32x4 (&sc)[TPW][2]) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) ak[h] = (i32x8){(int)k[h][0], (int)k[h][1], (int)k[h][2], (int)k[h][3], 0, 0, 0, 0};
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-  for (int t = 0; t < TPW; ++t)
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      sc[t][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ak[h], q[t].lo, (f32x4){0.f, 0.f, 0.f, 0.f}, 4, 0, 0, ks[h], 0, q[t].lo_scale);
-#pragma unroll
-  for (int t = 0; t < TPW; ++t)
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      sc[t][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ak[h], q[t].hi, sc[t][h], 4, 0, 0, ks[h], 0, q[t].hi_scale);
+    for (int t = 0; t < TPW; ++t)
+      sc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i], q[t][i], i ? sc[t][h] : (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 }
 
 // Softmax weights of a step's scores.  A row's reference is the largest score of the first step it sees, and moves when the
@@ -443,21 +401,13 @@ __device__ __forceinline__ void weigh_values(Rows<TPW, DB> &w, const unsigned ch
   accumulate<TPW, DB>(w, av, pb);
 }
 
-// A key's block of 32 values, widened, into its row in LDS
+// A key's block of 32 numbers, widened, into its row in LDS
 template <int DB>
-__device__ __forceinline__ void put_values(unsigned char *lv, int key, int kg, const u32x4 &codes, uint32_t scale) {
+__device__ __forceinline__ void put_block(unsigned char *lv, int key, int kg, const u32x4 &codes, uint32_t scale) {
   constexpr int kRow = 64 * DB;
-  const float s = __uint_as_float(scale << 23);
   const int x = v_swz(key) & (4 * DB - 1);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    u32x4 y;
-    y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 0));
-    y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 1));
-    y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 2));
-    y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 3));
-    *(u32x4 *)(lv + key * kRow + (((4 * kg + i) ^ x) * 16)) = y;
-  }
+  for (int i = 0; i < 4; ++i) *(u32x4 *)(lv + key * kRow + (((4 * kg + i) ^ x) * 16)) = widen8(codes[i], __uint_as_float(scale << 23));
 }
 
 template <typename T, int TPW, int DB, int W>
@@ -526,13 +476,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
     if constexpr (F32) {
       row_pieces<DB>((const float *)a.q + row_at(min(row, R - 1)) * D, row < R, kg, q32);
     } else {
-      u32x4 x[4] = {};
-      if (row < R) {
-        const u32x4 *src = (const u32x4 *)a.q + row_at(row) * (D / 8);
-        x[0] = src[2 * kg], x[1] = src[2 * kg + 1];
-        if (DB == 4) x[2] = src[8 + 2 * kg], x[3] = src[8 + 2 * kg + 1];
-      }
-      split_rows<DB>(x, w.q[t]);
+      row_operand<DB>((const u32x4 *)a.q + row_at(min(row, R - 1)) * (D / 8), row < R, kg, w.q[t]);
     }
     w.m[t] = kNegInf;
     w.ref[t] = 0.f;
@@ -611,27 +555,14 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
         if (b) w.lr[0] = lr;
       }
     } else {
-      bf16x8 ak[2][DB];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int node = min(first + 16 * h + j, n - 1);
-        const u32x4 *src = (const u32x4 *)a.k_tree + ((size_t)(n0 + node) * d.num_kv_heads + g) * (D / 8);
-#pragma unroll
-        for (int ks = 0; ks < DB; ++ks) ak[h][ks] = __builtin_bit_cast(bf16x8, src[4 * ks + kg]);
+        bf16x8 k[4];
+        row_operand<DB>((const u32x4 *)a.k_tree + ((size_t)(n0 + min(first + 16 * h + j, n - 1)) * d.num_kv_heads + g) * (D / 8), true, kg, k);
+        score_tiles<TPW>(k, w.q, h, sc);
       }
 #pragma unroll
-      for (int t = 0; t < TPW; ++t) {
-        const int row = (tile0 + t) * 16 + j;
-        const u32x4 *src = (const u32x4 *)a.q + row_at(min(row, R - 1)) * (D / 8);
-        sc[t][0] = sc[t][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < DB; ++ks) {
-          const bf16x8 qf = __builtin_bit_cast(bf16x8, src[4 * ks + kg]);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) sc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ak[h][ks], qf, sc[t][h], 0, 0, 0);
-        }
-        mask(t);
-      }
+      for (int t = 0; t < TPW; ++t) mask(t);
       // values: a node off a row's path weighs 0, and must not make that 0 * NaN
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -655,20 +586,19 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   auto attend = [&](auto tail, int step, Tile &x, int left) {
     constexpr bool kTail = decltype(tail)::value;
     f32x4 sc[TPW][2];
-    if constexpr (F32) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        bf16x8 k[4];
-        widen_key(x.k[h], x.ks[h], k);
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 k[4];
+      widen_key(x.k[h], x.ks[h], k);
+      if constexpr (F32) {
         sc[0][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int b = 2; b >= 0; --b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) sc[0][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i], q32[b][i], sc[0][h], 0, 0, 0);
+      } else {
+        score_tiles<TPW>(k, w.q, h, sc);
       }
-    } else {
-      const int ks[2] = {(int)x.ks[0], (int)x.ks[1]};
-      score_tiles<TPW>(x.k, ks, w.q, sc);
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -680,7 +610,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
         for (int e = 0; e < 4; ++e) c[e] = there ? c[e] : 0u;
         s = there ? s : 127u;
       }
-      if (DB == 4 || kg < DB) put_values<DB>(lv, 16 * h + j, kg, c, s);
+      if (DB == 4 || kg < DB) put_block<DB>(lv, 16 * h + j, kg, c, s);
     }
     if (kTail) {
 #pragma unroll
@@ -773,8 +703,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
 
 // ---- many rows ------------------------------------------------------------------------------------------
 // The same products where a (sequence, kv head) has many query rows (60 nodes of 7 heads: 27 tiles): the W wavefronts of a
-// workgroup have up to two tiles of rows each and share 64 keys at a time, whose values are widened into LDS once for all.  The
-// keys' codes lie there as they are; a wavefront's operand of 16 keys is one contiguous kilobyte.
+// workgroup have up to two tiles of rows each and share 64 keys at a time, which are widened into LDS once for all.
 // The loop over 32-key blocks is skewed by one: the matrix core gets a block's V^T P^T and the next one's scores in one go, and
 // the vector work that follows has its scores already.  A thread asks for its share of a tile (16 bytes of keys and of
 // values, two scales) two tiles ahead and puts it in LDS one tile ahead, while the matrix core has that work.  Two stages of
@@ -783,9 +712,9 @@ template <int DB, int W>
 __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4Plan plan) {
   constexpr int D = 32 * DB, kRow = 64 * DB, TPW = 2, kTile = 64, kThreads = 64 * W;
   constexpr int kPieces = kTile * DB, kShare = (kPieces + kThreads - 1) / kThreads;  // 16-byte pieces of a tile; of a thread
-  constexpr int kStage = kTile * (kRow + 16 * DB + DB);
+  constexpr int kStage = 2 * kTile * kRow;
   const hb_attn_desc &d = a.d;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[2 * kStage];  // [values 64 x kRow | key codes 64 x D / 2 | key scales]
+  __shared__ __attribute__((aligned(16))) unsigned char smem[2 * kStage];  // [values 64 x kRow | keys 64 x kRow]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 15, kg = lane >> 4;
   Piece ch;
@@ -849,9 +778,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
         for (int e = 0; e < 4; ++e) c[e] = there ? c[e] : 0u;
         s = there ? s : 127u;
       }
-      put_values<DB>(st, key, blk, c, s);
-      *(u32x4 *)(st + kTile * kRow + piece * 16) = x.k[i];
-      st[kTile * (kRow + 16 * DB) + piece] = (unsigned char)x.ks[i];
+      put_block<DB>(st, key, blk, c, s);
+      put_block<DB>(st + kTile * kRow, key, blk, x.k[i], x.ks[i]);
     }
   };
 
@@ -867,13 +795,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
 #pragma unroll
   for (int t = 0; t < TPW; ++t) {
     const int row = row_of(t);
-    u32x4 q[4] = {};
-    if (row < R) {
-      const u32x4 *src = (const u32x4 *)a.q + row_at(row) * (D / 8);
-      q[0] = src[2 * kg], q[1] = src[2 * kg + 1];
-      if (DB == 4) q[2] = src[8 + 2 * kg], q[3] = src[8 + 2 * kg + 1];
-    }
-    split_rows<DB>(q, w.q[t]);
+    row_operand<DB>((const u32x4 *)a.q + row_at(min(row, R - 1)) * (D / 8), row < R, kg, w.q[t]);
     w.m[t] = kNegInf;
     w.ref[t] = 0.f;
     w.limit[t] = -1.f;
@@ -907,19 +829,10 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
       const uint32_t mine = (uint32_t)(path >> (32 * blk));
       f32x4 sc[TPW][2];
 #pragma unroll
-      for (int t = 0; t < TPW; ++t) sc[t][0] = sc[t][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ks = 0; ks < DB; ++ks) {
-        bf16x8 ak[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          ak[h] = __builtin_bit_cast(bf16x8, ((const u32x4 *)a.k_tree)[((size_t)(n0 + min(32 * blk + 16 * h + j, n - 1)) * d.num_kv_heads + g) * (D / 8) + 4 * ks + kg]);
-#pragma unroll
-        for (int t = 0; t < TPW; ++t) {
-          const bf16x8 qf = __builtin_bit_cast(bf16x8, ((const u32x4 *)a.q)[row_at(min(row_of(t), R - 1)) * (D / 8) + 4 * ks + kg]);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) sc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ak[h], qf, sc[t][h], 0, 0, 0);
-        }
+      for (int h = 0; h < 2; ++h) {
+        bf16x8 k[4];
+        row_operand<DB>((const u32x4 *)a.k_tree + ((size_t)(n0 + min(32 * blk + 16 * h + j, n - 1)) * d.num_kv_heads + g) * (D / 8), true, kg, k);
+        score_tiles<TPW>(k, w.q, h, sc);
       }
 #pragma unroll
       for (int t = 0; t < TPW; ++t) {
@@ -940,22 +853,23 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
   if (n_tiles > 0) {
     f32x4 sc[TPW][2];
     bf16x8 av[2 * DB];
-    u32x4 kc[2];  // a block's keys
-    int ks[2];
+    bf16x8 ak[2][4];  // a block's keys
     auto read_keys = [&](auto stage, int blk) {
       const unsigned char *at = smem + decltype(stage)::value * kStage + kTile * kRow;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int key = 32 * blk + 16 * h + j;
-        kc[h] = (u32x4){0u, 0u, 0u, 0u};
-        ks[h] = 127;
-        if (DB == 4 || kg < DB) {
-          kc[h] = *(const u32x4 *)(at + (key * DB + kg) * 16);
-          ks[h] = at[kTile * 16 * DB + key * DB + kg];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ak[h][i] = __builtin_bit_cast(bf16x8, (u32x4){0u, 0u, 0u, 0u});
+          if (DB == 4 || kg < DB) ak[h][i] = *(const bf16x8 *)(at + key * kRow + (((4 * kg + i) ^ (v_swz(key) & (4 * DB - 1))) * 16));
         }
       }
     };
-    auto scores = [&] { score_tiles<TPW>(kc, ks, w.q, sc); };
+    auto scores = [&] {
+      score_tiles<TPW>(ak[0], w.q, 0, sc);
+      score_tiles<TPW>(ak[1], w.q, 1, sc);
+    };
     // softmax of the scores that there are; the values of their block are asked for first
     auto vector_work = [&](int tile, auto stage, int blk, f32x8 (&p)[TPW]) {
       read_values<DB>(smem + decltype(stage)::value * kStage + 32 * blk * kRow, j, kg, av);
