@@ -138,11 +138,9 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(hb_attn_desc d, int rows,
 // ---- eviction ------------------------------------------------------------------------------------------
 // order-preserving bits of a weight; not a number counts as the least, protected positions as the greatest
 __device__ inline uint32_t weight_key(float w, bool safe) {
-  if (safe) w = __builtin_huge_valf();
-  if (!(w == w)) w = -__builtin_huge_valf();
-  if (w == 0.f) w = 0.f;  // -0 weighs what 0 does
-  const uint32_t u = __float_as_uint(w);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+  w = fmaxf(w, -__builtin_huge_valf()) + 0.f;  // a number; and -0 weighs what 0 does
+  const uint32_t u = __float_as_uint(safe ? __builtin_huge_valf() : w);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 constexpr int kSelectThreads = 1024;
@@ -173,8 +171,11 @@ __device__ inline void load_keys(const float *w, const int32_t *pos, int s, int 
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     p[e] = y[e];
-    key[e] = s + e < L ? weight_key(x[e], y[e] >= recent_from || y[e] < sinks) : 0u;
+    key[e] = weight_key(x[e], y[e] >= recent_from || y[e] < sinks);
   }
+  if (s + 3 >= L)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) key[e] = s + e < L ? key[e] : 0u;
 }
 
 // number of the wavefront's slots in front of this lane's first one that a flag of theirs is set for: flag e of a lane is slot

@@ -57,9 +57,10 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_weight_kernel(Kv4WeightArgs a
   __shared__ float s_lse[kRows];
   __shared__ int s_path[64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, kg = lane >> 4;
-  const int h = blockIdx.y % d.num_kv_heads, b = blockIdx.y / d.num_kv_heads, G = d.num_q_heads / d.num_kv_heads;
+  // units are neighbours, not chunks: workgroup ids go round the XCDs, and the chunks behind short sequences are empty
+  const int h = blockIdx.x % d.num_kv_heads, b = blockIdx.x / d.num_kv_heads, G = d.num_q_heads / d.num_kv_heads;
   // a wavefront's keys: 64 in each round, the first at k0; what has to be known first is asked for in one go
-  const int begin = blockIdx.x * rounds * kWaves * kKeys, k0 = begin + wave * kKeys;
+  const int begin = (int)(blockIdx.z * gridDim.y + blockIdx.y) * rounds * kWaves * kKeys, k0 = begin + wave * kKeys;
   const int cap16 = d.max_blocks_per_seq * (d.page_size / 16);
   const int32_t *table = a.block_table + (size_t)b * d.max_blocks_per_seq;
   // lane 4 r + t: the page of the t-th 16 keys of round r
@@ -218,7 +219,8 @@ hipError_t launch_kv4_weight_mfma(const Kv4WeightArgs &a, int32_t longest, hipSt
   int64_t rounds = units * longest / (256 * 1024);
   rounds = rounds < 1 ? 1 : rounds > 8 ? 8 : rounds;  // a wavefront holds the pages of sixteen rounds
   const int keys = (int)rounds * kWaves * kKeys;
-  const dim3 grid((unsigned)((longest + keys - 1) / keys), (unsigned)units);
+  const unsigned chunks = (unsigned)((longest + keys - 1) / keys), rows_of_grid = chunks < 32768 ? chunks : 32768;
+  const dim3 grid((unsigned)units, rows_of_grid, (chunks + rows_of_grid - 1) / rows_of_grid);
   const bool f32 = a.d.dtype == HB_F32;
   if (a.d.head_dim == 128) {
     if (f32) kv4_weight_kernel<float, 4><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds);
