@@ -964,15 +964,32 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a, Kv4Plan plan) {
   const int D = a.d.head_dim, tpr = D / 4;
-  const int len = *a.cut;
+  const int len = *a.cut, lane = threadIdx.x & 63;
   const long gid = (long)blockIdx.x * 256 + threadIdx.x;
   const int row = (int)(gid / tpr), piece = (int)(gid - (long)row * tpr);
-  if (row >= a.d.total_nodes * a.d.num_q_heads) return;
-  const int node = row / a.d.num_q_heads, b = kv4_sequence(a.node_offset, a.d.batch, node);
-  const int first = a.node_offset[b], n = min(a.node_offset[b + 1] - first, a.d.max_nodes_per_tree);
-  if (node < first || node >= first + n || first + n > a.d.total_nodes) return;
-  const int chunks = chunks_of(grains_of(kv4_length(a.d, a.prefix_len, b)), len);
-  if (chunks == 1) return;
+  const int node = row / a.d.num_q_heads;
+  // the row's sequence: up to 64 of them by their offsets in the lanes, which is one round trip
+  int b, n0, n1, L;
+  if (a.d.batch <= 64) {
+    const bool there = lane < a.d.batch;
+    const int at = there ? a.node_offset[lane] : 0, behind = there ? a.node_offset[lane + 1] : 0;
+    const int length = there ? kv4_length(a.d, a.prefix_len, lane) : 0;
+    b = 0;
+    for (int r = 0; r < 64; r += tpr) {  // the wavefront's rows
+      const unsigned long long m = __ballot(there && at <= __builtin_amdgcn_readlane(node, r));
+      b = lane >= r && m ? 63 - __builtin_clzll(m) : b;
+    }
+    n0 = __shfl(at, b, 64);
+    n1 = __shfl(behind, b, 64);
+    L = __shfl(length, b, 64);
+  } else {
+    b = kv4_sequence(a.node_offset, a.d.batch, node < a.d.total_nodes ? node : 0);
+    n0 = a.node_offset[b];
+    n1 = a.node_offset[b + 1];
+    L = kv4_length(a.d, a.prefix_len, b);
+  }
+  const int chunks = chunks_of(grains_of(L), len);
+  if (row >= a.d.total_nodes * a.d.num_q_heads || node < n0 || node >= n0 + nodes_of(a.d, n0, n1) || chunks == 1) return;
   const kv4_f32x2 *ml = (const kv4_f32x2 *)a.part_ml + (size_t)row * plan.splits;
   const f32x4 *po = (const f32x4 *)a.part_o + (size_t)row * plan.splits * tpr + piece;
   float m = kNegInf, l = 0.f;
