@@ -27,13 +27,14 @@ struct Kv4AttnArgs {
   const int32_t *block_table, *prefix_len, *node_offset, *parent;
   void *out;
   float *lse, *part_o, *part_ml;
-  int32_t *cut;  // the matrix-core kernels' chunk length, in grains of 128 keys, or null where they do not cut
+  int32_t *cut;  // the matrix-core kernels' chunk length, in grains, or null where they do not cut
 };
 // How the matrix-core kernel cuts the prefixes, from what the host knows
 struct Kv4Plan {
   int32_t row_groups;   // workgroups that share a chunk's query rows, at most
   int32_t heads;        // query heads of a kv head
   int32_t group_shift;  // log2 of the query rows of a row group
+  int32_t grain_shift;  // log2 of the keys that a chunk's length is a multiple of, its grains
   int32_t target;       // workgroups per kv head, over all sequences
   int32_t fit;          // not more than these, if longer chunks can do it
   int32_t splits;       // chunks of a sequence, at most: slots of part_o and part_ml

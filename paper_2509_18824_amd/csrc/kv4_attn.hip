@@ -14,8 +14,13 @@
 // waits for anybody in between: a step's codes go from memory to registers two steps ahead, keys from there to the matrix core,
 // values through 8 KB of LDS of the wavefront's own, where a transposing read turns them.
 //
-// Chunks are cut on the device from the lengths (kv4_plan below), so that about as many workgroups start as the host planned
-// for, whatever the lengths are.
+// Chunks are cut on the device from the lengths (find_piece below), so that about as many workgroups start as the host planned
+// for, whatever the lengths are: one to a CU, of eight wavefronts of up to 256 registers each.
+//
+// What bounds it, single tokens: memory.  16 of them over 16384 to 32768 positions, 28/4 heads of 128, 214 MB: 51 us, the join
+// with 5 of them included, 4.2 TB/s (a large copy runs at 5.1); one over 2048, 1.1 MB: 12 and 4.5 us, the round trips to lengths,
+// pages, codes and back and the start of two launches.  16 chains of 8 nodes (56 rows) over 1024 to 4096: 25 and 5 us, a
+// few steps to a wavefront between the same round trips.  Two workgroups of four wavefronts to a CU: 53, 12.6 and 25.4 us.
 #include "kv4.h"
 #include "wave_ops.h"
 
@@ -37,9 +42,8 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int swap2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStep = 32;  // keys
-constexpr int kWaves = 4;  // of a workgroup
-constexpr int kGrain = kWaves * kStep;  // keys that a chunk's length is a multiple of
-constexpr int kSharing = 4;  // of one whose wavefronts share keys
+constexpr int kWaves = 8;    // of a workgroup, one on a CU
+constexpr int kSharing = 4;  // of one whose wavefronts share keys, two on a CU
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kMostSum = 4096.f;  // of eight weights against their row's reference
@@ -162,7 +166,7 @@ struct Piece {
 __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
 // chunks of a sequence of `grains` grains, len grains long
 __device__ __forceinline__ int chunks_of(int grains, int len) { return grains > 0 ? div_up(grains, len) : 1; }
-__device__ __forceinline__ int grains_of(int L) { return (L + kGrain - 1) / kGrain; }
+__device__ __forceinline__ int grains_of(int L, const Kv4Plan &plan) { return (L + (1 << plan.grain_shift) - 1) >> plan.grain_shift; }
 __device__ __forceinline__ int nodes_of(const hb_attn_desc &d, int n0, int n1) {
   const int n = n1 - n0 < 0 ? 0 : n1 - n0 > d.max_nodes_per_tree ? d.max_nodes_per_tree : n1 - n0;
   return n0 < 0 || n0 + n > d.total_nodes ? 0 : n;  // malformed offsets: touch nothing
@@ -172,7 +176,7 @@ __device__ __forceinline__ int groups_of(int n, const Kv4Plan &plan) {
   return (n * plan.heads + (1 << plan.group_shift) - 1) >> plan.group_shift;
 }
 
-// The workgroups' pieces.  Every sequence is cut into chunks of one length, a multiple of `grain` keys, the shortest with which
+// The workgroups' pieces.  Every sequence is cut into chunks of one length, a multiple of a grain, the shortest with which
 // about `target` workgroups a kv head (a chunk has one for each of the sequence's row groups) and no sequence in more than
 // `splits` chunks come out; a sequence without a prefix has one chunk, for its tree.  Every workgroup finds this out from the
 // lengths, a sequence to a lane, and then which piece is its own.  Row groups of a chunk are neighbours, so are the heads,
@@ -191,7 +195,7 @@ __device__ __forceinline__ bool find_piece(const Kv4AttnArgs &a, const Kv4Plan &
   int work = 0, longest = 0;  // grains, as often as there are row groups; of a sequence
   for (int b0 = 0; b0 < d.batch; b0 += 64) {
     ask(b0 + lane);
-    const int n = grains_of(L);
+    const int n = grains_of(L, plan);
     work += sum_lanes(n * groups_of(nodes_of(d, n0, n1), plan));
     longest = max(longest, max_lanes(n));
   }
@@ -201,7 +205,7 @@ __device__ __forceinline__ bool find_piece(const Kv4AttnArgs &a, const Kv4Plan &
     total = 0;
     for (int b0 = 0; b0 < d.batch; b0 += 64) {
       if (d.batch > 64) ask(b0 + lane);
-      total += sum_lanes(chunks_of(grains_of(L), len) * groups_of(nodes_of(d, n0, n1), plan));
+      total += sum_lanes(chunks_of(grains_of(L, plan), len) * groups_of(nodes_of(d, n0, n1), plan));
     }
     // short last chunks make more of them than were asked for: longer ones, unless there are too many sequences for that
     if (total <= plan.target || len >= longest || !plan.fit) break;
@@ -215,7 +219,7 @@ __device__ __forceinline__ bool find_piece(const Kv4AttnArgs &a, const Kv4Plan &
   const int at = index / d.num_kv_heads;
   for (int b0 = 0; b0 < d.batch; b0 += 64) {
     if (d.batch > 64) ask(b0 + lane);
-    const int chunks = chunks_of(grains_of(L), len), groups = groups_of(nodes_of(d, n0, n1), plan);
+    const int chunks = chunks_of(grains_of(L, plan), len), groups = groups_of(nodes_of(d, n0, n1), plan);
     const int up = scan_lanes(chunks * groups);
     const unsigned long long behind = __ballot(before + up > at);
     if (behind) {
@@ -229,8 +233,8 @@ __device__ __forceinline__ bool find_piece(const Kv4AttnArgs &a, const Kv4Plan &
       rest /= c.groups;
       c.g = rest % d.num_kv_heads;
       c.c = rest / d.num_kv_heads;
-      c.begin = c.c * len * kGrain;
-      c.end = min(c.L, c.begin + len * kGrain);
+      c.begin = (c.c * len) << plan.grain_shift;
+      c.end = min(c.L, c.begin + (len << plan.grain_shift));
       c.n0 = __builtin_amdgcn_readlane(n0, who);
       c.n = nodes_of(d, c.n0, __builtin_amdgcn_readlane(n1, who));
       return true;
@@ -704,6 +708,11 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
 // ---- many rows ------------------------------------------------------------------------------------------
 // The same products where a (sequence, kv head) has many query rows (60 nodes of 7 heads: 27 tiles): the W wavefronts of a
 // workgroup have up to two tiles of rows each and share 64 keys at a time, which are widened into LDS once for all.
+// What bounds it is the issue of vector instructions and MFMAs by the two wavefronts of a SIMD: some 140 of them, 16 exponentials
+// of four slots among them, are 750 clocks for 32 keys and 32 rows, 544 of them the matrix core's; it takes 900.  Two trees of 52
+// and 55 nodes, 28/4 heads, over 32768 positions: 85 us and 9 for the join, 42 GFLOP; 16 of 30 to 60 nodes over 1024 to
+// 8192: 86 and 10.  Eight wavefronts to a workgroup, which share the keys among twice the rows: 93 and 114 us for the calls
+// that take 89 and 95, since a barrier then holds up all of a CU.
 // The loop over 32-key blocks is skewed by one: the matrix core gets a block's V^T P^T and the next one's scores in one go, and
 // the vector work that follows has its scores already.  A thread asks for its share of a tile (16 bytes of keys and of
 // values, two scales) two tiles ahead and puts it in LDS one tile ahead, while the matrix core has that work.  Two stages of
@@ -988,7 +997,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a, Kv4Plan pl
     n1 = a.node_offset[b + 1];
     L = kv4_length(a.d, a.prefix_len, b);
   }
-  const int chunks = chunks_of(grains_of(L), len);
+  const int chunks = chunks_of(grains_of(L, plan), len);
   if (row >= a.d.total_nodes * a.d.num_q_heads || node < n0 || node >= n0 + nodes_of(a.d, n0, n1) || chunks == 1) return;
   const kv4_f32x2 *ml = (const kv4_f32x2 *)a.part_ml + (size_t)row * plan.splits;
   const f32x4 *po = (const f32x4 *)a.part_o + (size_t)row * plan.splits * tpr + piece;
@@ -1046,7 +1055,7 @@ constexpr int64_t kMostGroups = 1 << 22;  // workgroups
 bool kv4_attn_supports(const hb_attn_desc &d) {
   // what the workgroups count with 32 bits: pieces, and grains times row groups
   const int64_t ends = (int64_t)d.batch * tiles_of(d);
-  if (ends * d.num_kv_heads > kMostGroups || ends * (((int64_t)d.page_size * d.max_blocks_per_seq) / kGrain + 1) > 1 << 30) return false;
+  if (ends * d.num_kv_heads > kMostGroups || ends * (((int64_t)d.page_size * d.max_blocks_per_seq) / 128 + 1) > 1 << 30) return false;
   return (d.head_dim == 64 || d.head_dim == 128) && d.page_size % 16 == 0 && d.page_size <= 1024 &&
          d.softmax_scale > 0.f && d.softmax_scale < 1e30f && d.num_q_heads / d.num_kv_heads <= 512;
 }
@@ -1058,11 +1067,14 @@ void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
   plan->row_groups = (tiles + group - 1) / group;  // at most
   plan->group_shift = group == 1 ? 4 : group == 2 ? 5 : 7;
   static_assert(2 * kSharing == 8, "128 rows to a workgroup whose wavefronts share keys");
+  static_assert(kWaves * kStep == 256, "a step of every wavefront");
+  const bool sharing = group == 2 * kSharing;
+  plan->grain_shift = sharing ? 7 : 8;
   plan->heads = d.num_q_heads / d.num_kv_heads;
-  int64_t target = 512 / d.num_kv_heads;  // workgroups of a kv head
+  int64_t target = (sharing ? 512 : 256) / d.num_kv_heads;  // workgroups of a kv head
   target = target < 1 ? 1 : target;
   int64_t splits = d.num_splits ? d.num_splits : target;
-  const int64_t most = (span + kGrain - 1) / kGrain;
+  const int64_t most = (span + (1 << plan->grain_shift) - 1) >> plan->grain_shift;
   splits = splits > most ? most : splits;
   splits = splits < 1 ? 1 : splits > 1024 ? 1024 : splits;
   if (d.num_splits) target = (int64_t)d.num_splits * d.batch * plan->row_groups;
