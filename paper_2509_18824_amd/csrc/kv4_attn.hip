@@ -1073,8 +1073,16 @@ void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
   plan->heads = d.num_q_heads / d.num_kv_heads;
   int64_t target = (sharing ? 512 : 256) / d.num_kv_heads;  // workgroups of a kv head
   target = target < 1 ? 1 : target;
-  int64_t splits = d.num_splits ? d.num_splits : target;
   const int64_t most = (span + (1 << plan->grain_shift) - 1) >> plan->grain_shift;
+  int64_t splits = d.num_splits ? d.num_splits : target;
+  // Whole sequences where they are short, longer ones the more workgroups there are without a cut: that saves the write and the
+  // reading of partial results and a launch.  Cut and whole, us (28 / 4 heads of 128): one token of one sequence over 512 keys 11.2
+  // and 9.6, over 1024 11.4 and 11.1, over 1536 11.4 and 12.6; 16 chains of 8 nodes over 512 17.1 and 13.9, over 1024 19.2 and
+  // 15.8, over 2048 21.6 and 20.0, over 3000 23.7 and 24.8; 60-node trees, 4 over 256 20.7 and 19.2, over 768 23.4 and 31.7,
+  // 16 over 256 34.0 and 19.9, over 1536 54.3 and 51.8, over 2048 62.3 and 63.1.  Beyond those lengths never, for ragged ones.
+  const int64_t pieces = (int64_t)d.batch * d.num_kv_heads * plan->row_groups;
+  const int64_t whole = sharing ? std::min<int64_t>(pieces / 20, 12) : std::min<int64_t>(3 + pieces / 32, 8);
+  if (!d.num_splits && most <= whole) splits = 1;
   splits = splits > most ? most : splits;
   splits = splits < 1 ? 1 : splits > 1024 ? 1024 : splits;
   if (d.num_splits) target = (int64_t)d.num_splits * d.batch * plan->row_groups;
