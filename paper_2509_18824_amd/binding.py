@@ -607,6 +607,10 @@ def hb_kv4_attn_weight(desc: AttnDesc, q, k_codes, k_scales, block_table, prefix
     _kv4_pool(desc, k_codes, k_scales)
     _kv4_slots(desc, weight, None)
     _kv4_ints(block_table, prefix_len, node_offset, accept_len, accept_path)
+    rows = desc.total_nodes * desc.num_q_heads
+    if (q.numel() < rows * desc.head_dim or _dtype_code(q) != desc.dtype or lse is not None
+            and (lse.numel() < rows or lse.dtype is not torch.float32)):
+        raise ValueError("q must be [total_nodes, Hq, D] in the descriptor's dtype, lse float32 [total_nodes, Hq]")
     _check(lib.hb_kv4_attn_weight(C.byref(desc), _ptr(q), _ptr(k_codes), _ptr(k_scales), _ptr(block_table), _ptr(prefix_len),
                                   _ptr(node_offset), _ptr(accept_len), _ptr(accept_path), max_path, _ptr(lse), decay,
                                   _ptr(weight), _stream(stream)))

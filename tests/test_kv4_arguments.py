@@ -128,3 +128,17 @@ def test_the_binding_checks_types_and_shapes():
         hb.hb_kv4_append(d, rows, rows, *[x.transpose(0, 1).contiguous().transpose(0, 1) for x in pool], table, ints, ints)  # not dense
     with pytest.raises(ValueError):
         hb.hb_kv4_evict(d, 100, 1, 1, *pool, table, ints, ints, slots, pos, slots, pos, pos, None, None)
+
+
+def test_the_binding_checks_what_weights_are_made_from():
+    d = _desc(Hq=4, Hkv=2, D=64, num_blocks=9, total_nodes=5, max_nodes=5)
+    u8 = lambda *s: torch.zeros(s, dtype=torch.uint8)
+    codes, scales, table = u8(9, 2, 16, 32), u8(9, 2, 16, 2), torch.zeros((2, 64), dtype=torch.int32)
+    q, lse, ints, slots = torch.zeros((5, 4, 64), dtype=torch.bfloat16), torch.zeros(5, 4), torch.zeros(3, dtype=torch.int32), torch.zeros(2, 2, 1024)
+    call = lambda q, lse: hb.hb_kv4_attn_weight(d, q, codes, scales, table, ints, ints, ints, ints, 1, lse, 1.0, slots)
+    for bad in (q.float(), q[:4]):
+        with pytest.raises(ValueError):
+            call(bad, lse)
+    for bad in (lse.double(), lse[:4]):
+        with pytest.raises(ValueError):
+            call(q, bad)
