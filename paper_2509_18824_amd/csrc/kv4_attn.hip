@@ -1060,8 +1060,7 @@ bool kv4_attn_supports(const hb_attn_desc &d) {
          d.softmax_scale > 0.f && d.softmax_scale < 1e30f && d.num_q_heads / d.num_kv_heads <= 512;
 }
 
-
-// Chunks are planned for some 512 workgroups
+// Chunks are planned for a round of the CUs: one workgroup to each, or two that share keys
 void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
   const int tiles = tiles_of(d), group = d.dtype == HB_F32 ? 1 : shares_keys(d) ? 2 * kSharing : tiles > 1 ? 2 : 1;
   plan->row_groups = (tiles + group - 1) / group;  // at most

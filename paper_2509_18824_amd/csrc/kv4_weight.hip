@@ -2,8 +2,7 @@
 //
 //   S = Q K^T   v_mfma_f32_16x16x32_bf16: A = 16 query rows, B = 16 cached keys, widened to bf16, which is exact
 //   w_p = decay w_p + sum over rows of exp(S[row][p] - lse[row])
-// The weights are 32-bit results, so the scores are too: the scaled product that attention uses is some 5e-6 of a score's
-// spread off.  float32 queries are taken as three bf16 pieces of eight bits each, which is all of them, smallest first.
+// The weights are 32-bit results, so the scores are too.  float32 queries are taken as three bf16 pieces of eight bits each, which is all of them, smallest first.
 //
 // Each key is 4 bits an element and 8 bytes for its weight; up to some ten rows that bounds it, from there on the exponentials
 // (16 clocks for 64 of them): six nodes of 28/4 heads are 42 rows.  16 sequences of 1024 to 8192 positions, 23 MB, take 17 us (4.5 at
