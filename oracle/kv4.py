@@ -91,7 +91,7 @@ def kv4_evict_ref(length, budget, recent, sinks, seq_len, weight, pos):
     """One head: the slot whose position is afterwards in slot 0, 1, ..."""
     w = [-np.inf if np.isnan(x) else float(x) for x in weight[:length]]
     safe = [p >= seq_len - recent or p < sinks for p in pos[:length]]
-    ranking = sorted(range(length), key=lambda s: (-(np.inf if safe[s] else w[s]), s))
+    ranking = sorted(range(length), key=lambda s: (not safe[s], 0.0 if safe[s] else -w[s], s))
     stays = min(length, budget)
     chosen = set(ranking[:stays])
     arrivals = iter(sorted(s for s in chosen if s >= stays))

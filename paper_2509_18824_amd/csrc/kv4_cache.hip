@@ -138,11 +138,11 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(hb_attn_desc d, int rows,
 }
 
 // ---- eviction ------------------------------------------------------------------------------------------
-// order-preserving bits of a weight; not a number counts as the least, protected positions as the greatest
+// order-preserving bits of a weight; not a number counts as the least, protected positions as more than any
 __device__ inline uint32_t weight_key(float w, bool safe) {
   w = fmaxf(w, -__builtin_huge_valf()) + 0.f;  // a number; and -0 weighs what 0 does
-  const uint32_t u = __float_as_uint(safe ? __builtin_huge_valf() : w);
-  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  const uint32_t u = __float_as_uint(w);
+  return safe ? 0xffffffffu : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 constexpr int kSelectThreads = 1024;

@@ -361,3 +361,24 @@ def test_eviction(hb, step, budget, recent, sinks, in_place):
     assert np.array_equal(w_out.cpu().numpy(), want_w, equal_nan=True) and np.array_equal(p_out.cpu().numpy(), want_p)
     for got, ref in zip(dev, want):
         assert np.array_equal(got.cpu().numpy(), ref)
+
+
+@pytest.mark.parametrize("length", [300, 40000])
+def test_eviction_keeps_protected_positions_in_front_of_infinite_weights(hb, step, length):
+    """As many infinite weights as the budget holds, in front of what is protected."""
+    cap, budget, recent, sinks = (length + 15) // 16 * 16, 64, 5, 3
+    d = step.make_desc(dtype="bf16", B=1, Hq=1, Hkv=1, D=32, page=16, max_blocks=cap // 16, num_blocks=cap // 16, total_nodes=0, max_nodes=1, softmax_scale=1.0)
+    weight = np.full((1, 1, cap), np.inf, dtype=np.float32)
+    pos = np.zeros((1, 1, cap), dtype=np.int32)
+    pos[0, 0, :length] = np.arange(length)[::-1]  # the recent ones in front, the first ones last
+    weight[0, 0, :30] = 0.25
+    cuda = lambda x: torch.from_numpy(np.ascontiguousarray(x)).cuda()
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    pool = [torch.zeros(s, dtype=torch.uint8, device="cuda") for s in ((cap // 16, 1, 16, 16), (cap // 16, 1, 16, 1)) * 2]
+    kept, new = i32([[[-9] * budget]]), i32([-1])
+    w, p = cuda(weight), cuda(pos)
+    hb.hb_kv4_evict(d, budget, recent, sinks, *pool, i32([list(range(cap // 16))]), i32([length]), i32([length]), w, p, w, p, kept, new,
+                    step.alloc_workspace(hb.hb_kv4_evict_workspace_bytes(d, budget)))
+    torch.cuda.synchronize()
+    assert kept[0, 0].tolist() == kv4_evict_ref(length, budget, recent, sinks, length, weight[0, 0], pos[0, 0])
+    assert set(p[0, 0, :budget].tolist()) >= set(range(sinks)) | set(range(length - recent, length))

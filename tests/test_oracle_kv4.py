@@ -73,3 +73,8 @@ def test_eviction_by_brute_force_over_small_weights():
             assert all(kept[i] == i for i in range(len(kept)) if i in kept)
             moved = [k for i, k in enumerate(kept) if k != i]
             assert moved == sorted(moved) and all(m >= len(kept) for m in moved)
+
+
+def test_protected_positions_stay_in_front_of_infinite_weights():
+    assert kv4_evict_ref(4, 2, 1, 0, 9, [np.inf, np.inf, 0.5, 2.0], [0, 2, 3, 8]) == [0, 3]
+    assert kv4_evict_ref(4, 1, 1, 0, 9, [np.inf, np.inf, 0.5, 2.0], [0, 2, 3, 8]) == [3]
