@@ -45,7 +45,8 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   const long gid = (long)blockIdx.x * 256 + threadIdx.x;
   if (blockIdx.y == 0) {
     for (long b = gid; a.new_len && b < d.batch; b += (long)gridDim.x * 256) {
-      int n = PATH ? a.accept_len[b] : a.row_offset[b + 1] - a.row_offset[b];
+      const int rows = a.row_offset[b + 1] - a.row_offset[b];
+      int n = !PATH ? rows : rows > 0 && a.src_rows > 0 ? a.accept_len[b] : 0;
       n = n < 0 ? 0 : PATH && n > a.max_path ? a.max_path : n;
       const int L = a.prefix_len[b];
       a.new_len[b] = (L < 0 ? 0 : L) + n;
@@ -63,8 +64,8 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   if (PATH) {
     b = r / a.max_path;
     j = r - b * a.max_path;
-    live = j < a.accept_len[b];
     const int n0 = a.row_offset[b], n = a.row_offset[b + 1] - n0;
+    live = j < a.accept_len[b] && n > 0 && a.src_rows > 0;  // a tree without nodes has no path, whatever accept_len says
     int node = live ? a.accept_path[(size_t)b * a.max_path + j] : 0;
     node = node < 0 ? 0 : (node >= n ? n - 1 : node);
     src = n0 + node;
@@ -445,7 +446,8 @@ hipError_t launch_kv4_evict(const Kv4EvictArgs &a, hipStream_t s) {
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int each = 4 * (64 / (2 * (a.d.head_dim / kKv4Block)));  // moves of a workgroup
-  kv4_move_kernel<<<dim3((unsigned)((a.budget + each - 1) / each), (unsigned)units), 256, 0, s>>>(a);
+  const int most = a.budget < a.longest ? a.budget : a.longest;
+  kv4_move_kernel<<<dim3((unsigned)((most + each - 1) / each), (unsigned)units), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -382,3 +382,19 @@ def test_eviction_keeps_protected_positions_in_front_of_infinite_weights(hb, ste
     torch.cuda.synchronize()
     assert kept[0, 0].tolist() == kv4_evict_ref(length, budget, recent, sinks, length, weight[0, 0], pos[0, 0])
     assert set(p[0, 0, :budget].tolist()) >= set(range(sinks)) | set(range(length - recent, length))
+
+
+def test_a_tree_without_nodes_has_no_path(hb, step):
+    """accept_len that names nodes of an empty tree, for one sequence and for all: nothing is written, lengths stay."""
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    for offsets in ([0, 0, 2], [0, 0, 0]):
+        n = offsets[-1]
+        d = step.make_desc(dtype="bf16", B=2, Hq=2, Hkv=1, D=64, page=16, max_blocks=2, num_blocks=4, total_nodes=n, max_nodes=2, softmax_scale=1.0)
+        rows = torch.ones((max(n, 1), 1, 64), dtype=torch.bfloat16, device="cuda")[:n]
+        pool = [torch.full(s, 9, dtype=torch.uint8, device="cuda") for s in ((4, 1, 16, 32), (4, 1, 16, 2)) * 2]
+        slots, new = i32([[7, 7], [7, 7]]), i32([-1, -1])
+        hb.hb_kv4_compact(d, rows, rows, *pool, i32([[0, 1], [2, 3]]), i32([3, 4]), i32(offsets), i32([2, 1]), i32([[0, 1], [1, 0]]), 2,
+                          None, None, None, slots, new)
+        torch.cuda.synchronize()
+        assert new.tolist() == [3, 5 if n else 4] and slots.tolist() == [[-1, -1], [36 if n else -1, -1]]
+        assert all((p[:2] == 9).all() for p in pool) and (n or all((p == 9).all() for p in pool))
