@@ -594,7 +594,8 @@ int32_t hb_kv4_read(const hb_attn_desc *desc, int32_t n_rows, const void *k_code
 
 /*
  * hb_tree_verify_attn with the prefix in a 4-bit cache; the nodes' own K and V (k_tree, v_tree) are as they are there, in
- * desc->dtype.  Arguments, masks and errors as in hb_tree_verify_attn, and UNSUPPORTED for D % 32.
+ * desc->dtype.  Arguments, masks and errors as in hb_tree_verify_attn, and UNSUPPORTED for D % 32.  Values of nodes that are
+ * not finite reach the rows that see them, and no others.
  */
 int32_t hb_tree_verify_attn_kv4(const hb_attn_desc *desc, const void *q, const void *k_tree, const void *v_tree,
                                 const void *k_codes, const void *k_scales, const void *v_codes, const void *v_scales,

@@ -17,9 +17,9 @@
 // Chunks are cut on the device from the lengths (find_piece below), so that about as many workgroups start as the host planned
 // for, whatever the lengths are: one to a CU, of eight wavefronts of up to 256 registers each.
 //
-// What bounds it, single tokens: memory.  16 of them over 16384 to 32768 positions, 28/4 heads of 128, 214 MB: 51 us, the join
-// with 5 of them included, 4.2 TB/s (a large copy runs at 5.1); one over 2048, 1.1 MB: 12 and 4.5 us, the round trips to lengths,
-// pages, codes and back and the start of two launches.  16 chains of 8 nodes (56 rows) over 1024 to 4096: 25 and 5 us, a
+// What bounds it, single tokens: memory.  16 of them over 16384 to 32768 positions, 28/4 heads of 128, 214 MB: 50 us, the join
+// with 5 of them included, 4.3 TB/s (a large copy runs at 5.1); one over 2048, 1.1 MB: 12 us, the join with 3.5 of them included, the round trips to lengths,
+// pages, codes and back and the start of two launches.  16 chains of 8 nodes (56 rows) over 1024 to 4096: 24 us, join 5, a
 // few steps to a wavefront between the same round trips.  Two workgroups of four wavefronts to a CU: 53, 12.6 and 25.4 us.
 #include "kv4.h"
 #include "wave_ops.h"
@@ -258,6 +258,24 @@ __device__ __forceinline__ unsigned long long path_of(int par, int lane, int n) 
   return path;
 }
 
+// Values of nodes that are not finite count as 0 in the products, where they would reach every row.  Those that see them get them
+// here, in what this lane has written: the elements d .. d + 3 of a row, `seen` its path; v: the first node's values.
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+template <typename T, typename O>
+__device__ __forceinline__ void add_not_finite(const T *v, size_t stride, unsigned long long seen, int d, O *out) {
+#pragma nounroll
+  for (; seen; seen &= seen - 1) {
+    const T *x = v + __builtin_ctzll(seen) * stride + d;
+#pragma nounroll
+    for (int e = 0; e < 4; ++e)
+      if (const float y = load_f32(x + e); not_finite(y)) store_f32(out + e, load_f32(out + e) + y);
+  }
+}
+// the path of node `node`, asked for by every lane
+__device__ __forceinline__ unsigned long long path_at(unsigned long long path, int node) {
+  return ((unsigned long long)(uint32_t)__shfl((int)(path >> 32), node, 64) << 32) | (uint32_t)__shfl((int)path, node, 64);
+}
+
 template <int TPW, int DB>
 struct Rows {
   bf16x8 q[TPW][4];
@@ -423,6 +441,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   // values: 32 keys to a wavefront; at the end a tile's sums of all wavefronts; then references and sums
   __shared__ __attribute__((aligned(16))) unsigned char smem[W * (kStep * kRow > 64 * 16 * 2 * DB ? kStep * kRow : 64 * 16 * 2 * DB)];
   __shared__ float s_m[W][TPW * 16], s_l[W][TPW * 16];
+  __shared__ int s_odd[W];  // whether a wavefront's nodes have values that are not finite
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 15, kg = lane >> 4;
   Piece ch;
@@ -495,10 +514,12 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
   }
   const float c1 = d.softmax_scale * kLog2e;
   unsigned char *lv = smem + wave * kStep * kRow;
+  if (lane == 0) s_odd[wave] = 0;
 
   // ---- the nodes' own keys: 32 to a wavefront, chunk 0 only ------------------------------------------
   if (ch.c == 0 && wave < (n + 31) / 32) {
     const int first = 32 * wave;
+    bool odd = false;
     // node `first + i` is seen by the rows whose path it lies on; lane i holds node i's
     const unsigned long long path = path_of(lane < n ? a.parent[n0 + lane] : -1, lane, n);
     const uint32_t mine = (uint32_t)(path >> first);
@@ -530,29 +551,41 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
       weigh<TPW, DB>(w, sc, c1, p);
       bf16x8 weight[3];
       pieces_of(p[0], weight);
-      // the values a piece at a time; a node off a row's path weighs 0, and must not make that 0 * NaN
+      f32x8 x[2][DB];
 #pragma unroll
-      for (int b = 2; b >= 0; --b) {
+      for (int h = 0; h < 2; ++h) {
+        const int node = first + 16 * h + j;
+        const float *row = (const float *)a.v_tree + ((size_t)(n0 + min(node, n - 1)) * d.num_kv_heads + g) * D;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int key = 16 * h + j, node = first + key;
-          const float *row = (const float *)a.v_tree + ((size_t)(n0 + min(node, n - 1)) * d.num_kv_heads + g) * D;
+        for (int i = 0; i < DB; ++i) {
+          x[h][i] = load_f32x8(row + (DB * kg + i) * 8);
+          // a node off a row's path weighs 0, and must not make that 0 * NaN
 #pragma unroll
-          for (int i = 0; i < DB; ++i) {
-            f32x8 x = load_f32x8(row + (DB * kg + i) * 8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = node < n && (__float_as_uint(x[e]) & 0x7f800000u) != 0x7f800000u ? x[e] : 0.f;
-            bf16x8 y[3];
-            pieces_of(x, y);
-            *piece_at(key, DB * kg + i) = __builtin_bit_cast(u32x4, y[b]);
+          for (int e = 0; e < 8; ++e) {
+            const float y = x[h][i][e];
+            odd |= not_finite(y);
+            x[h][i][e] = node < n && !not_finite(y) ? y : 0.f;
           }
         }
+      }
+      // the values a piece at a time, by a loop: it is done once, and what costs then is to bring its instructions
+#pragma nounroll
+      for (int b = 0; b < 3; ++b) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < DB; ++i) {
+            const bf16x8 y = __builtin_convertvector(x[h][i], bf16x8);
+            x[h][i] -= __builtin_convertvector(y, f32x8);
+            *piece_at(16 * h + j, DB * kg + i) = __builtin_bit_cast(u32x4, y);
+          }
         bf16x8 av[2 * DB];
         read_values<DB>(lv, j, kg, av);
         // (the sums of the weights are those that the largest pieces of the values are weighed with)
         const f32x4 lr = w.lr[0];
 #pragma unroll
-        for (int e = 2 - b; e >= 0; --e) {
+        for (int e = 2; e >= 0; --e) {
+          if (e > 2 - b) continue;  // uniform
           const bf16x8 one[1] = {weight[e]};
           accumulate<TPW, DB>(w, av, one);
         }
@@ -576,13 +609,18 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
         for (int i = 0; i < DB; ++i) {
           u32x4 x = src[DB * kg + i];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = node < n ? finite_or_zero_bf16x2(x[e]) : 0u;
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t y = finite_or_zero_bf16x2(x[e]);
+            odd |= y != x[e];
+            x[e] = node < n ? y : 0u;
+          }
           *piece_at(key, DB * kg + i) = x;
         }
       }
       weigh<TPW, DB>(w, sc, c1, p);
       weigh_values<TPW, DB>(w, lv, j, kg, p, true);
     }
+    if (odd) s_odd[wave] = 1;
   }
 
   // ---- the prefix -------------------------------------------------------------------------------------
@@ -703,6 +741,20 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
     }
     if (t + 1 < TPW) __syncthreads();
   }
+  if (__builtin_expect(s_odd[0] | s_odd[1], 0)) {  // chunk 0 alone has nodes, and two wavefronts
+    const unsigned long long path = path_of(lane < n ? a.parent[n0 + lane] : -1, lane, n);
+    const T *v = (const T *)a.v_tree + ((size_t)n0 * d.num_kv_heads + g) * D;
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+      const int row = (tile0 + t) * 16 + j;
+      const unsigned long long seen = path_at(path, row < R ? small_div(row, G) : 0);
+      const size_t rr = row < R ? row_at(row) : 0;
+      for (int at = 16 * wave + 4 * kg; at < D && row < R; at += 16 * W) {
+        if (!F32 && ch.chunks == 1) add_not_finite(v, (size_t)d.num_kv_heads * D, seen, at, (T *)a.out + rr * D + at);
+        else add_not_finite(v, (size_t)d.num_kv_heads * D, seen, at, (ch.chunks == 1 ? (float *)a.out + rr * D : a.part_o + rr * plan.splits * D) + at);
+      }
+    }
+  }
 }
 
 // ---- many rows ------------------------------------------------------------------------------------------
@@ -724,6 +776,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
   constexpr int kStage = 2 * kTile * kRow;
   const hb_attn_desc &d = a.d;
   __shared__ __attribute__((aligned(16))) unsigned char smem[2 * kStage];  // [values 64 x kRow | keys 64 x kRow]
+  __shared__ int s_odd[W];  // whether a wavefront brought values of nodes that are not finite
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 15, kg = lane >> 4;
   Piece ch;
@@ -821,16 +874,22 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
   // ---- the nodes' own keys, chunk 0 only: values in the second stage, keys straight from memory -----
   if (ch.c == 0) {
     unsigned char *lv = smem + kStage;
+    bool odd = false;
     for (int i = tid; i < kTile * 2 * DB * 2; i += kThreads) {
       const int key = i / (4 * DB), piece = i % (4 * DB);
       u32x4 v = {0u, 0u, 0u, 0u};
       if (key < n) {
         v = ((const u32x4 *)a.v_tree)[((size_t)(n0 + key) * d.num_kv_heads + g) * (D / 8) + piece];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = finite_or_zero_bf16x2(v[e]);
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t y = finite_or_zero_bf16x2(v[e]);
+          odd |= y != v[e];
+          v[e] = y;
+        }
       }
       *(u32x4 *)(lv + key * kRow + ((piece ^ (v_swz(key) & (4 * DB - 1))) * 16)) = v;
     }
+    if (const bool any = __any(odd); lane == 0) s_odd[wave] = any;
     const unsigned long long path = path_of(lane < n ? a.parent[n0 + lane] : -1, lane, n);
     __syncthreads();
     for (int blk = 0; blk < 2; ++blk) {
@@ -964,6 +1023,24 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
 #pragma unroll
       for (int dt = 0; dt < 2 * DB; ++dt) *(f32x4 *)(po + 16 * dt + 4 * kg) = w.o[t][dt] * scale;
       if (kg == 0) *(kv4_f32x2 *)(a.part_ml + (rr * plan.splits + ch.c) * 2) = (kv4_f32x2){w.m[t], l};
+    }
+  }
+  if (ch.c == 0) {
+    int odd = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) odd |= s_odd[i];
+    if (__builtin_expect(!odd, 1)) return;
+    const unsigned long long path = path_of(lane < n ? a.parent[n0 + lane] : -1, lane, n);
+    const bf16_t *v = (const bf16_t *)a.v_tree + ((size_t)n0 * d.num_kv_heads + g) * D;
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+      const int row = row_of(t);
+      const unsigned long long seen = path_at(path, row < R ? small_div(row, G) : 0);
+      const size_t rr = row < R ? row_at(row) : 0;
+      for (int at = 4 * kg; at < D && row < R; at += 16) {
+        if (ch.chunks == 1) add_not_finite(v, (size_t)d.num_kv_heads * D, seen, at, (bf16_t *)a.out + rr * D + at);
+        else add_not_finite(v, (size_t)d.num_kv_heads * D, seen, at, a.part_o + rr * plan.splits * D + at);
+      }
     }
   }
 }

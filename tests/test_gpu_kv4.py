@@ -398,3 +398,34 @@ def test_a_tree_without_nodes_has_no_path(hb, step):
         torch.cuda.synchronize()
         assert new.tolist() == [3, 5 if n else 4] and slots.tolist() == [[-1, -1], [36 if n else -1, -1]]
         assert all((p[:2] == 9).all() for p in pool) and (n or all((p == 9).all() for p in pool))
+
+
+@pytest.mark.parametrize("dtype,Hq,D,nodes,lens", [("bf16", 14, 128, 3, [33, 5000]), ("bf16", 14, 128, 12, [0, 300]), ("bf16", 14, 128, 60, [100, 5000]),
+                                                   ("bf16", 4, 64, 40, [7, 90]), ("bf16", 16, 64, 60, [0, 3000]), ("bf16", 14, 128, 61, [33, 0]),
+                                                   ("f32", 6, 128, 50, [33, 2000]), ("f32", 2, 64, 5, [0, 100]), ("bf16", 4, 96, 12, [33, 2000])])
+def test_values_of_nodes_that_are_not_finite_reach_the_rows_that_see_them(hb, step, dtype, Hq, D, nodes, lens):
+    """Infinities and NaN in elements of an inner node, of the last one and of the root: the rows whose path they lie on have them in
+    these elements, and nothing else of any result changes by a bit."""
+    case = mixed_case(9, dtype, Hq, 2, D, 16, lens, [nodes, nodes])
+    i, G = case.inp, Hq // 2
+    n1, parent = int(i.node_offset[1]), i.parent.tolist()
+    clean = _attend(hb, step, case)
+    bad = {(0, 1, 5): float("inf"), (nodes // 2, 0, D - 1): -float("inf"), (nodes - 1, 1, 40): float("nan"), (nodes // 2, 1, 17): float("inf"),
+           (0, 0, 2): float("-inf")}
+    want = clean[0].float()
+    for (node, h, e), x in bad.items():
+        i.v_tree[n1 + node, h, e] = x
+        for row in range(nodes):
+            up = row
+            while up > node:
+                up = parent[n1 + up]
+            if up == node:
+                want[n1 + row, h * G:(h + 1) * G, e] = x
+    zeroed = mixed_case(9, dtype, Hq, 2, D, 16, lens, [nodes, nodes])
+    for node, h, e in bad:
+        zeroed.inp.v_tree[n1 + node, h, e] = 0
+    base = _attend(hb, step, zeroed)
+    got = _attend(hb, step, case)
+    odd = ~torch.isfinite(want)
+    assert odd.any() and torch.equal(torch.nan_to_num(got[0].float()[odd], nan=7.0), torch.nan_to_num(want[odd], nan=7.0))
+    assert torch.equal(got[0][~odd], base[0][~odd]) and torch.equal(got[1], base[1])
