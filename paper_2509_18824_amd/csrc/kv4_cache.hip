@@ -34,6 +34,29 @@ __device__ inline void store8(bf16_t *p, const float (&x)[8]) {
   *(u32x4 *)p = (u32x4){pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
 }
 
+// The sequence of row r, its rows [from, to) and where it starts, in one round trip up to 64 sequences (one to a lane, so every
+// lane of the wavefront has to ask).
+struct Place {
+  int b, from, to, start;
+};
+__device__ inline Place place_of(const int32_t *__restrict__ offset, const int32_t *__restrict__ start, int batch, int r) {
+  Place x;
+  if (batch > 64) {  // uniform
+    x.b = kv4_sequence(offset, batch, r);
+    x.from = offset[x.b];
+    x.to = offset[x.b + 1];
+    x.start = start[x.b];
+    return x;
+  }
+  const int lane = min((int)threadIdx.x & 63, batch - 1), from = offset[lane], to = offset[lane + 1], at = start[lane];
+  x.b = 0;
+  for (int i = 1; i < batch; ++i) x.b = __builtin_amdgcn_readlane(from, i) <= r ? i : x.b;
+  x.from = __shfl(from, x.b, 64);
+  x.to = __shfl(to, x.b, 64);
+  x.start = __shfl(at, x.b, 64);
+  return x;
+}
+
 // Quantises rows into the pages.  A thread takes eight elements, four threads a block of 32: its largest
 // magnitude is two exchanges away.  Threads run over the pieces of a head's row, then over rows, then over heads:
 // neighbouring rows of a head are neighbours in a page.  PATH: the rows that a path names, max_path to a sequence.
@@ -55,9 +78,12 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   // pieces is a multiple of four: a block's threads leave together.  (32 bits hold what a launch may have)
   const unsigned pieces = d.head_dim / 8, item = (unsigned)gid / pieces;
   const int piece = (int)((unsigned)gid - item * pieces);
-  if (gid >= (long)a.rows * d.num_kv_heads * pieces) return;
+  if (a.rows == 0) return;
   const int h = (int)(item / (unsigned)a.rows), r = (int)(item - (unsigned)h * (unsigned)a.rows);
-  int b, j, src = r;
+  Place at;
+  if (!PATH) at = place_of(a.row_offset, a.prefix_len, d.batch, r);
+  if (gid >= (long)a.rows * d.num_kv_heads * pieces) return;
+  int b, j, L, src = r;
   bool live;
   float x[8];
   if (!PATH) load8((const T *)(blockIdx.y ? a.v : a.k) + ((size_t)r * d.num_kv_heads + h) * d.head_dim + piece * 8, x);
@@ -70,12 +96,13 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
     node = node < 0 ? 0 : (node >= n ? n - 1 : node);
     src = n0 + node;
     src = src < 0 ? 0 : (src >= a.src_rows ? a.src_rows - 1 : src);
+    L = a.prefix_len[b];
   } else {
-    b = kv4_sequence(a.row_offset, d.batch, r);
-    j = r - a.row_offset[b];
-    live = j >= 0 && r < a.row_offset[b + 1];
+    b = at.b;
+    j = r - at.from;
+    live = j >= 0 && r < at.to;
+    L = at.start;
   }
-  int L = a.prefix_len[b];
   L = L < 0 ? 0 : L;
   const long p = (long)L + j;
   const bool in_table = live && p < (long)d.max_blocks_per_seq * d.page_size;
@@ -108,9 +135,9 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   *(uint32_t *)(to + row * (d.head_dim / 2) + piece * 4) = codes;
   if (piece % 4 == 0) to_scale[row * (d.head_dim / kKv4Block) + piece / 4] = (uint8_t)s;
   if (blockIdx.y == 0 && piece == 0) {
-    const size_t at = ((size_t)b * d.num_kv_heads + h) * d.max_blocks_per_seq * d.page_size + p;
-    if (a.weight) a.weight[at] = 0.f;
-    if (a.pos) a.pos[at] = (a.seq_len ? a.seq_len[b] : L) + j;
+    const size_t slot = ((size_t)b * d.num_kv_heads + h) * d.max_blocks_per_seq * d.page_size + p;
+    if (a.weight) a.weight[slot] = 0.f;
+    if (a.pos) a.pos[slot] = (a.seq_len ? a.seq_len[b] : L) + j;
   }
 }
 
@@ -122,10 +149,11 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(hb_attn_desc d, int rows,
   const long gid = (long)blockIdx.x * 256 + threadIdx.x;
   const unsigned pieces = d.head_dim / 8, item = (unsigned)gid / pieces;
   const int piece = (int)((unsigned)gid - item * pieces);
-  if (gid >= (long)rows * d.num_kv_heads * pieces) return;
   const int h = (int)(item / (unsigned)rows), r = (int)(item - (unsigned)h * (unsigned)rows);
-  const int b = kv4_sequence(row_offset, d.batch, r);
-  const long p = (long)first[b] + r - row_offset[b];
+  const Place at = place_of(row_offset, first, d.batch, r);
+  if (gid >= (long)rows * d.num_kv_heads * pieces) return;
+  const int b = at.b;
+  const long p = (long)at.start + r - at.from;
   const Kv4Pool &from = blockIdx.y ? vp : kp;
   float x[8] = {};
   if (p >= 0 && p < (long)d.max_blocks_per_seq * d.page_size) {
@@ -278,7 +306,6 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs
       __syncthreads();
       least |= (uint32_t)s_digit << shift;
       need = s_need;
-      __syncthreads();
     }
   }
   if (tid == 0) {
@@ -291,6 +318,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs
     if (slabs > 1) load(slab);
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
+      if (slab * kSlab + r * kSelectThreads * 4 >= L) break;  // uniform; what nobody counts, nobody reads: the parts end there
       unsigned long long ma[4], mt[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
