@@ -66,14 +66,12 @@ template <typename T, bool PATH>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   const hb_attn_desc &d = a.d;
   const long gid = (long)blockIdx.x * 256 + threadIdx.x;
-  if (blockIdx.y == 0) {
-    for (long b = gid; a.new_len && b < d.batch; b += (long)gridDim.x * 256) {
-      const int rows = a.row_offset[b + 1] - a.row_offset[b];
-      int n = !PATH ? rows : rows > 0 && a.src_rows > 0 ? a.accept_len[b] : 0;
-      n = n < 0 ? 0 : PATH && n > a.max_path ? a.max_path : n;
-      const int L = a.prefix_len[b];
-      a.new_len[b] = (L < 0 ? 0 : L) + n;
-    }
+  for (long b = gid; a.new_len && b < d.batch; b += (long)gridDim.x * 256) {
+    const int rows = a.row_offset[b + 1] - a.row_offset[b];
+    int n = !PATH ? rows : rows > 0 && a.src_rows > 0 ? a.accept_len[b] : 0;
+    n = n < 0 ? 0 : PATH && n > a.max_path ? a.max_path : n;
+    const int L = a.prefix_len[b];
+    a.new_len[b] = (L < 0 ? 0 : L) + n;
   }
   // pieces is a multiple of four: a block's threads leave together.  (32 bits hold what a launch may have)
   const unsigned pieces = d.head_dim / 8, item = (unsigned)gid / pieces;
@@ -85,8 +83,13 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   if (gid >= (long)a.rows * d.num_kv_heads * pieces) return;
   int b, j, L, src = r;
   bool live;
-  float x[8];
-  if (!PATH) load8((const T *)(blockIdx.y ? a.v : a.k) + ((size_t)r * d.num_kv_heads + h) * d.head_dim + piece * 8, x);
+  float x[2][8];
+  auto load = [&](int row) {
+    const size_t from = ((size_t)row * d.num_kv_heads + h) * d.head_dim + piece * 8;
+    load8((const T *)a.k + from, x[0]);
+    load8((const T *)a.v + from, x[1]);
+  };
+  if (!PATH) load(r);
   if (PATH) {
     b = r / a.max_path;
     j = r - b * a.max_path;
@@ -106,7 +109,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   L = L < 0 ? 0 : L;
   const long p = (long)L + j;
   const bool in_table = live && p < (long)d.max_blocks_per_seq * d.page_size;
-  if (PATH && a.out_slots && h == 0 && piece == 0 && blockIdx.y == 0) {
+  if (PATH && a.out_slots && h == 0 && piece == 0) {
     int slot = -1;
     if (in_table) {
       const size_t row = kv4_row(d, a.block_table, b, 0, (int)p);
@@ -116,25 +119,27 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   }
   if (!in_table) return;
   const size_t row = kv4_row(d, a.block_table, b, h, (int)p);
-  if (PATH) load8((const T *)(blockIdx.y ? a.v : a.k) + ((size_t)src * d.num_kv_heads + h) * d.head_dim + piece * 8, x);
-  uint32_t top = 0;  // magnitudes compare as their bits do, and what is not finite is above the rest
+  if (PATH) load(src);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
-  const uint32_t s = kv4_scale_of(top);
-  uint32_t codes = 0;  // to the nearest, ties to even; above 6: 6
-  if (s != kKv4NaN) {
-    const float scale = kv4_scale(s);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], scale, 0);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], scale, 2);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], scale, 3);
+  for (int v = 0; v < 2; ++v) {
+    uint32_t top = 0;  // magnitudes compare as their bits do, and what is not finite is above the rest
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[v][e]) & 0x7fffffffu);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+    const uint32_t s = kv4_scale_of(top);
+    uint32_t codes = 0;  // to the nearest, ties to even; above 6: 6
+    if (s != kKv4NaN) {
+      const float scale = kv4_scale(s);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[v][0], x[v][1], scale, 0);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[v][2], x[v][3], scale, 1);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[v][4], x[v][5], scale, 2);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[v][6], x[v][7], scale, 3);
+    }
+    *(uint32_t *)((v ? a.v_codes : a.k_codes) + row * (d.head_dim / 2) + piece * 4) = codes;
+    if (piece % 4 == 0) (v ? a.v_scales : a.k_scales)[row * (d.head_dim / kKv4Block) + piece / 4] = (uint8_t)s;
   }
-  uint8_t *to = blockIdx.y ? a.v_codes : a.k_codes, *to_scale = blockIdx.y ? a.v_scales : a.k_scales;
-  *(uint32_t *)(to + row * (d.head_dim / 2) + piece * 4) = codes;
-  if (piece % 4 == 0) to_scale[row * (d.head_dim / kKv4Block) + piece / 4] = (uint8_t)s;
-  if (blockIdx.y == 0 && piece == 0) {
+  if (piece == 0) {
     const size_t slot = ((size_t)b * d.num_kv_heads + h) * d.max_blocks_per_seq * d.page_size + p;
     if (a.weight) a.weight[slot] = 0.f;
     if (a.pos) a.pos[slot] = (a.seq_len ? a.seq_len[b] : L) + j;
@@ -154,16 +159,24 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(hb_attn_desc d, int rows,
   if (gid >= (long)rows * d.num_kv_heads * pieces) return;
   const int b = at.b;
   const long p = (long)at.start + r - at.from;
-  const Kv4Pool &from = blockIdx.y ? vp : kp;
-  float x[8] = {};
-  if (p >= 0 && p < (long)d.max_blocks_per_seq * d.page_size) {
-    const size_t row = kv4_row(d, block_table, b, h, (int)p);
-    const uint32_t c = *(const uint32_t *)(from.codes + row * (d.head_dim / 2) + piece * 4);
-    const float s = kv4_scale(from.scales[row * (d.head_dim / kKv4Block) + piece / 4]);
-    const kv4_f32x2 p0 = kv4_pair<0>(c, s), p1 = kv4_pair<1>(c, s), p2 = kv4_pair<2>(c, s), p3 = kv4_pair<3>(c, s);
-    x[0] = p0[0], x[1] = p0[1], x[2] = p1[0], x[3] = p1[1], x[4] = p2[0], x[5] = p2[1], x[6] = p3[0], x[7] = p3[1];
+  const bool there = p >= 0 && p < (long)d.max_blocks_per_seq * d.page_size;
+  uint32_t codes[2] = {0, 0}, scales[2] = {127, 127};
+  if (there) {
+    const size_t row = kv4_row(d, block_table, b, h, (int)p), code = row * (d.head_dim / 2) + piece * 4,
+                 scale = row * (d.head_dim / kKv4Block) + piece / 4;
+    codes[0] = *(const uint32_t *)(kp.codes + code);
+    codes[1] = *(const uint32_t *)(vp.codes + code);
+    scales[0] = kp.scales[scale];
+    scales[1] = vp.scales[scale];
   }
-  store8((blockIdx.y ? v : k) + ((size_t)r * d.num_kv_heads + h) * d.head_dim + piece * 8, x);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t c = codes[i];
+    const float s = kv4_scale(scales[i]);
+    const kv4_f32x2 p0 = kv4_pair<0>(c, s), p1 = kv4_pair<1>(c, s), p2 = kv4_pair<2>(c, s), p3 = kv4_pair<3>(c, s);
+    const float x[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+    store8((i ? v : k) + ((size_t)r * d.num_kv_heads + h) * d.head_dim + piece * 8, x);
+  }
 }
 
 // ---- eviction ------------------------------------------------------------------------------------------
@@ -442,7 +455,7 @@ __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4EvictArgs a) {
 
 hipError_t launch_kv4_append(const Kv4AppendArgs &a, hipStream_t s) {
   const long threads = (long)a.rows * a.d.num_kv_heads * (a.d.head_dim / 8);
-  const dim3 grid((unsigned)(threads ? (threads + 255) / 256 : 1), 2);
+  const unsigned grid = (unsigned)(threads ? (threads + 255) / 256 : 1);
   const bool path = a.accept_path != nullptr;
   if (a.d.dtype == HB_F32) {
     if (path) kv4_append_kernel<float, true><<<grid, 256, 0, s>>>(a);
@@ -457,7 +470,7 @@ hipError_t launch_kv4_append(const Kv4AppendArgs &a, hipStream_t s) {
 hipError_t launch_kv4_read(const hb_attn_desc &d, int32_t rows, const Kv4Pool &k, const Kv4Pool &v, const int32_t *block_table,
                            const int32_t *first, const int32_t *row_offset, void *k_rows, void *v_rows, hipStream_t s) {
   const long threads = (long)rows * d.num_kv_heads * (d.head_dim / 8);
-  const dim3 grid((unsigned)((threads + 255) / 256), 2);
+  const unsigned grid = (unsigned)((threads + 255) / 256);
   if (d.dtype == HB_F32)
     kv4_read_kernel<float><<<grid, 256, 0, s>>>(d, rows, k, v, block_table, first, row_offset, (float *)k_rows, (float *)v_rows);
   else
