@@ -57,11 +57,12 @@ __device__ inline Place place_of(const int32_t *__restrict__ offset, const int32
   return x;
 }
 
-// Quantises rows into the pages.  A thread takes eight elements, four threads a block of 32: its largest
+// Quantises rows into the pages.  A thread takes eight elements of K and of V, four threads a block of 32: its largest
 // magnitude is two exchanges away.  Threads run over the pieces of a head's row, then over rows, then over heads:
 // neighbouring rows of a head are neighbours in a page.  PATH: the rows that a path names, max_path to a sequence.
-// What bounds it is memory, and four round trips in a row to a row's place: 11320 rows of 4 heads of 128 in two prompts, 29 MB, take
-// 11 us (5.8 at the rate of a copy), 96 rows of paths 3.4.  Four pieces to a thread: 13.7 us.
+// What bounds it is memory, and round trips in a row, to lengths, page and store: 11320 rows of 4 heads of 128 in two prompts, 29 MB,
+// take 8.8 us (5.8 at the rate of a copy), 96 rows of paths 3.5.  K and V by threads of their own and a search for the sequence: 11.6
+// us; sixteen elements to a thread: 0.3 us more for both directions.
 template <typename T, bool PATH>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   const hb_attn_desc &d = a.d;
@@ -146,7 +147,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   }
 }
 
-// The other way: rows as the cache holds them; positions that the table does not cover read as zero.  The same 29 MB: 12 us.
+// The other way: rows as the cache holds them; positions that the table does not cover read as zero.  The same 29 MB: 8.4 to 10 us.
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_read_kernel(hb_attn_desc d, int rows, Kv4Pool kp, Kv4Pool vp,
                                                        const int32_t *__restrict__ block_table, const int32_t *__restrict__ first,
