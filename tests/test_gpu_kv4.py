@@ -429,3 +429,66 @@ def test_values_of_nodes_that_are_not_finite_reach_the_rows_that_see_them(hb, st
     odd = ~torch.isfinite(want)
     assert odd.any() and torch.equal(torch.nan_to_num(got[0].float()[odd], nan=7.0), torch.nan_to_num(want[odd], nan=7.0))
     assert torch.equal(got[0][~odd], base[0][~odd]) and torch.equal(got[1], base[1])
+
+
+@pytest.mark.parametrize("B", [2, 64, 65, 130])
+def test_append_and_read_of_many_sequences(hb, B):
+    """Prompts of none to a few rows each, several sequences to a wavefront's rows."""
+    rng = np.random.default_rng(B)
+    counts, lens = rng.integers(0, 6, B), rng.integers(0, 30, B)
+    counts[B // 2:B // 2 + 3] = 0
+    counts[-1] = 21
+    inp = W.make_verify_inputs(23, "bf16", 2, 2, 64, [int(x) for x in lens + counts], [W.chain_tree(1)] * B, page=16)
+    case = Kv4Case(inp)
+    pool, _, _ = _cache(case, rng)
+    n, offset = int(counts.sum()), np.concatenate([[0], np.cumsum(counts)])
+    x = [torch.from_numpy(rng.standard_normal((n, 2, 64))).to(torch.bfloat16) for _ in (0, 1)]
+    want = [p.copy() for p in pool]
+    kv4_append_ref(want, [W.widen(t) for t in x], inp.block_table.numpy(), lens, [range(offset[b], offset[b + 1]) for b in range(B)], None, None, None)
+    dev = [torch.from_numpy(p).cuda() for p in pool]
+    i32 = lambda v: torch.tensor(np.asarray(v), dtype=torch.int32, device="cuda")
+    new, table, first = i32([-1] * B), inp.block_table.cuda(), i32(lens)
+    hb.hb_kv4_append(case.desc(), x[0].cuda(), x[1].cuda(), *dev, table, first, i32(offset), new_len=new)
+    out = [torch.full((n, 2, 64), 5.0, dtype=torch.bfloat16, device="cuda") for _ in (0, 1)]
+    hb.hb_kv4_read(case.desc(), *dev, table, first, i32(offset), *out)
+    torch.cuda.synchronize()
+    assert new.tolist() == (lens + counts).tolist()
+    for got, ref in zip(dev, want):
+        assert np.array_equal(got.cpu().numpy(), ref)
+    for o, src in zip(out, x):
+        assert np.array_equal(W.widen(o), kv4_values_ref(*kv4_quantise_ref(W.widen(src))))
+
+
+@pytest.mark.parametrize("B,nodes,longest", [(1, 1, 768), (1, 1, 769), (1, 8, 1025), (8, 4, 1024), (8, 4, 1025), (2, 60, 256), (2, 60, 257), (6, 60, 1153)])
+def test_where_prefixes_begin_to_be_cut(hb, step, B, nodes, longest):
+    """The longest prefix at the bound that the call is given, the others anywhere below; and a bound that leaves room."""
+    lens = [longest] + [longest * (b + 1) % 700 for b in range(B - 1)]
+    case = mixed_case(51, "bf16", 28, 4, 64, 16, lens, [nodes] * B, peaked=True)
+    ref = case.attend()
+    for hint in (longest, longest + 300):
+        out, lse = _attend(hb, step, case, hint=hint)
+        case.check_attention(out, lse, ref, f"hint={hint}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_weights_of_paths_of_any_bound(hb, dtype):
+    """Bounds on a path's length beyond a wavefront; a path that names a node twice, and ids outside the tree, which are clamped."""
+    case = mixed_case(32, dtype, 14, 2, 128, 16, [70, 600], [64, 20])
+    i, max_path = case.inp, 100
+    _, lse = case.attend()
+    path = np.full((2, max_path), -5)
+    path[0, :64] = np.arange(64)[::-1]
+    path[1, :7] = [3, 3, 19, 0, 25, -2, 8]
+    accept = [64, 7]
+    took = [list(path[0, :64]), [64 + x for x in (3, 3, 19, 0, 19, 0, 8)]]
+    weight = np.random.default_rng(1).random((2, 2, case.cap)).astype(np.float32)
+    lse32 = torch.from_numpy(lse).float()
+    want = kv4_attn_weight_ref(W.widen(i.q), case.k, i.block_table.numpy(), i.prefix_len.numpy(), took, W.widen(lse32), i.softmax_scale, 0.5, weight)
+    pool, t = case.device()
+    w, i32 = torch.from_numpy(weight).cuda(), lambda v: torch.tensor(np.asarray(v), dtype=torch.int32, device="cuda")
+    hb.hb_kv4_attn_weight(case.desc(), t["q"], pool[0], pool[1], t["block_table"], t["prefix_len"], t["node_offset"], i32(accept), i32(path),
+                          max_path, lse32.cuda(), 0.5, w)
+    torch.cuda.synchronize()
+    # as in test_attention_weights; 64 nodes of seven heads are 448 float32 additions on top
+    tol = want * (4 * 2.0 ** -24 * math.sqrt(128) * (case.largest_sum() + 4) + 4e-6 + 448 * 2.0 ** -24)
+    assert (np.abs(W.widen(w) - want) <= tol).all(), (np.abs(W.widen(w) - want) / tol).max()
