@@ -18,7 +18,8 @@ struct Kv4Pool {
 };
 
 // part_o, part_ml: of row r = node * Hq + head and chunk c at (r * splits + c) * D and * 2: sums against the chunk's
-// largest score (natural units), that score, the sum of weights.  Unused where splits is 1.
+// largest score, that score (log2 units from the matrix-core kernels, natural ones from the scalar kernel), the sum of weights.
+// Unused where splits is 1.
 struct Kv4AttnArgs {
   hb_attn_desc d;
   int32_t splits, chunk;  // chunks of a prefix, and their length in positions
