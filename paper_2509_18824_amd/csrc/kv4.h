@@ -69,6 +69,13 @@ __device__ inline float kv4_scale(uint32_t s) {
 
 typedef float kv4_f32x2 __attribute__((ext_vector_type(2)));
 
+// A float32 as three bf16 pieces, which is all of it.  The first is cut off behind its eight bits: rounded, it would be an infinity
+// from 2^128 - 2^119 on, and the others infinities and NaN with it.
+__device__ __forceinline__ float kv4_cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ __forceinline__ uint32_t kv4_pack_cut(float lo, float hi) {  // of two
+  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
+}
+
 // two elements, from byte SEL of `codes`
 template <int SEL>
 __device__ inline kv4_f32x2 kv4_pair(uint32_t codes, float scale) {

@@ -117,6 +117,16 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 
 __device__ __forceinline__ void store4(bf16_t *p, f32x4 v) { *(u32x2 *)p = (u32x2){pack2(v[0], v[1]), pack2(v[2], v[3])}; }
 __device__ __forceinline__ void store4(float *p, f32x4 v) { *(f32x4 *)p = v; }
+// sum / weight of a row, a mean of values: where rounding takes it past the largest number of float32 it is that number.  (bf16's
+// largest is further from there than roundings go.)
+__device__ __forceinline__ f32x4 mean_of(bf16_t, f32x4 sum, float weight) { return sum * (1.f / weight); }
+__device__ __forceinline__ f32x4 mean_of(float, f32x4 sum, float weight) {
+  f32x4 v = sum * (1.f / weight);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (fabsf(v[e]) == -kNegInf && fabsf(sum[e]) != -kNegInf) v[e] = copysignf(__FLT_MAX__, v[e]);
+  return v;
+}
 
 // Pages of a chunk's keys, 64 times 16 keys to the registers of a wavefront (lane l: the l-th 16) and the next 64 on their way.
 // Asked for one by one, by scalar loads, they would be waited for with the LDS reads of every step.
@@ -285,31 +295,50 @@ struct Rows {
 };
 
 // ---- float32 ----------------------------------------------------------------------------------------
-// Queries, weights and the nodes' own keys and values are taken as three bf16 pieces of eight bits each, which is all of a
-// float32; cached keys are widened to bf16, which is exact.  A product of two such numbers keeps the six products of pieces that
-// matter to 2^-24, the smallest first.
-__device__ __forceinline__ void pieces_of(const f32x8 &x, bf16x8 (&p)[3]) {
-  f32x8 rest = x;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    p[i] = __builtin_convertvector(rest, bf16x8);
-    rest -= __builtin_convertvector(p[i], f32x8);
-  }
-}
+// Queries, weights and the nodes' own keys and values are taken as three bf16 pieces; cached keys are widened to bf16, which is
+// exact.  A product of two such numbers keeps the six products of pieces that matter to 2^-23, the smallest first.
 __device__ __forceinline__ f32x8 load_f32x8(const float *at) {
   const f32x4 a = *(const f32x4 *)at, b = *(const f32x4 *)(at + 4);
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
-// lane (j, kg) of the i-th operand of a row: d = 32 kg + 8 i + 0 .. 7, as a cached key's block lies
-template <int DB>
+__device__ __forceinline__ f32x8 within(f32x8 x, float most) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_fmed3f(x[e], -most, most);
+  return x;
+}
+// the first piece of a number up to the largest
+__device__ __forceinline__ bf16x8 cut_of(const f32x8 &x) {
+  u32x4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = kv4_pack_cut(x[2 * e], x[2 * e + 1]);
+  return __builtin_bit_cast(bf16x8, y);
+}
+__device__ __forceinline__ f32x8 rest_of(f32x8 x) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] -= kv4_cut(x[e]);
+  return x;
+}
+// of a softmax weight, which is far from the largest number: the first is rounded too
+__device__ __forceinline__ void pieces_of(f32x8 x, bf16x8 (&p)[3]) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    p[i] = __builtin_convertvector(x, bf16x8);
+    x -= __builtin_convertvector(p[i], f32x8);
+  }
+}
+// Lane (j, kg) of the i-th operand of a row: d = 32 kg + 8 i + 0 .. 7, as a cached key's block lies.  An infinity gives NaN in its
+// products.  INF: its first two pieces are finite, and the third, an infinity, meets the other factor's first piece alone.
+template <int DB, bool INF = false>
 __device__ __forceinline__ void row_pieces(const float *row, bool there, int kg, bf16x8 (&p)[3][4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     f32x8 x = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (there && (DB == 4 || kg < DB)) x = load_f32x8(row + 32 * kg + 8 * i);
-    bf16x8 y[3];
-    pieces_of(x, y);
-    p[0][i] = y[0], p[1][i] = y[1], p[2][i] = y[2];
+    p[0][i] = cut_of(INF ? within(x, __FLT_MAX__) : x);
+    x -= __builtin_convertvector(p[0][i], f32x8);
+    p[1][i] = __builtin_convertvector(INF ? within(x, 0x1p120f) : x, bf16x8);
+    x -= __builtin_convertvector(p[1][i], f32x8);
+    p[2][i] = __builtin_convertvector(x, bf16x8);
   }
 }
 // Scores of 16 keys
@@ -325,8 +354,9 @@ __device__ __forceinline__ void score_tiles(const bf16x8 (&k)[4], const bf16x8 (
 // Softmax weights of a step's scores.  A row's reference is the largest score of the first step it sees, and moves when the
 // weights of a lane's eight keys against it sum to more than 2^12 (or to no number): then one of them is 2^9 or more, and
 // the reference becomes the row's largest score of the step.  Their sum is needed anyway, so that the common case takes no
-// maximum at all.
-template <int TPW, int DB>
+// maximum at all.  F32: it lies a factor of two above that score, so that the nodes' weights, rounded as they are, stay below one and
+// the largest of float32 among the nodes' values does not overflow.
+template <bool F32, int TPW, int DB>
 __device__ __forceinline__ void weigh(Rows<TPW, DB> &w, const f32x4 (&sc)[TPW][2], float c1, f32x8 (&p)[TPW]) {
   float sum[TPW];
   auto weights = [&] {
@@ -346,7 +376,7 @@ __device__ __forceinline__ void weigh(Rows<TPW, DB> &w, const f32x4 (&sc)[TPW][2
 #pragma unroll
     for (int t = 0; t < TPW; ++t) {
       const float lm = fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), sc[t][0][2]), sc[t][0][3]), sc[t][1][0]), sc[t][1][1]), sc[t][1][2]), sc[t][1][3]);
-      const float mx = group_max(lm) * c1;  // c1 > 0
+      const float mx = group_max(lm) * c1 + (F32 ? 1.f : 0.f);  // c1 > 0
       const float old = w.m[t] == kNegInf ? mx : w.m[t];
       const bool grow = mx > old + kSlack;
       w.m[t] = grow ? mx : old;
@@ -534,20 +564,25 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
     auto piece_at = [&](int key, int piece) { return (u32x4 *)(lv + key * kRow + ((piece ^ (v_swz(key) & (4 * DB - 1))) * 16)); };
     f32x8 p[TPW];
     if constexpr (F32) {
+      auto scores = [&](auto inf) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        bf16x8 k[3][4];
-        row_pieces<DB>((const float *)a.k_tree + ((size_t)(n0 + min(first + 16 * h + j, n - 1)) * d.num_kv_heads + g) * D, true, kg, k);
-        sc[0][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        for (int h = 0; h < 2; ++h) {
+          bf16x8 k[3][4];
+          row_pieces<DB, decltype(inf)::value>((const float *)a.k_tree + ((size_t)(n0 + min(first + 16 * h + j, n - 1)) * d.num_kv_heads + g) * D, true, kg, k);
+          sc[0][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int sum = 2; sum >= 0; --sum)
+          for (int sum = 2; sum >= 0; --sum)
 #pragma unroll
-          for (int b = 0; b <= sum; ++b)
+            for (int b = 0; b <= sum; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sc[0][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b][i], q32[sum - b][i], sc[0][h], 0, 0, 0);
-      }
-      mask(0);
-      weigh<TPW, DB>(w, sc, c1, p);
+              for (int i = 0; i < 4; ++i) sc[0][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b][i], q32[sum - b][i], sc[0][h], 0, 0, 0);
+        }
+        mask(0);
+      };
+      scores(std::false_type());
+      const f32x4 both = sc[0][0] + sc[0][1];
+      if (const float sum = (both[0] + both[1]) + (both[2] + both[3]); __any(sum != sum)) scores(std::true_type());  // an infinity in a key, or NaN
+      weigh<F32>(w, sc, c1, p);
       bf16x8 weight[3];
       pieces_of(p[0], weight);
       f32x8 x[2][DB];
@@ -574,9 +609,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < DB; ++i) {
-            const bf16x8 y = __builtin_convertvector(x[h][i], bf16x8);
-            x[h][i] -= __builtin_convertvector(y, f32x8);
-            *piece_at(16 * h + j, DB * kg + i) = __builtin_bit_cast(u32x4, y);
+            *piece_at(16 * h + j, DB * kg + i) = __builtin_bit_cast(u32x4, cut_of(x[h][i]));  // (all three: 24 bits)
+            x[h][i] = rest_of(x[h][i]);
           }
         bf16x8 av[2 * DB];
         read_values<DB>(lv, j, kg, av);
@@ -616,7 +650,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
           *piece_at(key, DB * kg + i) = x;
         }
       }
-      weigh<TPW, DB>(w, sc, c1, p);
+      weigh<F32>(w, sc, c1, p);
       weigh_values<TPW, DB>(w, lv, j, kg, p, true);
     }
     if (odd) s_odd[wave] = 1;
@@ -664,7 +698,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
       load(step + 2 * W, x);
     }
     f32x8 p[TPW];
-    weigh<TPW, DB>(w, sc, c1, p);
+    weigh<F32>(w, sc, c1, p);
     if constexpr (F32) {
       bf16x8 weight[3], av[2 * DB];
       pieces_of(p[0], weight);
@@ -725,7 +759,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
       for (int i = 0; i < W; ++i) o += all[(dt * W + i) * 64 + lane];
       if (row < R) {
         if (ch.chunks == 1) {
-          store4((T *)a.out + rr * D + 16 * dt + 4 * kg, o * (1.f / l));
+          store4((T *)a.out + rr * D + 16 * dt + 4 * kg, mean_of(T(), o, l));
         } else {
           *(f32x4 *)(a.part_o + (rr * plan.splits + ch.c) * D + 16 * dt + 4 * kg) = o;
         }
@@ -911,7 +945,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
           for (int r = 0; r < 4; ++r) sc[t][h][r] = ((allow >> (16 * h + r)) & 1u) ? sc[t][h][r] : kNegInf;
       }
       f32x8 p[TPW];
-      weigh<TPW, DB>(w, sc, c1, p);
+      weigh<false>(w, sc, c1, p);
       weigh_values<TPW, DB>(w, lv + 32 * blk * kRow, j, kg, p, true);
     }
   }
@@ -950,7 +984,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
 #pragma unroll
             for (int r = 0; r < 4; ++r) sc[t][h][r] = 16 * h + 4 * kg + r < left ? sc[t][h][r] : kNegInf;
       }
-      weigh<TPW, DB>(w, sc, c1, p);
+      weigh<false>(w, sc, c1, p);
       if (left < 32) {  // few keys or many, a sequence's last ones may be all that it has: see weigh_values
         bf16x8 rest[TPW];
 #pragma unroll
@@ -1104,7 +1138,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a, Kv4Plan pl
       }
     }
   }
-  store4((T *)a.out + (size_t)row * D + piece * 4, o * (1.f / l));
+  store4((T *)a.out + (size_t)row * D + piece * 4, mean_of(T(), o, l));
   if (a.lse && piece == 0) a.lse[row] = (m + log2f(l)) * kLn2;
 }
 

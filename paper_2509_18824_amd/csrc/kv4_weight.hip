@@ -2,7 +2,7 @@
 //
 //   S = Q K^T   v_mfma_f32_16x16x32_bf16: A = 16 query rows, B = 16 cached keys, widened to bf16, which is exact
 //   w_p = decay w_p + sum over rows of exp(S[row][p] - lse[row])
-// The weights are 32-bit results, so the scores are too.  float32 queries are taken as three bf16 pieces of eight bits each, which is all of them, smallest first.
+// The weights are 32-bit results, so the scores are too.  float32 queries are taken as three bf16 pieces (kv4.h), smallest first.
 //
 // Each key is 4 bits an element and 8 bytes for its weight; up to some ten rows that bounds it, from there on the exponentials
 // (16 clocks for 64 of them): six nodes of 28/4 heads are 42 rows.  16 sequences of 1024 to 8192 positions, 23 MB, take 17 us (4.5 at
@@ -43,7 +43,7 @@ __device__ __forceinline__ void pieces_of(const float *p, u32x4 (&x)[3]) {
     float lo = e < 2 ? a[2 * e] : b[2 * e - 4], hi = e < 2 ? a[2 * e + 1] : b[2 * e - 3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      const uint32_t w = pack_bf16(lo, hi);
+      const uint32_t w = i == 0 ? kv4_pack_cut(lo, hi) : pack_bf16(lo, hi);
       x[i][e] = w;
       lo -= __uint_as_float(w << 16);
       hi -= __uint_as_float(w & 0xffff0000u);
