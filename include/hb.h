@@ -564,6 +564,7 @@ int32_t hb_meta_query_attn_project(int32_t S, int32_t L, int32_t D, int32_t H, i
  * Where a call takes weight (float32) and pos (int32), both device [B, Hkv, max_blocks_per_seq * page_size]: the attention
  * weight that the position in a slot has gathered, and its position in the sequence.  After evictions the heads of a sequence
  * hold different positions, all of them prefix_len[b]; seq_len[b] is the number of positions that there have been.
+ * desc->max_prefix_len_hint sizes the launches of these calls and no more: a longer prefix is taken whole, in more time.
  *
  * hb_kv4_append: rows row_offset[b] .. row_offset[b+1] - 1 of k_rows and v_rows (a prompt, or part of one) to positions
  * prefix_len[b], prefix_len[b] + 1, ... of sequence b; new_len[b] = prefix_len[b] + their number.

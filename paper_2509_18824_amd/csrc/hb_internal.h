@@ -257,9 +257,10 @@ struct Kv4EvictArgs {
   // least key that stays and how many that have it do; in front of every 256 slots, how many have a greater key and how many this
   int32_t *moves, *counts, *least, *parts;
   int32_t parts_each;
-  int32_t longest;  // no prefix is longer
+  int32_t longest;  // what the launches are sized for: longer prefixes go round in them
+  int32_t list_step, move_step;  // parts of 256 slots, and moves, of all workgroups of a head (set by the launch)
 };
-hipError_t launch_kv4_evict(const Kv4EvictArgs &a, hipStream_t s);
+hipError_t launch_kv4_evict(Kv4EvictArgs a, hipStream_t s);
 
 // ---- argmax key: (order-preserving float bits << 32) | (0xffffffff - index) ---------------
 // max over keys = largest value, lowest index among equal values.  NaN is mapped to -inf.

@@ -18,7 +18,7 @@ static int32_t check_kv4(const hb_attn_desc *desc) {
   return HB_OK;
 }
 
-// the cache alone: fields that only attention reads may hold anything
+// the cache alone: fields that only attention needs may hold anything (a bound on lengths sizes eviction's launches)
 static int32_t check_kv4_cache(const hb_attn_desc *desc) {
   if (!desc) return fail(HB_ERR_INVALID_ARG, "desc is NULL");
   hb_attn_desc d = *desc;
@@ -250,7 +250,7 @@ int32_t hb_kv4_evict(const hb_attn_desc *desc, int32_t budget, int32_t recent, i
   Kv4EvictArgs a = {*desc, budget, recent, sinks, (uint8_t *)k_codes, (uint8_t *)k_scales, (uint8_t *)v_codes, (uint8_t *)v_scales,
                     block_table, prefix_len, seq_len, weight, pos, weight_out, pos_out, kept, new_len, (int32_t *)workspace,
                     (int32_t *)((char *)workspace + at.counts), (int32_t *)((char *)workspace + at.least),
-                    (int32_t *)((char *)workspace + at.parts_at), (int32_t)at.parts, (int32_t)span_of(desc)};
+                    (int32_t *)((char *)workspace + at.parts_at), (int32_t)at.parts, (int32_t)span_of(desc), 0, 0};
   HB_HIP_TRY(launch_kv4_evict(a, (hipStream_t)stream));
   return HB_OK;
 }

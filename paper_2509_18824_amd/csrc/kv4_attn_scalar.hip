@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attn_scalar_kernel(Kv4AttnArgs a
   if (n0 < 0 || n0 + n > d.total_nodes) n = 0;
   if (node < n0 || node >= n0 + n) return;  // malformed offsets
   const int L = kv4_length(d, a.prefix_len, b);
-  const int begin = c * a.chunk, end = min(L, begin + a.chunk);
+  const int begin = c * a.chunk, end = c + 1 == a.splits ? L : min(L, begin + a.chunk);  // (lengths beyond the host's bound)
   for (int i = tid; i < D; i += kThreads) q[i] = load_f32((const T *)a.q + (size_t)r * D + i) * d.softmax_scale;
   if (tid == 0) {
     unsigned long long path = 0;
@@ -214,27 +214,30 @@ __global__ __launch_bounds__(kThreads) void kv4_weight_scalar_kernel(Kv4WeightAr
   const hb_attn_desc &d = a.d;
   __shared__ float q[256];
   const int tid = threadIdx.x, h = blockIdx.y % d.num_kv_heads, b = blockIdx.y / d.num_kv_heads, G = d.num_q_heads / d.num_kv_heads;
-  const int L = kv4_length(d, a.prefix_len, b), s = blockIdx.x * kThreads + tid;
-  if ((int)blockIdx.x * kThreads >= L) return;
+  const int L = kv4_length(d, a.prefix_len, b);
   const int n0 = a.node_offset[b];
   int n = a.node_offset[b + 1] - n0;
   n = n < 0 || n0 < 0 || n0 + n > d.total_nodes ? 0 : n;
   int rows = a.accept_path ? a.accept_len[b] : n;
   rows = rows < 0 || n == 0 ? 0 : a.accept_path && rows > a.max_path ? a.max_path : rows;
-  const size_t row = s < L ? kv4_row(d, a.block_table, b, h, s) : 0;
-  float sum = 0.f;
-  for (int i = 0; i < rows * G; ++i) {
-    int node = a.accept_path ? a.accept_path[(size_t)b * a.max_path + i / G] : i / G;
-    node = node < 0 ? 0 : node >= n ? n - 1 : node;
-    const size_t r = (size_t)(n0 + node) * d.num_q_heads + h * G + i % G;
-    __syncthreads();
-    for (int e = tid; e < d.head_dim; e += kThreads) q[e] = load_f32((const T *)a.q + r * d.head_dim + e) * d.softmax_scale;
-    __syncthreads();
-    if (s < L) sum += expf(dot_row(d, a.kp, row, q) - a.lse[r]);
-  }
-  if (s < L) {
-    float *w = a.weight + ((size_t)b * d.num_kv_heads + h) * d.max_blocks_per_seq * d.page_size + s;
-    *w = fmaf(*w, a.decay, sum);
+  // once, but where the prefix is longer than the host's bound
+  for (int s0 = blockIdx.x * kThreads; s0 < L; s0 += gridDim.x * kThreads) {
+    const int s = s0 + tid;
+    const size_t row = s < L ? kv4_row(d, a.block_table, b, h, s) : 0;
+    float sum = 0.f;
+    for (int i = 0; i < rows * G; ++i) {
+      int node = a.accept_path ? a.accept_path[(size_t)b * a.max_path + i / G] : i / G;
+      node = node < 0 ? 0 : node >= n ? n - 1 : node;
+      const size_t r = (size_t)(n0 + node) * d.num_q_heads + h * G + i % G;
+      __syncthreads();
+      for (int e = tid; e < d.head_dim; e += kThreads) q[e] = load_f32((const T *)a.q + r * d.head_dim + e) * d.softmax_scale;
+      __syncthreads();
+      if (s < L) sum += expf(dot_row(d, a.kp, row, q) - a.lse[r]);
+    }
+    if (s < L) {
+      float *w = a.weight + ((size_t)b * d.num_kv_heads + h) * d.max_blocks_per_seq * d.page_size + s;
+      *w = fmaf(*w, a.decay, sum);
+    }
   }
 }
 

@@ -253,7 +253,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs
   __shared__ int s_digit, s_need;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x / d.num_kv_heads;
   const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
-  const int L = min(kv4_length(d, a.prefix_len, b), a.longest), stays = L < a.budget ? L : a.budget;
+  const int L = kv4_length(d, a.prefix_len, b), stays = L < a.budget ? L : a.budget;
   const float *w = a.weight + (size_t)blockIdx.x * cap;
   const int32_t *pos = a.pos + (size_t)blockIdx.x * cap;
   const int recent_from = a.seq_len[b] - a.recent;
@@ -374,54 +374,53 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs
 __global__ __launch_bounds__(256) void kv4_list_kernel(Kv4EvictArgs a) {
   const hb_attn_desc &d = a.d;
   const int lane = threadIdx.x & 63, unit = blockIdx.y, b = unit / d.num_kv_heads;
-  const int part = blockIdx.x * 4 + (threadIdx.x >> 6), s0 = part * kPart;
   const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
-  const int L = min(kv4_length(d, a.prefix_len, b), a.longest), stays = L < a.budget ? L : a.budget;
+  const int L = kv4_length(d, a.prefix_len, b), stays = L < a.budget ? L : a.budget;
   int32_t *kept = a.kept + (size_t)unit * a.budget;
-  for (long s = stays + s0 + lane; s < (long)stays + s0 + kPart && s < a.budget; s += 64) kept[s] = -1;
-  // (budgets beyond the row: the last workgroup's part goes on to their end)
-  if (part == (int)gridDim.x * 4 - 1)
-    for (long s = (long)stays + s0 + kPart + lane; s < a.budget; s += 64) kept[s] = -1;
-  if (s0 >= L) return;
-  const int32_t *before = a.parts + ((size_t)unit * a.parts_each + part) * 2;
+  for (long s = (long)stays + blockIdx.x * 256 + threadIdx.x; s < a.budget; s += (long)a.list_step * 64) kept[s] = -1;
   const uint32_t least = (uint32_t)a.least[unit * 2];
-  const int need = a.least[unit * 2 + 1], above = before[0], ties = before[1];
+  const int need = a.least[unit * 2 + 1];
   const float *w = a.weight + unit * cap;
   const int32_t *pos = a.pos + unit * cap;
-  uint32_t key[4];
-  f32x4 x;
-  int32_t p[4];
-  const int s = s0 + lane * 4;
-  load_keys(w, pos, s, L, in_fours(a, cap), a.seq_len[b] - a.recent, a.sinks, key, x, p);
-  unsigned long long m[4];
+  // one part to a wavefront, more only where the row is longer than the host's bound
+  for (int part = blockIdx.x * 4 + (threadIdx.x >> 6), s0 = part * kPart; s0 < L; part += a.list_step, s0 = part * kPart) {
+    const int32_t *before = a.parts + ((size_t)unit * a.parts_each + part) * 2;
+    const int above = before[0], ties = before[1];
+    uint32_t key[4];
+    f32x4 x;
+    int32_t p[4];
+    const int s = s0 + lane * 4;
+    load_keys(w, pos, s, L, in_fours(a, cap), a.seq_len[b] - a.recent, a.sinks, key, x, p);
+    unsigned long long m[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) m[e] = __ballot(key[e] == least && least != 0);
-  int tie = ties + lanes_before(m);
-  bool stay[4];
+    for (int e = 0; e < 4; ++e) m[e] = __ballot(key[e] == least && least != 0);
+    int tie = ties + lanes_before(m);
+    bool stay[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const bool t = key[e] == least && least != 0;
-    stay[e] = key[e] > least || (t && tie < need);
-    tie += t ? 1 : 0;
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) m[e] = __ballot(stay[e]);
-  int n = above + min(ties, need) + lanes_before(m);  // that stay in front of slot s + e
-  int32_t *from = a.moves + (size_t)unit * 2 * a.budget, *to = from + a.budget;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int at = s + e;
-    if (at == stays && at < L) a.counts[unit] = stays - n;
-    if (stay[e] && at < stays) {
-      kept[at] = at;
-      a.weight_out[unit * cap + at] = x[e];
-      a.pos_out[unit * cap + at] = p[e];
-    } else if (stay[e]) {
-      from[stays - 1 - n] = at;
-    } else if (at < stays) {
-      to[at - n] = at;
+    for (int e = 0; e < 4; ++e) {
+      const bool t = key[e] == least && least != 0;
+      stay[e] = key[e] > least || (t && tie < need);
+      tie += t ? 1 : 0;
     }
-    n += stay[e] ? 1 : 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m[e] = __ballot(stay[e]);
+    int n = above + min(ties, need) + lanes_before(m);  // that stay in front of slot s + e
+    int32_t *from = a.moves + (size_t)unit * 2 * a.budget, *to = from + a.budget;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = s + e;
+      if (at == stays && at < L) a.counts[unit] = stays - n;
+      if (stay[e] && at < stays) {
+        kept[at] = at;
+        a.weight_out[unit * cap + at] = x[e];
+        a.pos_out[unit * cap + at] = p[e];
+      } else if (stay[e]) {
+        from[stays - 1 - n] = at;
+      } else if (at < stays) {
+        to[at - n] = at;
+      }
+      n += stay[e] ? 1 : 0;
+    }
   }
 }
 
@@ -431,25 +430,29 @@ __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4EvictArgs a) {
   const hb_attn_desc &d = a.d;
   const int blocks = d.head_dim / kKv4Block, lanes = 2 * blocks, each = 64 / lanes;
   const int lane = threadIdx.x & 63, part = lane % lanes, unit = blockIdx.y;
-  const int i = ((int)blockIdx.x * 4 + (threadIdx.x >> 6)) * each + lane / lanes;
+  int i = ((int)blockIdx.x * 4 + (threadIdx.x >> 6)) * each + lane / lanes;
   const int count = a.counts[unit];
   if (lane >= each * lanes || i >= count) return;
   const int b = unit / d.num_kv_heads, h = unit % d.num_kv_heads;
   const size_t cap = (size_t)d.max_blocks_per_seq * d.page_size;
   const int32_t *moves = a.moves + (size_t)unit * 2 * a.budget;
-  const int src = moves[count - 1 - i], dst = moves[a.budget + i];
-  const size_t s = kv4_row(d, a.block_table, b, h, src), t = kv4_row(d, a.block_table, b, h, dst);
-  const bool value = part >= blocks;
-  const int blk = value ? part - blocks : part;
-  uint8_t *codes = value ? a.v_codes : a.k_codes, *scales = value ? a.v_scales : a.k_scales;
-  ((u32x4 *)codes)[t * blocks + blk] = ((const u32x4 *)codes)[s * blocks + blk];
-  scales[t * blocks + blk] = scales[s * blocks + blk];
-  if (part == 0) {
-    a.kept[(size_t)unit * a.budget + dst] = src;
-    a.weight_out[unit * cap + dst] = a.weight[unit * cap + src];
-  } else if (part == 1) {
-    a.pos_out[unit * cap + dst] = a.pos[unit * cap + src];
-  }
+  auto move = [&] {
+    const int src = moves[count - 1 - i], dst = moves[a.budget + i];
+    const size_t s = kv4_row(d, a.block_table, b, h, src), t = kv4_row(d, a.block_table, b, h, dst);
+    const bool value = part >= blocks;
+    const int blk = value ? part - blocks : part;
+    uint8_t *codes = value ? a.v_codes : a.k_codes, *scales = value ? a.v_scales : a.k_scales;
+    ((u32x4 *)codes)[t * blocks + blk] = ((const u32x4 *)codes)[s * blocks + blk];
+    scales[t * blocks + blk] = scales[s * blocks + blk];
+    if (part == 0) {
+      a.kept[(size_t)unit * a.budget + dst] = src;
+      a.weight_out[unit * cap + dst] = a.weight[unit * cap + src];
+    } else if (part == 1) {
+      a.pos_out[unit * cap + dst] = a.pos[unit * cap + src];
+    }
+  };
+  move();
+  for (i += a.move_step; i < count; i += a.move_step) move();  // where the row is longer than the host's bound
 }
 
 }  // namespace
@@ -479,17 +482,21 @@ hipError_t launch_kv4_read(const hb_attn_desc &d, int32_t rows, const Kv4Pool &k
   return hipGetLastError();
 }
 
-hipError_t launch_kv4_evict(const Kv4EvictArgs &a, hipStream_t s) {
+hipError_t launch_kv4_evict(Kv4EvictArgs a, hipStream_t s) {
   const int units = a.d.batch * a.d.num_kv_heads;
+  const unsigned lists = (unsigned)((a.longest + 4 * kPart - 1) / (4 * kPart));
+  const int each = 4 * (64 / (2 * (a.d.head_dim / kKv4Block)));  // moves of a workgroup
+  const int most = a.budget < a.longest ? a.budget : a.longest;
+  const unsigned moves = (unsigned)((most + each - 1) / each);
+  a.list_step = (int32_t)lists * 4;
+  a.move_step = (int32_t)moves * each;
   kv4_select_kernel<<<units, kSelectThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  kv4_list_kernel<<<dim3((unsigned)((a.longest + 4 * kPart - 1) / (4 * kPart)), (unsigned)units), 256, 0, s>>>(a);
+  kv4_list_kernel<<<dim3(lists, (unsigned)units), 256, 0, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int each = 4 * (64 / (2 * (a.d.head_dim / kKv4Block)));  // moves of a workgroup
-  const int most = a.budget < a.longest ? a.budget : a.longest;
-  kv4_move_kernel<<<dim3((unsigned)((most + each - 1) / each), (unsigned)units), 256, 0, s>>>(a);
+  kv4_move_kernel<<<dim3(moves, (unsigned)units), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -52,7 +52,7 @@ __device__ __forceinline__ void pieces_of(const float *p, u32x4 (&x)[3]) {
 }
 
 template <typename T, int DB>
-__global__ __launch_bounds__(64 * kWaves) void kv4_weight_kernel(Kv4WeightArgs a, uint32_t page_magic, int rounds) {
+__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 4 ? 2 : 3) void kv4_weight_kernel(Kv4WeightArgs a, uint32_t page_magic, int rounds, int stride) {
   constexpr int P = sizeof(T) == 4 ? 3 : 1, kRows = sizeof(T) == 4 ? 32 : 64, D = 32 * DB;
   const hb_attn_desc &d = a.d;
   // 16-byte pieces [row][piece of bf16][d / 8], the last index XORed with the row so that 16 rows' reads spread over the banks
@@ -63,25 +63,29 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_weight_kernel(Kv4WeightArgs a
   // units are neighbours, not chunks: workgroup ids go round the XCDs, and the chunks behind short sequences are empty
   const int h = blockIdx.x % d.num_kv_heads, b = blockIdx.x / d.num_kv_heads, G = d.num_q_heads / d.num_kv_heads;
   // a wavefront's keys: 64 in each round, the first at k0; what has to be known first is asked for in one go
-  const int begin = (int)(blockIdx.z * gridDim.y + blockIdx.y) * rounds * kWaves * kKeys, k0 = begin + wave * kKeys;
+  const int share = rounds * kWaves * kKeys;
+  int begin = (int)(blockIdx.z * gridDim.y + blockIdx.y) * share, k0 = begin + wave * kKeys;
   const int cap16 = d.max_blocks_per_seq * (d.page_size / 16);
   const int32_t *table = a.block_table + (size_t)b * d.max_blocks_per_seq;
   // lane 4 r + t: the page of the t-th 16 keys of round r
-  const int at16 = min((k0 >> 4) + (lane >> 2) * (kWaves * 4) + (lane & 3), cap16 - 1);
-  int pages = table[page_magic ? (int)__umulhi((uint32_t)at16, page_magic) : at16];
+  auto ask_pages = [&] {
+    const int at16 = min((k0 >> 4) + (lane >> 2) * (kWaves * 4) + (lane & 3), cap16 - 1);
+    return table[page_magic ? (int)__umulhi((uint32_t)at16, page_magic) : at16];
+  };
+  int pages = ask_pages();
   const int n0 = a.node_offset[b], n1 = a.node_offset[b + 1], accepted = a.accept_path ? a.accept_len[b] : 0;
   const bool short_path = a.accept_path && a.max_path <= 64;
   if (short_path && tid < a.max_path) s_path[tid] = a.accept_path[(size_t)b * a.max_path + tid];
   const int L = kv4_length(d, a.prefix_len, b);
   if (begin >= L) return;
-  const int end = min(L, begin + rounds * kWaves * kKeys);
+  int end = min(L, begin + share);
   const int n = n1 - n0 < 0 || n0 < 0 || n1 > d.total_nodes ? 0 : n1 - n0;
   int nodes = a.accept_path ? accepted : n;
   nodes = nodes < 0 || n == 0 ? 0 : a.accept_path && nodes > a.max_path ? a.max_path : nodes;
   const int rows = nodes * G;
   const float c1 = d.softmax_scale * kLog2e;
   float *weight = a.weight + ((size_t)b * d.num_kv_heads + h) * d.max_blocks_per_seq * d.page_size;
-  pages = pages < 0 ? 0 : (pages >= d.num_blocks ? d.num_blocks - 1 : pages);
+  pages = max(0, min(pages, d.num_blocks - 1));
 
   struct Keys {
     u32x4 k[4];
@@ -152,59 +156,67 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_weight_kernel(Kv4WeightArgs a
     __syncthreads();
   }
   // every wavefront goes round as often as the others: there are barriers inside where rows come in batches
-  for (int round = 0; begin + round * kWaves * kKeys < end; ++round) {
-    const int first = k0 + round * kWaves * kKeys;
-    float old[4];
-    bf16x8 bk[4][4];
+  for (;;) {
+    for (int round = 0; begin + round * kWaves * kKeys < end; ++round) {
+      const int first = k0 + round * kWaves * kKeys;
+      float old[4];
+      bf16x8 bk[4][4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      old[t] = x.old[t];
-      const float s = __uint_as_float(x.scale[t] << 23);
+      for (int t = 0; t < 4; ++t) {
+        old[t] = x.old[t];
+        const float s = __uint_as_float(x.scale[t] << 23);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        u32x4 y;
-        y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 0));
-        y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 1));
-        y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 2));
-        y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 3));
-        bk[t][i] = __builtin_bit_cast(bf16x8, y);
+        for (int i = 0; i < 4; ++i) {
+          u32x4 y;
+          y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 0));
+          y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 1));
+          y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 2));
+          y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[t][i], s, 3));
+          bk[t][i] = __builtin_bit_cast(bf16x8, y);
+        }
+      }
+      load(round + 1, x);  // on its way during the products
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int r0 = 0; r0 < rows; r0 += kRows) {
+        if (!one_batch) {
+          __syncthreads();  // the batch before has been read
+          stage(r0);
+          __syncthreads();
+        }
+        const int tiles = (min(kRows, rows - r0) + 15) / 16;
+        for (int rt = 0; rt < tiles; ++rt) {
+          f32x4 sc[4] = {};
+#pragma unroll
+          for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int r = rt * 16 + j;
+              // d = 32 kg + 8 i + 0 .. 7; where a head has two blocks, the keys' other lanes hold zeros
+              const int piece = DB == 4 ? 4 * kg + i : 4 * (kg & 1) + i;
+              const bf16x8 q = __builtin_bit_cast(bf16x8, s_q[(r * P + p) * 4 * DB + (piece ^ (r & (4 * DB - 1)))]);
+#pragma unroll
+              for (int t = 0; t < 4; ++t) sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, bk[t][i], sc[t], 0, 0, 0);
+            }
+          const f32x4 lse = *(const f32x4 *)&s_lse[rt * 16 + 4 * kg];
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[t] += __builtin_amdgcn_exp2f(fmaf(sc[t][r], c1, -lse[r]));
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float all = group_sum(sum[t]);
+        // lane group t writes the t-th 16 keys
+        if (kg == t && first + 16 * t + j < end) weight[first + 16 * t + j] = fmaf(old[t], a.decay, all);
       }
     }
-    load(round + 1, x);  // on its way during the products
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int r0 = 0; r0 < rows; r0 += kRows) {
-      if (!one_batch) {
-        __syncthreads();  // the batch before has been read
-        stage(r0);
-        __syncthreads();
-      }
-      const int tiles = (min(kRows, rows - r0) + 15) / 16;
-      for (int rt = 0; rt < tiles; ++rt) {
-        f32x4 sc[4] = {};
-#pragma unroll
-        for (int p = P - 1; p >= 0; --p)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = rt * 16 + j;
-            // d = 32 kg + 8 i + 0 .. 7; where a head has two blocks, the keys' other lanes hold zeros
-            const int piece = DB == 4 ? 4 * kg + i : 4 * (kg & 1) + i;
-            const bf16x8 q = __builtin_bit_cast(bf16x8, s_q[(r * P + p) * 4 * DB + (piece ^ (r & (4 * DB - 1)))]);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, bk[t][i], sc[t], 0, 0, 0);
-          }
-        const f32x4 lse = *(const f32x4 *)&s_lse[rt * 16 + 4 * kg];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) sum[t] += __builtin_amdgcn_exp2f(fmaf(sc[t][r], c1, -lse[r]));
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const float all = group_sum(sum[t]);
-      // lane group t writes the t-th 16 keys
-      if (kg == t && first + 16 * t + j < end) weight[first + 16 * t + j] = fmaf(old[t], a.decay, all);
-    }
+    if (L - begin <= stride) break;  // always, but where the prefix is longer than the host's bound
+    begin += stride;
+    k0 += stride;
+    end = min(L, begin + share);
+    pages = max(0, min(ask_pages(), d.num_blocks - 1));
+    load(0, x);
   }
 }
 
@@ -224,13 +236,14 @@ hipError_t launch_kv4_weight_mfma(const Kv4WeightArgs &a, int32_t longest, hipSt
   const int keys = (int)rounds * kWaves * kKeys;
   const unsigned chunks = (unsigned)((longest + keys - 1) / keys), rows_of_grid = chunks < 32768 ? chunks : 32768;
   const dim3 grid((unsigned)units, rows_of_grid, (chunks + rows_of_grid - 1) / rows_of_grid);
+  const int stride = (int)(grid.y * grid.z) * keys;  // of all workgroups of a unit
   const bool f32 = a.d.dtype == HB_F32;
   if (a.d.head_dim == 128) {
-    if (f32) kv4_weight_kernel<float, 4><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds);
-    else kv4_weight_kernel<bf16_t, 4><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds);
+    if (f32) kv4_weight_kernel<float, 4><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds, stride);
+    else kv4_weight_kernel<bf16_t, 4><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds, stride);
   } else {
-    if (f32) kv4_weight_kernel<float, 2><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds);
-    else kv4_weight_kernel<bf16_t, 2><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds);
+    if (f32) kv4_weight_kernel<float, 2><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds, stride);
+    else kv4_weight_kernel<bf16_t, 2><<<grid, 64 * kWaves, 0, s>>>(a, magic, (int)rounds, stride);
   }
   return hipGetLastError();
 }
