@@ -355,8 +355,8 @@ __device__ __forceinline__ void score_tiles(const bf16x8 (&k)[4], const bf16x8 (
 // weights of a lane's eight keys against it sum to more than 2^12 (or to no number): then one of them is 2^9 or more, and
 // the reference becomes the row's largest score of the step.  Their sum is needed anyway, so that the common case takes no
 // maximum at all.  F32: it lies a factor of two above that score, so that the nodes' weights, rounded as they are, stay below one and
-// the largest of float32 among the nodes' values does not overflow.
-template <bool F32, int TPW, int DB>
+// the largest of float32 among the nodes' values does not overflow.  NODES: their second 32 as well, so it moves for any larger score.
+template <bool F32, bool NODES = false, int TPW, int DB>
 __device__ __forceinline__ void weigh(Rows<TPW, DB> &w, const f32x4 (&sc)[TPW][2], float c1, f32x8 (&p)[TPW]) {
   float sum[TPW];
   auto weights = [&] {
@@ -368,7 +368,7 @@ __device__ __forceinline__ void weigh(Rows<TPW, DB> &w, const f32x4 (&sc)[TPW][2
     }
   };
   weights();
-  bool need = false;
+  bool need = NODES;
 #pragma unroll
   for (int t = 0; t < TPW; ++t) need |= !(sum[t] <= w.limit[t]);
   if (__any(need)) {
@@ -378,7 +378,7 @@ __device__ __forceinline__ void weigh(Rows<TPW, DB> &w, const f32x4 (&sc)[TPW][2
       const float lm = fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), sc[t][0][2]), sc[t][0][3]), sc[t][1][0]), sc[t][1][1]), sc[t][1][2]), sc[t][1][3]);
       const float mx = group_max(lm) * c1 + (F32 ? 1.f : 0.f);  // c1 > 0
       const float old = w.m[t] == kNegInf ? mx : w.m[t];
-      const bool grow = mx > old + kSlack;
+      const bool grow = mx > old + (NODES ? 0.f : kSlack);
       w.m[t] = grow ? mx : old;
       w.ref[t] = w.m[t] == kNegInf ? 0.f : w.m[t];
       w.limit[t] = w.m[t] == kNegInf ? -1.f : kMostSum;
@@ -945,7 +945,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
           for (int r = 0; r < 4; ++r) sc[t][h][r] = ((allow >> (16 * h + r)) & 1u) ? sc[t][h][r] : kNegInf;
       }
       f32x8 p[TPW];
-      weigh<false>(w, sc, c1, p);
+      weigh<false, true>(w, sc, c1, p);
       weigh_values<TPW, DB>(w, lv + 32 * blk * kRow, j, kg, p, true);
     }
   }

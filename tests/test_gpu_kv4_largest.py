@@ -32,7 +32,7 @@ def test_off_the_path_they_do_not_matter(hb, step, dtype, Hq, D, nodes):
         assert all(torch.equal(g[others], w[others]) for g, w in zip(got, want)), bad
 
 
-@pytest.mark.parametrize("dtype,Hq,D,nodes", [x for x in LAYOUTS if x[0] == "f32" or x[3] < 60])
+@pytest.mark.parametrize("dtype,Hq,D,nodes", LAYOUTS + [("bf16", 14, 64, 40), ("bf16", 28, 128, 64)])
 @pytest.mark.parametrize("lens", [[33, 100], [0, 3000]])
 def test_values_that_are_seen(hb, step, dtype, Hq, D, nodes, lens):
     """One node's value in an element: sums in float32 hold it.  Elements beside it are as they would be without."""
