@@ -33,15 +33,19 @@ __device__ inline float dot_row(const hb_attn_desc &d, const Kv4Pool &pool, size
   float sum = 0.f;
   for (int blk = 0; blk < d.head_dim / kKv4Block; ++blk) {
     const u32x4 c = codes[blk];
-    float part = 0.f;  // the scale is a power of two: it may as well be applied to the sum
+    const uint32_t scale = scales[blk];
+    // scaled one by one, which costs nothing and is exact: queries times codes alone may be larger than any product
+    const float s = __uint_as_float((scale == kKv4NaN ? 127u : scale) << 23);
+    float part = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float *x = q + blk * kKv4Block + i * 8;
-      const kv4_f32x2 a = kv4_pair<0>(c[i], 1.f), b = kv4_pair<1>(c[i], 1.f), e = kv4_pair<2>(c[i], 1.f), f = kv4_pair<3>(c[i], 1.f);
+      const kv4_f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[i], s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[i], s, 1);
+      const kv4_f32x2 e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[i], s, 2), f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[i], s, 3);
       part = fmaf(a[0], x[0], part), part = fmaf(a[1], x[1], part), part = fmaf(b[0], x[2], part), part = fmaf(b[1], x[3], part);
       part = fmaf(e[0], x[4], part), part = fmaf(e[1], x[5], part), part = fmaf(f[0], x[6], part), part = fmaf(f[1], x[7], part);
     }
-    sum = fmaf(part, kv4_scale(scales[blk]), sum);
+    sum += scale == kKv4NaN ? __builtin_nanf("") : part;
   }
   return sum;
 }

@@ -94,7 +94,7 @@ def test_a_seen_key_whose_score_is_minus_infinity_weighs_nothing(hb, step, dtype
     case.check_attention(out, lse, ref)
 
 
-@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("D", [64, 128, 96])
 def test_weights_of_queries_up_to_the_largest(hb, D):
     """Queries at the type's largest in a block whose cached keys lie about the smallest normal number."""
     case = mixed_case(31, "f32", 4, 2, D, 16, [17, 300], [3, 12])
@@ -116,3 +116,13 @@ def test_weights_of_queries_up_to_the_largest(hb, D):
     # a score's sum of D products in float32, then an exponential and a sum of the rows: relative to the weight
     tol = want * (4 * 2.0 ** -24 * math.sqrt(D) * (case.largest_sum() + 4) + 4e-6)
     assert (np.abs(W.widen(w) - want) <= tol).all(), (np.abs(W.widen(w) - want) / tol).max()
+
+
+@pytest.mark.parametrize("dtype,D", [("f32", 128), ("f32", 96), ("bf16", 64), ("bf16", 96)])
+def test_a_block_of_keys_that_is_no_number_reaches_its_head_alone(hb, step, dtype, D):
+    case = mixed_case(14, dtype, 4, 2, D, 16, [256, 90], [1, 1])
+    clean = _attend(hb, step, case)
+    case.pool[1][int(case.inp.block_table[0, 3]), 1, 7, 1] = 255
+    out, lse = _attend(hb, step, case)
+    assert torch.isnan(out[0, 2:].float()).all() and torch.isnan(lse[0, 2:]).all()
+    assert torch.equal(out[0, :2], clean[0][0, :2]) and torch.equal(out[1], clean[0][1]) and torch.equal(lse[1], clean[1][1])
