@@ -574,7 +574,8 @@ int32_t hb_meta_query_attn_project(int32_t S, int32_t L, int32_t D, int32_t H, i
  * hb_kv4_read: row r of sequence b (row_offset as above) = position first[b] + r - row_offset[b] as the cache holds it; zero
  * where the table has no such position.
  *   k_rows, v_rows  device [n_rows, Hkv, D]  desc->dtype      row_offset, first, seq_len  device int32
- * seq_len, weight, pos, out_slots and new_len may be NULL.
+ * seq_len, weight, pos, out_slots and new_len may be NULL.  out_slots and new_len are written while the lengths, offsets and paths
+ * are read, so they must not overlap these: new_len is not prefix_len, which is advanced by a copy behind the call.
  * Uses desc->{dtype, batch, num_q_heads, num_kv_heads, head_dim, page_size, max_blocks_per_seq, num_blocks, total_nodes}.
  * Errors: INVALID_ARG, UNSUPPORTED (also: D % 32, more rows than one launch takes), DEVICE.  Nothing to do is a success.
  */
@@ -631,7 +632,7 @@ int32_t hb_kv4_attn_weight(const hb_attn_desc *desc, const void *q, const void *
  *   weight_out, pos_out  as weight and pos, which they may be: slots below new_len are written, no others
  *   workspace   device, hb_kv4_evict_workspace_bytes(desc, budget) bytes, 256-byte aligned
  * Pages behind new_len are free afterwards.  Pages must not be shared between sequences.  new_len may be NULL
- * and must not overlap prefix_len.
+ * and must not overlap prefix_len or seq_len.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, DEVICE.
  */
 int32_t hb_kv4_evict(const hb_attn_desc *desc, int32_t budget, int32_t recent, int32_t sinks, void *k_codes, void *k_scales,

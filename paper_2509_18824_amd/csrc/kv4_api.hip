@@ -1,6 +1,8 @@
 // Host side of the calls over the 4-bit cache: argument validation, the cut of the prefix, dispatch.
 #include "kv4.h"
 
+#include <initializer_list>
+
 namespace hb {
 
 static size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
@@ -32,6 +34,20 @@ static int32_t check_pool(const void *k_codes, const void *k_scales, const void 
   if (!k_codes || !k_scales || !v_codes || !v_scales) return fail(HB_ERR_INVALID_ARG, "a pool's device pointer is NULL");
   if (misaligned(k_codes, 16) || misaligned(k_scales, 16) || misaligned(v_codes, 16) || misaligned(v_scales, 16))
     return fail(HB_ERR_INVALID_ARG, "codes and scales must be 16-byte aligned");
+  return HB_OK;
+}
+
+// What a call writes while other workgroups read its integers
+struct Ints {
+  const int32_t *at;
+  int64_t n;
+};
+static int32_t check_apart(const char *name, Ints out, std::initializer_list<Ints> in) {
+  for (const Ints &x : in) {
+    const uintptr_t o = (uintptr_t)out.at, i = (uintptr_t)x.at;
+    if (o && i && o < i + (uint64_t)x.n * 4 && i < o + (uint64_t)out.n * 4)
+      return fail(HB_ERR_INVALID_ARG, "%s must not overlap the lengths, offsets and paths that the call reads", name);
+  }
   return HB_OK;
 }
 
@@ -101,6 +117,8 @@ int32_t hb_kv4_append(const hb_attn_desc *desc, int32_t n_rows, const void *k_ro
   if ((rc = check_rows(n_rows, desc)) || (rc = check_pool(k_codes, k_scales, v_codes, v_scales))) return rc;
   if ((n_rows && (!k_rows || !v_rows)) || !block_table || !prefix_len || !row_offset)
     return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
+  const int64_t B = desc->batch;
+  if ((rc = check_apart("new_len", {new_len, B}, {{prefix_len, B}, {row_offset, B + 1}, {seq_len, B}}))) return rc;
   if (misaligned(k_rows, 16) || misaligned(v_rows, 16)) return fail(HB_ERR_INVALID_ARG, "k_rows and v_rows must be 16-byte aligned");
   Kv4AppendArgs a = {*desc, n_rows, n_rows, 0, k_rows, v_rows, (uint8_t *)k_codes, (uint8_t *)k_scales, (uint8_t *)v_codes,
                      (uint8_t *)v_scales, block_table, prefix_len, row_offset, nullptr, nullptr, seq_len, weight, pos, nullptr, new_len};
@@ -120,6 +138,9 @@ int32_t hb_kv4_compact(const hb_attn_desc *desc, const void *k_tree, const void 
   if (!block_table || !prefix_len || !node_offset || !accept_len || !accept_path)
     return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
   if (desc->total_nodes && (!k_tree || !v_tree)) return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
+  const int64_t B = desc->batch;
+  const std::initializer_list<Ints> in = {{prefix_len, B}, {node_offset, B + 1}, {accept_len, B}, {accept_path, B * max_path}, {seq_len, B}};
+  if ((rc = check_apart("new_len", {new_len, B}, in)) || (rc = check_apart("out_slots", {out_slots, B * max_path}, in))) return rc;
   if (misaligned(k_tree, 16) || misaligned(v_tree, 16)) return fail(HB_ERR_INVALID_ARG, "k_tree and v_tree must be 16-byte aligned");
   Kv4AppendArgs a = {*desc, desc->batch * max_path, desc->total_nodes, max_path, k_tree, v_tree, (uint8_t *)k_codes, (uint8_t *)k_scales,
                      (uint8_t *)v_codes, (uint8_t *)v_scales, block_table, prefix_len, node_offset, accept_len, accept_path, seq_len,
@@ -242,6 +263,7 @@ int32_t hb_kv4_evict(const hb_attn_desc *desc, int32_t budget, int32_t recent, i
   if ((rc = check_pool(k_codes, k_scales, v_codes, v_scales))) return rc;
   if (!block_table || !prefix_len || !seq_len || !weight || !pos || !weight_out || !pos_out || !kept)
     return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
+  if ((rc = check_apart("new_len", {new_len, desc->batch}, {{prefix_len, desc->batch}, {seq_len, desc->batch}}))) return rc;
   const EvictLayout at = evict_layout(desc, budget);
   const size_t need = at.bytes;
   if (!workspace || workspace_bytes < need)
