@@ -596,6 +596,7 @@ def hb_tree_verify_attn_kv4(desc: AttnDesc, q, k_tree, v_tree, k_codes, k_scales
         raise ValueError("q and out must be [total_nodes, Hq, D] in the descriptor's dtype")
     if _kv4_rows(desc, k_tree, v_tree) < desc.total_nodes or lse is not None and (lse.numel() < rows or lse.dtype is not torch.float32):
         raise ValueError("k_tree and v_tree must be [total_nodes, Hkv, D], lse float32 [total_nodes, Hq]")
+    _kv4_ints(block_table, prefix_len, node_offset, parent)
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(lib.hb_tree_verify_attn_kv4(C.byref(desc), _ptr(q), _ptr(k_tree), _ptr(v_tree), _ptr(k_codes), _ptr(k_scales),
                                        _ptr(v_codes), _ptr(v_scales), _ptr(block_table), _ptr(prefix_len), _ptr(node_offset),
