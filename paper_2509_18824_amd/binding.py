@@ -512,17 +512,22 @@ hb_lmhead_accept = _lmhead_accept(lib.hb_lmhead_accept)
 hb_lmhead_accept_cleared = _lmhead_accept(lib.hb_lmhead_accept_cleared)
 
 
-# (sizes rather than shapes: a call's checks cost microseconds)
+# Checks by sizes rather than shapes, one pass over a tensor, each name looked up once: a call's checks cost microseconds
+_u8, _i32, _f32 = torch.uint8, torch.int32, torch.float32
+_of_code = {HB_F32: torch.float32, HB_BF16: torch.bfloat16}
+
+
+def _of_desc(desc: AttnDesc, t) -> bool:
+    return t.dtype is _of_code.get(desc.dtype) or _dtype_code(t) == desc.dtype  # (raises for one that nothing here takes)
+
+
 def _kv4_rows(desc: AttnDesc, k_rows, v_rows) -> int:
-    n, row = k_rows.shape[0], desc.num_kv_heads * desc.head_dim
-    if k_rows.numel() != n * row or v_rows.numel() != n * row:
+    n, size = k_rows.shape[0], k_rows.numel()
+    if size != n * desc.num_kv_heads * desc.head_dim or v_rows.numel() != size:
         raise ValueError("rows must be [n, Hkv, D], K and V alike")
-    if _dtype_code(k_rows) != desc.dtype or v_rows.dtype != k_rows.dtype:
+    if not _of_desc(desc, k_rows) or v_rows.dtype is not k_rows.dtype:
         raise ValueError("rows must have the descriptor's dtype")
     return n
-
-
-_u8 = torch.uint8
 
 
 def _kv4_pool(desc: AttnDesc, k_codes, k_scales, v_codes=None, v_scales=None) -> None:
@@ -535,15 +540,20 @@ def _kv4_pool(desc: AttnDesc, k_codes, k_scales, v_codes=None, v_scales=None) ->
 
 def _kv4_slots(desc: AttnDesc, weight, pos) -> None:
     n = desc.batch * desc.num_kv_heads * desc.max_blocks_per_seq * desc.page_size
-    if (weight is not None and (weight.dtype is not torch.float32 or weight.numel() != n)
-            or pos is not None and (pos.dtype is not torch.int32 or pos.numel() != n)):
+    if (weight is not None and (weight.dtype is not _f32 or weight.numel() != n)
+            or pos is not None and (pos.dtype is not _i32 or pos.numel() != n)):
         raise ValueError("weight (float32) and pos (int32) must be [B, Hkv, max_blocks * page]")
 
 
-def _kv4_ints(*tensors) -> None:
-    for t in tensors:
-        if t is not None and t.dtype is not torch.int32:
-            raise ValueError("lengths, offsets, positions, paths and tables are int32 tensors")
+# lengths, offsets, parents, paths and tables, with the number of them that a call's kernels read or write
+def _ints(t, n: int):
+    if t is None:
+        return None
+    if t.dtype is not _i32 or t.numel() < n:
+        raise ValueError(f"lengths, offsets, parents, paths and tables are int32 tensors; one of them has to hold {n} numbers")
+    if not t.is_contiguous():
+        raise ValueError("tensors handed to libhb must be contiguous")
+    return t.data_ptr()
 
 
 def hb_kv4_append(desc: AttnDesc, k_rows, v_rows, k_codes, k_scales, v_codes, v_scales, block_table, prefix_len, row_offset,
@@ -551,10 +561,10 @@ def hb_kv4_append(desc: AttnDesc, k_rows, v_rows, k_codes, k_scales, v_codes, v_
     n = _kv4_rows(desc, k_rows, v_rows)
     _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
     _kv4_slots(desc, weight, pos)
-    _kv4_ints(block_table, prefix_len, row_offset, seq_len, new_len)
+    B = desc.batch
     _check(lib.hb_kv4_append(C.byref(desc), n, _ptr(k_rows), _ptr(v_rows), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes),
-                             _ptr(v_scales), _ptr(block_table), _ptr(prefix_len), _ptr(row_offset), _ptr(seq_len), _ptr(weight),
-                             _ptr(pos), _ptr(new_len), _stream(stream)))
+                             _ptr(v_scales), _ints(block_table, B * desc.max_blocks_per_seq), _ints(prefix_len, B),
+                             _ints(row_offset, B + 1), _ints(seq_len, B), _ptr(weight), _ptr(pos), _ints(new_len, B), _stream(stream)))
 
 
 def hb_kv4_compact(desc: AttnDesc, k_tree, v_tree, k_codes, k_scales, v_codes, v_scales, block_table, prefix_len, node_offset,
@@ -564,20 +574,22 @@ def hb_kv4_compact(desc: AttnDesc, k_tree, v_tree, k_codes, k_scales, v_codes, v
         raise ValueError("rows must be [total_nodes, Hkv, D]")
     _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
     _kv4_slots(desc, weight, pos)
-    _kv4_ints(block_table, prefix_len, node_offset, accept_len, accept_path, seq_len, out_slots, new_len)
+    B = desc.batch
     _check(lib.hb_kv4_compact(C.byref(desc), _ptr(k_tree), _ptr(v_tree), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes),
-                              _ptr(v_scales), _ptr(block_table), _ptr(prefix_len), _ptr(node_offset), _ptr(accept_len),
-                              _ptr(accept_path), max_path, _ptr(seq_len), _ptr(weight), _ptr(pos), _ptr(out_slots),
-                              _ptr(new_len), _stream(stream)))
+                              _ptr(v_scales), _ints(block_table, B * desc.max_blocks_per_seq), _ints(prefix_len, B),
+                              _ints(node_offset, B + 1), _ints(accept_len, B), _ints(accept_path, B * max_path), max_path,
+                              _ints(seq_len, B), _ptr(weight), _ptr(pos), _ints(out_slots, B * max_path), _ints(new_len, B),
+                              _stream(stream)))
 
 
 def hb_kv4_read(desc: AttnDesc, k_codes, k_scales, v_codes, v_scales, block_table, first, row_offset, k_rows, v_rows,
                 stream=None) -> None:
     n = _kv4_rows(desc, k_rows, v_rows)
     _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
-    _kv4_ints(block_table, first, row_offset)
-    _check(lib.hb_kv4_read(C.byref(desc), n, _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(block_table),
-                           _ptr(first), _ptr(row_offset), _ptr(k_rows), _ptr(v_rows), _stream(stream)))
+    B = desc.batch
+    _check(lib.hb_kv4_read(C.byref(desc), n, _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales),
+                           _ints(block_table, B * desc.max_blocks_per_seq), _ints(first, B), _ints(row_offset, B + 1), _ptr(k_rows),
+                           _ptr(v_rows), _stream(stream)))
 
 
 def hb_tree_verify_attn_kv4_workspace_bytes(desc: AttnDesc) -> int:
@@ -592,29 +604,30 @@ def hb_tree_verify_attn_kv4(desc: AttnDesc, q, k_tree, v_tree, k_codes, k_scales
                             node_offset, parent, out, lse=None, workspace=None, stream=None) -> None:
     _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
     rows = desc.total_nodes * desc.num_q_heads
-    if q.numel() < rows * desc.head_dim or out.numel() < rows * desc.head_dim or _dtype_code(q) != desc.dtype or out.dtype is not q.dtype:
+    if q.numel() < rows * desc.head_dim or out.numel() < rows * desc.head_dim or not _of_desc(desc, q) or out.dtype is not q.dtype:
         raise ValueError("q and out must be [total_nodes, Hq, D] in the descriptor's dtype")
-    if _kv4_rows(desc, k_tree, v_tree) < desc.total_nodes or lse is not None and (lse.numel() < rows or lse.dtype is not torch.float32):
+    if _kv4_rows(desc, k_tree, v_tree) < desc.total_nodes or lse is not None and (lse.numel() < rows or lse.dtype is not _f32):
         raise ValueError("k_tree and v_tree must be [total_nodes, Hkv, D], lse float32 [total_nodes, Hq]")
-    _kv4_ints(block_table, prefix_len, node_offset, parent)
-    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    ws_bytes = workspace.nbytes if workspace is not None else 0
+    B = desc.batch
     _check(lib.hb_tree_verify_attn_kv4(C.byref(desc), _ptr(q), _ptr(k_tree), _ptr(v_tree), _ptr(k_codes), _ptr(k_scales),
-                                       _ptr(v_codes), _ptr(v_scales), _ptr(block_table), _ptr(prefix_len), _ptr(node_offset),
-                                       _ptr(parent), _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream)))
+                                       _ptr(v_codes), _ptr(v_scales), _ints(block_table, B * desc.max_blocks_per_seq),
+                                       _ints(prefix_len, B), _ints(node_offset, B + 1), _ints(parent, desc.total_nodes), _ptr(out), _ptr(lse),
+                                       _ptr(workspace), ws_bytes, _stream(stream)))
 
 
 def hb_kv4_attn_weight(desc: AttnDesc, q, k_codes, k_scales, block_table, prefix_len, node_offset, accept_len, accept_path,
                        max_path: int, lse, decay: float, weight, stream=None) -> None:
     _kv4_pool(desc, k_codes, k_scales)
     _kv4_slots(desc, weight, None)
-    _kv4_ints(block_table, prefix_len, node_offset, accept_len, accept_path)
     rows = desc.total_nodes * desc.num_q_heads
-    if (q.numel() < rows * desc.head_dim or _dtype_code(q) != desc.dtype or lse is not None
-            and (lse.numel() < rows or lse.dtype is not torch.float32)):
+    if (q.numel() < rows * desc.head_dim or not _of_desc(desc, q) or lse is not None
+            and (lse.numel() < rows or lse.dtype is not _f32)):
         raise ValueError("q must be [total_nodes, Hq, D] in the descriptor's dtype, lse float32 [total_nodes, Hq]")
-    _check(lib.hb_kv4_attn_weight(C.byref(desc), _ptr(q), _ptr(k_codes), _ptr(k_scales), _ptr(block_table), _ptr(prefix_len),
-                                  _ptr(node_offset), _ptr(accept_len), _ptr(accept_path), max_path, _ptr(lse), decay,
-                                  _ptr(weight), _stream(stream)))
+    B = desc.batch
+    _check(lib.hb_kv4_attn_weight(C.byref(desc), _ptr(q), _ptr(k_codes), _ptr(k_scales),
+                                  _ints(block_table, B * desc.max_blocks_per_seq), _ints(prefix_len, B), _ints(node_offset, B + 1), _ints(accept_len, B),
+                                  _ints(accept_path, B * max_path), max_path, _ptr(lse), decay, _ptr(weight), _stream(stream)))
 
 
 def hb_kv4_evict_workspace_bytes(desc: AttnDesc, budget: int) -> int:
@@ -626,10 +639,11 @@ def hb_kv4_evict(desc: AttnDesc, budget: int, recent: int, sinks: int, k_codes, 
     _kv4_pool(desc, k_codes, k_scales, v_codes, v_scales)
     _kv4_slots(desc, weight, pos)
     _kv4_slots(desc, weight_out, pos_out)
-    _kv4_ints(block_table, prefix_len, seq_len, kept, new_len)
-    if kept.numel() != desc.batch * desc.num_kv_heads * budget:
+    B = desc.batch
+    if kept.numel() != B * desc.num_kv_heads * budget:
         raise ValueError("kept must be [B, Hkv, budget]")
-    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    ws_bytes = workspace.nbytes if workspace is not None else 0
     _check(lib.hb_kv4_evict(C.byref(desc), budget, recent, sinks, _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales),
-                            _ptr(block_table), _ptr(prefix_len), _ptr(seq_len), _ptr(weight), _ptr(pos), _ptr(weight_out),
-                            _ptr(pos_out), _ptr(kept), _ptr(new_len), _ptr(workspace), ws_bytes, _stream(stream)))
+                            _ints(block_table, B * desc.max_blocks_per_seq), _ints(prefix_len, B), _ints(seq_len, B), _ptr(weight),
+                            _ptr(pos), _ptr(weight_out), _ptr(pos_out), _ints(kept, 0), _ints(new_len, B), _ptr(workspace), ws_bytes,
+                            _stream(stream)))

@@ -72,3 +72,17 @@ def test_integers_of_another_type(reached, name, arg):
         with pytest.raises(ValueError):
             call({**args, arg: other})
     assert len(reached) == 1
+
+
+@pytest.mark.parametrize("name,arg", EACH)
+def test_integers_that_are_too_few(reached, name, arg):
+    """What the kernels would read or write behind."""
+    call, args = _calls()[name]
+    flat = args[arg].reshape(-1)
+    call({**args, arg: flat})
+    call({**args, arg: torch.cat((flat, flat))})  # more than the call needs
+    assert len(reached) == 2
+    for few in (flat[:-1], flat[:0]):
+        with pytest.raises(ValueError):
+            call({**args, arg: few})
+    assert len(reached) == 2
