@@ -999,11 +999,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(Kv4AttnArgs a, Kv4P
       accumulate<TPW, DB>(w, av, pb);
     };
     // Barrier without the fence of __syncthreads(), which would wait for every load in flight: what has to be done in front of
-    // it are reads and writes of LDS
-    auto barrier = [] {
-      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-      asm volatile("s_barrier" ::: "memory");
-    };
+    // it are reads and writes of LDS, and the wait for them is one statement with it
+    auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
     const std::integral_constant<int, 0> even;
     const std::integral_constant<int, 1> odd;
     put(0, even, x);
