@@ -47,6 +47,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kMostSum = 4096.f;  // of eight weights against their row's reference
 constexpr float kSlack = 8.f;       // log2 units: a largest score that is no further above the reference leaves it where it is
+constexpr float kFar = 0x1p27f;     // log2 units: half a unit in the last place of a larger score is more than eight
 constexpr float kNegInf = -__builtin_huge_valf();
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -357,17 +358,16 @@ __device__ __forceinline__ void score_tiles(const bf16x8 (&k)[4], const bf16x8 (
 // maximum at all.  F32: it lies a factor of two above that score, so that the nodes' weights, rounded as they are, stay below one and
 // the largest of float32 among the nodes' values does not overflow.  NODES: their second 32 as well, so it moves for any larger score.
 template <bool F32, bool NODES = false, int TPW, int DB>
-__device__ __forceinline__ void weigh(Rows<TPW, DB> &w, const f32x4 (&sc)[TPW][2], float c1, f32x8 (&p)[TPW]) {
+__device__ __forceinline__ void weigh(Rows<TPW, DB> &w, f32x4 (&sc)[TPW][2], float c1, f32x8 (&p)[TPW]) {
+#pragma clang fp contract(off)
   float sum[TPW];
-  auto weights = [&] {
+  auto weights = [&](int t, float scale) {
 #pragma unroll
-    for (int t = 0; t < TPW; ++t) {
-#pragma unroll
-      for (int r = 0; r < 8; ++r) p[t][r] = fast_exp2(fmaf(sc[t][r >> 2][r & 3], c1, -w.ref[t]));
-      sum[t] = ((p[t][0] + p[t][1]) + (p[t][2] + p[t][3])) + ((p[t][4] + p[t][5]) + (p[t][6] + p[t][7]));
-    }
+    for (int r = 0; r < 8; ++r) p[t][r] = fast_exp2(fmaf(sc[t][r >> 2][r & 3], scale, -w.ref[t]));
+    sum[t] = ((p[t][0] + p[t][1]) + (p[t][2] + p[t][3])) + ((p[t][4] + p[t][5]) + (p[t][6] + p[t][7]));
   };
-  weights();
+#pragma unroll
+  for (int t = 0; t < TPW; ++t) weights(t, c1);
   bool need = NODES;
 #pragma unroll
   for (int t = 0; t < TPW; ++t) need |= !(sum[t] <= w.limit[t]);
@@ -381,7 +381,8 @@ __device__ __forceinline__ void weigh(Rows<TPW, DB> &w, const f32x4 (&sc)[TPW][2
       const bool grow = mx > old + (NODES ? 0.f : kSlack);
       w.m[t] = grow ? mx : old;
       w.ref[t] = w.m[t] == kNegInf ? 0.f : w.m[t];
-      w.limit[t] = w.m[t] == kNegInf ? -1.f : kMostSum;
+      const bool far = fabsf(w.ref[t]) > kFar;
+      w.limit[t] = w.m[t] == kNegInf || far ? -1.f : kMostSum;
       if (__any(grow)) {
         const float alpha = grow ? fast_exp2(old - mx) : 1.f;
         w.l[t] *= alpha;
@@ -393,8 +394,12 @@ __device__ __forceinline__ void weigh(Rows<TPW, DB> &w, const f32x4 (&sc)[TPW][2
           asm volatile("" : "+v"(w.o[t][dt]));
         }
       }
+      if (__any(far)) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) sc[t][r >> 2][r & 3] *= far ? c1 : 1.f;
+      }
+      weights(t, far ? 1.f : c1);
     }
-    weights();
   }
 #pragma unroll
   for (int t = 0; t < TPW; ++t) w.l[t] += sum[t];
