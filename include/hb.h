@@ -598,6 +598,12 @@ int32_t hb_kv4_read(const hb_attn_desc *desc, int32_t n_rows, const void *k_code
  * hb_tree_verify_attn with the prefix in a 4-bit cache; the nodes' own K and V (k_tree, v_tree) are as they are there, in
  * desc->dtype.  Arguments, masks and errors as in hb_tree_verify_attn, and UNSUPPORTED for D % 32.  Values of nodes that are
  * not finite reach the rows that see them, and no others.
+ * Scores, softmax statistics and sums are float32.  In bf16 on the matrix cores a softmax weight is rounded to bf16 for its product with a value
+ * (by 2^-8 of itself at most; the sum that it is divided by is of the rounded ones; what the rounding lost of the nodes' weights and of a
+ * sequence's last keys' is added).  Sums of weights times values are divided at the end, and weights may be up to 2^12 until
+ * then: cached values beyond 2^100 may overflow, as may a row that sees several values of nodes at the type's largest.  float32 numbers
+ * of the nodes below 2^-117 are taken with fewer bits, eight at 2^-126.  Scale bytes 253 and 254, which no call writes, stand for numbers
+ * outside bf16 and are not taken.
  */
 int32_t hb_tree_verify_attn_kv4(const hb_attn_desc *desc, const void *q, const void *k_tree, const void *v_tree,
                                 const void *k_codes, const void *k_scales, const void *v_codes, const void *v_scales,

@@ -800,7 +800,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_attn_kernel(Kv4AttnArgs a, Kv4P
 // workgroup have up to two tiles of rows each and share 64 keys at a time, which are widened into LDS once for all.
 // What bounds it is the issue of vector instructions and MFMAs by the two wavefronts of a SIMD: some 140 of them, 16 exponentials
 // of four slots among them, are 750 clocks for 32 keys and 32 rows, 544 of them the matrix core's; it takes 900.  Two trees of 52
-// and 55 nodes, 28/4 heads, over 32768 positions: 85 us and 9 for the join, 42 GFLOP; 16 of 30 to 60 nodes over 1024 to
+// and 55 nodes, 28/4 heads, over 32768 positions: 84 us and 8 for the join, 50 GFLOP; 16 of 30 to 60 nodes over 1024 to
 // 8192: 86 and 10.  Eight wavefronts to a workgroup, which share the keys among twice the rows: 93 and 114 us for the calls
 // that take 89 and 95, since a barrier then holds up all of a CU.
 // The loop over 32-key blocks is skewed by one: the matrix core gets a block's V^T P^T and the next one's scores in one go, and
@@ -1158,7 +1158,13 @@ hipError_t launch_rows(const Kv4AttnArgs &a, const Kv4Plan &plan, hipStream_t s)
 
 }  // namespace
 
-// Rows of (sequence, kv head) from which on wavefronts share the keys: four tiles and less, each wavefront has keys of its own
+// Rows of (sequence, kv head) from which on wavefronts share the keys: four tiles and less, each wavefront has keys of its own.
+// Own and shared, us (28 / 4 heads of 128; of 64 the same within a tenth): one sequence over 4096 keys, 63 rows 16.9 and 18.5, 70 17.1 and 19.0,
+// 259 19.1 and 27.6; 16 over 2048, 63 21.7 and 28.9, 70 21.1 and 30.0, 126 22.2 and 33.9, 133 37.9 and 40.9; 16 over 300, 161 24.4
+// and 18.7; 16 over 8192, 161 98 and 89, 420 195 and 162; 24 over 4000, 63 34.4 and 44.5, 70 59 and 47; two over 32768, 63 26.7 and
+// 37.4, 126 35 and 43, 259 72 and 75, 364 99 and 76; 64 over 1000, 63 32.3 and 32.8, 126 60 and 38; 64 over 300, 35 26.0 and 16.1, 63 26.5
+// and 16.9.  So 64 is low where workgroups of 32 rows are a round of the CUs or less and prefixes are not the longest, and high
+// for many short sequences: what decides is how full either kernel's last round is, which this bound does not ask.
 static bool shares_keys(const hb_attn_desc &d) { return d.num_q_heads / d.num_kv_heads * d.max_nodes_per_tree > 64; }
 
 static int tiles_of(const hb_attn_desc &d) { return (d.num_q_heads / d.num_kv_heads * d.max_nodes_per_tree + 15) / 16; }
@@ -1191,6 +1197,8 @@ void kv4_attn_plan(const hb_attn_desc &d, int64_t span, Kv4Plan *plan) {
   // and 9.6, over 1024 11.4 and 11.1, over 1536 11.4 and 12.6; 16 chains of 8 nodes over 512 17.1 and 13.9, over 1024 19.2 and
   // 15.8, over 2048 21.6 and 20.0, over 3000 23.7 and 24.8; 60-node trees, 4 over 256 20.7 and 19.2, over 768 23.4 and 31.7,
   // 16 over 256 34.0 and 19.9, over 1536 54.3 and 51.8, over 2048 62.3 and 63.1.  Beyond those lengths never, for ragged ones.
+  // Heads of 64, 8 / 8, 32 / 8 and 16 / 2 heads, float32, 204 calls of one to 16 sequences over 512 to 3000: the rule's choice is
+  // the better or within 9 % of it.
   const int64_t pieces = (int64_t)d.batch * d.num_kv_heads * plan->row_groups;
   const int64_t whole = sharing ? std::min<int64_t>(pieces / 20, 12) : std::min<int64_t>(3 + pieces / 32, 8);
   if (!d.num_splits && most <= whole) splits = 1;

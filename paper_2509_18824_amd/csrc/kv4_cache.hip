@@ -242,9 +242,10 @@ __device__ inline bool in_fours(const Kv4EvictArgs &a, size_t cap) {
 
 // One workgroup per (sequence, head) finds the least key that stays, digit by digit (11 bits, a histogram each: the exponent's eight
 // alone would send most weights to a few counters), how many of the positions that have it stay (the first ones do), and how
-// many stay in front of every 256 slots.  A CU's vector instructions bound it (32768 slots: 32 keys to a thread), so
-// what can be done by more CUs is left to the next launch.  Up to 32768 slots their keys stay in registers; longer rows are
-// read again for every digit.  Eight heads of 32768 slots 19 us, four of 2048 9 us; a histogram for each quarter of
+// many stay in front of every 256 slots.  What bounds it is one CU: of 32768 slots' 46 K clocks its vector units work 19 K (32 keys to a
+// thread, 1170 instructions to a wavefront, as many scalar ones) and its wavefronts wait for 60 % of theirs, at the barriers of
+// three digits and for what lies between them, so what can be done by more CUs is left to the next launch.  Up to 32768 slots their keys
+// stay in registers; longer rows are read again for every digit.  Eight heads of 32768 slots 19 us, four of 2048 8 us; a histogram for each quarter of
 // the lanes takes half a microsecond off both.  (One launch that also ranked and listed: 55 and 30 us.)
 __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictArgs a) {
   const hb_attn_desc &d = a.d;
@@ -425,7 +426,7 @@ __global__ __launch_bounds__(256) void kv4_list_kernel(Kv4EvictArgs a) {
 }
 
 // Rows of K and V to the slots that came free for them: a lane takes a block of K or V (16 bytes and a scale), 2 D / 32 lanes a
-// move, so that a wavefront has several in flight.  49 K rows of heads of 128, 27 MB read and written: 6 us (a wavefront a row: 22).
+// move, so that a wavefront has several in flight.  49 K rows of heads of 128, 13.4 MB read and written, scattered: 6 us, 2.2 TB/s (a wavefront a row: 22).
 __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4EvictArgs a) {
   const hb_attn_desc &d = a.d;
   const int blocks = d.head_dim / kKv4Block, lanes = 2 * blocks, each = 64 / lanes;

@@ -5,7 +5,7 @@
 // The weights are 32-bit results, so the scores are too.  float32 queries are taken as three bf16 pieces (kv4.h), smallest first.
 //
 // Each key is 4 bits an element and 8 bytes for its weight; up to some ten rows that bounds it, from there on the exponentials
-// (16 clocks for 64 of them): six nodes of 28/4 heads are 42 rows.  16 sequences of 1024 to 8192 positions, 23 MB, take 17 us (4.5 at
+// (16 clocks for 64 of them): six nodes of 28/4 heads are 42 rows.  16 sequences of 1024 to 8192 positions, 23 MB, take 15 to 17 us (4.5 at
 // the rate of a copy), of which the matrix cores work 1 and the vector unit 4; the rest are round trips, to lengths, paths and
 // pages, to codes, to queries, and workgroups that find their chunk behind the end of a sequence.  One token over 2048: 5 us.
 // A wavefront takes 64 keys, requested in one go; lane
@@ -51,6 +51,7 @@ __device__ __forceinline__ void pieces_of(const float *p, u32x4 (&x)[3]) {
   }
 }
 
+// (three wavefronts to a SIMD: 16 sequences 16.7 us, with registers for two 18.8, for four 17.3; float32's allow three untold)
 template <typename T, int DB>
 __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 4 ? 2 : 3) void kv4_weight_kernel(Kv4WeightArgs a, uint32_t page_magic, int rounds, int stride) {
   constexpr int P = sizeof(T) == 4 ? 3 : 1, kRows = sizeof(T) == 4 ? 32 : 64, D = 32 * DB;
