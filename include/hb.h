@@ -77,6 +77,7 @@ typedef struct hb_attn_desc {
   int32_t max_prefix_len_hint; /* upper bound on prefix_len known to the host, 0 = unknown  */
                                /* (then max_blocks_per_seq * page_size is assumed); with a  */
                                /* prefix longer than a given bound the result is unspecified */
+                               /* (the calls over a 4-bit cache take it whole: see there)   */
   int32_t algo;                /* hb_attn_algo                                              */
   float softmax_scale;         /* scores are softmax_scale * <q, k>                         */
 } hb_attn_desc;
