@@ -10,9 +10,9 @@
  * the append of the accepted nodes' K/V to the cache (the paper keeps committed context in the
  * KV cache, Section 4.1).  Around it: the rest of the target's decoder layer (positions, rotary
  * table, fused QKV projection, output projection, normalisation, feed-forward block), the
- * construction of the draft tree from the draft model's logits, and the draft model's
+ * construction of the draft tree from the draft model's logits, the draft model's
  * intermediate layer (aggregation of the target's layer features with meta queries, Section
- * 3.1.1).
+ * 3.1.1), and what brings requests in (pages, prompts) and keeps their own sampling rules.
  *
  * Conventions for every entry point
  *   - Returns an hb_status; on failure hb_last_error() gives a thread-local message.
@@ -648,6 +648,116 @@ int32_t hb_kv4_evict(const hb_attn_desc *desc, int32_t budget, int32_t recent, i
                      int32_t *new_len_or_null, void *workspace, size_t workspace_bytes, void *stream);
 
 size_t hb_kv4_evict_workspace_bytes(const hb_attn_desc *desc, int32_t budget);
+
+/*
+ * ---- Requests: pages, prompts, sampling rules ----------------------------------------------------
+ * What comes before a request's first verification step (committed context lives in the KV cache, Section 4.1), and the
+ * request's own rules for the target's next token.
+ *
+ * hb_pages_take: table entries for requests that grow, from a list of free pages.  Sequence b has prefix_len[b] positions in
+ * pages[b] pages (entries 0 .. pages[b] - 1 of its row of block_table) and gets n = row_offset[b+1] - row_offset[b] new rows;
+ * it wants w = ceil((prefix_len[b] + n + reserve) / page_size) pages.  In the order of the batch, sequences that need more
+ * pages get them, all or none, until the first that is not served; after that only those get their way that need no page.  One
+ * that wants more than max_blocks_per_seq is not served and stands in nobody's way.  For one that is served: granted[b] = 1,
+ * pages_out[b] = max(w, pages[b]), new_len[b] = prefix_len[b] + n, the new entries are written, and slots[row_offset[b] + j] =
+ * block_table[b][p / page_size] * page_size + p % page_size for p = prefix_len[b] + j (-1 where that entry is no page).  For one
+ * that is not: granted[b] = 0, pages_out[b] = pages[b], new_len[b] = prefix_len[b], slots -1.  Pages are taken from the end of
+ * the list: the c-th of the call is free_pages[free_count - 1 - c]; free_left = free_count - their number.
+ *   prefix_len, pages, new_len, pages_out, granted  device int32 [B]     row_offset  device int32 [B+1]
+ *   block_table  device int32 [B, max_blocks_per_seq]                    slots       device int32 [n_rows]
+ *   free_pages   device int32 [num_blocks], free_count, free_left  device int32 [1]
+ * slots, new_len and granted may be NULL.  Rows behind the last sequence and all other entries stay as they are.
+ * hb_pages_give: the pages behind a sequence's first keep_len[b] positions go back: entries ceil(keep_len[b] / page_size) to
+ * pages[b] - 1, the c-th of m in all to free_pages[free_count + m - 1 - c], so that giving what was just taken restores the
+ * list; pages_out[b] = the pages it keeps, free_now = free_count + m.  keep_len 0: all of them.  block_table is not written.
+ * What the calls write must not overlap what they read, nor each other (pages_out is not pages): a copy behind the call
+ * advances them.
+ * Errors: INVALID_ARG, UNSUPPORTED (B > 8192, page table or slots beyond 2^30 and 2^31), DEVICE.  B == 0 is a no-op.
+ */
+int32_t hb_pages_take(int32_t B, int32_t page_size, int32_t max_blocks_per_seq, int32_t num_blocks, int32_t n_rows, int32_t reserve,
+                      const int32_t *prefix_len, const int32_t *row_offset, const int32_t *pages, const int32_t *free_pages,
+                      const int32_t *free_count, int32_t *block_table, int32_t *slots_or_null, int32_t *new_len_or_null,
+                      int32_t *pages_out, int32_t *granted_or_null, int32_t *free_left, void *stream);
+
+int32_t hb_pages_give(int32_t B, int32_t page_size, int32_t max_blocks_per_seq, int32_t num_blocks, const int32_t *keep_len,
+                      const int32_t *pages, const int32_t *block_table, int32_t *free_pages, const int32_t *free_count,
+                      int32_t *pages_out, int32_t *free_now, void *stream);
+
+/*
+ * Rows of K and V (a prompt's, or any) bit for bit to their slots: row r to pool[slots[r] / page_size][:][slots[r] % page_size][:].
+ * A slot outside [0, num_blocks * page_size) has no place and its row is skipped; of two rows with the same slot one wins.
+ *   k_rows, v_rows  device [n_rows, Hkv, D]     slots  device int32 [n_rows]     pools as in hb_tree_verify_attn
+ * Uses desc->{dtype, num_kv_heads, head_dim, page_size, num_blocks}.  Errors: INVALID_ARG, UNSUPPORTED, DEVICE.
+ */
+int32_t hb_kv_append(const hb_attn_desc *desc, int32_t n_rows, const void *k_rows, const void *v_rows, const int32_t *slots, void *k_pool,
+                     void *v_pool, void *stream);
+
+/*
+ * Attention of prompts, whole or in parts, packed one behind the other: row i of sequence b (row_offset[b] + i of the batch)
+ * sees prefix positions 0 .. prefix_len[b] - 1 of the paged cache and the rows 0 .. i of its own sequence.
+ *   out, lse, softmax_scale, heads, pools and block_table as in hb_tree_verify_attn, with rows for nodes:
+ *   q, out          device [total_nodes, Hq, D]      k_rows, v_rows  device [total_nodes, Hkv, D]      desc->dtype
+ *   prefix_len      device int32 [B], or NULL: no sequence has anything cached (pools and block_table may be NULL then)
+ *   row_offset      device int32 [B+1]; sequences may be empty.  Rows behind the last one stay as they are.
+ *   workspace       device, hb_prompt_attn_workspace_bytes(desc) bytes, 256-byte aligned; may be NULL when that size is 0
+ * max_nodes_per_tree is not read.  num_splits is the most parts that a row's keys are cut into (0: the library's choice, from
+ * the lengths); max_prefix_len_hint sizes workspace and launch and no more: a longer prefix is taken whole.
+ * What a row does not see has no influence on it, whatever bits it holds: later rows, slots behind the prefix, other sequences.
+ * Accumulation is float32; on the matrix cores in bf16 a softmax weight is rounded to bf16 for its product with a value (by 2^-8
+ * of itself at most), the sum that it is divided by is not.  bf16 results are rounded once at the end.
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype, D; total_nodes * Hq beyond 2^30; HB_ATTN_MFMA on a shape it cannot take),
+ * WORKSPACE, DEVICE.  batch == 0 or total_nodes == 0 is a successful no-op.
+ */
+int32_t hb_prompt_attn(const hb_attn_desc *desc, const void *q, const void *k_rows, const void *v_rows, const void *k_pool_or_null,
+                       const void *v_pool_or_null, const int32_t *block_table_or_null, const int32_t *prefix_len_or_null,
+                       const int32_t *row_offset, void *out, float *lse_or_null, void *workspace, size_t workspace_bytes, void *stream);
+
+size_t hb_prompt_attn_workspace_bytes(const hb_attn_desc *desc);
+
+/*
+ * A request's sampling rules, applied to the target's (or the draft's) logits after each node of its tree.
+ *   c      how often the request's output holds the token: counts, and the drafted tokens on the node's path below the root
+ *          (the root is the pending committed token, which counts holds already)
+ *   z      = logit; if c > 0 or the token is in the prompt: z / repetition where z > 0, z * repetition elsewhere
+ *   z      = z - (presence * [c > 0] + frequency * c) + bias;  -infinity where the mask forbids the token or z is no number
+ * in float32, operation by operation as written.
+ * hb_rules_logits: out = z, in the type of the logits (which out may be).
+ * hb_rules_probs:  probs = exp((z - max z) / temperature) / sum, what hb_tree_accept_sample takes; temperature 0 (or less, or
+ *   no number): 1 at the largest z, the lowest token among equals, which makes that call's rule the greedy one.  Infinite z
+ *   share the whole.  A row that the rules leave nothing of is zero.
+ * hb_rules_count: tokens into counts: each adds 1 to its sequence's entry, or with prompt = 1 marks it as one of the prompt's
+ *   (2^30).  Tokens outside [0, V) are skipped, so out_tokens of an acceptance is counted as it is.
+ *
+ *   logits       device [T, V]  dtype             out  device [T, V]  dtype        probs  device float32 [T, V]
+ *   node_offset  device int32 [B+1], or NULL: T == B, row b is sequence b's.  Rows that no sequence has are not written.
+ *   parent, draft_ids  device int32 [T], both or neither (NULL: no path counts); trees of at most max_nodes_per_tree <= 64 nodes
+ *   counts       device int32 [B, V], or NULL: none        rules  device float32 [B, 4]: temperature, repetition, presence,
+ *                                                                 frequency; or NULL: 1, 1, 0, 0
+ *   bias_offset  device int32 [B+1], bias_id device int32 [n_bias], bias_value device float32 [n_bias]: sequence b's biases are
+ *                bias_offset[b] .. bias_offset[b+1] - 1; a token given twice has both, added in their order.  n_bias 0: none
+ *   mask         device uint32 [num_masks, ceil(V / 32)], bit v % 32 of word v / 32: the token is allowed; or NULL
+ *   mask_row     device int32 [T]: the mask of each row, outside [0, num_masks): none; or NULL: row t's is mask t
+ *   workspace    device, hb_rules_probs_workspace_bytes(T, V) bytes, 16-byte aligned, overwritten
+ *   tokens       device int32 [n]; row_offset device int32 [B+1], or NULL: n / B of every sequence (out_tokens [B, max_path])
+ * logits, out, probs, counts, rules and mask are 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED (dtype,
+ * max_nodes_per_tree > 64, V > 2^30), WORKSPACE, DEVICE.  T == 0 or B == 0 is a no-op.
+ */
+int32_t hb_rules_count(int32_t B, int32_t V, int32_t n, const int32_t *row_offset_or_null, const int32_t *tokens, int32_t prompt,
+                       int32_t *counts, void *stream);
+
+int32_t hb_rules_logits(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, int32_t T, int32_t V, const void *logits,
+                        const int32_t *node_offset_or_null, const int32_t *parent_or_null, const int32_t *draft_ids_or_null,
+                        const int32_t *counts_or_null, const float *rules_or_null, const int32_t *bias_offset, int32_t n_bias,
+                        const int32_t *bias_id, const float *bias_value, int32_t num_masks, const uint32_t *mask_or_null,
+                        const int32_t *mask_row_or_null, void *out, void *stream);
+
+int32_t hb_rules_probs(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, int32_t T, int32_t V, const void *logits,
+                       const int32_t *node_offset_or_null, const int32_t *parent_or_null, const int32_t *draft_ids_or_null,
+                       const int32_t *counts_or_null, const float *rules_or_null, const int32_t *bias_offset, int32_t n_bias,
+                       const int32_t *bias_id, const float *bias_value, int32_t num_masks, const uint32_t *mask_or_null,
+                       const int32_t *mask_row_or_null, float *probs, void *workspace, size_t workspace_bytes, void *stream);
+
+size_t hb_rules_probs_workspace_bytes(int32_t T, int32_t V);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,7 @@ target's own greedy stream):
   draft_tree.topk_logprob_ref / DraftTreeRef / build_draft_tree_ref   the draft tree's construction
   meta_query.meta_query_attn_ref / fc_concat_ref   the draft's intermediate layer (Section 3.1.1, Eq. 1)
   kv4.kv4_quantise_ref / kv4_values_ref / kv4_append_ref / kv4_attn_weight_ref / kv4_evict_ref   the cache held in 4 bits
+  requests.pages_take_ref / pages_give_ref / prompt_attn_ref / rules_logits_ref / rules_probs_ref   requests: pages, prompts, sampling rules
   toy_decoder.ToyDecoderRef        small random-weight decoder: greedy autoregressive stream and
                                    greedy speculative decoding built from the four functions above
 
@@ -38,6 +39,7 @@ from .stochastic_acceptance import tree_accept_sample_ref
 from .draft_tree import topk_logprob_ref, DraftTreeRef, build_draft_tree_ref
 from .meta_query import meta_query_attn_ref, fc_concat_ref
 from .kv4 import kv4_quantise_ref, kv4_values_ref, kv4_append_ref, kv4_attn_weight_ref, kv4_evict_ref
+from .requests import pages_take_ref, pages_give_ref, prompt_attn_ref, rules_logits_ref, rules_probs_ref
 from .projections import tree_positions_ref, rope_ref, qkv_rope_project_ref, linear_ref, rmsnorm_ref, swiglu_ref
 
 __all__ = [
@@ -65,4 +67,9 @@ __all__ = [
     "kv4_append_ref",
     "kv4_attn_weight_ref",
     "kv4_evict_ref",
+    "pages_take_ref",
+    "pages_give_ref",
+    "prompt_attn_ref",
+    "rules_logits_ref",
+    "rules_probs_ref",
 ]

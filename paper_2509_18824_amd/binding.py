@@ -145,6 +145,25 @@ def _load():
     lib.hb_kv4_evict.argtypes = [C.POINTER(AttnDesc), i32, i32, i32] + [p] * 14 + [sz, p]
     lib.hb_kv4_evict_workspace_bytes.restype = sz
     lib.hb_kv4_evict_workspace_bytes.argtypes = [C.POINTER(AttnDesc), i32]
+    lib.hb_pages_take.restype = i32
+    lib.hb_pages_take.argtypes = [i32] * 6 + [p] * 11 + [p]
+    lib.hb_pages_give.restype = i32
+    lib.hb_pages_give.argtypes = [i32] * 4 + [p] * 7 + [p]
+    lib.hb_kv_append.restype = i32
+    lib.hb_kv_append.argtypes = [C.POINTER(AttnDesc), i32] + [p] * 5 + [p]
+    lib.hb_prompt_attn.restype = i32
+    lib.hb_prompt_attn.argtypes = [C.POINTER(AttnDesc)] + [p] * 10 + [p, sz, p]
+    lib.hb_prompt_attn_workspace_bytes.restype = sz
+    lib.hb_prompt_attn_workspace_bytes.argtypes = [C.POINTER(AttnDesc)]
+    lib.hb_rules_count.restype = i32
+    lib.hb_rules_count.argtypes = [i32] * 3 + [p, p, i32, p, p]
+    rules = [i32] * 5 + [p] * 7 + [i32, p, p, i32, p, p]
+    lib.hb_rules_logits.restype = i32
+    lib.hb_rules_logits.argtypes = rules + [p, p]
+    lib.hb_rules_probs.restype = i32
+    lib.hb_rules_probs.argtypes = rules + [p, p, sz, p]
+    lib.hb_rules_probs_workspace_bytes.restype = sz
+    lib.hb_rules_probs_workspace_bytes.argtypes = [i32, i32]
     return lib
 
 
@@ -647,3 +666,98 @@ def hb_kv4_evict(desc: AttnDesc, budget: int, recent: int, sinks: int, k_codes, 
                             _ints(block_table, B * desc.max_blocks_per_seq), _ints(prefix_len, B), _ints(seq_len, B), _ptr(weight),
                             _ptr(pos), _ptr(weight_out), _ptr(pos_out), _ints(kept, 0), _ints(new_len, B), _ptr(workspace), ws_bytes,
                             _stream(stream)))
+
+
+def hb_pages_take(page_size: int, reserve: int, prefix_len, row_offset, pages, free_pages, free_count, block_table, slots, new_len,
+                  pages_out, granted, free_left, stream=None) -> None:
+    """``block_table`` [B, max_blocks]; ``free_pages`` [num_blocks]; ``slots`` [n_rows], or None."""
+    B, max_blocks = block_table.shape
+    n_rows = slots.numel() if slots is not None else 2 ** 31 - 1  # without slots, offsets are not bounded by them
+    _check(lib.hb_pages_take(B, page_size, max_blocks, free_pages.numel(), n_rows, reserve, _ints(prefix_len, B), _ints(row_offset, B + 1),
+                             _ints(pages, B), _ints(free_pages, 0), _ints(free_count, 1), _ints(block_table, 0), _ints(slots, 0),
+                             _ints(new_len, B), _ints(pages_out, B), _ints(granted, B), _ints(free_left, 1), _stream(stream)))
+
+
+def hb_pages_give(page_size: int, keep_len, pages, block_table, free_pages, free_count, pages_out, free_now, stream=None) -> None:
+    B, max_blocks = block_table.shape
+    _check(lib.hb_pages_give(B, page_size, max_blocks, free_pages.numel(), _ints(keep_len, B), _ints(pages, B), _ints(block_table, 0),
+                             _ints(free_pages, 0), _ints(free_count, 1), _ints(pages_out, B), _ints(free_now, 1), _stream(stream)))
+
+
+def _pool(desc: AttnDesc, k_pool, v_pool) -> None:
+    n = desc.num_blocks * desc.num_kv_heads * desc.page_size * desc.head_dim
+    if k_pool.numel() != n or v_pool.numel() != n or not _of_desc(desc, k_pool) or v_pool.dtype is not k_pool.dtype:
+        raise ValueError("pools must be [num_blocks, Hkv, page, D] in the descriptor's dtype")
+
+
+def hb_kv_append(desc: AttnDesc, k_rows, v_rows, slots, k_pool, v_pool, stream=None) -> None:
+    n = _kv4_rows(desc, k_rows, v_rows)
+    _pool(desc, k_pool, v_pool)
+    _check(lib.hb_kv_append(C.byref(desc), n, _ptr(k_rows), _ptr(v_rows), _ints(slots, n), _ptr(k_pool), _ptr(v_pool), _stream(stream)))
+
+
+def hb_prompt_attn_workspace_bytes(desc: AttnDesc) -> int:
+    return int(lib.hb_prompt_attn_workspace_bytes(C.byref(desc)))
+
+
+def hb_prompt_attn(desc: AttnDesc, q, k_rows, v_rows, k_pool, v_pool, block_table, prefix_len, row_offset, out, lse=None, workspace=None,
+                   stream=None) -> None:
+    """``prefix_len`` None: nothing is cached, and pools and table may be None too."""
+    rows = desc.total_nodes * desc.num_q_heads
+    if q.numel() < rows * desc.head_dim or out.numel() < rows * desc.head_dim or not _of_desc(desc, q) or out.dtype is not q.dtype:
+        raise ValueError("q and out must be [total_nodes, Hq, D] in the descriptor's dtype")
+    if _kv4_rows(desc, k_rows, v_rows) < desc.total_nodes or lse is not None and (lse.numel() < rows or lse.dtype is not _f32):
+        raise ValueError("k_rows and v_rows must be [total_nodes, Hkv, D], lse float32 [total_nodes, Hq]")
+    if prefix_len is not None:
+        _pool(desc, k_pool, v_pool)
+    ws_bytes = workspace.nbytes if workspace is not None else 0
+    B = desc.batch
+    _check(lib.hb_prompt_attn(C.byref(desc), _ptr(q), _ptr(k_rows), _ptr(v_rows), _ptr(k_pool), _ptr(v_pool),
+                              _ints(block_table, B * desc.max_blocks_per_seq), _ints(prefix_len, B), _ints(row_offset, B + 1), _ptr(out),
+                              _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def hb_rules_count(tokens, counts, row_offset=None, prompt: bool = False, stream=None) -> None:
+    """``counts`` int32 [B, V]; ``tokens`` int32, as many of every sequence unless ``row_offset`` says otherwise."""
+    B, V = counts.shape
+    _check(lib.hb_rules_count(B, V, tokens.numel(), _ints(row_offset, B + 1), _ints(tokens, 0), int(prompt), _ints(counts, 0),
+                              _stream(stream)))
+
+
+def _rules(logits, max_nodes_per_tree, node_offset, parent, draft_ids, counts, rules, bias_offset, bias_id, bias_value, mask, mask_row):
+    T, V = logits.shape
+    B = node_offset.numel() - 1 if node_offset is not None else T
+    if rules is not None and (rules.dtype is not _f32 or rules.numel() != B * 4):
+        raise ValueError("rules must be float32 [B, 4]")
+    n_bias = bias_id.numel() if bias_id is not None else 0
+    if n_bias and (bias_value.dtype is not _f32 or bias_value.numel() != n_bias):
+        raise ValueError("bias_value must be float32, one for each bias_id")
+    masks = 0
+    if mask is not None:
+        masks, words = mask.shape
+        if mask.element_size() != 4 or words != (V + 31) // 32:
+            raise ValueError("mask must be 32-bit words [num_masks, ceil(V / 32)]")
+    return (_dtype_code(logits), B, max_nodes_per_tree, T, V, _ptr(logits), _ints(node_offset, B + 1), _ints(parent, T), _ints(draft_ids, T),
+            _ints(counts, B * V), _ptr(rules), _ints(bias_offset, B + 1), n_bias, _ints(bias_id, 0), _ptr(bias_value), masks, _ptr(mask),
+            _ints(mask_row, T))
+
+
+def hb_rules_logits(logits, max_nodes_per_tree: int, node_offset, parent, draft_ids, counts, rules, bias_offset, bias_id, bias_value, mask,
+                    mask_row, out, stream=None) -> None:
+    if out.shape != logits.shape or out.dtype is not logits.dtype:
+        raise ValueError("out must be [T, V] in the dtype of the logits")
+    _check(lib.hb_rules_logits(*_rules(logits, max_nodes_per_tree, node_offset, parent, draft_ids, counts, rules, bias_offset, bias_id,
+                                       bias_value, mask, mask_row), _ptr(out), _stream(stream)))
+
+
+def hb_rules_probs_workspace_bytes(T: int, V: int) -> int:
+    return int(lib.hb_rules_probs_workspace_bytes(T, V))
+
+
+def hb_rules_probs(logits, max_nodes_per_tree: int, node_offset, parent, draft_ids, counts, rules, bias_offset, bias_id, bias_value, mask,
+                   mask_row, probs, workspace, stream=None) -> None:
+    if probs.shape != logits.shape or probs.dtype is not _f32:
+        raise ValueError("probs must be float32 [T, V]")
+    ws_bytes = workspace.nbytes if workspace is not None else 0
+    _check(lib.hb_rules_probs(*_rules(logits, max_nodes_per_tree, node_offset, parent, draft_ids, counts, rules, bias_offset, bias_id,
+                                      bias_value, mask, mask_row), _ptr(probs), _ptr(workspace), ws_bytes, _stream(stream)))

@@ -65,9 +65,9 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
 
 def build_host_sanitizer_check(driver_c: str) -> str:
     """Builds a host program from `driver_c` and the library's objects, with the host code of
-    csrc/hb_api.hip and csrc/kv4_api.hip (validation, planning, error text) compiled under AddressSanitizer
+    csrc/hb_api.hip, csrc/kv4_api.hip and csrc/requests_api.hip (validation, planning, error text) compiled under AddressSanitizer
     and UndefinedBehaviorSanitizer (device code is not instrumented).  Returns the executable."""
-    api = ("hb_api.hip", "kv4_api.hip")
+    api = ("hb_api.hip", "kv4_api.hip", "requests_api.hip")
     out_dir = os.path.join(BUILD, "san")
     os.makedirs(out_dir, exist_ok=True)
     others = [os.path.join(BUILD, s.replace(".hip", ".o")) for s in sources() if s not in api]

@@ -1,0 +1,277 @@
+// Host side of the calls that bring requests in and apply their sampling rules: argument validation, plans, dispatch.
+#include <initializer_list>
+
+#include "pages.h"
+#include "prompt.h"
+#include "rules.h"
+
+namespace hb {
+
+static size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+static bool misaligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+
+// What a call writes while other workgroups read, or write something else
+struct Span {
+  const void *at;
+  int64_t bytes;
+};
+static int32_t check_apart(const char *name, Span out, std::initializer_list<Span> in) {
+  for (const Span &x : in) {
+    const uintptr_t o = (uintptr_t)out.at, i = (uintptr_t)x.at;
+    if (o && i && out.bytes > 0 && x.bytes > 0 && o < i + (uint64_t)x.bytes && i < o + (uint64_t)out.bytes)
+      return fail(HB_ERR_INVALID_ARG, "%s must not overlap another argument of the call", name);
+  }
+  return HB_OK;
+}
+
+static int32_t check_pages(int32_t B, int32_t page_size, int32_t max_blocks, int32_t num_blocks) {
+  if (B < 0) return fail(HB_ERR_INVALID_ARG, "negative batch");
+  if (page_size <= 0 || max_blocks <= 0 || num_blocks <= 0)
+    return fail(HB_ERR_INVALID_ARG, "page_size, max_blocks_per_seq and num_blocks must be positive");
+  if (B > 8192) return fail(HB_ERR_UNSUPPORTED, "batch %d: at most 8192", B);
+  if ((int64_t)page_size * max_blocks > (int64_t)1 << 30)
+    return fail(HB_ERR_UNSUPPORTED, "page table covers more than 2^30 positions");
+  if ((int64_t)page_size * num_blocks > INT32_MAX)
+    return fail(HB_ERR_UNSUPPORTED, "%d pages of %d: slots are 32-bit numbers", num_blocks, page_size);
+  return HB_OK;
+}
+
+// the descriptor as calls without trees read it
+static int32_t check_rows_desc(const hb_attn_desc *desc) {
+  if (!desc) return fail(HB_ERR_INVALID_ARG, "desc is NULL");
+  hb_attn_desc d = *desc;
+  d.max_nodes_per_tree = 1;
+  int32_t rc = check_attn_desc(&d);
+  if (rc) return rc;
+  if (d.num_kv_heads > 65535) return fail(HB_ERR_UNSUPPORTED, "num_kv_heads %d: at most 65535", d.num_kv_heads);
+  return HB_OK;
+}
+
+struct PromptPlan {
+  bool mfma;
+  int32_t rows;  // of a tile
+  int32_t tiles, parts, units;
+  size_t ml_offset, bytes;
+};
+
+static int32_t make_prompt_plan(const hb_attn_desc *d, PromptPlan *p) {
+  int32_t rc = check_rows_desc(d);
+  if (rc) return rc;
+  if ((int64_t)d->total_nodes * d->num_q_heads > 1 << 30)
+    return fail(HB_ERR_UNSUPPORTED, "total_nodes * num_q_heads %lld: at most 2^30", (long long)d->total_nodes * d->num_q_heads);
+  const bool can = prompt_mfma_supports(*d);
+  if (d->algo == HB_ATTN_MFMA && !can)
+    return fail(HB_ERR_UNSUPPORTED, "HB_ATTN_MFMA for prompts needs bf16, head_dim 64 or 128, page_size a power of two and a positive "
+                "softmax_scale");
+  p->mfma = can && d->algo != HB_ATTN_SCALAR;
+  const int64_t G = d->num_q_heads / d->num_kv_heads;
+  int64_t span = (int64_t)d->page_size * d->max_blocks_per_seq;
+  if (d->max_prefix_len_hint > 0 && d->max_prefix_len_hint < span) span = d->max_prefix_len_hint;
+  span += d->total_nodes;
+  p->rows = kPromptAnyRows;
+  p->units = 1024;
+  const int64_t least = 128;  // keys of a part
+  const int64_t tiles = d->total_nodes * G / p->rows + (d->batch < d->total_nodes ? d->batch : d->total_nodes);
+  p->tiles = (int32_t)tiles;
+  int64_t parts = d->num_splits;
+  if (parts == 0) parts = tiles > 0 ? 2 * p->units / (tiles * d->num_kv_heads) : 1;
+  if (parts > (span + least - 1) / least) parts = (span + least - 1) / least;
+  if (parts > 256) parts = 256;
+  if (parts < 1) parts = 1;
+  p->parts = (int32_t)parts;
+  p->ml_offset = p->bytes = 0;
+  if (parts > 1) {
+    const size_t slots = (size_t)tiles * d->num_kv_heads * parts * p->rows;
+    p->ml_offset = round_up(slots * d->head_dim * sizeof(float), 256);
+    p->bytes = p->ml_offset + round_up(slots * 2 * sizeof(float), 256);
+  }
+  return HB_OK;
+}
+
+struct RulesCall {
+  const int32_t *node_offset, *parent, *draft_ids, *counts;
+  const float *rules;
+  const int32_t *bias_offset;
+  int32_t n_bias;
+  const int32_t *bias_id;
+  const float *bias_value;
+  int32_t num_masks;
+  const uint32_t *mask;
+  const int32_t *mask_row;
+};
+
+static int32_t check_rules(int32_t dtype, int32_t B, int32_t max_nodes, int32_t T, int32_t V, const void *logits, const RulesCall &r,
+                           const void *out, RulesArgs *a) {
+  if (dtype != HB_F32 && dtype != HB_BF16) return fail(HB_ERR_UNSUPPORTED, "dtype %d: only HB_F32 and HB_BF16 are supported", dtype);
+  if (B < 0 || T < 0 || V <= 0 || max_nodes <= 0 || r.n_bias < 0 || r.num_masks < 0)
+    return fail(HB_ERR_INVALID_ARG, "batch, rows, biases and masks must not be negative, V and max_nodes_per_tree positive");
+  if (max_nodes > 64) return fail(HB_ERR_UNSUPPORTED, "max_nodes_per_tree %d: trees of more than 64 nodes are not supported", max_nodes);
+  if (V > 1 << 30) return fail(HB_ERR_UNSUPPORTED, "V %d: at most 2^30", V);
+  if (T == 0 || B == 0) return HB_OK;
+  if (!logits || !out) return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
+  if (!r.node_offset && T != B) return fail(HB_ERR_INVALID_ARG, "without node_offset every sequence has one row: %d of %d", T, B);
+  if (!r.parent != !r.draft_ids || (r.parent && !r.node_offset))
+    return fail(HB_ERR_INVALID_ARG, "node_offset, parent and draft_ids come together");
+  if (r.n_bias > 0 && (!r.bias_offset || !r.bias_id || !r.bias_value))
+    return fail(HB_ERR_INVALID_ARG, "bias_offset, bias_id and bias_value come together");
+  if (!r.mask && r.mask_row) return fail(HB_ERR_INVALID_ARG, "mask_row without masks");
+  if (r.mask && !r.mask_row && r.num_masks < T) return fail(HB_ERR_INVALID_ARG, "without mask_row there is a mask for every row");
+  if (misaligned(logits, 16) || misaligned(out, 16) || misaligned(r.counts, 16) || misaligned(r.rules, 16) || misaligned(r.mask, 16))
+    return fail(HB_ERR_INVALID_ARG, "logits, out, counts, rules and masks must be 16-byte aligned");
+  *a = {dtype, B, max_nodes, T, V, r.n_bias, r.num_masks, logits, r.node_offset, r.parent, r.draft_ids, r.counts, r.rules,
+        r.n_bias > 0 ? r.bias_offset : nullptr, r.bias_id, r.bias_value, r.mask, r.mask_row, (void *)out, nullptr, 0, 0};
+  return HB_OK;
+}
+
+}  // namespace hb
+
+using namespace hb;
+
+extern "C" {
+
+int32_t hb_pages_take(int32_t B, int32_t page_size, int32_t max_blocks_per_seq, int32_t num_blocks, int32_t n_rows, int32_t reserve,
+                      const int32_t *prefix_len, const int32_t *row_offset, const int32_t *pages, const int32_t *free_pages,
+                      const int32_t *free_count, int32_t *block_table, int32_t *slots, int32_t *new_len, int32_t *pages_out,
+                      int32_t *granted, int32_t *free_left, void *stream) {
+  int32_t rc = check_pages(B, page_size, max_blocks_per_seq, num_blocks);
+  if (rc) return rc;
+  if (n_rows < 0 || reserve < 0) return fail(HB_ERR_INVALID_ARG, "n_rows and reserve must not be negative");
+  if (B == 0) return HB_OK;
+  if (!prefix_len || !row_offset || !pages || !free_pages || !free_count || !block_table || !pages_out || !free_left)
+    return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
+  const Span table = {block_table, (int64_t)B * max_blocks_per_seq * 4}, s = {slots, (int64_t)n_rows * 4}, len = {new_len, (int64_t)B * 4},
+             have = {pages_out, (int64_t)B * 4}, ok = {granted, (int64_t)B * 4}, left = {free_left, 4};
+  const Span in[] = {{prefix_len, (int64_t)B * 4}, {row_offset, (int64_t)B * 4 + 4}, {pages, (int64_t)B * 4},
+                     {free_pages, (int64_t)num_blocks * 4}, {free_count, 4}};
+  const Span out[] = {table, s, len, have, ok, left};
+  static const char *const names[] = {"block_table", "slots", "new_len", "pages_out", "granted", "free_left"};
+  for (int i = 0; i < 6; ++i) {
+    if ((rc = check_apart(names[i], out[i], {in[0], in[1], in[2], in[3], in[4]}))) return rc;
+    for (int k = 0; k < i; ++k)
+      if ((rc = check_apart(names[i], out[i], {out[k]}))) return rc;
+  }
+  PagesArgs a = {B, page_size, max_blocks_per_seq, num_blocks, n_rows, reserve, prefix_len, row_offset, pages, free_pages, free_count,
+                 block_table, nullptr, n_rows ? slots : nullptr, new_len, pages_out, granted, free_left};
+  HB_HIP_TRY(launch_pages_take(a, (hipStream_t)stream));
+  return HB_OK;
+}
+
+int32_t hb_pages_give(int32_t B, int32_t page_size, int32_t max_blocks_per_seq, int32_t num_blocks, const int32_t *keep_len,
+                      const int32_t *pages, const int32_t *block_table, int32_t *free_pages, const int32_t *free_count,
+                      int32_t *pages_out, int32_t *free_now, void *stream) {
+  int32_t rc = check_pages(B, page_size, max_blocks_per_seq, num_blocks);
+  if (rc) return rc;
+  if (B == 0) return HB_OK;
+  if (!keep_len || !pages || !free_pages || !free_count || !block_table || !pages_out || !free_now)
+    return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
+  const Span in[] = {{keep_len, (int64_t)B * 4}, {pages, (int64_t)B * 4}, {block_table, (int64_t)B * max_blocks_per_seq * 4}, {free_count, 4}};
+  const Span out[] = {{free_pages, (int64_t)num_blocks * 4}, {pages_out, (int64_t)B * 4}, {free_now, 4}};
+  static const char *const names[] = {"free_pages", "pages_out", "free_now"};
+  for (int i = 0; i < 3; ++i) {
+    if ((rc = check_apart(names[i], out[i], {in[0], in[1], in[2], in[3]}))) return rc;
+    for (int k = 0; k < i; ++k)
+      if ((rc = check_apart(names[i], out[i], {out[k]}))) return rc;
+  }
+  PagesArgs a = {B, page_size, max_blocks_per_seq, num_blocks, 0, 0, keep_len, nullptr, pages, nullptr, free_count,
+                 (int32_t *)block_table, free_pages, nullptr, nullptr, pages_out, nullptr, free_now};
+  HB_HIP_TRY(launch_pages_give(a, (hipStream_t)stream));
+  return HB_OK;
+}
+
+int32_t hb_kv_append(const hb_attn_desc *desc, int32_t n_rows, const void *k_rows, const void *v_rows, const int32_t *slots, void *k_pool,
+                     void *v_pool, void *stream) {
+  int32_t rc = check_rows_desc(desc);
+  if (rc) return rc;
+  if (n_rows < 0) return fail(HB_ERR_INVALID_ARG, "negative n_rows");
+  if ((int64_t)desc->page_size * desc->num_blocks > INT32_MAX)
+    return fail(HB_ERR_UNSUPPORTED, "%d pages of %d: slots are 32-bit numbers", desc->num_blocks, desc->page_size);
+  if (n_rows == 0) return HB_OK;
+  if (!k_rows || !v_rows || !slots || !k_pool || !v_pool) return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
+  if (misaligned(k_rows, 16) || misaligned(v_rows, 16) || misaligned(k_pool, 16) || misaligned(v_pool, 16))
+    return fail(HB_ERR_INVALID_ARG, "rows and pools must be 16-byte aligned");
+  HB_HIP_TRY(launch_kv_append(*desc, n_rows, k_rows, v_rows, slots, k_pool, v_pool, (hipStream_t)stream));
+  return HB_OK;
+}
+
+size_t hb_prompt_attn_workspace_bytes(const hb_attn_desc *desc) {
+  PromptPlan p;
+  return make_prompt_plan(desc, &p) ? 0 : p.bytes;
+}
+
+int32_t hb_prompt_attn(const hb_attn_desc *desc, const void *q, const void *k_rows, const void *v_rows, const void *k_pool,
+                       const void *v_pool, const int32_t *block_table, const int32_t *prefix_len, const int32_t *row_offset, void *out,
+                       float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+  PromptPlan p;
+  int32_t rc = make_prompt_plan(desc, &p);
+  if (rc) return rc;
+  if (desc->batch == 0 || desc->total_nodes == 0) return HB_OK;
+  if (!q || !k_rows || !v_rows || !row_offset || !out) return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
+  if (prefix_len && (!k_pool || !v_pool || !block_table))
+    return fail(HB_ERR_INVALID_ARG, "prefix_len without pools and block_table");
+  if (misaligned(q, 16) || misaligned(k_rows, 16) || misaligned(v_rows, 16) || misaligned(k_pool, 16) || misaligned(v_pool, 16) ||
+      misaligned(out, 16))
+    return fail(HB_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
+  if (p.bytes) {
+    if (!workspace || workspace_bytes < p.bytes)
+      return fail(HB_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", p.bytes, workspace ? workspace_bytes : (size_t)0);
+    if (misaligned(workspace, 256)) return fail(HB_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  }
+  PromptArgs a = {*desc, q, k_rows, v_rows, k_pool, v_pool, block_table, prefix_len, row_offset, out, lse,
+                  p.bytes ? (float *)workspace : nullptr, p.bytes ? (float *)((char *)workspace + p.ml_offset) : nullptr, p.tiles,
+                  p.parts, p.units};
+  HB_HIP_TRY(launch_prompt_any(a, (hipStream_t)stream));
+  return HB_OK;
+}
+
+int32_t hb_rules_count(int32_t B, int32_t V, int32_t n, const int32_t *row_offset, const int32_t *tokens, int32_t prompt, int32_t *counts,
+                       void *stream) {
+  if (B < 0 || n < 0 || V <= 0) return fail(HB_ERR_INVALID_ARG, "batch and n must not be negative, V positive");
+  if (prompt != 0 && prompt != 1) return fail(HB_ERR_INVALID_ARG, "prompt must be 0 or 1");
+  if (B == 0 || n == 0) return HB_OK;
+  if (!tokens || !counts) return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
+  if (!row_offset && n % B) return fail(HB_ERR_INVALID_ARG, "without row_offset every sequence has as many tokens: %d of %d", n, B);
+  HB_HIP_TRY(launch_rules_count(B, V, n, row_offset, tokens, prompt, counts, (hipStream_t)stream));
+  return HB_OK;
+}
+
+int32_t hb_rules_logits(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, int32_t T, int32_t V, const void *logits,
+                        const int32_t *node_offset, const int32_t *parent, const int32_t *draft_ids, const int32_t *counts,
+                        const float *rules, const int32_t *bias_offset, int32_t n_bias, const int32_t *bias_id, const float *bias_value,
+                        int32_t num_masks, const uint32_t *mask, const int32_t *mask_row, void *out, void *stream) {
+  RulesArgs a;
+  int32_t rc = check_rules(dtype, B, max_nodes_per_tree, T, V, logits,
+                           {node_offset, parent, draft_ids, counts, rules, bias_offset, n_bias, bias_id, bias_value, num_masks, mask, mask_row},
+                           out, &a);
+  if (rc || T == 0 || B == 0) return rc;
+  HB_HIP_TRY(launch_rules_logits(a, (hipStream_t)stream));
+  return HB_OK;
+}
+
+size_t hb_rules_probs_workspace_bytes(int32_t T, int32_t V) {
+  if (T <= 0 || V <= 0 || V > 1 << 30) return 0;
+  int32_t chunk;
+  return (size_t)T * rules_parts(T, V, &chunk) * 16;
+}
+
+int32_t hb_rules_probs(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, int32_t T, int32_t V, const void *logits,
+                       const int32_t *node_offset, const int32_t *parent, const int32_t *draft_ids, const int32_t *counts,
+                       const float *rules, const int32_t *bias_offset, int32_t n_bias, const int32_t *bias_id, const float *bias_value,
+                       int32_t num_masks, const uint32_t *mask, const int32_t *mask_row, float *probs, void *workspace,
+                       size_t workspace_bytes, void *stream) {
+  RulesArgs a;
+  int32_t rc = check_rules(dtype, B, max_nodes_per_tree, T, V, logits,
+                           {node_offset, parent, draft_ids, counts, rules, bias_offset, n_bias, bias_id, bias_value, num_masks, mask, mask_row},
+                           probs, &a);
+  if (rc || T == 0 || B == 0) return rc;
+  const size_t need = hb_rules_probs_workspace_bytes(T, V);
+  if (!workspace || workspace_bytes < need)
+    return fail(HB_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
+  if (misaligned(workspace, 16)) return fail(HB_ERR_WORKSPACE, "workspace must be 16-byte aligned");
+  const int64_t el = dtype == HB_F32 ? 4 : 2;
+  if ((rc = check_apart("probs", {probs, (int64_t)T * V * 4}, {{logits, (int64_t)T * V * el}}))) return rc;
+  a.stats = (float *)workspace;
+  HB_HIP_TRY(launch_rules_probs(a, (hipStream_t)stream));
+  return HB_OK;
+}
+
+}  // extern "C"
