@@ -99,6 +99,10 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptArgs &a, int tile,
 }
 
 bool prompt_mfma_supports(const hb_attn_desc &d);
+int32_t prompt_mfma_rows(const hb_attn_desc &d);  // of a tile
+hipError_t launch_prompt_mfma(const PromptArgs &a, hipStream_t s);
+// for tiles of `rows` rows whose parts begin at multiples of `keys`
+hipError_t launch_prompt_join(const PromptArgs &a, int32_t rows, int32_t keys, hipStream_t s);
 constexpr int kPromptAnyRows = 64;
 hipError_t launch_prompt_any(const PromptArgs &a, hipStream_t s);
 

@@ -1,199 +1,23 @@
-// Attention of prompts for every shape and type (hb_prompt_attn): float32 throughout, on the float32 matrix instructions.
-// And the join of the parts that a tile's keys were cut into.
-//
-// One workgroup owns one tile of 64 rows (prompt.h) and one part of its keys; four wavefronts with sixteen rows each share
-// the keys, 32 at a time, widened to float32 in LDS.  As in the bf16 kernels the products are transposed, so that no score
-// crosses lanes between them:
-//   S^T = K Q^T     16x16x4: A = 16 keys x 4 of D, B = 4 of D x 16 rows
-//   O^T = V^T P^T   16x16x4: A = 16 of D x 4 keys, B = 4 keys x 16 rows
-// The accumulator of lane (j, g), j = lane % 16, g = lane / 16, holds row j's scores for keys 4g + r, r = 0..3: what the
-// r-th instruction of the second product wants in that lane when its four keys are r, 4 + r, 8 + r, 12 + r.
-// Softmax is online per row in base 2.  Rows of K and V are four floats apart from a multiple of 64 in LDS: no operand read
-// has a bank conflict.  A head dimension between the sizes built here is filled up with zeros.
-#include "prompt.h"
+// hb_prompt_attn's kernel for every shape (prompt_any.h), and the join of the parts that a tile's keys were cut into.
+#include "prompt_any.h"
 
 namespace hb {
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kKeys = 32;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-#define HB_NEG_INF (-__builtin_huge_valf())
-
-__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-
-__device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
-  const f32x4 lo = *(const f32x4 *)p, hi = *(const f32x4 *)(p + 4);
-  for (int i = 0; i < 4; ++i) {
-    x[i] = lo[i];
-    x[4 + i] = hi[i];
-  }
-}
-__device__ __forceinline__ void load8(const bf16_t *p, float (&x)[8]) {
-  const u32x4 w = *(const u32x4 *)p;
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void prompt_any_kernel(PromptArgs a) {
-  constexpr int BM = kPromptAnyRows, kRow = DP + 4, kTiles = DP / 16, kSteps = DP / 4, kPieces = DP / 8;
   extern __shared__ __attribute__((aligned(16))) float lds[];
-  float *lk = lds, *lv = lds + kKeys * kRow;
-  __shared__ int bad;  // a value of this tile's is left out, see below
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, j = lane & 15, kg = lane >> 4;
-  const int h = blockIdx.y, G = a.d.num_q_heads / a.d.num_kv_heads, D = a.d.head_dim, Hkv = a.d.num_kv_heads;
-  const PromptTile w = prompt_tile<BM, kKeys>(a, blockIdx.x, blockIdx.z);
+  const int h = blockIdx.y;
+  const PromptTile w = prompt_tile<kPromptAnyRows, kAnyKeys>(a, blockIdx.x, blockIdx.z);
   if (w.t < 0) return;
-
-  const int row = w.t * BM + wave * 16 + j;
-  const bool there = (int64_t)row < (int64_t)w.n * G;
-  const int token = there ? row / G : w.n - 1, head = there ? row - token * G : 0;
-  const size_t at = (size_t)(w.row0 + token) * a.d.num_q_heads + (size_t)h * G + head;
-  const int sees = w.P + token;  // the last key of this row
-  const int all_see = w.P + w.t * BM / G;  // ... and of the tile's first
-
-  float qf[kSteps];
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) qf[s] = there && 4 * s + kg < D ? load_f32((const T *)a.q + at * D + 4 * s + kg) : 0.f;
-  f32x4 o[kTiles];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-  float m = HB_NEG_INF, l = 0.f;
-  const float c1 = a.d.softmax_scale * kLog2e;
-
-  for (int k0 = w.begin; k0 < w.end; k0 += kKeys) {
-    __syncthreads();
-    if (tid == 0) bad = 0;
-    __syncthreads();
-    for (int i = tid; i < kKeys * kPieces; i += 256) {
-      const int key = i / kPieces, d0 = i % kPieces * 8, kk = k0 + key;
-      float x[8] = {}, y[8] = {};
-      if (kk < w.end && d0 < D) {
-        const T *ks, *vs;
-        size_t from;
-        if (kk < w.P) {
-          const int page = kk / a.d.page_size;
-          int id = a.block_table[(size_t)w.b * a.d.max_blocks_per_seq + page];
-          id = id < 0 ? 0 : id >= a.d.num_blocks ? a.d.num_blocks - 1 : id;
-          from = (((size_t)id * Hkv + h) * a.d.page_size + (kk - page * a.d.page_size)) * D;
-          ks = (const T *)a.k_pool;
-          vs = (const T *)a.v_pool;
-        } else {
-          from = ((size_t)(w.row0 + kk - w.P) * Hkv + h) * D;
-          ks = (const T *)a.k;
-          vs = (const T *)a.v;
-        }
-        load8(ks + from + d0, x);
-        load8(vs + from + d0, y);
-      }
-      // a key that some row does not see has weight 0 there, and 0 times a value that is not finite is none: such values
-      // are added below, to the rows that see them
-      if (kk > all_see) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (!(fabsf(y[e]) < __builtin_huge_valf())) {
-            y[e] = 0.f;
-            bad = 1;
-          }
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        lk[key * kRow + d0 + e] = x[e];
-        lv[key * kRow + d0 + e] = y[e];
-      }
-    }
-    __syncthreads();
-
-    f32x4 sc[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      sc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-        sc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(lk[(16 * t + j) * kRow + 4 * s + kg], qf[s], sc[t], 0, 0, 0);
-    }
-    // masked scores are replaced before anything is made of them
-    float top = HB_NEG_INF;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int kk = k0 + 16 * t + 4 * kg + r;
-        sc[t][r] = kk <= sees && kk < w.end ? sc[t][r] * c1 : HB_NEG_INF;
-        top = fmaxf(top, sc[t][r]);
-      }
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float next = fmaxf(m, top), ref = next == HB_NEG_INF ? 0.f : next;
-    const float alpha = m == next ? 1.f : exp2_of(m - ref);  // m may be -infinity: nothing so far
-    m = next;
-    l *= alpha;
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) o[t] *= alpha;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float p = exp2_of(sc[t][r] - ref);
-        l += p;
-        const float *vr = lv + (16 * t + 4 * kg + r) * kRow + j;
-#pragma unroll
-        for (int dt = 0; dt < kTiles; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[16 * dt], p, o[dt], 0, 0, 0);
-      }
-    if (bad) {  // every thread's: it is set in front of a barrier
-      const int last = min(min(sees, w.end - 1), k0 + kKeys - 1);
-      for (int kk = max(k0, all_see + 1); kk <= last; ++kk) {  // prompt rows: the prefix is seen by all
-        const T *vs = (const T *)a.v + ((size_t)(w.row0 + kk - w.P) * Hkv + h) * D;
-#pragma unroll
-        for (int dt = 0; dt < kTiles; ++dt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int d = 16 * dt + 4 * kg + r;
-            const float y = d < D ? load_f32(vs + d) : 0.f;
-            if (!(fabsf(y) < __builtin_huge_valf())) o[dt][r] += y;
-          }
-      }
-    }
-  }
-
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
-  if (!there) return;
-  if (w.parts == 1) {
-    const float inv = 1.f / l;
-#pragma unroll
-    for (int dt = 0; dt < kTiles; ++dt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int d = 16 * dt + 4 * kg + r;
-        if (d < D) store_f32((T *)a.out + at * D + d, o[dt][r] * inv);
-      }
-    if (a.lse && kg == 0) a.lse[at] = (m + log2f(l)) * kLn2;
-  } else {
-    const size_t slot = ((((size_t)blockIdx.x * Hkv + h) * a.parts + blockIdx.z) * BM + wave * 16 + j);
-#pragma unroll
-    for (int dt = 0; dt < kTiles; ++dt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int d = 16 * dt + 4 * kg + r;
-        if (d < D) a.part_o[slot * D + d] = o[dt][r];
-      }
-    if (kg == 0) {
-      a.part_ml[slot * 2] = m;
-      a.part_ml[slot * 2 + 1] = l;
-    }
-  }
+  prompt_any_rows<T, DP, 4>(a, w, h, w.t * kPromptAnyRows,
+                            (((size_t)blockIdx.x * a.d.num_kv_heads + h) * a.parts + blockIdx.z) * kPromptAnyRows, lds);
 }
 
 template <typename T, int DP>
 hipError_t launch_any(const PromptArgs &a, hipStream_t s) {
-  constexpr int kBytes = 2 * kKeys * (DP + 4) * 4;
+  constexpr int kBytes = any_lds_floats<DP> * 4;
   auto kern = prompt_any_kernel<T, DP>;
   hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
   if (e != hipSuccess) return e;
@@ -237,7 +61,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
 }
 
 template <int BM, int KEYS>
-hipError_t launch_join(const PromptArgs &a, hipStream_t s) {
+hipError_t join(const PromptArgs &a, hipStream_t s) {
   // a thread for two pieces or fewer
   const dim3 grid(a.tiles, a.d.num_kv_heads, (BM * (a.d.head_dim / 8) + 511) / 512);
   if (a.d.dtype == HB_F32)
@@ -257,9 +81,13 @@ static hipError_t go(const PromptArgs &a, hipStream_t s) {
 
 hipError_t launch_prompt_any(const PromptArgs &a, hipStream_t s) {
   hipError_t e = go(a, s);
-  if (e == hipSuccess && a.parts > 1) e = launch_join<kPromptAnyRows, kKeys>(a, s);
+  if (e == hipSuccess && a.parts > 1) e = join<kPromptAnyRows, kAnyKeys>(a, s);
   return e;
 }
 
+hipError_t launch_prompt_join(const PromptArgs &a, int32_t rows, int32_t keys, hipStream_t s) {
+  if (rows == 256) return join<256, 64>(a, s);
+  return keys == 64 ? join<128, 64>(a, s) : join<64, 32>(a, s);
+}
+
 }  // namespace hb
-namespace hb { bool prompt_mfma_supports(const hb_attn_desc &) { return false; } }

@@ -68,9 +68,9 @@ static int32_t make_prompt_plan(const hb_attn_desc *d, PromptPlan *p) {
   int64_t span = (int64_t)d->page_size * d->max_blocks_per_seq;
   if (d->max_prefix_len_hint > 0 && d->max_prefix_len_hint < span) span = d->max_prefix_len_hint;
   span += d->total_nodes;
-  p->rows = kPromptAnyRows;
-  p->units = 1024;
-  const int64_t least = 128;  // keys of a part
+  p->rows = p->mfma ? prompt_mfma_rows(*d) : kPromptAnyRows;
+  p->units = p->mfma ? 256 : 1024;
+  const int64_t least = p->mfma ? 256 : 128;  // keys of a part
   const int64_t tiles = d->total_nodes * G / p->rows + (d->batch < d->total_nodes ? d->batch : d->total_nodes);
   p->tiles = (int32_t)tiles;
   int64_t parts = d->num_splits;
@@ -219,7 +219,10 @@ int32_t hb_prompt_attn(const hb_attn_desc *desc, const void *q, const void *k_ro
   PromptArgs a = {*desc, q, k_rows, v_rows, k_pool, v_pool, block_table, prefix_len, row_offset, out, lse,
                   p.bytes ? (float *)workspace : nullptr, p.bytes ? (float *)((char *)workspace + p.ml_offset) : nullptr, p.tiles,
                   p.parts, p.units};
-  HB_HIP_TRY(launch_prompt_any(a, (hipStream_t)stream));
+  if (p.mfma)
+    HB_HIP_TRY(launch_prompt_mfma(a, (hipStream_t)stream));
+  else
+    HB_HIP_TRY(launch_prompt_any(a, (hipStream_t)stream));
   return HB_OK;
 }
 
