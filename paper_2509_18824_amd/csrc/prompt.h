@@ -63,7 +63,7 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptArgs &a, int tile,
     if (w.b < 0) {
       const unsigned long long hit = __ballot(upto > tile);
       if (hit) {
-        const int at = __builtin_ctzll(hit);
+        const int at = __builtin_ctzll(hit);  // everything from here on is the same in every lane, and known to be
         w.b = b0 + at;
         w.n = __builtin_amdgcn_readlane(n, at);
         w.P = __builtin_amdgcn_readlane(P, at);
@@ -86,7 +86,7 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptArgs &a, int tile,
     float each = work * (float)a.d.num_kv_heads / (float)a.units;
     each = fmaxf(each, (float)(4 * KEYS));
     const float n = ceilf((float)keys / each);
-    w.parts = n < (float)a.parts ? (int)n : a.parts;
+    w.parts = __builtin_amdgcn_readfirstlane(n < (float)a.parts ? (int)n : a.parts);
     if (w.parts > 1) {
       const int len = ((keys + w.parts - 1) / w.parts + KEYS - 1) / KEYS * KEYS;
       w.parts = (keys + len - 1) / len;

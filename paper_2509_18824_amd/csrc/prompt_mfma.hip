@@ -1,4 +1,6 @@
 // Attention of prompts on the bf16 matrix cores (hb_prompt_attn; head sizes 64 and 128, pages of a power of two).
+#include <type_traits>
+
 #include "prompt.h"
 
 namespace hb {
@@ -12,9 +14,9 @@ typedef __attribute__((address_space(1))) const void *gptr_t;
 typedef __attribute__((address_space(3))) void *lptr_t;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef const __attribute__((address_space(4))) int32_t *table_t;
 typedef unsigned int swap2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -33,6 +35,11 @@ __device__ __forceinline__ float half_sum(float x) {
   const swap2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
+}
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ __forceinline__ float max16(const f32x16 &s) {
   return fmaxf(max3(max3(max3(s[0], s[1], s[2]), s[3], s[4]), max3(s[5], s[6], s[7]), max3(s[8], s[9], s[10])),
@@ -47,11 +54,20 @@ struct Shape {
   static constexpr int kPer = kLoads / NW;             // of a wavefront
   static constexpr int kSteps = D / 16, kSlabs = D / 32, kBlocks = KT / 32;
   static constexpr size_t kLds = (size_t)NS * kStage;
+  static_assert(KT == 64, "an even and an odd block a tile");
+  static_assert(NW * kKeysPerLoad % 16 == 0, "a wavefront's loads lie sixteens apart");
   static_assert(kLoads % NW == 0 && kLds <= 160 * 1024, "a tile's loads are dealt evenly");
   // XOR on a row's 16-byte pieces
   static __device__ __forceinline__ int k_swz(int key) { return D == 128 ? key & 15 : (key >> 1) & 7; }
   static __device__ __forceinline__ int v_swz(int key) { return D == 128 ? (key & 3) << 2 : ((key >> 1) & 1) << 2; }
 };
+
+// the kernel's first argument, from where the launch has put it
+__device__ __forceinline__ const PromptArgs &again(const PromptArgs &a) {
+  uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return *(const PromptArgs *)at;
+}
 
 template <int D, int NW, int KT, int NS>
 __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, int page_shift, const bf16_t *__restrict__ kr,
@@ -70,22 +86,19 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
 
   // ---- rows: 32 of each of the wavefront's two tiles, one a lane (two lanes share it) ------------------------------
   int sees[2], first_sees[2];
-  size_t at[2];
-  bool there[2];
   bf16x8 qf[2][KS];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int row0 = w.t * S::kRows + wave * 64 + 32 * t, row = row0 + j;
-    there[t] = row < rows_all;
-    const int token = there[t] ? row / G : w.n - 1, head = there[t] ? row - token * G : 0;
-    at[t] = (size_t)(w.row0 + token) * Hq + (size_t)h * G + head;
+    const int row = w.t * S::kRows + wave * 64 + 32 * t + j;
+    const bool there = row < rows_all;
+    const int token = there ? row / G : w.n - 1, head = there ? row - token * G : 0;
     sees[t] = min(P + token, end - 1);
     first_sees[t] = __builtin_amdgcn_readfirstlane(sees[t]);
-    const u32x4 *src = (const u32x4 *)a.q + at[t] * (D / 8);
+    const u32x4 *src = (const u32x4 *)a.q + ((size_t)(w.row0 + token) * Hq + (size_t)h * G + head) * (D / 8);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       u32x4 x = {0u, 0u, 0u, 0u};
-      if (there[t]) x = src[2 * s + hf];
+      if (there) x = src[2 * s + hf];
       qf[t][s] = __builtin_bit_cast(bf16x8, x);
     }
   }
@@ -96,9 +109,13 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
   const int n_tiles = (end - begin + KT - 1) / KT;
   const bool no_rows = w.t * S::kRows + wave * 64 >= rows_all;
   const int my_tiles = no_rows || last_sees < begin ? 0 : (last_sees - begin) / KT + 1;
-  const int lkey = lane / S::kPieces;                        // key of a load's group
-  const int piece = lane % S::kPieces;
-  const int64_t row_step = (int64_t)Hkv * D;                 // elements between keys of the prompt
+  // A load moves 64 pieces of 16 bytes: kKeysPerLoad keys, whose rows in memory are `row_bytes` (prompt) or kRowBytes (page)
+  // apart.  The lane that fills piece p of a row in LDS takes piece p ^ swizzle(row) from memory; the swizzles repeat from one
+  // of a wavefront's loads to the next, so that a lane's part of the address is one number for all.
+  const int lkey = lane / S::kPieces, piece = lane % S::kPieces;
+  const uint32_t row_bytes = (uint32_t)Hkv * S::kRowBytes;
+  const int key_of_first = wave * S::kKeysPerLoad + lkey;
+  const uint32_t k_piece = (piece ^ S::k_swz(key_of_first)) * 16, v_piece = (piece ^ S::v_swz(key_of_first)) * 16;
   const bool wide_pages = page_shift >= 4;
   const int page = 1 << page_shift;
   const int32_t *bt = block_table ? block_table + (size_t)w.b * a.d.max_blocks_per_seq : nullptr;
@@ -106,51 +123,56 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
     int id = bt[idx];
     return id < 0 ? 0 : id >= a.d.num_blocks ? a.d.num_blocks - 1 : id;
   };
-  int ids[KT / 16];
-  auto fetch = [&](int i) {  // pages of tile i's sixteens, where it lies in the prefix as a whole
+  int ids[S::kPer];
+  auto fetch = [&](int i) {  // pages of the wavefront's loads of tile i, where it lies in the prefix as a whole
     const int k0 = begin + i * KT;
     if (wide_pages && k0 + KT <= P && i < n_tiles)
 #pragma unroll
-      for (int c = 0; c < KT / 16; ++c) ids[c] = page_at((k0 + 16 * c) >> page_shift);
+      for (int x = 0; x < S::kPer; ++x) {
+        // through the scalar cache: a vector load here would wait for every load of keys that is under way
+        const int id = ((table_t)bt)[(k0 + (wave + NW * x) * S::kKeysPerLoad) >> page_shift];
+        ids[x] = id < 0 ? 0 : id >= a.d.num_blocks ? a.d.num_blocks - 1 : id;
+      }
   };
-  auto issue = [&](int i) {  // the loads of tile i (past the last: of the last once more, into a stage that is free)
+  uint64_t k_from[S::kPer], v_from[S::kPer];  // a lane's addresses
+  auto place = [&](int i) {                    // ... of tile i (past the last: of the last once more)
     const int ti = i < n_tiles ? i : n_tiles - 1;
     const int k0 = begin + ti * KT;
-    unsigned char *st = smem + (i % NS) * S::kStage;
-    const bool prefix = wide_pages && k0 + KT <= P && i < n_tiles, own = k0 >= P && k0 + KT <= end;
+    if (wide_pages && k0 + KT <= P && i < n_tiles) {
 #pragma unroll
-    for (int x = 0; x < S::kPer; ++x) {
-      const int n = wave + NW * x, key0 = n * S::kKeysPerLoad, key = key0 + lkey;
-      const int kpiece = (piece ^ S::k_swz(key)) * 8, vpiece = (piece ^ S::v_swz(key)) * 8;
-      const bf16_t *ks, *vs;
-      if (prefix) {
-        const int pos = k0 + key0;  // a load's keys lie in one page
-        const size_t from = (((size_t)ids[key0 / 16] * Hkv + h) * page + (pos & (page - 1))) * D;
-        ks = kp + from + lkey * D;
-        vs = vp + from + lkey * D;
-      } else if (own) {
-        const size_t from = ((size_t)(w.row0 + k0 + key0 - P) * Hkv + h) * D;
-        ks = kr + from + lkey * row_step;
-        vs = vr + from + lkey * row_step;
-      } else {
-        int pos = k0 + key;
-        pos = pos < end ? pos : end - 1;
-        size_t from;
-        if (pos < P) {
-          from = (((size_t)page_at(pos >> page_shift) * Hkv + h) * page + (pos & (page - 1))) * D;
-          ks = kp + from;
-          vs = vp + from;
-        } else {
-          from = ((size_t)(w.row0 + pos - P) * Hkv + h) * D;
-          ks = kr + from;
-          vs = vr + from;
-        }
+      for (int x = 0; x < S::kPer; ++x) {  // a load's keys lie in one page
+        const size_t from = (((size_t)ids[x] * Hkv + h) * page + ((k0 + (wave + NW * x) * S::kKeysPerLoad) & (page - 1))) * S::kRowBytes;
+        k_from[x] = (uint64_t)kp + from + (lkey * S::kRowBytes + k_piece);
+        v_from[x] = (uint64_t)vp + from + (lkey * S::kRowBytes + v_piece);
       }
-      __builtin_amdgcn_global_load_lds((gptr_t)(ks + kpiece), (lptr_t)(st + n * 1024), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((gptr_t)(vs + vpiece), (lptr_t)(st + S::kTileBytes + n * 1024), 16, 0, 0);
+    } else if (k0 >= P && k0 + KT <= end) {
+      size_t from = ((size_t)(w.row0 + k0 - P + wave * S::kKeysPerLoad) * Hkv + h) * S::kRowBytes;
+#pragma unroll
+      for (int x = 0; x < S::kPer; ++x) {
+        k_from[x] = (uint64_t)kr + from + (lkey * row_bytes + k_piece);
+        v_from[x] = (uint64_t)vr + from + (lkey * row_bytes + v_piece);
+        from += (size_t)(NW * S::kKeysPerLoad) * row_bytes;
+      }
+    } else {  // the end of the prefix, the end of the keys, narrow pages: every key for itself
+#pragma unroll
+      for (int x = 0; x < S::kPer; ++x) {
+        int pos = k0 + (wave + NW * x) * S::kKeysPerLoad + lkey;
+        pos = pos < end ? pos : end - 1;
+        const bool old = pos < P;
+        size_t row = (size_t)(w.row0 + pos - P) * Hkv + h;
+        if (old) row = ((size_t)page_at(pos >> page_shift) * Hkv + h) * page + (pos & (page - 1));
+        k_from[x] = (uint64_t)(old ? kp : kr) + row * S::kRowBytes + k_piece;
+        v_from[x] = (uint64_t)(old ? vp : vr) + row * S::kRowBytes + v_piece;
+      }
     }
   };
-
+  auto load = [&](int i, int x) {  // one of tile i's loads of keys (x < kPer) and of values (behind)
+    unsigned char *st = smem + (i % NS) * S::kStage + wave * 1024;
+    if (x < S::kPer)
+      __builtin_amdgcn_global_load_lds((gptr_t)k_from[x], (lptr_t)(st + NW * x * 1024), 16, 0, 0);
+    else
+      __builtin_amdgcn_global_load_lds((gptr_t)v_from[x - S::kPer], (lptr_t)(st + S::kTileBytes + NW * (x - S::kPer) * 1024), 16, 0, 0);
+  };
   // the last key that all of the workgroup's rows see
   const int all_see = P + w.t * S::kRows / G;
   auto clean = [&](int i) {  // values of tile i, by the wavefront that loaded them
@@ -170,7 +192,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
 
   // ---- state ----------------------------------------------------------------------------------------------------------
   f32x16 o[2][DT], s[2];
-  bf16x8 kf[KS], vf[DT][2], pb[2][2];
+  bf16x8 kf[2][KS], vf[2][DT][2], pb[2][2];  // keys and values of an even and of an odd block: none is ever copied
   float ref[2], limit[2], l[2];  // base-2 reference of a row's scores, the unscaled score that it holds up to, sum of weights
   const float c1 = a.d.softmax_scale * kLog2e;
 #pragma unroll 1
@@ -188,28 +210,19 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int c = 0; c < 2; ++c) vf[dt][c] = (bf16x8)((__bf16)0.f);
+    for (int c = 0; c < 2; ++c) vf[0][dt][c] = (bf16x8)((__bf16)0.f);
 
   const int k_lane = j * S::kRowBytes, kx = hf ^ S::k_swz(j);
-  auto read_k = [&](const unsigned char *st, int blk, bf16x8 (&k)[KS]) {
-    const unsigned char *p = st + blk * 32 * S::kRowBytes + k_lane;
-#pragma unroll
-    for (int q = 0; q < KS; ++q) k[q] = __builtin_bit_cast(bf16x8, *(const u32x4 *)(p + (((2 * q) ^ kx) << 4)));
-  };
+  auto k_at = [&](const unsigned char *st, int blk) { return st + blk * 32 * S::kRowBytes + k_lane; };
+  auto one_k = [&](const unsigned char *p, int q) { return __builtin_bit_cast(bf16x8, *(const u32x4 *)(p + (((2 * q) ^ kx) << 4))); };
   const int s4 = lane & 15, e = (lane >> 4) & 1, vkey = 4 * hf + (s4 >> 2);
   const int v_lane = vkey * S::kRowBytes + 8 * (s4 & 1), vx = S::v_swz(vkey);
-  auto read_v = [&](const unsigned char *st, int blk, bf16x8 (&v)[DT][2]) {
-    const unsigned char *p = st + S::kTileBytes + blk * 32 * S::kRowBytes + v_lane;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const unsigned char *pd = p + (((4 * dt + 2 * e + ((s4 >> 1) & 1)) ^ vx) << 4);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr)(pd + 16 * c * S::kRowBytes));
-        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr)(pd + (16 * c + 8) * S::kRowBytes));
-        v[dt][c] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-    }
+  auto v_at = [&](const unsigned char *st, int blk) { return st + S::kTileBytes + blk * 32 * S::kRowBytes + v_lane; };
+  auto one_v = [&](const unsigned char *p, int dt, int c) {
+    const unsigned char *pd = p + (((4 * dt + 2 * e + ((s4 >> 1) & 1)) ^ vx) << 4);
+    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr)(pd + 16 * c * S::kRowBytes));
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr)(pd + (16 * c + 8) * S::kRowBytes));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
 
   // masks, and the row's reference moved where a score has outgrown it; block of keys from k0
@@ -237,34 +250,62 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
     }
   };
 
-  // One step: the scores of tile t (settled) become weights, while the matrix core makes the other tile's next scores and
-  // adds the other tile's last weights' products.
-  auto step = [&](int t, const bf16x8 (&k)[KS], const bf16x8 (&v)[DT][2], float &top) {
-    const int u = 1 - t;
-    f32x16 sn = (f32x16)(0.f);
+  // One step: the scores of tile t (settled) become weights, while the matrix core makes the other tile's next scores (first)
+  // and adds the other tile's last weights' products.  None needs what another makes, so that they can be laid side by side
+  // by hand: an instruction of the matrix core (32 clocks), then a sixteenth of the vector work and of the reads from LDS,
+  // and a fence for the scheduler, which would put them one behind the other.
+  auto step = [&](auto T, const bf16x8 (&k)[KS], const bf16x8 (&v)[DT][2], float &top, auto read) {
+    constexpr int t = decltype(T)::value, u = 1 - t, kAll = KS + 2 * DT, kEach = 16 / kAll;
+    f32x16 sn, p;
+    float m0 = 0.f, m1 = 0.f;
+    uint32_t w[8];
 #pragma unroll
-    for (int q = 0; q < KS; ++q) sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[q], qf[u][q], sn, 0, 0, 0);
-    f32x16 p;
+    for (int x = 0; x < kAll; ++x) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (x < KS)
+        sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[x], qf[u][x], x ? sn : (f32x16)(0.f), 0, 0, 0);
+      else
+        o[u][(x - KS) % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[(x - KS) % DT][(x - KS) / DT], pb[u][(x - KS) / DT], o[u][(x - KS) % DT], 0, 0, 0);
+      read(x);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c1, -ref[t]));
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[u][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[dt][c], pb[u][c], o[u][dt], 0, 0, 0);
-    float sum = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) sum += p[r];
-    l[t] += sum;
-    f32x8 lo, hi;
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      lo[r] = p[r];
-      hi[r] = p[8 + r];
+      for (int r = kEach * x; r < kEach * x + kEach; ++r) {
+        p[r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c1, -ref[t]));
+        float y = p[r], sum = l[t];
+        if (r > 0) sum += p[r - 1];
+        if (r > 1 && r % 2 == 0) {
+          uint32_t two = pack2(p[r - 2], p[r - 1]);
+          asm volatile("" : "+v"(y), "+v"(sum), "+v"(two));
+          w[r / 2 - 1] = two;
+        } else {
+          asm volatile("" : "+v"(y), "+v"(sum));
+        }
+        p[r] = y;
+        l[t] = sum;
+      }
+      // the largest of the new scores, a sixth at a time
+      if (x >= kAll - 3) {
+        const int g = x - (kAll - 3);
+        if (g == 0) {
+          m0 = max3(sn[0], sn[1], sn[2]);
+          m1 = max3(sn[3], sn[4], sn[5]);
+        } else if (g == 1) {
+          m0 = max3(m0, sn[6], sn[7]);
+          m1 = max3(m1, sn[8], sn[9]);
+        } else {
+          m0 = max3(m0, sn[10], sn[11]);
+          m1 = max3(m1, sn[12], sn[13]);
+        }
+        asm volatile("" : "+v"(m0), "+v"(m1));
+      }
     }
-    pb[t][0] = __builtin_convertvector(lo, bf16x8);
-    pb[t][1] = __builtin_convertvector(hi, bf16x8);
+    __builtin_amdgcn_sched_barrier(0);
+    w[7] = pack2(p[14], p[15]);
+    l[t] += p[15];
+    pb[t][0] = __builtin_bit_cast(bf16x8, (u32x4){w[0], w[1], w[2], w[3]});
+    pb[t][1] = __builtin_bit_cast(bf16x8, (u32x4){w[4], w[5], w[6], w[7]});
     s[u] = sn;
-    top = max16(sn);
+    top = fmaxf(max3(m0, sn[14], sn[15]), m1);
+    asm volatile("" : "+v"(pb[t][0]), "+v"(pb[t][1]), "+v"(l[t]), "+v"(top));
   };
 
   // ---- the loop -----------------------------------------------------------------------------------------------------
@@ -275,17 +316,20 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
   fetch(0);
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i) {
-    issue(i);
+    place(i);
+#pragma unroll
+    for (int x = 0; x < 2 * S::kPer; ++x) load(i, x);
     fetch(i + 1);
   }
   __builtin_amdgcn_s_waitcnt(kWaitFirst);
   if (careful) clean(0);
   HB_BARRIER();
   float top;
-  read_k(smem, 0, kf);
+#pragma unroll
+  for (int q = 0; q < KS; ++q) kf[0][q] = one_k(k_at(smem, 0), q);
   s[0] = (f32x16)(0.f);
 #pragma unroll
-  for (int q = 0; q < KS; ++q) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[q], qf[0][q], s[0], 0, 0, 0);
+  for (int q = 0; q < KS; ++q) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[0][q], qf[0][q], s[0], 0, 0, 0);
   top = max16(s[0]);
   settle(0, begin, top);
 
@@ -301,23 +345,25 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
         __builtin_amdgcn_s_waitcnt(kWait);
         if (careful) clean(i + 1);
         HB_BARRIER();
-        issue(i + NS - 1);
+        place(i + NS - 1);
         fetch(i + NS);
+        if (!mine)
+#pragma unroll
+          for (int x = 0; x < 2 * S::kPer; ++x) load(i + NS - 1, x);
       }
       if (mine) {
-        bf16x8 kn[KS], vn[DT][2];
-        read_k(b == S::kBlocks - 1 ? next : st, (b + 1) % S::kBlocks, kn);
-        step(0, kf, vf, top);
-        read_v(st, b, vn);
+        const int now = b, then = 1 - b;
+        const unsigned char *pk = k_at(b == S::kBlocks - 1 ? next : st, (b + 1) % S::kBlocks), *pv = v_at(st, b);
+        step(std::integral_constant<int, 0>(), kf[now], vf[now], top, [&](int x) {
+          if (x < KS) kf[then][x] = one_k(pk, x);
+          if (b == S::kBlocks - 1 && x < 2 * S::kPer) load(i + NS - 1, x);
+        });
         settle(1, k0 + 32 * b, top);
-        step(1, kn, vn, top);
+        step(std::integral_constant<int, 1>(), kf[then], vf[then], top, [&](int x) {
+          if (x < DT) vf[then][x][0] = one_v(pv, x, 0);
+          else if (x < 2 * DT) vf[then][x - DT][1] = one_v(pv, x - DT, 1);
+        });
         settle(0, k0 + 32 * b + 32, top);
-#pragma unroll
-        for (int q = 0; q < KS; ++q) kf[q] = kn[q];
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) vf[dt][c] = vn[dt][c];
       }
     }
   }
@@ -325,7 +371,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
 #pragma unroll
   for (int c = 0; c < 2; ++c)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[1][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt][c], pb[1][c], o[1][dt], 0, 0, 0);
+    for (int dt = 0; dt < DT; ++dt) o[1][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[0][dt][c], pb[1][c], o[1][dt], 0, 0, 0);
   __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // loads past the end land before the workgroup gives up its LDS
 
   // Keys that a row does not see have weight 0 in the products, and 0 times a value that is not finite is no number.  Where
@@ -359,11 +405,17 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
   }  // careful
 
   // ---- results ------------------------------------------------------------------------------------------------------
+  // (the arguments are read again, so that the loop need not keep them in its registers)
+  const PromptArgs &z = again(a);
+  const int zHq = z.d.num_q_heads, zHkv = z.d.num_kv_heads, zG = zHq / zHkv;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const float sum = half_sum(l[t]);
-    if (!there[t]) continue;
+    const int r0 = wave * 64 + 32 * t + j, row = w.t * S::kRows + r0;
+    if (row >= w.n * zG) continue;
     if (w.parts == 1) {
+      const int token = row / zG;
+      const size_t at = (size_t)(w.row0 + token) * zHq + (size_t)h * zG + (row - token * zG);
       const float inv = 1.f / sum;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
@@ -372,11 +424,11 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
           u32x2 x;
           x[0] = pack_bf16(o[t][dt][4 * g] * inv, o[t][dt][4 * g + 1] * inv);
           x[1] = pack_bf16(o[t][dt][4 * g + 2] * inv, o[t][dt][4 * g + 3] * inv);
-          *(u32x2 *)((bf16_t *)a.out + at[t] * D + 32 * dt + 8 * g + 4 * hf) = x;
+          *(u32x2 *)((bf16_t *)z.out + at * D + 32 * dt + 8 * g + 4 * hf) = x;
         }
-      if (a.lse && hf == 0) a.lse[at[t]] = (ref[t] + log2f(sum)) * kLn2;
+      if (z.lse && hf == 0) z.lse[at] = (ref[t] + log2f(sum)) * kLn2;
     } else {
-      const size_t slot = (((size_t)tile_id * Hkv + h) * a.parts + blockIdx.y) * S::kRows + wave * 64 + 32 * t + j;
+      const size_t slot = (((size_t)(blockIdx.x / zHkv) * zHkv + h) * z.parts + blockIdx.y) * S::kRows + r0;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -384,11 +436,11 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
           f32x4 x;
 #pragma unroll
           for (int r = 0; r < 4; ++r) x[r] = o[t][dt][4 * g + r];
-          *(f32x4 *)(a.part_o + slot * D + 32 * dt + 8 * g + 4 * hf) = x;
+          *(f32x4 *)(z.part_o + slot * D + 32 * dt + 8 * g + 4 * hf) = x;
         }
       if (hf == 0) {
-        a.part_ml[slot * 2] = limit[t] == HB_NEG_INF ? HB_NEG_INF : ref[t];
-        a.part_ml[slot * 2 + 1] = sum;
+        z.part_ml[slot * 2] = limit[t] == HB_NEG_INF ? HB_NEG_INF : ref[t];
+        z.part_ml[slot * 2 + 1] = sum;
       }
     }
   }
