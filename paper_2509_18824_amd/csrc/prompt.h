@@ -18,7 +18,8 @@ struct PromptArgs {
   const int32_t *block_table, *prefix_len, *row_offset;
   void *out;
   float *lse;             // may be null
-  float *part_o, *part_ml;  // [tile][kv head][part][row of bm][D], and [..][2]: largest score (base 2), sum
+  float *part_o, *part_ml;  // [tile][kv head][part][row of bm][D], and [..][4]: largest score (base 2), sum that
+                            // results are divided by, sum for the log-sum-exp, nothing
   int32_t tiles, parts;   // tiles of all sequences at most; parts of a tile's keys at most
   int32_t units;          // (tile, part, kv head) that the launch should come to
 };
@@ -57,7 +58,7 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptArgs &a, int tile,
       P = a.prefix_len ? a.prefix_len[b] : 0;
       P = P < 0 ? 0 : P > cap ? (int)cap : P;
     }
-    const int tiles = (int)(((int64_t)n * G + BM - 1) / BM);
+    const int tiles = (int)(((uint32_t)(n * G) + BM - 1) / BM);  // total_nodes * Hq is at most 2^30
     if (a.parts > 1) work += (float)tiles * ((float)P + 0.5f * (float)n);
     const int upto = scan_lanes(tiles) + before;
     if (w.b < 0) {
@@ -75,8 +76,8 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptArgs &a, int tile,
     if (w.b >= 0 && a.parts <= 1) break;
   }
   if (w.b < 0) return w;
-  const int64_t last = ((int64_t)(w.t + 1) * BM + G - 1) / G;  // tokens up to the tile's last row
-  w.tokens_end = last < w.n ? (int)last : w.n;
+  const int last = (int)(((uint32_t)(w.t + 1) * BM + G - 1) / (uint32_t)G);  // tokens up to the tile's last row
+  w.tokens_end = last < w.n ? last : w.n;
   const int keys = w.P + w.tokens_end;
   w.parts = 1;
   w.begin = 0;

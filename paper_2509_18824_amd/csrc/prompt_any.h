@@ -187,8 +187,7 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
         if (d < D) a.part_o[slot * D + d] = o[dt][r];
       }
     if (kg == 0) {
-      a.part_ml[slot * 2] = m;
-      a.part_ml[slot * 2 + 1] = l;
+      *(f32x4 *)(a.part_ml + slot * 4) = (f32x4){m, l, l, 0.f};
     }
   }
 }

@@ -40,23 +40,24 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
     const int64_t token = row / G;
     const size_t at = (size_t)(w.row0 + token) * a.d.num_q_heads + (size_t)h * G + (row - token * G);
     const size_t slot = (((size_t)blockIdx.x * Hkv + h) * a.parts) * BM + r;
-    float m = HB_NEG_INF, l = 0.f, x[8] = {};
-    for (int p = 0; p < w.parts; ++p) m = fmaxf(m, a.part_ml[(slot + (size_t)p * BM) * 2]);
+    float m = HB_NEG_INF, l = 0.f, whole = 0.f, x[8] = {};
+    for (int p = 0; p < w.parts; ++p) m = fmaxf(m, a.part_ml[(slot + (size_t)p * BM) * 4]);
     for (int p = 0; p < w.parts; ++p) {
       const size_t s = slot + (size_t)p * BM;
-      const float mp = a.part_ml[s * 2], lp = a.part_ml[s * 2 + 1];
-      if (mp == HB_NEG_INF && lp == 0.f) continue;  // sees none of this part's keys
-      const float c = exp2_of(mp - m);
+      const f32x4 ml = *(const f32x4 *)(a.part_ml + s * 4);
+      if (ml[0] == HB_NEG_INF && ml[1] == 0.f) continue;  // sees none of this part's keys
+      const float c = exp2_of(ml[0] - m);
       float y[8];
       load8(a.part_o + s * D + d0, y);
-      l += c * lp;
+      l += c * ml[1];
+      whole += c * ml[2];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] += c * y[e];
     }
     const float inv = 1.f / l;
 #pragma unroll
     for (int e = 0; e < 8; ++e) store_f32((T *)a.out + at * D + d0 + e, x[e] * inv);
-    if (a.lse && d0 == 0) a.lse[at] = (m + log2f(l)) * kLn2;
+    if (a.lse && d0 == 0) a.lse[at] = (m + log2f(whole)) * kLn2;
   }
 }
 

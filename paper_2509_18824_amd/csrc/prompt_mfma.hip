@@ -21,7 +21,7 @@ typedef unsigned int swap2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 #define HB_NEG_INF (-__builtin_huge_valf())
-constexpr float kSlack = 8.f;  // log2 units that a score may exceed its row's reference by
+constexpr float kMost = 256.f;  // sum of a lane's weights of a step, up to which their row's reference stays
 
 __device__ __forceinline__ uint32_t finite_or_zero(uint32_t w) {  // of two bf16
   const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu, hi = (w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u;
@@ -40,6 +40,11 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
 }
+// sum + both numbers of a pair
+__device__ __forceinline__ float add2(uint32_t two, float sum) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
+}
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ __forceinline__ float max16(const f32x16 &s) {
   return fmaxf(max3(max3(max3(s[0], s[1], s[2]), s[3], s[4]), max3(s[5], s[6], s[7]), max3(s[8], s[9], s[10])),
@@ -48,28 +53,37 @@ __device__ __forceinline__ float max16(const f32x16 &s) {
 
 template <int D, int NW, int KT, int NS>
 struct Shape {
-  static constexpr int kRows = 64 * NW, kRowBytes = 2 * D, kPieces = D / 8, kKeysPerLoad = 64 / kPieces;
+  static constexpr int kRows = 32 * NW, kRowBytes = 2 * D, kPieces = D / 8, kKeysPerLoad = 64 / kPieces;
   static constexpr int kTileBytes = KT * kRowBytes, kStage = 2 * kTileBytes;
   static constexpr int kLoads = KT / kKeysPerLoad;     // of K, and as many of V, a tile
   static constexpr int kPer = kLoads / NW;             // of a wavefront
   static constexpr int kSteps = D / 16, kSlabs = D / 32, kBlocks = KT / 32;
+  // tiles that have landed beside the one in work when its last block begins; tiles that may still be under way then
+  static constexpr int kAhead = kBlocks == 1 ? 3 : 2, kLate = NS - 1 - kAhead;
   static constexpr size_t kLds = (size_t)NS * kStage;
-  static_assert(KT == 64, "an even and an odd block a tile");
+  static_assert(KT == 32 || KT == 64, "blocks of 32 keys, one or two a tile");
   static_assert(NW * kKeysPerLoad % 16 == 0, "a wavefront's loads lie sixteens apart");
-  static_assert(kLoads % NW == 0 && kLds <= 160 * 1024, "a tile's loads are dealt evenly");
+  static_assert(kLoads % NW == 0 && kLate >= 0 && kLds <= 160 * 1024, "a tile's loads are dealt evenly");
   // XOR on a row's 16-byte pieces
   static __device__ __forceinline__ int k_swz(int key) { return D == 128 ? key & 15 : (key >> 1) & 7; }
   static __device__ __forceinline__ int v_swz(int key) { return D == 128 ? (key & 3) << 2 : ((key >> 1) & 1) << 2; }
 };
 
+struct Sums {  // of a step's weights
+  float rounded, whole;
+};
+
 // the kernel's first argument, from where the launch has put it
-__device__ __forceinline__ const PromptArgs &again(const PromptArgs &a) {
+typedef const __attribute__((address_space(4))) PromptArgs *args_t;
+__device__ __forceinline__ args_t again() {
   uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(at));
-  return *(const PromptArgs *)at;
+  return (args_t)at;
 }
+template <typename T>
+using global_t = __attribute__((address_space(1))) T *;
 
-template <int D, int NW, int KT, int NS>
+template <int D, int NW, int KT, int NS, bool LSE>
 __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, int page_shift, const bf16_t *__restrict__ kr,
                                                                  const bf16_t *__restrict__ vr, const bf16_t *__restrict__ kp,
                                                                  const bf16_t *__restrict__ vp, const int32_t *__restrict__ block_table) {
@@ -79,35 +93,31 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 31, hf = lane >> 5;
   const int Hkv = a.d.num_kv_heads, Hq = a.d.num_q_heads, G = Hq / Hkv;
-  const int h = blockIdx.x % Hkv, tile_id = blockIdx.x / Hkv;
+  const int tile_id = blockIdx.x / (uint32_t)Hkv, h = blockIdx.x - tile_id * Hkv;
   const PromptTile w = prompt_tile<S::kRows, KT>(a, tile_id, blockIdx.y);
   if (w.t < 0) return;
   const int P = w.P, begin = w.begin, end = w.end, rows_all = w.n * G;
 
-  // ---- rows: 32 of each of the wavefront's two tiles, one a lane (two lanes share it) ------------------------------
-  int sees[2], first_sees[2];
-  bf16x8 qf[2][KS];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int row = w.t * S::kRows + wave * 64 + 32 * t + j;
+  // ---- rows: 32 of the wavefront's, one a lane (two lanes share it) -------------------------------------------------
+  const int my_row0 = w.t * S::kRows + wave * 32;
+  int sees;
+  bf16x8 qf[KS];
+  {
+    const int row = my_row0 + j;
     const bool there = row < rows_all;
-    const int token = there ? row / G : w.n - 1, head = there ? row - token * G : 0;
-    sees[t] = min(P + token, end - 1);
-    first_sees[t] = __builtin_amdgcn_readfirstlane(sees[t]);
+    const int token = there ? (int)((uint32_t)row / (uint32_t)G) : w.n - 1, head = there ? row - token * G : 0;
+    sees = min(P + token, end - 1);
     const u32x4 *src = (const u32x4 *)a.q + ((size_t)(w.row0 + token) * Hq + (size_t)h * G + head) * (D / 8);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      u32x4 x = {0u, 0u, 0u, 0u};
-      if (there) x = src[2 * s + hf];
-      qf[t][s] = __builtin_bit_cast(bf16x8, x);
-    }
+    for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(bf16x8, src[2 * s + hf]);  // a row that is not there: some row's, for nobody
   }
+  const int first_sees = __builtin_amdgcn_readfirstlane(sees);
   // what the wavefront's last row sees: behind it there is nothing for it to do
-  const int last_sees = __builtin_amdgcn_readlane(max(sees[0], sees[1]), 31);
+  const int last_sees = __builtin_amdgcn_readlane(sees, 31);
 
   // ---- keys' way to LDS ---------------------------------------------------------------------------------------------
   const int n_tiles = (end - begin + KT - 1) / KT;
-  const bool no_rows = w.t * S::kRows + wave * 64 >= rows_all;
+  const bool no_rows = my_row0 >= rows_all;
   const int my_tiles = no_rows || last_sees < begin ? 0 : (last_sees - begin) / KT + 1;
   // A load moves 64 pieces of 16 bytes: kKeysPerLoad keys, whose rows in memory are `row_bytes` (prompt) or kRowBytes (page)
   // apart.  The lane that fills piece p of a row in LDS takes piece p ^ swizzle(row) from memory; the swizzles repeat from one
@@ -125,28 +135,29 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
   };
   int ids[S::kPer];
   auto fetch = [&](int i) {  // pages of the wavefront's loads of tile i, where it lies in the prefix as a whole
-    const int k0 = begin + i * KT;
+    int k0 = begin + i * KT, wv = wave;
+    asm volatile("" : "+s"(k0), "+s"(wv));
     if (wide_pages && k0 + KT <= P && i < n_tiles)
 #pragma unroll
       for (int x = 0; x < S::kPer; ++x) {
         // through the scalar cache: a vector load here would wait for every load of keys that is under way
-        const int id = ((table_t)bt)[(k0 + (wave + NW * x) * S::kKeysPerLoad) >> page_shift];
+        const int id = ((table_t)bt)[(k0 + (wv + NW * x) * S::kKeysPerLoad) >> page_shift];
         ids[x] = id < 0 ? 0 : id >= a.d.num_blocks ? a.d.num_blocks - 1 : id;
       }
   };
   uint64_t k_from[S::kPer], v_from[S::kPer];  // a lane's addresses
-  auto place = [&](int i) {                    // ... of tile i (past the last: of the last once more)
-    const int ti = i < n_tiles ? i : n_tiles - 1;
-    const int k0 = begin + ti * KT;
-    if (wide_pages && k0 + KT <= P && i < n_tiles) {
+  auto place = [&](int i) {                    // ... of tile i
+    int k0 = begin + i * KT, wv = wave;
+    asm volatile("" : "+s"(k0), "+s"(wv));  // or a hundred numbers are made in front of the loop, and kept in lanes of registers
+    if (wide_pages && k0 + KT <= P) {
 #pragma unroll
       for (int x = 0; x < S::kPer; ++x) {  // a load's keys lie in one page
-        const size_t from = (((size_t)ids[x] * Hkv + h) * page + ((k0 + (wave + NW * x) * S::kKeysPerLoad) & (page - 1))) * S::kRowBytes;
+        const size_t from = (((size_t)ids[x] * Hkv + h) * page + ((k0 + (wv + NW * x) * S::kKeysPerLoad) & (page - 1))) * S::kRowBytes;
         k_from[x] = (uint64_t)kp + from + (lkey * S::kRowBytes + k_piece);
         v_from[x] = (uint64_t)vp + from + (lkey * S::kRowBytes + v_piece);
       }
     } else if (k0 >= P && k0 + KT <= end) {
-      size_t from = ((size_t)(w.row0 + k0 - P + wave * S::kKeysPerLoad) * Hkv + h) * S::kRowBytes;
+      size_t from = ((size_t)(w.row0 + k0 - P + wv * S::kKeysPerLoad) * Hkv + h) * S::kRowBytes;
 #pragma unroll
       for (int x = 0; x < S::kPer; ++x) {
         k_from[x] = (uint64_t)kr + from + (lkey * row_bytes + k_piece);
@@ -156,13 +167,17 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
     } else {  // the end of the prefix, the end of the keys, narrow pages: every key for itself
 #pragma unroll
       for (int x = 0; x < S::kPer; ++x) {
-        int pos = k0 + (wave + NW * x) * S::kKeysPerLoad + lkey;
+        int pos = k0 + (wv + NW * x) * S::kKeysPerLoad + lkey;
         pos = pos < end ? pos : end - 1;
-        const bool old = pos < P;
-        size_t row = (size_t)(w.row0 + pos - P) * Hkv + h;
-        if (old) row = ((size_t)page_at(pos >> page_shift) * Hkv + h) * page + (pos & (page - 1));
-        k_from[x] = (uint64_t)(old ? kp : kr) + row * S::kRowBytes + k_piece;
-        v_from[x] = (uint64_t)(old ? vp : vr) + row * S::kRowBytes + v_piece;
+        uint64_t row = (uint64_t)(w.row0 + pos - P) * Hkv + h, kb = (uint64_t)kr, vb = (uint64_t)vr;
+        if (pos < P) {
+          row = ((uint64_t)page_at(pos >> page_shift) * Hkv + h) * page + (pos & (page - 1));
+          kb = (uint64_t)kp;
+          vb = (uint64_t)vp;
+        }
+        asm volatile("" : "+v"(kb), "+v"(vb));  // values: no choice among their places in memory is made of this
+        k_from[x] = kb + row * S::kRowBytes + k_piece;
+        v_from[x] = vb + row * S::kRowBytes + v_piece;
       }
     }
   };
@@ -191,26 +206,15 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
   };
 
   // ---- state ----------------------------------------------------------------------------------------------------------
-  f32x16 o[2][DT], s[2];
-  bf16x8 kf[2][KS], vf[2][DT][2], pb[2][2];  // keys and values of an even and of an odd block: none is ever copied
-  float ref[2], limit[2], l[2];  // base-2 reference of a row's scores, the unscaled score that it holds up to, sum of weights
+  f32x16 o[DT], s;
+  bf16x8 kf[KS], vf[DT][2], pb[2];
+  // base-2 reference of a row's scores; sum of its weights as they are multiplied with values, in bf16, which results are
+  // divided by; and as they are in float32, for the log-sum-exp
+  float ref, l, le;
   const float c1 = a.d.softmax_scale * kLog2e;
 #pragma unroll 1
   for (int careful = 0;; careful = 1) {
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    ref[t] = 0.f;
-    limit[t] = HB_NEG_INF;
-    l[t] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[t][dt] = (f32x16)(0.f);
-#pragma unroll
-    for (int c = 0; c < 2; ++c) pb[t][c] = (bf16x8)((__bf16)0.f);
-  }
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) vf[0][dt][c] = (bf16x8)((__bf16)0.f);
+  ref = 0.f;
 
   const int k_lane = j * S::kRowBytes, kx = hf ^ S::k_swz(j);
   auto k_at = [&](const unsigned char *st, int blk) { return st + blk * 32 * S::kRowBytes + k_lane; };
@@ -225,154 +229,168 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
 
-  // masks, and the row's reference moved where a score has outgrown it; block of keys from k0
-  auto settle = [&](int t, int k0, float top) {
-    if (k0 + 31 > first_sees[t]) {  // uniform: some row does not see some key
-      const int lim = sees[t] - k0 - 4 * hf;
+  // scores against the block of keys from k0: those of keys that a row does not see go
+  auto mask = [&](int k0) {
+    asm volatile("" : "+s"(k0));
+    if (k0 + 31 > first_sees) {  // uniform: some row does not see some key
+      const int lim = sees - k0 - 4 * hf;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[t][r] = 8 * (r >> 2) + (r & 3) <= lim ? s[t][r] : HB_NEG_INF;
-      top = max16(s[t]);
-    }
-    if (__any(!(top <= limit[t]))) {
-      asm volatile("" ::: "memory");
-      const float mx = half_max(top) * c1;
-      const bool none = limit[t] == HB_NEG_INF;  // nothing accumulated yet
-      const bool grow = mx > (none ? HB_NEG_INF : ref[t] + kSlack);
-      const float next = grow ? mx : ref[t];
-      const float alpha = none || !grow ? 1.f : __builtin_amdgcn_exp2f(ref[t] - mx);
-      ref[t] = next;
-      limit[t] = none && !grow ? HB_NEG_INF : (next + kSlack) / c1;
-      l[t] *= alpha;
-      if (__any(alpha != 1.f)) {
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[t][dt] *= alpha;
-      }
+      for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) <= lim ? s[r] : HB_NEG_INF;
     }
   };
-
-  // One step: the scores of tile t (settled) become weights, while the matrix core makes the other tile's next scores (first)
-  // and adds the other tile's last weights' products.  None needs what another makes, so that they can be laid side by side
-  // by hand: an instruction of the matrix core (32 clocks), then a sixteenth of the vector work and of the reads from LDS,
-  // and a fence for the scheduler, which would put them one behind the other.
-  auto step = [&](auto T, const bf16x8 (&k)[KS], const bf16x8 (&v)[DT][2], float &top, auto read) {
-    constexpr int t = decltype(T)::value, u = 1 - t, kAll = KS + 2 * DT, kEach = 16 / kAll;
-    f32x16 sn, p;
-    float m0 = 0.f, m1 = 0.f;
+  auto weights = [&](const f32x16 &x, bf16x8 (&p)[2]) {  // of a block, plainly
+    Sums part = {0.f, 0.f};
     uint32_t w[8];
 #pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const float a0 = __builtin_amdgcn_exp2f(fmaf(x[2 * r], c1, -ref)), a1 = __builtin_amdgcn_exp2f(fmaf(x[2 * r + 1], c1, -ref));
+      w[r] = pack2(a0, a1);
+      part.rounded = add2(w[r], part.rounded);
+      part.whole += a0 + a1;
+    }
+    p[0] = __builtin_bit_cast(bf16x8, (u32x4){w[0], w[1], w[2], w[3]});
+    p[1] = __builtin_bit_cast(bf16x8, (u32x4){w[4], w[5], w[6], w[7]});
+    return part;
+  };
+  // A block's weights, whose sum in this lane is `part`, are in pb in bf16; x: the scores.  A row's reference stays while
+  // weights are small: all of a lane's are, if their sum is (they are not negative).  Else, and for the first block (a row sees
+  // its first key, or nothing at all of this part), the reference becomes the row's largest score of the block and the weights
+  // are made anew.
+  auto settle = [&](const f32x16 &x, Sums part, bool first) {
+    if (first || __any(!(part.rounded <= kMost))) {
+      asm volatile("" ::: "memory");
+      const float mx = half_max(max16(x)) * c1;  // c1 > 0
+      // (a row's own weights decide, not those of the others in the wavefront)
+      const bool grow = first ? mx > HB_NEG_INF : half_max(part.rounded) > kMost && mx > ref;
+      const float alpha = grow ? __builtin_amdgcn_exp2f(ref - mx) : 1.f;
+      ref = grow ? mx : ref;
+      if (first) {  // what the sums hold so far is nothing
+        l = le = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] = (f32x16)(0.f);
+      } else if (__any(alpha != 1.f)) {
+        l *= alpha;
+        le *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
+      }
+      part = weights(x, pb);
+    }
+    l += part.rounded;
+    if (LSE) le += part.whole;
+  };
+
+  // One step: a block's scores become weights, while the matrix core makes the next block's scores (first) and adds the last
+  // block's weights' products.  None needs what another makes, so that they can be laid side by side by hand: an instruction
+  // of the matrix core (32 clocks), then a sixteenth of the vector work and of the reads from LDS (the last block's values,
+  // then the keys of the block behind the next), and a fence for the scheduler, which would put them one behind the other.
+  auto step = [&](const unsigned char *pv, const unsigned char *pk, bool first, auto middle) {
+    constexpr int kAll = KS + 2 * DT, kEach = 16 / kAll;
+    f32x16 sn;
+    bf16x8 pn[2];
+    float p[2];
+    Sums part = {0.f, 0.f};
+    uint32_t w[8];
+    auto pair = [&](int q) {
+      w[q] = pack2(p[0], p[1]);
+      part.rounded = add2(w[q], part.rounded);
+      asm volatile("" : "+v"(w[q]), "+v"(part.rounded));
+      if (LSE) {
+        part.whole += p[0] + p[1];
+        asm volatile("" : "+v"(part.whole));
+      }
+    };
+#pragma unroll
     for (int x = 0; x < kAll; ++x) {
+      if (x == KS) middle();
       __builtin_amdgcn_sched_barrier(0);
-      if (x < KS)
-        sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[x], qf[u][x], x ? sn : (f32x16)(0.f), 0, 0, 0);
-      else
-        o[u][(x - KS) % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[(x - KS) % DT][(x - KS) / DT], pb[u][(x - KS) / DT], o[u][(x - KS) % DT], 0, 0, 0);
-      read(x);
+      if (x < KS) {
+        sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x], qf[x], x ? sn : (f32x16)(0.f), 0, 0, 0);
+        vf[x % DT][x / DT] = one_v(pv, x % DT, x / DT);
+      } else {
+        const int y = x - KS;
+        o[y % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[y % DT][y / DT], pb[y / DT], o[y % DT], 0, 0, 0);
+        kf[y] = one_k(pk, y);
+      }
 #pragma unroll
       for (int r = kEach * x; r < kEach * x + kEach; ++r) {
-        p[r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c1, -ref[t]));
-        float y = p[r], sum = l[t];
-        if (r > 0) sum += p[r - 1];
-        if (r > 1 && r % 2 == 0) {
-          uint32_t two = pack2(p[r - 2], p[r - 1]);
-          asm volatile("" : "+v"(y), "+v"(sum), "+v"(two));
-          w[r / 2 - 1] = two;
-        } else {
-          asm volatile("" : "+v"(y), "+v"(sum));
-        }
-        p[r] = y;
-        l[t] = sum;
-      }
-      // the largest of the new scores, a sixth at a time
-      if (x >= kAll - 3) {
-        const int g = x - (kAll - 3);
-        if (g == 0) {
-          m0 = max3(sn[0], sn[1], sn[2]);
-          m1 = max3(sn[3], sn[4], sn[5]);
-        } else if (g == 1) {
-          m0 = max3(m0, sn[6], sn[7]);
-          m1 = max3(m1, sn[8], sn[9]);
-        } else {
-          m0 = max3(m0, sn[10], sn[11]);
-          m1 = max3(m1, sn[12], sn[13]);
-        }
-        asm volatile("" : "+v"(m0), "+v"(m1));
+        float y = __builtin_amdgcn_exp2f(fmaf(s[r], c1, -ref));
+        asm volatile("" : "+v"(y));
+        if (r % 2 == 0 && r > 0) pair(r / 2 - 1);  // (an exponential's result has to wait an instruction)
+        p[r % 2] = y;
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    w[7] = pack2(p[14], p[15]);
-    l[t] += p[15];
-    pb[t][0] = __builtin_bit_cast(bf16x8, (u32x4){w[0], w[1], w[2], w[3]});
-    pb[t][1] = __builtin_bit_cast(bf16x8, (u32x4){w[4], w[5], w[6], w[7]});
-    s[u] = sn;
-    top = fmaxf(max3(m0, sn[14], sn[15]), m1);
-    asm volatile("" : "+v"(pb[t][0]), "+v"(pb[t][1]), "+v"(l[t]), "+v"(top));
+    pair(7);
+    pb[0] = __builtin_bit_cast(bf16x8, (u32x4){w[0], w[1], w[2], w[3]});
+    pb[1] = __builtin_bit_cast(bf16x8, (u32x4){w[4], w[5], w[6], w[7]});
+    settle(s, part, first);
+    s = sn;
   };
 
   // ---- the loop -----------------------------------------------------------------------------------------------------
 #define HB_BARRIER() asm volatile("s_barrier" ::: "memory")
-  constexpr int kKeep = 2 * S::kPer * (NS - 3);
-  constexpr int kWait = (kKeep & 15) | ((kKeep >> 4) << 14) | (7 << 4) | (15 << 8);  // vmcnt alone
-  constexpr int kWaitFirst = (2 * S::kPer * (NS - 2) & 15) | ((2 * S::kPer * (NS - 2) >> 4) << 14) | (7 << 4) | (15 << 8);
-  fetch(0);
-#pragma unroll
-  for (int i = 0; i < NS - 1; ++i) {
+#define HB_WAIT_LOADS(N_) __builtin_amdgcn_s_waitcnt(((N_) & 15) | (((N_) >> 4) << 14) | (7 << 4) | (15 << 8))  // vmcnt alone
+  auto stage = [&](int i) { return smem + i % NS * S::kStage; };
+  auto block_k = [&](int b) { return k_at(stage(b / S::kBlocks), b % S::kBlocks); };
+  auto next_tile = [&](int i) {  // of those that are asked for one behind the other, fetch(i) before
     place(i);
 #pragma unroll
     for (int x = 0; x < 2 * S::kPer; ++x) load(i, x);
     fetch(i + 1);
-  }
-  __builtin_amdgcn_s_waitcnt(kWaitFirst);
-  if (careful) clean(0);
-  HB_BARRIER();
-  float top;
-#pragma unroll
-  for (int q = 0; q < KS; ++q) kf[0][q] = one_k(k_at(smem, 0), q);
-  s[0] = (f32x16)(0.f);
-#pragma unroll
-  for (int q = 0; q < KS; ++q) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[0][q], qf[0][q], s[0], 0, 0, 0);
-  top = max16(s[0]);
-  settle(0, begin, top);
-
+  };
+  // In the middle of block kBlocks (i + 1), tile i + kAhead has to have landed, for everybody; and everybody is done with tile
+  // i, whose stage takes tile i + NS.
+  auto turn = [&](int i) {
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): reads of tile i have come back
+    if (i + NS <= n_tiles)
+      HB_WAIT_LOADS(2 * S::kPer * S::kLate);
+    else
+      HB_WAIT_LOADS(0);
+    if (careful) clean(i + S::kAhead);
+    HB_BARRIER();
+    if (i + NS < n_tiles) next_tile(i + NS);
+  };
+  fetch(0);
 #pragma unroll 1
-  for (int i = 0; i < n_tiles; ++i) {
-    const unsigned char *st = smem + (i % NS) * S::kStage, *next = smem + ((i + 1) % NS) * S::kStage;
-    const int k0 = begin + i * KT;
-    const bool mine = i < my_tiles;
+  for (int i = 0; i < NS && i < n_tiles; ++i) next_tile(i);
+  if (NS <= n_tiles)
+    HB_WAIT_LOADS(2 * S::kPer * (NS - S::kAhead));
+  else
+    HB_WAIT_LOADS(0);
+  if (careful)
+    for (int i = 0; i < S::kAhead; ++i) clean(i);
+  HB_BARRIER();
+
+  if (my_tiles > 0) {
 #pragma unroll
-    for (int b = 0; b < S::kBlocks; ++b) {
-      if (b == S::kBlocks - 1) {
-        // Tile i + 1 has landed, for everybody; and everybody is done with tile i - 1, whose stage takes tile i + NS - 1.
-        __builtin_amdgcn_s_waitcnt(kWait);
-        if (careful) clean(i + 1);
-        HB_BARRIER();
-        place(i + NS - 1);
-        fetch(i + NS);
-        if (!mine)
+    for (int q = 0; q < KS; ++q) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(one_k(block_k(0), q), qf[q], q ? s : (f32x16)(0.f), 0, 0, 0);
 #pragma unroll
-          for (int x = 0; x < 2 * S::kPer; ++x) load(i + NS - 1, x);
-      }
-      if (mine) {
-        const int now = b, then = 1 - b;
-        const unsigned char *pk = k_at(b == S::kBlocks - 1 ? next : st, (b + 1) % S::kBlocks), *pv = v_at(st, b);
-        step(std::integral_constant<int, 0>(), kf[now], vf[now], top, [&](int x) {
-          if (x < KS) kf[then][x] = one_k(pk, x);
-          if (b == S::kBlocks - 1 && x < 2 * S::kPer) load(i + NS - 1, x);
+    for (int q = 0; q < KS; ++q) kf[q] = one_k(block_k(1), q);
+    pb[0] = pb[1] = (bf16x8)((__bf16)0.f);
+    mask(begin);
+    // (the first step has no block behind it: it multiplies some values of the first tile's with no weights, and forgets it)
+    step(v_at(stage(0), 0), block_k(2), true, [] {});
+    mask(begin + 32);
+#pragma unroll 1
+    for (int i = 0; i < my_tiles; ++i) {
+      const unsigned char *st = stage(i);
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b) {
+        const int blk = i * S::kBlocks + b + 1;
+        step(v_at(st, b), k_at(stage(i + (b + 3) / S::kBlocks), (b + 3) % S::kBlocks), false, [&] {
+          if (b == S::kBlocks - 1) turn(i);
         });
-        settle(1, k0 + 32 * b, top);
-        step(std::integral_constant<int, 1>(), kf[then], vf[then], top, [&](int x) {
-          if (x < DT) vf[then][x][0] = one_v(pv, x, 0);
-          else if (x < 2 * DT) vf[then][x - DT][1] = one_v(pv, x - DT, 1);
-        });
-        settle(0, k0 + 32 * b + 32, top);
+        mask(begin + 32 * (blk + 1));
       }
     }
+  } else {
+    l = le = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt] = (f32x16)(0.f);
   }
-  // the last weights of the second tile
-#pragma unroll
-  for (int c = 0; c < 2; ++c)
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[1][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[0][dt][c], pb[1][c], o[1][dt], 0, 0, 0);
-  __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // loads past the end land before the workgroup gives up its LDS
+#pragma unroll 1
+  for (int i = my_tiles; i < n_tiles; ++i) turn(i);
 
   // Keys that a row does not see have weight 0 in the products, and 0 times a value that is not finite is no number.  Where
   // that, or anything else, has made results that are not finite, the workgroup does its part once more, `careful`: such
@@ -381,76 +399,76 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
   if (careful) {
     for (int kk = max(begin, all_see + 1); kk < end; ++kk) {  // a row of the prompt: the prefix is seen by all
       const bf16_t *vs = vr + ((size_t)(w.row0 + kk - P) * Hkv + h) * D;
+      if (kk <= sees)
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (kk <= sees[t])
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const float y = bf16_to_f32(vs[32 * dt + 8 * (r >> 2) + 4 * hf + (r & 3)]);
-              if (!(fabsf(y) < __builtin_huge_valf())) o[t][dt][r] += y;
-            }
+          for (int r = 0; r < 16; ++r) {
+            const float y = bf16_to_f32(vs[32 * dt + 8 * (r >> 2) + 4 * hf + (r & 3)]);
+            if (!(fabsf(y) < __builtin_huge_valf())) o[dt][r] += y;
+          }
     }
     break;
   }
-  bool wrong = false;
+  float none = 0.f;  // 0, or no number
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) wrong |= !(fabsf(o[t][dt][r]) < __builtin_huge_valf());
-  if (!__syncthreads_or(wrong && !no_rows)) break;
+    for (int r = 0; r < 16; ++r) none = fmaf(o[dt][r], 0.f, none);
+  // (everybody is behind the last reads of the stages)
+  __syncthreads();
+  if (tid == 0) *(int *)smem = 0;
+  __syncthreads();
+  if (!no_rows && my_tiles > 0 && none != none) *(int *)smem = 1;
+  __syncthreads();
+  if (*(int *)smem == 0) break;
+  __syncthreads();
   }  // careful
 
   // ---- results ------------------------------------------------------------------------------------------------------
   // (the arguments are read again, so that the loop need not keep them in its registers)
-  const PromptArgs &z = again(a);
-  const int zHq = z.d.num_q_heads, zHkv = z.d.num_kv_heads, zG = zHq / zHkv;
+  const args_t z = again();
+  const int zHq = z->d.num_q_heads, zHkv = z->d.num_kv_heads, zG = zHq / zHkv;
+  const float sum = half_sum(l), whole = half_sum(le);
+  const int r0 = wave * 32 + j, row = w.t * S::kRows + r0;
+  if (row >= w.n * zG) return;
+  if (w.parts == 1) {
+    const int token = (int)((uint32_t)row / (uint32_t)zG);
+    const size_t at = (size_t)(w.row0 + token) * zHq + (size_t)h * zG + (row - token * zG);
+    const float inv = 1.f / sum;
+    const global_t<bf16_t> out = (global_t<bf16_t>)z->out;
+    const global_t<float> lse = (global_t<float>)z->lse;
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const float sum = half_sum(l[t]);
-    const int r0 = wave * 64 + 32 * t + j, row = w.t * S::kRows + r0;
-    if (row >= w.n * zG) continue;
-    if (w.parts == 1) {
-      const int token = row / zG;
-      const size_t at = (size_t)(w.row0 + token) * zHq + (size_t)h * zG + (row - token * zG);
-      const float inv = 1.f / sum;
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          u32x2 x;
-          x[0] = pack_bf16(o[t][dt][4 * g] * inv, o[t][dt][4 * g + 1] * inv);
-          x[1] = pack_bf16(o[t][dt][4 * g + 2] * inv, o[t][dt][4 * g + 3] * inv);
-          *(u32x2 *)((bf16_t *)z.out + at * D + 32 * dt + 8 * g + 4 * hf) = x;
-        }
-      if (z.lse && hf == 0) z.lse[at] = (ref[t] + log2f(sum)) * kLn2;
-    } else {
-      const size_t slot = (((size_t)(blockIdx.x / zHkv) * zHkv + h) * z.parts + blockIdx.y) * S::kRows + r0;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          f32x4 x;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) x[r] = o[t][dt][4 * g + r];
-          *(f32x4 *)(z.part_o + slot * D + 32 * dt + 8 * g + 4 * hf) = x;
-        }
-      if (hf == 0) {
-        z.part_ml[slot * 2] = limit[t] == HB_NEG_INF ? HB_NEG_INF : ref[t];
-        z.part_ml[slot * 2 + 1] = sum;
+      for (int g = 0; g < 4; ++g) {
+        u32x2 x;
+        x[0] = pack2(o[dt][4 * g] * inv, o[dt][4 * g + 1] * inv);
+        x[1] = pack2(o[dt][4 * g + 2] * inv, o[dt][4 * g + 3] * inv);
+        *(global_t<u32x2>)(out + at * D + 32 * dt + 8 * g + 4 * hf) = x;
       }
-    }
+    if (LSE && hf == 0) lse[at] = (ref + log2f(whole)) * kLn2;
+  } else {
+    const size_t slot = (((size_t)(blockIdx.x / zHkv) * zHkv + h) * z->parts + blockIdx.y) * S::kRows + r0;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = o[dt][4 * g + r];
+        *(global_t<f32x4>)((global_t<float>)z->part_o + slot * D + 32 * dt + 8 * g + 4 * hf) = x;
+      }
+    if (hf == 0) *(global_t<f32x4>)((global_t<float>)z->part_ml + slot * 4) = (f32x4){sum == 0.f ? HB_NEG_INF : ref, sum, whole, 0.f};
   }
 #undef HB_BARRIER
+#undef HB_WAIT_LOADS
 }
 
 template <int D, int NW, int KT, int NS>
 hipError_t launch(const PromptArgs &a, hipStream_t s) {
   using S = Shape<D, NW, KT, NS>;
-  auto kern = prompt_mfma_kernel<D, NW, KT, NS>;
+  auto kern = a.lse ? prompt_mfma_kernel<D, NW, KT, NS, true> : prompt_mfma_kernel<D, NW, KT, NS, false>;
   hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kLds);
   if (e != hipSuccess) return e;
   kern<<<dim3(a.tiles * a.d.num_kv_heads, a.parts), 64 * NW, S::kLds, s>>>(
@@ -471,7 +489,7 @@ bool prompt_mfma_supports(const hb_attn_desc &d) {
 int32_t prompt_mfma_rows(const hb_attn_desc &) { return 256; }
 
 hipError_t launch_prompt_mfma(const PromptArgs &a, hipStream_t s) {
-  return a.d.head_dim == 128 ? launch<128, 4, 64, 4>(a, s) : launch<64, 4, 64, 4>(a, s);
+  return a.d.head_dim == 128 ? launch<128, 8, 64, 4>(a, s) : launch<64, 8, 64, 4>(a, s);
 }
 
 }  // namespace hb

@@ -83,7 +83,7 @@ static int32_t make_prompt_plan(const hb_attn_desc *d, PromptPlan *p) {
   if (parts > 1) {
     const size_t slots = (size_t)tiles * d->num_kv_heads * parts * p->rows;
     p->ml_offset = round_up(slots * d->head_dim * sizeof(float), 256);
-    p->bytes = p->ml_offset + round_up(slots * 2 * sizeof(float), 256);
+    p->bytes = p->ml_offset + round_up(slots * 4 * sizeof(float), 256);
   }
   return HB_OK;
 }
