@@ -20,6 +20,11 @@ struct PromptArgs {
   float *lse;             // may be null
   float *part_o, *part_ml;  // [tile][kv head][part][row of bm][D], and [..][4]: largest score (base 2), sum that
                             // results are divided by, sum for the log-sum-exp, nothing
+  // [tile]: first row of the sequence in the batch, rows (token, head) in front of the tile's, its rows, parts of its keys.  Where
+  // a tile's keys may be cut, the workgroups of part 0 write it, for the join.
+  struct Head {
+    int32_t row0, first, rows, parts;
+  } *heads;
   int32_t tiles, parts;   // tiles of all sequences at most; parts of a tile's keys at most
   int32_t units;          // (tile, part, kv head) that the launch should come to
 };
@@ -39,36 +44,81 @@ __device__ __forceinline__ int prompt_rows_of(const PromptArgs &a, int b, int &r
   return n;
 }
 
+// What the lanes know about sequences b0 .. b0 + 63
+struct PromptLane {
+  int n, P, row0, tiles;
+};
+template <int BM>
+__device__ __forceinline__ PromptLane prompt_lane(const PromptArgs &a, int b) {
+  const int G = a.d.num_q_heads / a.d.num_kv_heads, cap = a.d.max_blocks_per_seq * a.d.page_size;
+  PromptLane s = {0, 0, 0, 0};
+  if (b < a.d.batch) {
+    s.n = prompt_rows_of(a, b, s.row0);
+    s.P = a.prefix_len ? a.prefix_len[b] : 0;
+    s.P = s.P < 0 ? 0 : s.P > cap ? cap : s.P;
+    s.tiles = (int)(((uint32_t)(s.n * G) + BM - 1) / BM);  // total_nodes * Hq is at most 2^30
+  }
+  return s;
+}
+
+// Length of a part of a tile's keys.  Lane c looks at the length that makes (c + 1) / 8 of `units` parts of all the work, and
+// says when such a plan is done, in keys: whole rounds of the longest part where all are alike, or the work of a unit and a
+// shortest part where they are not (the shortest begin last); and what parts cost beside their keys.
+template <int BM, int KEYS>
+__device__ __forceinline__ float prompt_part(const PromptArgs &a, float work) {
+  // Of a part (its start, its results written), of the join, and of every part to it.  Workgroups go round the dies and
+  // their shader engines in turn, so that a round is full at nine tenths.  One prompt of 1024, 2048, 4096 rows whole 36, 64, 137 us,
+  // cut 52, 71, 186; 512 rows over 32 K in 1, 2, 3, 4 parts 814, 440, 309, 263, in 5 (252 of 256 CUs, nominally) 393, in 9 350;
+  // 64 rows over 8 K in 4, 8, 12, 16 parts 79, 58, 56, 59.
+  constexpr float kCost = 512.f, kJoin = 768.f, kEach = 64.f, kFull = 0.9f;
+  const int lane = threadIdx.x & 63;
+  const float units = (float)a.units, heads = (float)a.d.num_kv_heads;
+  const float each = fmaxf(work * heads * 8.f / (units * (float)(lane + 1)), 2.f * KEYS);
+  float parts = 0.f, longest = 0.f, shortest = 3e38f;
+  float deepest = 1.f;
+  for (int b0 = 0; b0 < a.d.batch; b0 += 64) {
+    const PromptLane s = prompt_lane<BM>(a, b0 + lane);
+    for (unsigned long long left = __ballot(s.tiles > 0); left; left &= left - 1) {
+      const int at = __builtin_ctzll(left);
+      const float tiles = (float)__builtin_amdgcn_readlane(s.tiles, at), P = (float)__builtin_amdgcn_readlane(s.P, at),
+                  n = (float)__builtin_amdgcn_readlane(s.n, at);
+      const float most = (float)a.parts, cuts = fminf(ceilf((P + n) / each), most);
+      parts += 0.5f * tiles * (cuts + fminf(fmaxf(ceilf((P + 0.5f * n) / each), 1.f), most));
+      longest = fmaxf(longest, cuts > 1.f ? fmaxf(each, (P + n) / most) : P + n);
+      shortest = fminf(shortest, (P + n / tiles) / cuts);
+      deepest = fmaxf(deepest, cuts);
+    }
+  }
+  const float rounds = ceilf(parts * heads / (kFull * units)) * longest, mixed = work * heads / units + shortest;
+  const float cost = fmaxf(longest, fminf(rounds, mixed)) + kCost * fmaxf(parts * heads / units, 1.f) + (deepest > 1.f ? kJoin + kEach * deepest : 0.f);
+  float best = cost;
+  for (int m = 32; m; m >>= 1) best = fminf(best, __shfl_xor(best, m, 64));
+  const unsigned long long win = __ballot(cost == best);
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(each), win ? __builtin_ctzll(win) : 0));
+}
+
 // Every lane of the wavefront calls it with the same arguments.  Tiles of a sequence are numbered from its last (which sees
 // the most keys) to its first, so that the longest work begins first.
 template <int BM, int KEYS>
 __device__ __forceinline__ PromptTile prompt_tile(const PromptArgs &a, int tile, int part) {
   const int lane = threadIdx.x & 63, G = a.d.num_q_heads / a.d.num_kv_heads;
-  const int64_t cap = (int64_t)a.d.max_blocks_per_seq * a.d.page_size;
   PromptTile w;
   w.b = w.t = -1;
   w.n = w.P = w.row0 = 0;
   int before = 0;
   float work = 0.f;
   for (int b0 = 0; b0 < a.d.batch; b0 += 64) {
-    const int b = b0 + lane;
-    int n = 0, row0 = 0, P = 0;
-    if (b < a.d.batch) {
-      n = prompt_rows_of(a, b, row0);
-      P = a.prefix_len ? a.prefix_len[b] : 0;
-      P = P < 0 ? 0 : P > cap ? (int)cap : P;
-    }
-    const int tiles = (int)(((uint32_t)(n * G) + BM - 1) / BM);  // total_nodes * Hq is at most 2^30
-    if (a.parts > 1) work += (float)tiles * ((float)P + 0.5f * (float)n);
-    const int upto = scan_lanes(tiles) + before;
+    const PromptLane s = prompt_lane<BM>(a, b0 + lane);
+    if (a.parts > 1) work += (float)s.tiles * ((float)s.P + 0.5f * (float)s.n);
+    const int upto = scan_lanes(s.tiles) + before;
     if (w.b < 0) {
       const unsigned long long hit = __ballot(upto > tile);
       if (hit) {
         const int at = __builtin_ctzll(hit);  // everything from here on is the same in every lane, and known to be
         w.b = b0 + at;
-        w.n = __builtin_amdgcn_readlane(n, at);
-        w.P = __builtin_amdgcn_readlane(P, at);
-        w.row0 = __builtin_amdgcn_readlane(row0, at);
+        w.n = __builtin_amdgcn_readlane(s.n, at);
+        w.P = __builtin_amdgcn_readlane(s.P, at);
+        w.row0 = __builtin_amdgcn_readlane(s.row0, at);
         w.t = __builtin_amdgcn_readlane(upto, at) - 1 - tile;
       }
       before = __builtin_amdgcn_readlane(upto, 63);
@@ -84,9 +134,7 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptArgs &a, int tile,
   w.end = keys;
   if (a.parts > 1) {
     for (int m = 32; m; m >>= 1) work += __shfl_xor(work, m, 64);
-    float each = work * (float)a.d.num_kv_heads / (float)a.units;
-    each = fmaxf(each, (float)(4 * KEYS));
-    const float n = ceilf((float)keys / each);
+    const float n = ceilf((float)keys / prompt_part<BM, KEYS>(a, work));
     w.parts = __builtin_amdgcn_readfirstlane(n < (float)a.parts ? (int)n : a.parts);
     if (w.parts > 1) {
       const int len = ((keys + w.parts - 1) / w.parts + KEYS - 1) / KEYS * KEYS;
@@ -99,11 +147,19 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptArgs &a, int tile,
   return w;
 }
 
+// by every workgroup, before it leaves
+template <int BM>
+__device__ __forceinline__ void prompt_head(const PromptArgs &a, const PromptTile &w, int tile, int h, int part) {
+  if (a.parts > 1 && h == 0 && part == 0 && threadIdx.x == 0) {
+    const int G = a.d.num_q_heads / a.d.num_kv_heads, first = w.t * BM;
+    a.heads[tile] = w.b < 0 ? PromptArgs::Head{0, 0, 0, 1} : PromptArgs::Head{w.row0, first, min(BM, w.n * G - first), w.parts};
+  }
+}
+
 bool prompt_mfma_supports(const hb_attn_desc &d);
 int32_t prompt_mfma_rows(const hb_attn_desc &d);  // of a tile
 hipError_t launch_prompt_mfma(const PromptArgs &a, hipStream_t s);
-// for tiles of `rows` rows whose parts begin at multiples of `keys`
-hipError_t launch_prompt_join(const PromptArgs &a, int32_t rows, int32_t keys, hipStream_t s);
+hipError_t launch_prompt_join(const PromptArgs &a, int32_t rows, hipStream_t s);  // for tiles of `rows` rows
 constexpr int kPromptAnyRows = 64;
 hipError_t launch_prompt_any(const PromptArgs &a, hipStream_t s);
 

@@ -45,6 +45,14 @@ __device__ __forceinline__ void load8(const bf16_t *p, float (&x)[8]) {
 template <int DP>
 constexpr int any_lds_floats = 2 * kAnyKeys * (DP + 4) + 4;
 
+__device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
+  *(f32x4 *)p = (f32x4){x[0], x[1], x[2], x[3]};
+  *(f32x4 *)(p + 4) = (f32x4){x[4], x[5], x[6], x[7]};
+}
+__device__ __forceinline__ void store8(bf16_t *p, const float (&x)[8]) {
+  *(u32x4 *)p = (u32x4){pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+}
+
 template <typename T, int DP, int NW>
 __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const PromptTile &w, int h, int first, size_t slot0, float *lds) {
   constexpr int kKeys = kAnyKeys, kRow = DP + 4, kTiles = DP / 16, kSteps = DP / 4, kPieces = DP / 8;

@@ -84,7 +84,7 @@ template <typename T>
 using global_t = __attribute__((address_space(1))) T *;
 
 template <int D, int NW, int KT, int NS, bool LSE>
-__global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, int page_shift, const bf16_t *__restrict__ kr,
+__global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, int page_shift, const bf16_t *__restrict__ kr,
                                                                  const bf16_t *__restrict__ vr, const bf16_t *__restrict__ kp,
                                                                  const bf16_t *__restrict__ vp, const int32_t *__restrict__ block_table) {
   using S = Shape<D, NW, KT, NS>;
@@ -95,6 +95,7 @@ __global__ __launch_bounds__(64 * NW, 1) void prompt_mfma_kernel(PromptArgs a, i
   const int Hkv = a.d.num_kv_heads, Hq = a.d.num_q_heads, G = Hq / Hkv;
   const int tile_id = blockIdx.x / (uint32_t)Hkv, h = blockIdx.x - tile_id * Hkv;
   const PromptTile w = prompt_tile<S::kRows, KT>(a, tile_id, blockIdx.y);
+  prompt_head<S::kRows>(a, w, tile_id, h, blockIdx.y);
   if (w.t < 0) return;
   const int P = w.P, begin = w.begin, end = w.end, rows_all = w.n * G;
 
@@ -475,7 +476,7 @@ hipError_t launch(const PromptArgs &a, hipStream_t s) {
       a, __builtin_ctz(a.d.page_size), (const bf16_t *)a.k, (const bf16_t *)a.v, (const bf16_t *)a.k_pool, (const bf16_t *)a.v_pool,
       a.block_table);
   e = hipGetLastError();
-  if (e == hipSuccess && a.parts > 1) e = launch_prompt_join(a, S::kRows, KT, s);
+  if (e == hipSuccess && a.parts > 1) e = launch_prompt_join(a, S::kRows, s);
   return e;
 }
 

@@ -51,7 +51,7 @@ struct PromptPlan {
   bool mfma;
   int32_t rows;  // of a tile
   int32_t tiles, parts, units;
-  size_t ml_offset, bytes;
+  size_t ml_offset, heads_offset, bytes;
 };
 
 static int32_t make_prompt_plan(const hb_attn_desc *d, PromptPlan *p) {
@@ -69,21 +69,22 @@ static int32_t make_prompt_plan(const hb_attn_desc *d, PromptPlan *p) {
   if (d->max_prefix_len_hint > 0 && d->max_prefix_len_hint < span) span = d->max_prefix_len_hint;
   span += d->total_nodes;
   p->rows = p->mfma ? prompt_mfma_rows(*d) : kPromptAnyRows;
-  p->units = p->mfma ? 256 : 1024;
-  const int64_t least = p->mfma ? 256 : 128;  // keys of a part
+  p->units = p->mfma ? 256 : 512;
+  const int64_t least = p->mfma ? 256 : 64;  // keys of a part, about
   const int64_t tiles = d->total_nodes * G / p->rows + (d->batch < d->total_nodes ? d->batch : d->total_nodes);
   p->tiles = (int32_t)tiles;
   int64_t parts = d->num_splits;
-  if (parts == 0) parts = tiles > 0 ? 2 * p->units / (tiles * d->num_kv_heads) : 1;
-  if (parts > (span + least - 1) / least) parts = (span + least - 1) / least;
+  if (parts == 0) parts = tiles > 0 ? 2 * p->units / (tiles * d->num_kv_heads) : 1;  // more find nothing to do, at some cost
+  if (parts > span / least) parts = span / least;
   if (parts > 256) parts = 256;
   if (parts < 1) parts = 1;
   p->parts = (int32_t)parts;
-  p->ml_offset = p->bytes = 0;
+  p->ml_offset = p->heads_offset = p->bytes = 0;
   if (parts > 1) {
     const size_t slots = (size_t)tiles * d->num_kv_heads * parts * p->rows;
     p->ml_offset = round_up(slots * d->head_dim * sizeof(float), 256);
-    p->bytes = p->ml_offset + round_up(slots * 4 * sizeof(float), 256);
+    p->heads_offset = p->ml_offset + round_up(slots * 4 * sizeof(float), 256);
+    p->bytes = p->heads_offset + round_up((size_t)tiles * sizeof(PromptArgs::Head), 256);
   }
   return HB_OK;
 }
@@ -217,8 +218,8 @@ int32_t hb_prompt_attn(const hb_attn_desc *desc, const void *q, const void *k_ro
     if (misaligned(workspace, 256)) return fail(HB_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   }
   PromptArgs a = {*desc, q, k_rows, v_rows, k_pool, v_pool, block_table, prefix_len, row_offset, out, lse,
-                  p.bytes ? (float *)workspace : nullptr, p.bytes ? (float *)((char *)workspace + p.ml_offset) : nullptr, p.tiles,
-                  p.parts, p.units};
+                  p.bytes ? (float *)workspace : nullptr, p.bytes ? (float *)((char *)workspace + p.ml_offset) : nullptr,
+                  p.bytes ? (PromptArgs::Head *)((char *)workspace + p.heads_offset) : nullptr, p.tiles, p.parts, p.units};
   if (p.mfma)
     HB_HIP_TRY(launch_prompt_mfma(a, (hipStream_t)stream));
   else
