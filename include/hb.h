@@ -737,7 +737,7 @@ size_t hb_prompt_attn_workspace_bytes(const hb_attn_desc *desc);
  *                bias_offset[b] .. bias_offset[b+1] - 1; a token given twice has both, added in their order.  n_bias 0: none
  *   mask         device uint32 [num_masks, ceil(V / 32)], bit v % 32 of word v / 32: the token is allowed; or NULL
  *   mask_row     device int32 [T]: the mask of each row, outside [0, num_masks): none; or NULL: row t's is mask t
- *   workspace    device, hb_rules_probs_workspace_bytes(T, V) bytes, 16-byte aligned, overwritten
+ *   workspace    device, hb_rules_probs_workspace_bytes(T, V) bytes, 16-byte aligned, overwritten; may be NULL when that is 0
  *   tokens       device int32 [n]; row_offset device int32 [B+1], or NULL: n / B of every sequence (out_tokens [B, max_path])
  * logits, out, probs, counts, rules and mask are 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED (dtype,
  * max_nodes_per_tree > 64, V > 2^30), WORKSPACE, DEVICE.  T == 0 or B == 0 is a no-op.

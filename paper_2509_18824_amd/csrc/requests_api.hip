@@ -268,12 +268,12 @@ int32_t hb_rules_probs(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, int
                            probs, &a);
   if (rc || T == 0 || B == 0) return rc;
   const size_t need = hb_rules_probs_workspace_bytes(T, V);
-  if (!workspace || workspace_bytes < need)
+  if (need && (!workspace || workspace_bytes < need))
     return fail(HB_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
-  if (misaligned(workspace, 16)) return fail(HB_ERR_WORKSPACE, "workspace must be 16-byte aligned");
+  if (need && misaligned(workspace, 16)) return fail(HB_ERR_WORKSPACE, "workspace must be 16-byte aligned");
   const int64_t el = dtype == HB_F32 ? 4 : 2;
   if ((rc = check_apart("probs", {probs, (int64_t)T * V * 4}, {{logits, (int64_t)T * V * el}}))) return rc;
-  a.stats = (float *)workspace;
+  a.stats = need ? (float *)workspace : nullptr;
   HB_HIP_TRY(launch_rules_probs(a, (hipStream_t)stream));
   return HB_OK;
 }

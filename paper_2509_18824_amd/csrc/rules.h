@@ -19,7 +19,7 @@ struct RulesArgs {
   const int32_t *mask_row;
   void *out;
   float *stats;  // [rows][parts][4]: largest, sum, its token (as an integer), nothing
-  int32_t parts, chunk;  // of a row: workgroups, and tokens of each
+  int32_t parts, chunk;  // of a row: workgroups (0: one, without stats), and tokens of each
 };
 int32_t rules_parts(int32_t rows, int32_t V, int32_t *chunk);
 hipError_t launch_rules_logits(RulesArgs a, hipStream_t s);
