@@ -120,7 +120,7 @@ static int32_t check_rules(int32_t dtype, int32_t B, int32_t max_nodes, int32_t 
   if (misaligned(logits, 16) || misaligned(out, 16) || misaligned(r.counts, 16) || misaligned(r.rules, 16) || misaligned(r.mask, 16))
     return fail(HB_ERR_INVALID_ARG, "logits, out, counts, rules and masks must be 16-byte aligned");
   *a = {dtype, B, max_nodes, T, V, r.n_bias, r.num_masks, logits, r.node_offset, r.parent, r.draft_ids, r.counts, r.rules,
-        r.n_bias > 0 ? r.bias_offset : nullptr, r.bias_id, r.bias_value, r.mask, r.mask_row, (void *)out, nullptr, 0, 0};
+        r.n_bias > 0 ? r.bias_offset : nullptr, r.bias_id, r.bias_value, r.mask, r.mask_row, (void *)out, nullptr, nullptr, 0, 0};
   return HB_OK;
 }
 
@@ -254,7 +254,9 @@ int32_t hb_rules_logits(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, in
 size_t hb_rules_probs_workspace_bytes(int32_t T, int32_t V) {
   if (T <= 0 || V <= 0 || V > 1 << 30) return 0;
   int32_t chunk;
-  return (size_t)T * rules_parts(T, V, &chunk) * 16;
+  const int32_t parts = rules_parts(T, V, &chunk);
+  if (parts) return (size_t)T * parts * 16;
+  return (size_t)(T / 4) * (((size_t)V + 31) / 32) * 4;  // marks of at most so many sequences: with more, there are none
 }
 
 int32_t hb_rules_probs(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, int32_t T, int32_t V, const void *logits,
@@ -273,7 +275,11 @@ int32_t hb_rules_probs(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, int
   if (need && misaligned(workspace, 16)) return fail(HB_ERR_WORKSPACE, "workspace must be 16-byte aligned");
   const int64_t el = dtype == HB_F32 ? 4 : 2;
   if ((rc = check_apart("probs", {probs, (int64_t)T * V * 4}, {{logits, (int64_t)T * V * el}}))) return rc;
-  a.stats = need ? (float *)workspace : nullptr;
+  int32_t chunk;
+  if (rules_parts(T, V, &chunk))
+    a.stats = (float *)workspace;
+  else if (counts && rules_marks(B, T))
+    a.marks = (uint32_t *)workspace;
   HB_HIP_TRY(launch_rules_probs(a, (hipStream_t)stream));
   return HB_OK;
 }

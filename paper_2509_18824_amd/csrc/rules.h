@@ -18,9 +18,11 @@ struct RulesArgs {
   const uint32_t *mask;
   const int32_t *mask_row;
   void *out;
+  uint32_t *marks;  // null, or [batch][(V + 31) / 32]: where rows have a workgroup each, and are several to a sequence
   float *stats;  // [rows][parts][4]: largest, sum, its token (as an integer), nothing
   int32_t parts, chunk;  // of a row: workgroups (0: one, without stats), and tokens of each
 };
+bool rules_marks(int32_t B, int32_t T);
 int32_t rules_parts(int32_t rows, int32_t V, int32_t *chunk);
 hipError_t launch_rules_logits(RulesArgs a, hipStream_t s);
 hipError_t launch_rules_probs(RulesArgs a, hipStream_t s);

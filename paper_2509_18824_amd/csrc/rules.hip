@@ -7,10 +7,10 @@
 //
 // A workgroup has a row, or a chunk of one.  Few tokens have anything to them but their logit and their mask: those with a
 // count, those on the path and those with a bias.  It finds them first (one pass over the counts, which all nodes of a tree
-// share), marks them in a bitmap in LDS and puts what is to be done to each into a table there, in the order of the tokens, so that
-// a token's place is the number of marks in front of it.  What is then done for every token is little, and a wavefront that
-// meets marks takes one of each lane's at a time.  (With the penalties' code at each of a thread's eight tokens the loop was
-// twenty times as long: 16 trees of 60 nodes over 152064 tokens 472 us.)
+// share) and marks them in a bitmap in LDS.  The row is then gone through without them, eight tokens a thread and little to do
+// for each, and they are done behind it, a thread each.  With the penalties' code at each of a thread's eight tokens 16 trees of
+// 60 nodes over 152064 tokens took 472 us, with a loop over the marks that a wavefront meets 331 (one in a hundred tokens is
+// marked: nearly every wavefront met some), so 2xx.
 // In float32, in the order that is written above, without contraction: two sides that follow it agree about which z is the
 // largest.
 #include "rules.h"
@@ -23,6 +23,7 @@ namespace {
 #pragma clang fp contract(off)
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSplit = 256, kStep = kSplit * 8, kMostChunk = 32768, kBiases = 1024;  // threads of a workgroup that has a chunk of a row
@@ -36,20 +37,18 @@ struct Row {
   const int32_t *counts;     // of its sequence, or null
   const uint8_t *mask;       // bytes of its mask, or null
   int path, bias0, biases;   // tokens on the path; biases
-  const uint32_t *marked;    // a bit for every token of the chunk
-  const uint16_t *before;    // marks in front of every 32 (at most 65535)
+  int marks, first;          // marked tokens of the chunk, and those of the threads in front of this one
 };
 
-extern __shared__ uint32_t chunk_lds[];  // marked and before
+extern __shared__ uint32_t marked_lds[];  // a bit for every token of the chunk
 
-// What is done to marked tokens, for the first `kEntries` of them; the others are looked up again
 template <int kThreads>
 struct RowLds {
-  static constexpr int kEntries = kThreads * 4;
-  float less[kEntries], more[kEntries];  // the penalty that is subtracted, and the bias
-  uint8_t seen[kEntries];
+  static constexpr int kSome = 2 * kThreads;
+  int32_t some[kSome];  // marked tokens, so many at a time, and
+  float value[kSome];   // their values
   int32_t path[64];
-  int32_t bias_id[kBiases];
+  alignas(16) int32_t bias_id[kBiases];
   float bias_value[kBiases];
   int32_t sums[kThreads / 64];
   int32_t found[2];
@@ -64,13 +63,19 @@ __device__ __forceinline__ void look_up(const RulesArgs &a, const Row &r, const 
   seen = c > 0 || (had & kPromptFlag);
   less = (c > 0 ? r.presence : 0.f) + r.frequency * (float)c;
   more = 0.f;
-  for (int i = 0; i < r.biases; ++i) {
-    const int id = i < kBiases ? s.bias_id[i] : a.bias_id[r.bias0 + i];
-    if (id == v) more += i < kBiases ? s.bias_value[i] : a.bias_value[r.bias0 + i];
+  const int here = min(r.biases, kBiases);
+  for (int i = 0; i < here; i += 4) {  // (the list is filled up with tokens that there are not)
+    const int4 id = *(const int4 *)&s.bias_id[i];
+    if (id.x == v) more += s.bias_value[i];
+    if (id.y == v) more += s.bias_value[i + 1];
+    if (id.z == v) more += s.bias_value[i + 2];
+    if (id.w == v) more += s.bias_value[i + 3];
   }
+  for (int i = here; i < r.biases; ++i)
+    if (a.bias_id[r.bias0 + i] == v) more += a.bias_value[r.bias0 + i];
 }
 
-// The row's rules, and the marks of its chunk [v0, v1).  Every one of kThreads threads calls it; ends with a barrier.
+// The row's rules, and the marks of its chunk [v0, v1), which nobody changes behind it.  Every one of kThreads threads calls it.
 template <int kThreads>
 __device__ __forceinline__ Row row_of(const RulesArgs &a, int t, int v0, int v1, RowLds<kThreads> &s) {
   const int tid = threadIdx.x, lane = tid & 63;
@@ -116,9 +121,10 @@ __device__ __forceinline__ Row row_of(const RulesArgs &a, int t, int v0, int v1,
     }
   }
   const int words = (v1 - v0 + 31) / 32;
-  uint32_t *marked = chunk_lds;
-  uint16_t *before = (uint16_t *)(chunk_lds + words);
-  for (int i = tid; i < words; i += kThreads) marked[i] = 0;
+  uint32_t *marked = marked_lds;
+  // where many rows have the same counts, their marks have been made already
+  const bool made = a.marks && r.counts;
+  for (int i = tid; i < words; i += kThreads) marked[i] = made ? a.marks[(size_t)r.b * ((a.V + 31) / 32) + v0 / 32 + i] : 0;
   if (tid < 64) {
     // the path: parents and tokens a lane each, walked by reading lanes
     int n = 0;
@@ -137,9 +143,9 @@ __device__ __forceinline__ Row row_of(const RulesArgs &a, int t, int v0, int v1,
     }
     if (lane == 0) s.found[1] = n;
   }
-  for (int i = tid; i < min(r.biases, kBiases); i += kThreads) {
-    s.bias_id[i] = a.bias_id[r.bias0 + i];
-    s.bias_value[i] = a.bias_value[r.bias0 + i];
+  for (int i = tid; i < min((r.biases + 3) & ~3, kBiases); i += kThreads) {
+    s.bias_id[i] = i < r.biases ? a.bias_id[r.bias0 + i] : -1;
+    s.bias_value[i] = i < r.biases ? a.bias_value[r.bias0 + i] : 0.f;
   }
   __syncthreads();
   r.path = s.found[1];
@@ -148,7 +154,7 @@ __device__ __forceinline__ Row row_of(const RulesArgs &a, int t, int v0, int v1,
   };
   if (tid < r.path) mark(s.path[tid]);
   for (int i = tid; i < r.biases; i += kThreads) mark(i < kBiases ? s.bias_id[i] : a.bias_id[r.bias0 + i]);
-  if (r.counts) {
+  if (r.counts && !made) {
     if (a.V % 4 == 0) {
 #pragma unroll 4
       for (int v = v0 + tid * 4; v < v1; v += kThreads * 4) {
@@ -162,146 +168,133 @@ __device__ __forceinline__ Row row_of(const RulesArgs &a, int t, int v0, int v1,
     }
   }
   __syncthreads();
-  // marks in front of every word: a thread has a run of words
-  const int each = (words + kThreads - 1) / kThreads, w0 = min(tid * each, words), w1 = min(w0 + each, words);
+  // a thread has every kThreads-th word: marks come in heaps
   int mine = 0;
-  for (int i = w0; i < w1; ++i) mine += __popc(marked[i]);
+  for (int i = tid; i < words; i += kThreads) mine += __popc(marked[i]);
   int upto = scan_lanes(mine);
   if (lane == 63) s.sums[tid >> 6] = upto;
   __syncthreads();
-  int total = 0;
+  r.marks = 0;
   for (int w = 0; w < kThreads / 64; ++w) {
     if (w < tid >> 6) upto += s.sums[w];
-    total += s.sums[w];
+    r.marks += s.sums[w];
   }
-  int at = upto - mine;
-  for (int i = w0; i < w1; ++i) {
-    before[i] = (uint16_t)min(at, 65535);
-    for (uint32_t m = marked[i]; m; m &= m - 1, ++at)
-      if (at < RowLds<kThreads>::kEntries) s.more[at] = __int_as_float(v0 + 32 * i + __ffs(m) - 1);  // the token, for the next step
-  }
-  r.marked = marked;
-  r.before = before;
-  __syncthreads();
-  for (int i = tid; i < min(total, RowLds<kThreads>::kEntries); i += kThreads) {
-    bool seen;
-    float less, more;
-    look_up(a, r, s, __float_as_int(s.more[i]), seen, less, more);
-    s.seen[i] = seen;
-    s.less[i] = less;
-    s.more[i] = more;
-  }
-  __syncthreads();
+  r.first = upto - mine;
   return r;
 }
 
-// Eight tokens' values from v on; `allowed`: a bit each
-template <int kThreads>
-__device__ __forceinline__ void apply(const RulesArgs &a, const Row &r, const RowLds<kThreads> &s, int v, int v0, uint32_t allowed, float (&z)[8]) {
-  const int rel = v - v0;
-  const uint32_t word = r.marked[rel >> 5];
-  uint32_t rare = word >> (rel & 31) & 0xffu;
-  while (rare) {
-    const int e = __ffs(rare) - 1;
-    rare &= rare - 1;
-    float x = z[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) x = e == i ? z[i] : x;
-    const int at = r.before[rel >> 5] + __popc(word & ((1u << ((rel & 31) + e)) - 1u));
-    bool seen;
-    float less, more;
-    if (at < RowLds<kThreads>::kEntries) {
-      seen = s.seen[at];
-      less = s.less[at];
-      more = s.more[at];
-    } else {
-      look_up(a, r, s, v + e, seen, less, more);
-    }
-    if (seen) x = x > 0.f ? x / r.repetition : x * r.repetition;
-    x = x - less;
-    x = x + more;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = e == i ? x : z[i];
+// f(v, its adjusted value) for the marked tokens of the chunk [v0, v1).  Every thread calls it; it begins with a barrier.
+// again: it has been called before, with the same arguments.
+template <typename T, int kThreads, typename F>
+__device__ __forceinline__ void each_marked(const RulesArgs &a, const Row &r, RowLds<kThreads> &s, int t, int v0, int v1, bool again, F f) {
+  constexpr int kSome = RowLds<kThreads>::kSome;
+  const int words = (v1 - v0 + 31) / 32;
+  if (again && r.marks <= kSome) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < r.marks; i += kThreads) f(s.some[i], s.value[i]);
+    return;
   }
-  // -infinity where the bit is not set; and what is no number gives way to it
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t keep = (uint32_t)((int32_t)(allowed << (31 - e)) >> 31);
-    z[e] = fmaxf(__uint_as_float((__float_as_uint(z[e]) & keep) | (0xff800000u & ~keep)), -HB_INF);
+  for (int from = 0; from < r.marks; from += kSome) {
+    __syncthreads();
+    int at = r.first - from;
+    for (int i = threadIdx.x; i < words && at < kSome; i += kThreads)
+      for (uint32_t m = marked_lds[i]; m; m &= m - 1, ++at)
+        if (at >= 0 && at < kSome) s.some[at] = v0 + 32 * i + __ffs(m) - 1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < min(r.marks - from, kSome); i += kThreads) {
+      const int v = s.some[i];
+      float z = load_f32((const T *)a.logits + (size_t)t * a.V + v);
+      const uint32_t bits = r.mask ? r.mask[v >> 3] : 0xffu;
+      bool seen;
+      float less, more;
+      look_up(a, r, s, v, seen, less, more);
+      if (seen) z = z > 0.f ? z / r.repetition : z * r.repetition;
+      z = z - less;
+      z = z + more;
+      z = (bits >> (v & 7) & 1) && z == z ? z : -HB_INF;
+      s.value[i] = z;
+      f(v, z);
+    }
   }
 }
 
-// Eight tokens' logits and bits as they lie in memory; WHOLE: rows are a multiple of eight long, and pieces aligned
+// -infinity where the bit of `keep` is not set; and what is no number gives way to it
+__device__ __forceinline__ void keep_of(uint32_t keep, float (&z)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t k = (uint32_t)((int32_t)(keep << (31 - e)) >> 31);
+    z[e] = fmaxf(__uint_as_float((__float_as_uint(z[e]) & k) | (0xff800000u & ~k)), -HB_INF);
+  }
+}
+
+// Four tokens' logits as they lie in memory; WHOLE: rows are a multiple of four long, and pieces aligned
 template <typename T, bool WHOLE>
 struct Piece {
-  T x[8];
+  T x[4];
 };
 template <>
 struct Piece<float, true> {
-  f32x4 x[2];
+  f32x4 x;
 };
 template <>
 struct Piece<bf16_t, true> {
-  u32x4 x;
+  u32x2 x;
 };
 template <typename T>
 __device__ __forceinline__ void load_piece(const T *p, int n, Piece<T, false> &y) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) y.x[e] = e < n ? p[e] : T(0);
+  for (int e = 0; e < 4; ++e) y.x[e] = e < n ? p[e] : T(0);
 }
-__device__ __forceinline__ void load_piece(const float *p, int, Piece<float, true> &y) {
-  y.x[0] = *(const f32x4 *)p;
-  y.x[1] = *(const f32x4 *)(p + 4);
-}
-__device__ __forceinline__ void load_piece(const bf16_t *p, int, Piece<bf16_t, true> &y) { y.x = *(const u32x4 *)p; }
+__device__ __forceinline__ void load_piece(const float *p, int, Piece<float, true> &y) { y.x = *(const f32x4 *)p; }
+__device__ __forceinline__ void load_piece(const bf16_t *p, int, Piece<bf16_t, true> &y) { y.x = *(const u32x2 *)p; }
 template <typename T>
-__device__ __forceinline__ void widen(const Piece<T, false> &y, int n, float (&z)[8]) {
+__device__ __forceinline__ void widen(const Piece<T, false> &y, int n, float (&z)[4]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) z[e] = e < n ? load_f32(&y.x[e]) : -HB_INF;
+  for (int e = 0; e < 4; ++e) z[e] = e < n ? load_f32(&y.x[e]) : -HB_INF;
 }
-__device__ __forceinline__ void widen(const Piece<float, true> &y, int, float (&z)[8]) {
+__device__ __forceinline__ void widen(const Piece<float, true> &y, int, float (&z)[4]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) z[e] = y.x[e / 4][e % 4];
+  for (int e = 0; e < 4; ++e) z[e] = y.x[e];
 }
-__device__ __forceinline__ void widen(const Piece<bf16_t, true> &y, int, float (&z)[8]) {
+__device__ __forceinline__ void widen(const Piece<bf16_t, true> &y, int, float (&z)[4]) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < 2; ++e) {
     z[2 * e] = __uint_as_float(y.x[e] << 16);
     z[2 * e + 1] = __uint_as_float(y.x[e] & 0xffff0000u);
   }
 }
 
 template <bool WHOLE>
-__device__ __forceinline__ void store_eight(float *p, int n, const float (&z)[8]) {
+__device__ __forceinline__ void store_four(float *p, int n, const float (&z)[4]) {
   if (WHOLE) {
     *(f32x4 *)p = (f32x4){z[0], z[1], z[2], z[3]};
-    *(f32x4 *)(p + 4) = (f32x4){z[4], z[5], z[6], z[7]};
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < 4; ++e)
       if (e < n) p[e] = z[e];
   }
 }
 template <bool WHOLE>
-__device__ __forceinline__ void store_eight(bf16_t *p, int n, const float (&z)[8]) {
+__device__ __forceinline__ void store_four(bf16_t *p, int n, const float (&z)[4]) {
   if (WHOLE) {
-    *(u32x4 *)p = (u32x4){pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]), pack_bf16(z[4], z[5]), pack_bf16(z[6], z[7])};
+    *(u32x2 *)p = (u32x2){pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3])};
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < 4; ++e)
       if (e < n) p[e] = f32_to_bf16(z[e]);
   }
 }
 
-// What row t has to tokens v0 .. v1 - 1, eight at a time: f(v, adjusted values).  The logits of the next two turns are asked for
-// before this one's are worked on.
-template <typename T, bool WHOLE, int kThreads, typename F>
-__device__ __forceinline__ void each_eight(const RulesArgs &a, const Row &r, const RowLds<kThreads> &s, int t, int v0, int v1, F f) {
-  constexpr int kTurn = kThreads * 8, kDeep = 2;
+// Tokens v0 .. v1 - 1 four at a time (what a wavefront stores is whole lines then: with eight, in two halves of 16 bytes, half the
+// requests to L2 were for parts of one): f(v, values), those of marked tokens -infinity, or (MARKED) as they are.  The logits
+// of the next turns are asked for before this one's are worked on.
+template <typename T, bool WHOLE, bool MARKED, int kThreads, typename F>
+__device__ __forceinline__ void each_four(const RulesArgs &a, const Row &r, const RowLds<kThreads> &, int t, int v0, int v1, F f) {
+  constexpr int kTurn = kThreads * 4, kDeep = 4;
   const T *row = (const T *)a.logits + (size_t)t * a.V;
   Piece<T, WHOLE> y[kDeep];
   uint32_t allowed[kDeep];
-  const int first = v0 + (int)threadIdx.x * 8;
+  const int first = v0 + (int)threadIdx.x * 4;
   auto ask = [&](int v, int at) {
     if (v >= v1) return;
     load_piece(row + v, a.V - v, y[at]);
@@ -314,11 +307,11 @@ __device__ __forceinline__ void each_eight(const RulesArgs &a, const Row &r, con
     for (int i = 0; i < kDeep; ++i) {
       const int at = v + i * kTurn;
       if (at >= v1) break;
-      float z[8];
+      float z[4];
       widen(y[i], a.V - at, z);
-      const uint32_t bits = allowed[i];
+      const uint32_t bits = allowed[i] >> (at & 4), marked = marked_lds[(at - v0) >> 5] >> ((at - v0) & 31);
       ask(at + kDeep * kTurn, i);
-      apply(a, r, s, at, v0, bits, z);
+      keep_of(MARKED ? bits | marked : bits & ~marked, z);
       f(at, z);
     }
 }
@@ -329,108 +322,141 @@ __global__ __launch_bounds__(kSplit) void rules_logits_kernel(RulesArgs a) {
   const int t = blockIdx.x, v0 = blockIdx.y * a.chunk, v1 = min(a.V, v0 + a.chunk);
   const Row r = row_of<kSplit>(a, t, v0, v1, s);
   if (r.b < 0) return;
-  each_eight<T, WHOLE>(a, r, s, t, v0, v1, [&](int v, float (&z)[8]) { store_eight<WHOLE>((T *)a.out + (size_t)t * a.V + v, a.V - v, z); });
+  T *out = (T *)a.out + (size_t)t * a.V;
+  each_four<T, WHOLE, true>(a, r, s, t, v0, v1, [&](int v, float (&z)[4]) { store_four<WHOLE>(out + v, a.V - v, z); });
+  // (which may have been written where the logits are: marked ones as they were)
+  each_marked<T>(a, r, s, t, v0, v1, false, [&](int v, float z) { store_f32(out + v, z); });
 }
 
-// largest value, the lowest token that has it, and the sum of 2^((z - largest) k)
+// What is known of some tokens of a row: of a greedy one (k = 0) the largest value and the lowest token that has it; of the
+// others the largest value, or the lowest that there is, and the sum of 2^((z - largest) k), 0 where nothing is left
 struct Stat {
   float top, sum;
   int token;
 };
+constexpr float kLowest = -3.402823466e38f;
 __device__ __forceinline__ float weight_of(float z, float top, float k) {
   const float d = z == top ? 0.f : z - top;  // also where both are infinite
   return z > -HB_INF ? __builtin_amdgcn_exp2f(d * k) : 0.f;
 }
-// eight values' weights: plainly where the largest is finite and k above 0 (-infinity gives 0 then)
-__device__ __forceinline__ void weigh(float (&z)[8], float top, float k, bool plain) {
+// four values' weights.  Plainly they are what they should be for every finite `top` and k > 0: -infinity gives 0.
+__device__ __forceinline__ void weigh(float (&z)[4], float top, float k) {
+  if (__any(!(top < HB_INF)) || !(k > 0.f)) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) z[e] = plain ? __builtin_amdgcn_exp2f((z[e] - top) * k) : weight_of(z[e], top, k);
+    for (int e = 0; e < 4; ++e) z[e] = weight_of(z[e], top, k);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = __builtin_amdgcn_exp2f((z[e] - top) * k);
+  }
 }
-__device__ __forceinline__ Stat joined(const Stat x, const Stat y, float k) {
+__device__ __forceinline__ Stat joined(const Stat x, const Stat y, float k, bool greedy) {
   Stat j;
   const bool second = y.top > x.top || (y.top == x.top && y.token < x.token);
   j.top = second ? y.top : x.top;
   j.token = second ? y.token : x.token;
-  j.sum = x.sum * weight_of(x.top, j.top, k) + y.sum * weight_of(y.top, j.top, k);
+  j.sum = greedy ? 0.f : x.sum * weight_of(x.top, j.top, k) + y.sum * weight_of(y.top, j.top, k);
   return j;
 }
-__device__ __forceinline__ Stat joined_lanes(Stat x, float k) {
+__device__ __forceinline__ Stat joined_lanes(Stat x, float k, bool greedy) {
   for (int m = 32; m; m >>= 1) {
     Stat y;
     y.top = __shfl_xor(x.top, m, 64);
     y.sum = __shfl_xor(x.sum, m, 64);
     y.token = __shfl_xor(x.token, m, 64);
-    x = joined(x, y, k);
+    x = joined(x, y, k, greedy);
   }
   return x;
 }
+__device__ __forceinline__ Stat nothing_of(bool greedy) { return {greedy ? -HB_INF : kLowest, 0.f, 0x7fffffff}; }
+// (the same in every lane, and known to be)
 __device__ __forceinline__ float slope_of(const Row &r) {
-  return r.temperature > 0.f ? fminf(kLog2e / r.temperature, 3e38f) : 0.f;
+  const float k = fminf(kLog2e / r.temperature, 3e38f);
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(r.temperature > 0.f ? k : 0.f)));
 }
+__device__ __forceinline__ bool greedy_of(const Row &r) { return __builtin_amdgcn_readfirstlane(!(r.temperature > 0.f)); }
 
 // Of tokens v0 .. v1 - 1, over all of the workgroup's kThreads threads
 template <typename T, bool WHOLE, int kThreads>
-__device__ __forceinline__ Stat stat_of(const RulesArgs &a, const Row &r, const RowLds<kThreads> &s, int t, int v0, int v1, float k) {
+__device__ __forceinline__ Stat stat_of(const RulesArgs &a, const Row &r, RowLds<kThreads> &s, int t, int v0, int v1, float k) {
   __shared__ Stat waves[kThreads / 64];
-  Stat mine = {-HB_INF, 0.f, 0x7fffffff};
-  each_eight<T, WHOLE>(a, r, s, t, v0, v1, [&](int v, float (&z)[8]) {
-    float top = z[0];
+  const bool greedy = greedy_of(r);
+  Stat mine = nothing_of(greedy);
+  if (greedy)
+    each_four<T, WHOLE, false>(a, r, s, t, v0, v1, [&](int v, float (&z)[4]) {
+      float top = z[0];
 #pragma unroll
-    for (int e = 1; e < 8; ++e) top = fmaxf(top, z[e]);
-    if (top > mine.top) {  // seldom, after the first few
-      mine.sum *= weight_of(mine.top, top, k);
-      mine.top = top;
+      for (int e = 1; e < 4; ++e) top = fmaxf(top, z[e]);
+      if (top > mine.top) {
+        mine.top = top;
 #pragma unroll
-      for (int e = 7; e >= 0; --e)
-        if (z[e] == top) mine.token = v + e;
-    }
-    if (k > 0.f) {
-      weigh(z, mine.top, k, fabsf(mine.top) < HB_INF && k < 3e38f);
-      mine.sum += ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
-    } else if (r.temperature > 0.f) {  // without end: all the same
+        for (int e = 3; e >= 0; --e)
+          if (z[e] == top) mine.token = v + e;
+      }
+    });
+  else
+    each_four<T, WHOLE, false>(a, r, s, t, v0, v1, [&](int, float (&z)[4]) {
+      const float last = mine.top;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) mine.sum += weight_of(z[e], mine.top, k);
-    }
+      for (int e = 0; e < 4; ++e) mine.top = fmaxf(mine.top, z[e]);
+      if (__any(last != mine.top)) mine.sum *= weight_of(last, mine.top, k);
+      weigh(z, mine.top, k);
+      mine.sum += (z[0] + z[1]) + (z[2] + z[3]);
+    });
+  each_marked<T>(a, r, s, t, v0, v1, false, [&](int v, float z) {
+    if (z > -HB_INF) mine = joined(mine, {z, 1.f, v}, k, greedy);
   });
-  mine = joined_lanes(mine, k);
+  mine = joined_lanes(mine, k, greedy);
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = mine;
   __syncthreads();
   const int lane = threadIdx.x & 63;
-  return joined_lanes(lane < kThreads / 64 ? waves[lane] : Stat{-HB_INF, 0.f, 0x7fffffff}, k);
+  return joined_lanes(lane < kThreads / 64 ? waves[lane] : nothing_of(greedy), k, greedy);
 }
 
 template <typename T, bool WHOLE, int kThreads>
-__device__ __forceinline__ void probs_of(const RulesArgs &a, const Row &r, const RowLds<kThreads> &s, int t, int v0, int v1, const Stat &all, float k) {
+__device__ __forceinline__ void probs_of(const RulesArgs &a, const Row &r, RowLds<kThreads> &s, int t, int v0, int v1, const Stat &all, float k, bool again) {
   float *out = (float *)a.out + (size_t)t * a.V;
-  if (r.temperature > 0.f) {
-    const float scale = all.top > -HB_INF ? 1.f / all.sum : 0.f;
-    const bool plain = fabsf(all.top) < HB_INF && k > 0.f && k < 3e38f;
-    each_eight<T, WHOLE>(a, r, s, t, v0, v1, [&](int v, float (&z)[8]) {
-      weigh(z, all.top, k, plain);
+  if (!greedy_of(r)) {
+    const float scale = all.sum > 0.f ? 1.f / all.sum : 0.f;
+    each_four<T, WHOLE, false>(a, r, s, t, v0, v1, [&](int v, float (&z)[4]) {
+      weigh(z, all.top, k);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] *= scale;
-      store_eight<WHOLE>(out + v, a.V - v, z);
+      for (int e = 0; e < 4; ++e) z[e] *= scale;
+      store_four<WHOLE>(out + v, a.V - v, z);
     });
+    each_marked<T>(a, r, s, t, v0, v1, again, [&](int v, float z) { out[v] = weight_of(z, all.top, k) * scale; });
   } else {
-    for (int v = v0 + (int)threadIdx.x * 8; v < v1; v += kThreads * 8) {
-      float z[8];
+    for (int v = v0 + (int)threadIdx.x * 4; v < v1; v += kThreads * 4) {
+      float z[4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = all.top > -HB_INF && v + e == all.token ? 1.f : 0.f;
-      store_eight<WHOLE>(out + v, a.V - v, z);
+      for (int e = 0; e < 4; ++e) z[e] = all.top > -HB_INF && v + e == all.token ? 1.f : 0.f;
+      store_four<WHOLE>(out + v, a.V - v, z);
     }
+  }
+}
+
+// A bit for every token that has a count, [batch][words]
+__global__ __launch_bounds__(kSplit) void rules_marks_kernel(const int32_t *counts, int V, uint32_t *marks) {
+  const int words = (V + 31) / 32, lane = threadIdx.x & 63;
+  const int32_t *row = counts + (size_t)blockIdx.x * V;
+  for (int64_t v = ((int64_t)blockIdx.y * kSplit + threadIdx.x); v < (int64_t)words * 32; v += (int64_t)gridDim.y * kSplit) {
+    const unsigned long long bits = __ballot(v < V && row[v] != 0);  // of two words, by a wavefront
+    const int word = (int)(v >> 5);
+    if ((lane & 31) == 0) marks[(size_t)blockIdx.x * words + word] = (uint32_t)(bits >> (lane & 32));
   }
 }
 
 // A row by one workgroup: twice over it, the second time out of the last cache
 template <typename T, bool WHOLE>
-__global__ __launch_bounds__(kWhole) void rules_row_kernel(RulesArgs a) {
+__global__ __launch_bounds__(kWhole, 8) void rules_row_kernel(RulesArgs a) {
   __shared__ RowLds<kWhole> s;
-  const int t = blockIdx.x;
+  // consecutive workgroups land on different dies: rows are dealt so that a die has neighbours, which share their counts
+  const int each = gridDim.x / 8, t = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+  if (t >= a.rows) return;
   const Row r = row_of<kWhole>(a, t, 0, a.V, s);
   if (r.b < 0) return;
   const float k = slope_of(r);
   const Stat all = stat_of<T, WHOLE, kWhole>(a, r, s, t, 0, a.V, k);
-  probs_of<T, WHOLE>(a, r, s, t, 0, a.V, all, k);
+  probs_of<T, WHOLE>(a, r, s, t, 0, a.V, all, k, true);
 }
 
 // A row by several, for few rows: what each finds in its chunk, and then, the row
@@ -452,13 +478,14 @@ __global__ __launch_bounds__(kSplit) void rules_probs_kernel(RulesArgs a) {
   const Row r = row_of<kSplit>(a, t, v0, v1, s);
   if (r.b < 0) return;
   const float k = slope_of(r);
-  Stat all = {-HB_INF, 0.f, 0x7fffffff};
+  const bool greedy = greedy_of(r);
+  Stat all = nothing_of(greedy);
   for (int p = threadIdx.x & 63; p < a.parts; p += 64) {  // (chunks in front have the lower tokens)
     const f32x4 x = *(const f32x4 *)(a.stats + ((size_t)t * a.parts + p) * 4);
-    all = joined(all, {x[0], x[1], __float_as_int(x[2])}, k);
+    all = joined(all, {x[0], x[1], __float_as_int(x[2])}, k, greedy);
   }
-  all = joined_lanes(all, k);
-  probs_of<T, WHOLE>(a, r, s, t, v0, v1, all, k);
+  all = joined_lanes(all, k, greedy);
+  probs_of<T, WHOLE>(a, r, s, t, v0, v1, all, k, false);
 }
 
 __global__ __launch_bounds__(kSplit) void rules_count_kernel(int B, int V, int n, const int32_t *row_offset, const int32_t *tokens,
@@ -481,16 +508,22 @@ __global__ __launch_bounds__(kSplit) void rules_count_kernel(int B, int V, int n
   }
 }
 
-size_t chunk_bytes(int32_t tokens) { return ((size_t)tokens + 31) / 32 * 6 + 2; }
+size_t chunk_bytes(int32_t tokens) { return ((size_t)tokens + 31) / 32 * 4; }
 
 template <typename T, bool WHOLE>
 hipError_t go_probs(const RulesArgs &a, hipStream_t s) {
   if (a.parts == 0) {
     const size_t bytes = chunk_bytes(a.V);
+    if (a.marks) {
+      const int64_t y = ((int64_t)a.V + 4 * kSplit - 1) / (4 * kSplit);
+      rules_marks_kernel<<<dim3(a.batch, (unsigned)(y > 64 ? 64 : y)), kSplit, 0, s>>>(a.counts, a.V, a.marks);
+      hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
     auto kern = rules_row_kernel<T, WHOLE>;
     hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)chunk_bytes(kMostWhole));
     if (e != hipSuccess) return e;
-    kern<<<a.rows, kWhole, bytes, s>>>(a);
+    kern<<<(unsigned)((a.rows + 7) / 8 * 8), kWhole, bytes, s>>>(a);
     return hipGetLastError();
   }
   const dim3 grid(a.rows, a.parts);
@@ -519,6 +552,8 @@ static int32_t split(int32_t rows, int32_t V, int32_t *chunk) {
   return (int32_t)(((int64_t)V + len - 1) / len);
 }
 
+bool rules_marks(int32_t B, int32_t T) { return T >= 4 * (int64_t)B; }
+
 // 0: a workgroup has a row for itself
 int32_t rules_parts(int32_t rows, int32_t V, int32_t *chunk) {
   return rows >= 128 && V <= kMostWhole ? 0 : split(rows, V, chunk);
@@ -526,14 +561,14 @@ int32_t rules_parts(int32_t rows, int32_t V, int32_t *chunk) {
 
 hipError_t launch_rules_logits(RulesArgs a, hipStream_t s) {
   a.parts = split(a.rows, a.V, &a.chunk);
-  if (a.dtype == HB_F32) return a.V % 8 ? go_logits<float, false>(a, s) : go_logits<float, true>(a, s);
-  return a.V % 8 ? go_logits<bf16_t, false>(a, s) : go_logits<bf16_t, true>(a, s);
+  if (a.dtype == HB_F32) return a.V % 4 ? go_logits<float, false>(a, s) : go_logits<float, true>(a, s);
+  return a.V % 4 ? go_logits<bf16_t, false>(a, s) : go_logits<bf16_t, true>(a, s);
 }
 
 hipError_t launch_rules_probs(RulesArgs a, hipStream_t s) {
   a.parts = rules_parts(a.rows, a.V, &a.chunk);
-  if (a.dtype == HB_F32) return a.V % 8 ? go_probs<float, false>(a, s) : go_probs<float, true>(a, s);
-  return a.V % 8 ? go_probs<bf16_t, false>(a, s) : go_probs<bf16_t, true>(a, s);
+  if (a.dtype == HB_F32) return a.V % 4 ? go_probs<float, false>(a, s) : go_probs<float, true>(a, s);
+  return a.V % 4 ? go_probs<bf16_t, false>(a, s) : go_probs<bf16_t, true>(a, s);
 }
 
 hipError_t launch_rules_count(int32_t B, int32_t V, int32_t n, const int32_t *row_offset, const int32_t *tokens, int32_t prompt,
