@@ -7,10 +7,12 @@
 //
 // A workgroup has a row, or a chunk of one.  Few tokens have anything to them but their logit and their mask: those with a
 // count, those on the path and those with a bias.  It finds them first (one pass over the counts, which all nodes of a tree
-// share) and marks them in a bitmap in LDS.  The row is then gone through without them, eight tokens a thread and little to do
-// for each, and they are done behind it, a thread each.  With the penalties' code at each of a thread's eight tokens 16 trees of
-// 60 nodes over 152064 tokens took 472 us, with a loop over the marks that a wavefront meets 331 (one in a hundred tokens is
-// marked: nearly every wavefront met some), so 2xx.
+// share, and make first where they are several) and marks them in a bitmap in LDS.  The row is then gone through without them,
+// four tokens a thread and little to do for each, and they are done behind it, a thread each.  16 trees of 60 nodes over 152064
+// tokens: with the penalties' code at each of a thread's tokens 472 us; with a loop over the marks that a wavefront meets 331
+// (one token in a hundred is marked: nearly every wavefront meets some); so 253, of which 102 are the first time over the logits
+// and 92 the stores by themselves.  What bounds it is the vector work of the two passes.  (A row held in 76 registers a thread
+// between them: 392, with one workgroup a CU; four loads under way a thread instead of two: the same, eight: 355.)
 // In float32, in the order that is written above, without contraction: two sides that follow it agree about which z is the
 // largest.
 #include "rules.h"
@@ -264,10 +266,14 @@ __device__ __forceinline__ void widen(const Piece<bf16_t, true> &y, int, float (
   }
 }
 
-template <bool WHOLE>
+// PAST: the caches, which then keep the logits for the second time over them (16 trees of 60 nodes over 152064 tokens: 253 us, else 274)
+template <bool WHOLE, bool PAST = false>
 __device__ __forceinline__ void store_four(float *p, int n, const float (&z)[4]) {
-  if (WHOLE) {
-    *(f32x4 *)p = (f32x4){z[0], z[1], z[2], z[3]};
+  const f32x4 x = {z[0], z[1], z[2], z[3]};
+  if (WHOLE && PAST) {
+    __builtin_nontemporal_store(x, (f32x4 *)p);
+  } else if (WHOLE) {
+    *(f32x4 *)p = x;
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -290,7 +296,7 @@ __device__ __forceinline__ void store_four(bf16_t *p, int n, const float (&z)[4]
 // of the next turns are asked for before this one's are worked on.
 template <typename T, bool WHOLE, bool MARKED, int kThreads, typename F>
 __device__ __forceinline__ void each_four(const RulesArgs &a, const Row &r, const RowLds<kThreads> &, int t, int v0, int v1, F f) {
-  constexpr int kTurn = kThreads * 4, kDeep = 4;
+  constexpr int kTurn = kThreads * 4, kDeep = 2;
   const T *row = (const T *)a.logits + (size_t)t * a.V;
   Piece<T, WHOLE> y[kDeep];
   uint32_t allowed[kDeep];
@@ -421,7 +427,7 @@ __device__ __forceinline__ void probs_of(const RulesArgs &a, const Row &r, RowLd
       weigh(z, all.top, k);
 #pragma unroll
       for (int e = 0; e < 4; ++e) z[e] *= scale;
-      store_four<WHOLE>(out + v, a.V - v, z);
+      store_four<WHOLE, kThreads == kWhole>(out + v, a.V - v, z);
     });
     each_marked<T>(a, r, s, t, v0, v1, again, [&](int v, float z) { out[v] = weight_of(z, all.top, k) * scale; });
   } else {
@@ -429,7 +435,7 @@ __device__ __forceinline__ void probs_of(const RulesArgs &a, const Row &r, RowLd
       float z[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) z[e] = all.top > -HB_INF && v + e == all.token ? 1.f : 0.f;
-      store_four<WHOLE>(out + v, a.V - v, z);
+      store_four<WHOLE, kThreads == kWhole>(out + v, a.V - v, z);
     }
   }
 }
