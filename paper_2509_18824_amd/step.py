@@ -236,6 +236,81 @@ def kv4_pool(num_blocks: int, Hkv: int, page: int, D: int, device="cuda") -> Kv4
     return Kv4Pool(u8(D // 2), u8(D // 32), u8(D // 2), u8(D // 32))
 
 
+class PagePool:
+    """Who has which page of a cache: every sequence's pages and committed length, and the pages that are free, on the device.
+
+    ``take`` gives pages to sequences that get ``row_offset[b+1] - row_offset[b]`` new positions (and ``reserve`` more, for a tree's
+    accepted nodes) and says where the new rows go; ``length`` is advanced by ``advance``, when they are there.  A sequence that is not
+    ``granted`` keeps its length, and its rows' slots are -1, which the append passes over.  ``give`` takes back what is behind
+    ``keep_len`` positions (all: 0); a sequence that ends has ``length`` set to 0 as well.  Nothing is synchronised or allocated, so a HIP
+    graph can hold it all."""
+
+    def __init__(self, B: int, page: int, max_blocks: int, num_blocks: int, max_rows: int, reserve: int = 0, device="cuda"):
+        i32 = lambda n, value=0: torch.full((n,), value, dtype=torch.int32, device=device)
+        self.page, self.reserve = page, reserve
+        self.block_table = i32(B * max_blocks, -1).view(B, max_blocks)
+        self.length, self.pages, self.new_len, self.granted = i32(B), i32(B), i32(B), i32(B)
+        self.free_pages = torch.arange(num_blocks - 1, -1, -1, dtype=torch.int32, device=device)  # page 0 is the first to go
+        self.free_count = i32(1, num_blocks)
+        self.slots = i32(max_rows, -1)
+        self._pages, self._free = i32(B), i32(1)
+
+    def take(self, row_offset):
+        self.slots.fill_(-1)  # rows behind the last sequence have no place
+        hb.hb_pages_take(self.page, self.reserve, self.length, row_offset, self.pages, self.free_pages, self.free_count, self.block_table,
+                         self.slots, self.new_len, self._pages, self.granted, self._free)
+        self._keep()
+
+    def advance(self):
+        self.length.copy_(self.new_len)
+
+    def give(self, keep_len):
+        hb.hb_pages_give(self.page, keep_len, self.pages, self.block_table, self.free_pages, self.free_count, self._pages, self._free)
+        self._keep()
+
+    def _keep(self):
+        self.pages.copy_(self._pages)
+        self.free_count.copy_(self._free)
+
+
+def prompt_attn(desc: hb.AttnDesc, q, k_rows, v_rows, row_offset, k_pool=None, v_pool=None, block_table=None, prefix_len=None, want_lse=True,
+                workspace=None, out=None):
+    """Returns (out, lse).  Allocates what is not passed in."""
+    if out is None:
+        out = torch.empty_like(q)
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        workspace = alloc_workspace(hb.hb_prompt_attn_workspace_bytes(desc), q.device)
+    hb.hb_prompt_attn(desc, q, k_rows, v_rows, k_pool, v_pool, block_table, prefix_len, row_offset, out, lse, workspace)
+    return out, lse
+
+
+@dataclass
+class SamplingRules:
+    """What a batch's requests want of the next token (field names as in the C ABI); a field that is None is not there."""
+
+    counts: Optional[torch.Tensor] = None       # int32 [B, V]
+    rules: Optional[torch.Tensor] = None        # float32 [B, 4]: temperature, repetition, presence, frequency
+    bias_offset: Optional[torch.Tensor] = None  # int32 [B + 1]
+    bias_id: Optional[torch.Tensor] = None      # int32 [n_bias]
+    bias_value: Optional[torch.Tensor] = None   # float32 [n_bias]
+    mask: Optional[torch.Tensor] = None         # int32 [num_masks, ceil(V / 32)]
+    mask_row: Optional[torch.Tensor] = None     # int32 [T]
+
+    def fields(self):
+        return self.counts, self.rules, self.bias_offset, self.bias_id, self.bias_value, self.mask, self.mask_row
+
+
+def rules_probs(logits, rules: SamplingRules, node_offset=None, parent=None, draft_ids=None, max_nodes: int = 1, probs=None, workspace=None):
+    """The probabilities of each row's next token.  ``node_offset`` None: one row a sequence.  Allocates what is not passed in."""
+    if probs is None:
+        probs = torch.empty(logits.shape, dtype=torch.float32, device=logits.device)
+    if workspace is None:
+        workspace = alloc_workspace(hb.hb_rules_probs_workspace_bytes(*logits.shape), logits.device)
+    hb.hb_rules_probs(logits, max_nodes, node_offset, parent, draft_ids, *rules.fields(), probs, workspace)
+    return probs
+
+
 class VerifyStep:
     """Pre-allocated buffers for one full verification step (attention of one layer, LM head,
     acceptance, compaction); ``run`` only enqueues kernels."""
@@ -267,6 +342,45 @@ class VerifyStep:
                                     self.target_ids, self.accept_len, self.accept_path, self.out_tokens, self.bonus, self.ws_lm,
                                     int(bool(compact)), (dev.k_tree, dev.v_tree, dev.k_pool, dev.v_pool), dev.block_table,
                                     dev.prefix_len, self.out_slots, self.new_len)
+
+
+class SampledVerifyStep:
+    """Buffers of a verification step whose tokens are sampled as each request wants them: attention of one layer, logits, their
+    probabilities by the rules, acceptance by sampling, compaction, and the count of what came out.  ``q_draft`` is what the nodes were
+    drawn from (float32 [T, V]); ``u_accept`` and ``u_bonus`` hold the step's random bits.  ``rules.counts`` holds the trees' roots when
+    ``run`` is called, and what the step emitted when it is done.  ``run`` only enqueues kernels."""
+
+    def __init__(self, desc: hb.AttnDesc, dev: DeviceInputs, weight: torch.Tensor, draft_ids, q_draft, u_accept, u_bonus, max_path: int,
+                 rules: SamplingRules):
+        self.desc, self.dev, self.weight, self.max_path, self.rules = desc, dev, weight, max_path, rules
+        self.draft_ids, self.q_draft, self.u_accept, self.u_bonus = draft_ids, q_draft, u_accept, u_bonus
+        d, B = dev.q.device, desc.batch
+        (V, K), T = weight.shape, dev.q.shape[0]
+        i32 = lambda *shape: torch.empty(shape, dtype=torch.int32, device=d)
+        self.out = torch.empty_like(dev.q)
+        self.logits = torch.empty((T, V), dtype=weight.dtype, device=d)
+        self.probs = torch.empty((T, V), dtype=torch.float32, device=d)
+        self.ws_attn = alloc_workspace(hb.hb_tree_verify_attn_workspace_bytes(desc), d)
+        self.ws_proj = alloc_workspace(hb.hb_proj_workspace_bytes(T, K, V), d)
+        self.ws_rules = alloc_workspace(hb.hb_rules_probs_workspace_bytes(T, V), d)
+        self.ws_accept = alloc_workspace(max(4, hb.hb_tree_accept_sample_workspace_bytes(B, V)), d)
+        self.accept_len, self.bonus, self.new_len = i32(B), i32(B), i32(B)
+        self.accept_path, self.out_tokens, self.out_slots = i32(B, max_path), i32(B, max_path), i32(B, max_path)
+
+    def run(self, compact=True):
+        dev, desc = self.dev, self.desc
+        hb.hb_tree_verify_attn(desc, dev.q, dev.k_tree, dev.v_tree, dev.k_pool, dev.v_pool, dev.block_table, dev.prefix_len,
+                               dev.node_offset, dev.parent, self.out, None, self.ws_attn)
+        hb.hb_out_project_ws(self.out.view(self.out.shape[0], -1), self.weight, None, self.logits, self.ws_proj)
+        rules_probs(self.logits, self.rules, dev.node_offset, dev.parent, self.draft_ids, desc.max_nodes_per_tree, self.probs, self.ws_rules)
+        hb.hb_tree_accept_sample(desc.batch, desc.max_nodes_per_tree, dev.node_offset, dev.parent, self.draft_ids, self.probs, self.q_draft,
+                                 self.u_accept, self.u_bonus, self.max_path, self.accept_len, self.accept_path, self.out_tokens, self.bonus,
+                                 self.ws_accept)
+        if compact:
+            hb.hb_kv_compact(desc, dev.k_tree, dev.v_tree, dev.k_pool, dev.v_pool, dev.block_table, dev.prefix_len, dev.node_offset,
+                             self.accept_len, self.accept_path, self.max_path, self.out_slots, self.new_len)
+        if self.rules.counts is not None:
+            hb.hb_rules_count(self.out_tokens, self.rules.counts)
 
 
 class Kv4VerifyStep:
@@ -447,3 +561,70 @@ class VerifyLayerStack:
         accept(desc, x, self.lm_weight, self.draft_ids, dev.node_offset, dev.parent, self.max_path, self.target_ids,
                self.accept_len, self.accept_path, self.out_tokens, self.bonus, self.ws_lm, self.n_layers if compact else 0,
                self.ptr_tables, dev.block_table, dev.prefix_len, self.out_slots, self.new_len)
+
+
+class PromptLayerStack:
+    """Buffers and call chain that take prompts, whole or in parts, through ``n_layers`` decoder layers (those of
+    ``VerifyLayerStack``, with the same weights): pages for the new rows, then in each layer the rows' attention over what the cache
+    holds and over each other, and their append; at the end each sequence's last row through the LM head.  ``first_ids[b]`` is the token
+    that follows the rows (-1: sequence b had none, or no pages).  ``desc`` is a batch of at most ``desc.total_nodes`` rows; ``row_offset`` may say
+    fewer.  Pools and pages are those that the verification steps go on with.  ``run`` only enqueues kernels."""
+
+    def __init__(self, desc: hb.AttnDesc, pages: PagePool, pools, w_qkv, w_o, lm_weight, row_offset, hidden0: torch.Tensor,
+                 theta: float = 1e6, mlp=None):
+        self.desc, self.pages, self.pools, self.w_qkv, self.w_o, self.lm_weight = desc, pages, pools, w_qkv, w_o, lm_weight
+        self.row_offset, self.hidden0, self.theta, self.mlp = row_offset, hidden0, theta, mlp
+        d, (T, K), B = hidden0.device, hidden0.shape, desc.batch
+        like = lambda *shape: torch.empty(shape, dtype=hidden0.dtype, device=d)
+        self.rows = torch.arange(T, dtype=torch.int32, device=d)
+        self.cos = torch.empty((T, desc.head_dim // 2), dtype=torch.float32, device=d)
+        self.sin = torch.empty_like(self.cos)
+        self.q, self.attn_out = like(T, desc.num_q_heads, desc.head_dim), like(T, desc.num_q_heads, desc.head_dim)
+        self.k, self.v = like(T, desc.num_kv_heads, desc.head_dim), like(T, desc.num_kv_heads, desc.head_dim)
+        self.hidden = [like(T, K), like(T, K)]
+        shapes = [(K, w_qkv[0].shape[0]), (w_o[0].shape[1], K)]
+        if mlp is not None:
+            F = mlp["w_down"][0].shape[1]
+            shapes += [(K, 2 * F), (F, K)]
+            self.normed, self.mid, self.act = like(T, K), like(T, K), like(T, F)
+        self.ws_proj = alloc_workspace(max(hb.hb_proj_workspace_bytes(T, k, n) for k, n in shapes), d)
+        self.ws_attn = alloc_workspace(hb.hb_prompt_attn_workspace_bytes(desc), d)
+        self.ws_lm = alloc_workspace(max(8, hb.hb_lmhead_argmax_workspace_bytes(B)), d)
+        self.ids = torch.empty(B, dtype=torch.int32, device=d)
+        self.first_ids = torch.empty_like(self.ids)
+
+    def run(self):
+        desc, pages, mlp, offset = self.desc, self.pages, self.mlp, self.row_offset
+        T = self.hidden0.shape[0]
+        pages.take(offset)
+        # a row's position: behind what its sequence has in the cache
+        seq = torch.bucketize(self.rows, offset[1:], right=True).clamp_(max=desc.batch - 1)
+        hb.hb_rope_table(desc.head_dim, self.theta, self.rows + (pages.length - offset[:-1])[seq], self.cos, self.sin)
+
+        def project(x, w, residual, out, norm):
+            if norm is None:
+                hb.hb_out_project_ws(x, w, residual, out, self.ws_proj)
+            else:
+                hb.hb_out_project_norm_ws(x, w, residual, out, norm, mlp["eps"], self.normed, self.ws_proj)
+
+        x, n = self.hidden0, len(self.pools)
+        if mlp is not None:
+            first = mlp["norm1"][0] if n else mlp.get("norm_f")
+            if first is not None:
+                hb.hb_rmsnorm(x, first, mlp["eps"], self.normed)
+        for l, (kp, vp) in enumerate(self.pools):
+            nxt = self.hidden[l & 1]
+            y = nxt if mlp is None else self.mid
+            hb.hb_qkv_rope_project_ws(x if mlp is None else self.normed, self.w_qkv[l], None, self.cos, self.sin, self.q, self.k, self.v,
+                                      self.ws_proj)
+            hb.hb_prompt_attn(desc, self.q, self.k, self.v, kp, vp, pages.block_table, pages.length, offset, self.attn_out, None, self.ws_attn)
+            hb.hb_kv_append(desc, self.k, self.v, pages.slots, kp, vp)
+            project(self.attn_out.view(T, -1), self.w_o[l], x, y, None if mlp is None else mlp["norm2"][l])
+            if mlp is not None:
+                hb.hb_swiglu_project(self.normed, mlp["w_gate_up"][l], self.act, self.ws_proj)
+                project(self.act, mlp["w_down"][l], y, nxt, mlp["norm1"][l + 1] if l + 1 < n else mlp.get("norm_f"))
+            x = nxt
+        self.final_hidden = self.normed if mlp is not None and mlp.get("norm_f") is not None else x
+        hb.hb_lmhead_argmax(self.final_hidden[(offset[1:] - 1).clamp(min=0)], self.lm_weight, self.ids, None, self.ws_lm)
+        self.first_ids.copy_(torch.where((offset[1:] > offset[:-1]) & (pages.granted > 0), self.ids, -1))
+        pages.advance()
