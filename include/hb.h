@@ -703,8 +703,9 @@ int32_t hb_kv_append(const hb_attn_desc *desc, int32_t n_rows, const void *k_row
  * max_nodes_per_tree is not read.  num_splits is the most parts that a row's keys are cut into (0: the library's choice, from
  * the lengths); max_prefix_len_hint sizes workspace and launch and no more: a longer prefix is taken whole.
  * What a row does not see has no influence on it, whatever bits it holds: later rows, slots behind the prefix, other sequences.
- * Accumulation is float32; on the matrix cores in bf16 a softmax weight is rounded to bf16 for its product with a value (by 2^-8
- * of itself at most), the sum that it is divided by is not.  bf16 results are rounded once at the end.
+ * Accumulation is float32; on the matrix cores in bf16 a softmax weight is rounded to bf16 (by 2^-8 of itself at most) for its
+ * product with a value and for the sum that results are divided by, not for lse.  bf16 results are rounded once at the end.
+ * out, lse and workspace overlap neither each other nor what is read.
  * Errors: INVALID_ARG, UNSUPPORTED (dtype, D; total_nodes * Hq beyond 2^30; HB_ATTN_MFMA on a shape it cannot take),
  * WORKSPACE, DEVICE.  batch == 0 or total_nodes == 0 is a successful no-op.
  */
@@ -721,7 +722,7 @@ size_t hb_prompt_attn_workspace_bytes(const hb_attn_desc *desc);
  *   z      = logit; if c > 0 or the token is in the prompt: z / repetition where z > 0, z * repetition elsewhere
  *   z      = z - (presence * [c > 0] + frequency * c) + bias;  -infinity where the mask forbids the token or z is no number
  * in float32, operation by operation as written.
- * hb_rules_logits: out = z, in the type of the logits (which out may be).
+ * hb_rules_logits: out = z, in the type of the logits (which out may be, all of it, and must not overlap otherwise).
  * hb_rules_probs:  probs = exp((z - max z) / temperature) / sum, what hb_tree_accept_sample takes; temperature 0 (or less, or
  *   no number): 1 at the largest z, the lowest token among equals, which makes that call's rule the greedy one.  Infinite z
  *   share the whole.  A row that the rules leave nothing of is zero.

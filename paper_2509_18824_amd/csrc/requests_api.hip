@@ -212,10 +212,15 @@ int32_t hb_prompt_attn(const hb_attn_desc *desc, const void *q, const void *k_ro
   if (misaligned(q, 16) || misaligned(k_rows, 16) || misaligned(v_rows, 16) || misaligned(k_pool, 16) || misaligned(v_pool, 16) ||
       misaligned(out, 16))
     return fail(HB_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
+  const int64_t el = desc->dtype == HB_F32 ? 4 : 2, rows = (int64_t)desc->total_nodes * desc->head_dim;
+  const Span in[] = {{q, rows * desc->num_q_heads * el}, {k_rows, rows * desc->num_kv_heads * el}, {v_rows, rows * desc->num_kv_heads * el}},
+             o = {out, rows * desc->num_q_heads * el}, l = {lse, (int64_t)desc->total_nodes * desc->num_q_heads * 4};
+  if ((rc = check_apart("out", o, {in[0], in[1], in[2], l})) || (rc = check_apart("lse", l, {in[0], in[1], in[2]}))) return rc;
   if (p.bytes) {
     if (!workspace || workspace_bytes < p.bytes)
       return fail(HB_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", p.bytes, workspace ? workspace_bytes : (size_t)0);
     if (misaligned(workspace, 256)) return fail(HB_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    if ((rc = check_apart("workspace", {workspace, (int64_t)p.bytes}, {in[0], in[1], in[2], o, l}))) return rc;
   }
   PromptArgs a = {*desc, q, k_rows, v_rows, k_pool, v_pool, block_table, prefix_len, row_offset, out, lse,
                   p.bytes ? (float *)workspace : nullptr, p.bytes ? (float *)((char *)workspace + p.ml_offset) : nullptr,
@@ -247,6 +252,8 @@ int32_t hb_rules_logits(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, in
                            {node_offset, parent, draft_ids, counts, rules, bias_offset, n_bias, bias_id, bias_value, num_masks, mask, mask_row},
                            out, &a);
   if (rc || T == 0 || B == 0) return rc;
+  const int64_t bytes = (int64_t)T * V * (dtype == HB_F32 ? 4 : 2);
+  if (out != logits && (rc = check_apart("out", {out, bytes}, {{logits, bytes}}))) return rc;
   HB_HIP_TRY(launch_rules_logits(a, (hipStream_t)stream));
   return HB_OK;
 }
@@ -274,7 +281,8 @@ int32_t hb_rules_probs(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, int
     return fail(HB_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
   if (need && misaligned(workspace, 16)) return fail(HB_ERR_WORKSPACE, "workspace must be 16-byte aligned");
   const int64_t el = dtype == HB_F32 ? 4 : 2;
-  if ((rc = check_apart("probs", {probs, (int64_t)T * V * 4}, {{logits, (int64_t)T * V * el}}))) return rc;
+  const Span in = {logits, (int64_t)T * V * el}, o = {probs, (int64_t)T * V * 4};
+  if ((rc = check_apart("probs", o, {in})) || (need && (rc = check_apart("workspace", {workspace, (int64_t)need}, {in, o})))) return rc;
   int32_t chunk;
   if (rules_parts(T, V, &chunk))
     a.stats = (float *)workspace;

@@ -159,3 +159,14 @@ def test_the_binding_refuses_other_types_and_shapes():
         hb.hb_rules_logits(z, 4, **ok, out=z.bfloat16())
     with pytest.raises(ValueError):
         hb.hb_rules_probs(z.bfloat16(), 4, **ok, probs=z.bfloat16(), workspace=None)
+
+
+def test_what_is_written_has_a_place_of_its_own():
+    assert _attn(_desc(), out=P[0]) == 1 and "out" in hb.hb_last_error()
+    d = _desc()
+    lse = lambda at: L.hb_prompt_attn(C.byref(d), P[0], P[1], P[1], P[2], P[2], P[3], P[4], P[3], P[5], at, P[6], 1 << 40, None)
+    assert lse(P[0]) == 1 and "lse" in hb.hb_last_error()
+    assert lse(P[5]) == 1 and "overlap" in hb.hb_last_error()
+    assert _attn(_desc(num_splits=4), ws=P[0]) == 1 and "workspace" in hb.hb_last_error()
+    assert _rules(L.hb_rules_logits, out=C.c_void_p(P[0].value + 16)) == 1 and "out" in hb.hb_last_error()  # neither in place nor apart
+    assert _rules(ws=P[0]) == 1 and "workspace" in hb.hb_last_error()
