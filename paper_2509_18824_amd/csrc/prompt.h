@@ -160,7 +160,7 @@ bool prompt_mfma_supports(const hb_attn_desc &d);
 int32_t prompt_mfma_rows(const hb_attn_desc &d);  // of a tile
 hipError_t launch_prompt_mfma(const PromptArgs &a, hipStream_t s);
 hipError_t launch_prompt_join(const PromptArgs &a, int32_t rows, hipStream_t s);  // for tiles of `rows` rows
-constexpr int kPromptAnyRows = 64;
+constexpr int kPromptAnyRows = 16;
 hipError_t launch_prompt_any(const PromptArgs &a, hipStream_t s);
 
 }  // namespace hb

@@ -1,12 +1,17 @@
 // Attention of prompts for every shape and type (hb_prompt_attn): float32 throughout, on the float32 matrix instructions.
 //
-// One workgroup owns one tile of 64 rows (prompt.h) and one part of its keys; four wavefronts with sixteen rows each share
-// the keys, 32 at a time, widened to float32 in LDS.  As in the bf16 kernels the products are transposed, so that no score
-// crosses lanes between them:
+// One workgroup owns one tile of 16 rows (prompt.h) and one part of its keys.  64 keys at a time are widened to float32 in LDS,
+// the next ones under way to registers meanwhile; each of four wavefronts has sixteen of them, and its own softmax and result of
+// the rows, which are joined in LDS at the end.  As in the bf16 kernels the products are transposed, so that no score crosses
+// lanes between them:
 //   S^T = K Q^T     16x16x4: A = 16 keys x 4 of D, B = 4 of D x 16 rows
 //   O^T = V^T P^T   16x16x4: A = 16 of D x 4 keys, B = 4 keys x 16 rows
 // The accumulator of lane (j, g), j = lane % 16, g = lane / 16, holds row j's scores for keys 4g + r, r = 0..3: what the
 // r-th instruction of the second product wants in that lane when its four keys are r, 4 + r, 8 + r, 12 + r.
+// A tile of 16 x 64 x 128 is 64 matrix instructions of 32 cycles for each wavefront, 1 us; it takes 2 with one workgroup on a CU (the
+// softmax between the products waits for lanes and LDS) and 1.2 with two.  2 prompts of 200 to 256 rows, 4 heads: 11.7 us; one
+// of 2048 rows 63, of 8192 500 (137 TFLOP/s of the 153 that a large float32 product has).  With sixteen rows
+// for each wavefront, which share the keys, these are 20.3 (four times fewer workgroups, and a join of parts) and 72.
 // Softmax is online per row in base 2.  Rows of K and V are four floats apart from a multiple of 64 in LDS: no operand read
 // has a bank conflict.  A head dimension between the sizes built here is filled up with zeros.
 #pragma once
@@ -16,7 +21,7 @@ namespace hb {
 
 namespace {
 
-constexpr int kAnyKeys = 32;
+constexpr int kAnyKeys = 64;  // of a tile
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -32,16 +37,6 @@ __device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
     x[4 + i] = hi[i];
   }
 }
-__device__ __forceinline__ void load8(const bf16_t *p, float (&x)[8]) {
-  const u32x4 w = *(const u32x4 *)p;
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-
-// Rows first .. first + 16 NW - 1 of (sequence, kv head h) by NW wavefronts, which all call it: their keys w.begin .. w.end - 1,
-// to the results, or to the partial results from `slot0` on.  lds: any_lds_floats<DP>.
 template <int DP>
 constexpr int any_lds_floats = 2 * kAnyKeys * (DP + 4) + 4;
 
@@ -53,15 +48,49 @@ __device__ __forceinline__ void store8(bf16_t *p, const float (&x)[8]) {
   *(u32x4 *)p = (u32x4){pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
 }
 
-template <typename T, int DP, int NW>
+// 16 bytes or 32 of K or V as they are in memory
+template <typename T>
+struct Raw;
+template <>
+struct Raw<float> {
+  f32x4 lo, hi;
+  __device__ __forceinline__ void load(const float *p) {
+    lo = *(const f32x4 *)p;
+    hi = *(const f32x4 *)(p + 4);
+  }
+  __device__ __forceinline__ void widen(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = lo[i];
+      x[4 + i] = hi[i];
+    }
+  }
+};
+template <>
+struct Raw<bf16_t> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const bf16_t *p) { w = *(const u32x4 *)p; }
+  __device__ __forceinline__ void widen(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+};
+
+// Rows first .. first + 15 of (sequence, kv head h) by four wavefronts, which all call it: their keys w.begin .. w.end - 1, to the
+// results, or to the partial results from `slot0` on.  lds: any_lds_floats<DP>.
+template <typename T, int DP>
 __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const PromptTile &w, int h, int first, size_t slot0, float *lds) {
-  constexpr int kKeys = kAnyKeys, kRow = DP + 4, kTiles = DP / 16, kSteps = DP / 4, kPieces = DP / 8;
+  constexpr int kKeys = kAnyKeys, kRow = DP + 4, kTiles = DP / 16, kSteps = DP / 4, kPieces = DP / 8, kAsks = kKeys * kPieces / 256;
   float *lk = lds, *lv = lds + kKeys * kRow;
   int &bad = *(int *)(lds + 2 * kKeys * kRow);  // a value of this tile's is left out, see below
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, j = lane & 15, kg = lane >> 4;
   const int G = a.d.num_q_heads / a.d.num_kv_heads, D = a.d.head_dim, Hkv = a.d.num_kv_heads;
+  const int own = wave * 16;  // this wavefront's first key of a tile
 
-  const int row = first + wave * 16 + j;
+  const int row = first + j;
   const bool there = (int64_t)row < (int64_t)w.n * G;
   const int token = there ? row / G : w.n - 1, head = there ? row - token * G : 0;
   const size_t at = (size_t)(w.row0 + token) * a.d.num_q_heads + (size_t)h * G + head;
@@ -77,13 +106,14 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
   float m = HB_NEG_INF, l = 0.f;
   const float c1 = a.d.softmax_scale * kLog2e;
 
-  for (int k0 = w.begin; k0 < w.end; k0 += kKeys) {
-    __syncthreads();
-    if (tid == 0) bad = 0;
-    __syncthreads();
-    for (int i = tid; i < kKeys * kPieces; i += 64 * NW) {
-      const int key = i / kPieces, d0 = i % kPieces * 8, kk = k0 + key;
-      float x[8] = {}, y[8] = {};
+  // the next tile is on its way to registers while this one is worked on
+  const int key0 = tid / kPieces, d0 = tid % kPieces * 8;
+  Raw<T> kx[kAsks], vx[kAsks];
+  auto ask = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < kAsks; ++i) {
+      const int kk = k0 + key0 + i * (256 / kPieces);
+      kx[i] = vx[i] = Raw<T>{};
       if (kk < w.end && d0 < D) {
         const T *ks, *vs;
         size_t from;
@@ -99,12 +129,26 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
           ks = (const T *)a.k;
           vs = (const T *)a.v;
         }
-        load8(ks + from + d0, x);
-        load8(vs + from + d0, y);
+        kx[i].load(ks + from + d0);
+        vx[i].load(vs + from + d0);
       }
+    }
+  };
+  ask(w.begin);
+
+  for (int k0 = w.begin; k0 < w.end; k0 += kKeys) {
+    __syncthreads();
+    if (tid == 0) bad = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kAsks; ++i) {
+      const int key = key0 + i * (256 / kPieces);
+      float x[8], y[8];
+      kx[i].widen(x);
+      vx[i].widen(y);
       // a key that some row does not see has weight 0 there, and 0 times a value that is not finite is none: such values
       // are added below, to the rows that see them
-      if (kk > all_see) {
+      if (k0 + key > all_see) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (!(fabsf(y[e]) < __builtin_huge_valf())) {
@@ -119,25 +163,19 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
       }
     }
     __syncthreads();
+    ask(k0 + kKeys);
 
-    f32x4 sc[2];
+    f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      sc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-        sc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(lk[(16 * t + j) * kRow + 4 * s + kg], qf[s], sc[t], 0, 0, 0);
-    }
+    for (int s = 0; s < kSteps; ++s) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(lk[(own + j) * kRow + 4 * s + kg], qf[s], sc, 0, 0, 0);
     // masked scores are replaced before anything is made of them
     float top = HB_NEG_INF;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int kk = k0 + 16 * t + 4 * kg + r;
-        sc[t][r] = kk <= sees && kk < w.end ? sc[t][r] * c1 : HB_NEG_INF;
-        top = fmaxf(top, sc[t][r]);
-      }
+    for (int r = 0; r < 4; ++r) {
+      const int kk = k0 + own + 4 * kg + r;
+      sc[r] = kk <= sees && kk < w.end ? sc[r] * c1 : HB_NEG_INF;
+      top = fmaxf(top, sc[r]);
+    }
     top = fmaxf(top, __shfl_xor(top, 16, 64));
     top = fmaxf(top, __shfl_xor(top, 32, 64));
     const float next = fmaxf(m, top), ref = next == HB_NEG_INF ? 0.f : next;
@@ -147,18 +185,16 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) o[t] *= alpha;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int r = 0; r < 4; ++r) {
+      const float p = exp2_of(sc[r] - ref);
+      l += p;
+      const float *vr = lv + (own + 4 * kg + r) * kRow + j;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float p = exp2_of(sc[t][r] - ref);
-        l += p;
-        const float *vr = lv + (16 * t + 4 * kg + r) * kRow + j;
-#pragma unroll
-        for (int dt = 0; dt < kTiles; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[16 * dt], p, o[dt], 0, 0, 0);
-      }
+      for (int dt = 0; dt < kTiles; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[16 * dt], p, o[dt], 0, 0, 0);
+    }
     if (bad) {  // every thread's: it is set in front of a barrier
-      const int last = min(min(sees, w.end - 1), k0 + kKeys - 1);
-      for (int kk = max(k0, all_see + 1); kk <= last; ++kk) {  // prompt rows: the prefix is seen by all
+      const int last = min(min(sees, w.end - 1), k0 + own + 15);
+      for (int kk = max(k0 + own, all_see + 1); kk <= last; ++kk) {  // prompt rows: the prefix is seen by all
         const T *vs = (const T *)a.v + ((size_t)(w.row0 + kk - w.P) * Hkv + h) * D;
 #pragma unroll
         for (int dt = 0; dt < kTiles; ++dt)
@@ -174,30 +210,45 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
 
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
-  if (!there) return;
-  if (w.parts == 1) {
-    const float inv = 1.f / l;
+  // one result of the wavefronts': through LDS, where the keys were
+  float *lo = lds, *ml = lds + 64 * kRow;  // [wavefront][row]
+  __syncthreads();
 #pragma unroll
-    for (int dt = 0; dt < kTiles; ++dt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int d = 16 * dt + 4 * kg + r;
-        if (d < D) store_f32((T *)a.out + at * D + d, o[dt][r] * inv);
-      }
-    if (a.lse && kg == 0) a.lse[at] = (m + log2f(l)) * kLn2;
-  } else {
-    const size_t slot = slot0 + wave * 16 + j;
-#pragma unroll
-    for (int dt = 0; dt < kTiles; ++dt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int d = 16 * dt + 4 * kg + r;
-        if (d < D) a.part_o[slot * D + d] = o[dt][r];
-      }
-    if (kg == 0) {
-      *(f32x4 *)(a.part_ml + slot * 4) = (f32x4){m, l, l, 0.f};
-    }
+  for (int dt = 0; dt < kTiles; ++dt) *(f32x4 *)(lo + (wave * 16 + j) * kRow + 16 * dt + 4 * kg) = o[dt];
+  if (kg == 0) {
+    ml[2 * (wave * 16 + j)] = m;
+    ml[2 * (wave * 16 + j) + 1] = l;
   }
+  __syncthreads();
+  float scale[4], most = HB_NEG_INF, sum = 0.f;
+  const int r = tid >> 4, of = tid & 15;  // this thread's row, and its pieces of eight: of, of + 16
+#pragma unroll
+  for (int v = 0; v < 4; ++v) most = fmaxf(most, ml[2 * (16 * v + r)]);
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const float mv = ml[2 * (16 * v + r)], lv = ml[2 * (16 * v + r) + 1];
+    scale[v] = mv == HB_NEG_INF && lv == 0.f ? 0.f : exp2_of(mv - most);  // 0: sees none of those keys
+    sum += scale[v] * lv;
+  }
+  const int mine = first + r, t2 = mine / G;
+  if ((int64_t)mine >= (int64_t)w.n * G) return;
+  const size_t to = (size_t)(w.row0 + t2) * a.d.num_q_heads + (size_t)h * G + (mine - t2 * G);
+  const float inv = w.parts == 1 ? 1.f / sum : 1.f;
+  for (int d0 = 8 * of; d0 < D; d0 += 128) {
+    float x[8] = {};
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += scale[v] * lo[(v * 16 + r) * kRow + d0 + e];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= inv;
+    if (w.parts == 1)
+      store8((T *)a.out + to * D + d0, x);
+    else
+      store8(a.part_o + (slot0 + r) * D + d0, x);
+  }
+  if (of == 0 && w.parts > 1) *(f32x4 *)(a.part_ml + (slot0 + r) * 4) = (f32x4){most, sum, sum, 0.f};
+  if (of == 0 && w.parts == 1 && a.lse) a.lse[to] = (most + log2f(sum)) * kLn2;
 }
 
 }  // namespace

@@ -7,13 +7,13 @@ namespace {
 
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void prompt_any_kernel(PromptArgs a) {
+  constexpr int kRows = kPromptAnyRows;
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int h = blockIdx.y;
-  const PromptTile w = prompt_tile<kPromptAnyRows, kAnyKeys>(a, blockIdx.x, blockIdx.z);
-  prompt_head<kPromptAnyRows>(a, w, blockIdx.x, h, blockIdx.z);
+  const PromptTile w = prompt_tile<kRows, kAnyKeys>(a, blockIdx.x, blockIdx.z);
+  prompt_head<kRows>(a, w, blockIdx.x, h, blockIdx.z);
   if (w.t < 0) return;
-  prompt_any_rows<T, DP, 4>(a, w, h, w.t * kPromptAnyRows,
-                            (((size_t)blockIdx.x * a.d.num_kv_heads + h) * a.parts + blockIdx.z) * kPromptAnyRows, lds);
+  prompt_any_rows<T, DP>(a, w, h, w.t * kRows, (((size_t)blockIdx.x * a.d.num_kv_heads + h) * a.parts + blockIdx.z) * kRows, lds);
 }
 
 template <typename T, int DP>
@@ -62,14 +62,14 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int bm) 
 
 }  // namespace
 
+template <typename T>
 static hipError_t go(const PromptArgs &a, hipStream_t s) {
   const int D = a.d.head_dim;
-  if (a.d.dtype == HB_F32) return D <= 64 ? launch_any<float, 64>(a, s) : D <= 128 ? launch_any<float, 128>(a, s) : launch_any<float, 256>(a, s);
-  return D <= 64 ? launch_any<bf16_t, 64>(a, s) : D <= 128 ? launch_any<bf16_t, 128>(a, s) : launch_any<bf16_t, 256>(a, s);
+  return D <= 64 ? launch_any<T, 64>(a, s) : D <= 128 ? launch_any<T, 128>(a, s) : launch_any<T, 256>(a, s);
 }
 
 hipError_t launch_prompt_any(const PromptArgs &a, hipStream_t s) {
-  hipError_t e = go(a, s);
+  hipError_t e = a.d.dtype == HB_F32 ? go<float>(a, s) : go<bf16_t>(a, s);
   if (e == hipSuccess && a.parts > 1) e = launch_prompt_join(a, kPromptAnyRows, s);
   return e;
 }

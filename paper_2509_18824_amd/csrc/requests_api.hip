@@ -74,7 +74,12 @@ static int32_t make_prompt_plan(const hb_attn_desc *d, PromptPlan *p) {
   const int64_t tiles = d->total_nodes * G / p->rows + (d->batch < d->total_nodes ? d->batch : d->total_nodes);
   p->tiles = (int32_t)tiles;
   int64_t parts = d->num_splits;
-  if (parts == 0) parts = tiles > 0 ? 2 * p->units / (tiles * d->num_kv_heads) : 1;  // more find nothing to do, at some cost
+  if (parts == 0) {
+    parts = tiles > 0 ? 2 * p->units / (tiles * d->num_kv_heads) : 1;  // more find nothing to do, at some cost
+    // The float32 kernel's tiles are short, and a join costs as much as two or three of them: 2 prompts of 200 to 256 rows 11.7 us whole, 14.2 cut;
+    // one of 512 18.1 and 20.8; one row over 512 keys 20.7 and 14.9.
+    if (!p->mfma && (parts < 8 || span <= 512)) parts = 1;
+  }
   if (parts > span / least) parts = span / least;
   if (parts > 256) parts = 256;
   if (parts < 1) parts = 1;
