@@ -1,4 +1,28 @@
 // Attention of prompts on the bf16 matrix cores (hb_prompt_attn; head sizes 64 and 128, pages of a power of two).
+//
+// A workgroup has 256 rows, pairs (token, query head of the group) of one (sequence, kv head), and a part of their keys; each of
+// its eight wavefronts has 32 rows, which all share the keys: tiles of 64, four stages of them in LDS.  Both products are
+// transposed, with 32x32x16 instructions:
+//   S^T = K Q^T     A = 32 keys x 16 of D from LDS, B = the rows' queries, which stay in registers
+//   O^T = V^T P^T   A = 32 of D x 16 keys, by the transposing reads of LDS, B = the weights
+// so that a lane's scores are all of one row (two lanes share it), a row's sum and reference are numbers of a lane, and the scores
+// of the first product are, exponentiated and packed in place, the second one's operand.
+//   softmax   in base 2, online.  A row's reference is the largest score of its first block of 32 keys, and moves only when a lane's
+//             weights of a step sum to more than 256: float32 and bf16 have the room, and a step needs no maximum, no exchange between
+//             lanes and no scaling of the result.  A weight is rounded to bf16; results are divided by the sum of the rounded ones
+//             (errors of the two then cancel in part), the log-sum-exp is made of the others.
+//   loads     global to LDS, 16 bytes a lane, each piece of a row at its place XOR a number of the row, so that neither product's
+//             reads meet in a bank.  A tile is asked for three tiles ahead; its addresses are made once.
+//   a step    is 16 matrix instructions of 32 clocks and, between each two, a sixteenth of the last block's softmax and of the
+//             next reads from LDS, laid side by side by hand: left alone, the compiler puts them one behind the other
+//             (8192 rows: 0.62 ms, so 0.50).
+//
+// What bounds it is the matrix cores' rate at the clock that they leave (2.0 of 2.4 GHz under this load).  28 query and 4 kv heads of 128:
+//   one prompt of 8192 rows 479 us, 997 TFLOP/s; of 32768 1106 TFLOP/s (a large bf16 product: 1201 to 1510)
+//   512 rows over 32 K cached 275 us, 859 TFLOP/s: 57 tiles in 4 parts of 256 compute units
+//   8 prompts of 1 to 2048 rows, some behind a cached beginning, 228 us, 836 TFLOP/s
+// Not taken: 64 rows a wavefront, one a SIMD (500 us; 8 ragged prompts 295); tiles of 128 rows by four wavefronts (64 rows alone 9 us
+// instead of 12, but 1024 43 to 52 instead of 36); 512 rows over 32 K in one to three parts (814, 440, 309 us).
 #include <type_traits>
 
 #include "prompt.h"
@@ -216,6 +240,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, i
 #pragma unroll 1
   for (int careful = 0;; careful = 1) {
   ref = 0.f;
+  const float most = careful ? -1.f : kMost;  // careful: every step looks
 
   const int k_lane = j * S::kRowBytes, kx = hf ^ S::k_swz(j);
   auto k_at = [&](const unsigned char *st, int blk) { return st + blk * 32 * S::kRowBytes + k_lane; };
@@ -258,12 +283,14 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, i
   // its first key, or nothing at all of this part), the reference becomes the row's largest score of the block and the weights
   // are made anew.
   auto settle = [&](const f32x16 &x, Sums part, bool first) {
-    if (first || __any(!(part.rounded <= kMost))) {
+    if (first || __any(!(part.rounded <= most))) {
       asm volatile("" ::: "memory");
       const float mx = half_max(max16(x)) * c1;  // c1 > 0
       // (a row's own weights decide, not those of the others in the wavefront)
-      const bool grow = first ? mx > HB_NEG_INF : half_max(part.rounded) > kMost && mx > ref;
-      const float alpha = grow ? __builtin_amdgcn_exp2f(ref - mx) : 1.f;
+      // nothing: no score so far that was more than -infinity, or none that is not lost against the reference of such a beginning
+      const bool nothing = first || (careful && half_sum(l) == 0.f);
+      const bool grow = nothing ? mx > HB_NEG_INF : half_max(part.rounded) > kMost && mx > ref;
+      const float alpha = grow && !nothing ? __builtin_amdgcn_exp2f(ref - mx) : 1.f;
       ref = grow ? mx : ref;
       if (first) {  // what the sums hold so far is nothing
         l = le = 0.f;
@@ -288,7 +315,6 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, i
   auto step = [&](const unsigned char *pv, const unsigned char *pk, bool first, auto middle) {
     constexpr int kAll = KS + 2 * DT, kEach = 16 / kAll;
     f32x16 sn;
-    bf16x8 pn[2];
     float p[2];
     Sums part = {0.f, 0.f};
     uint32_t w[8];
@@ -394,9 +420,10 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, i
   for (int i = my_tiles; i < n_tiles; ++i) turn(i);
 
   // Keys that a row does not see have weight 0 in the products, and 0 times a value that is not finite is no number.  Where
-  // that, or anything else, has made results that are not finite, the workgroup does its part once more, `careful`: such
-  // values of keys that some row does not see are zeros in LDS, and are added here to the rows that see them.  Rows that do
-  // not get the bits that they get from any other value there.
+  // that, or anything else, has made results that are not finite, or left a row that sees keys without weights (its first
+  // block's scores were all -infinity, and those behind are far below 0), the workgroup does its part once more, `careful`: such
+  // values of keys that some row does not see are zeros in LDS, and are added here to the rows that see them, and a row's reference
+  // is made when it has a score.  All others get the bits that they had.
   if (careful) {
     for (int kk = max(begin, all_see + 1); kk < end; ++kk) {  // a row of the prompt: the prefix is seen by all
       const bf16_t *vs = vr + ((size_t)(w.row0 + kk - P) * Hkv + h) * D;
@@ -411,7 +438,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, i
     }
     break;
   }
-  float none = 0.f;  // 0, or no number
+  float none = half_sum(l) == 0.f && sees >= begin ? __builtin_nanf("") : 0.f;  // 0, or no number
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll

@@ -111,6 +111,26 @@ def test_values_that_are_not_finite_reach_those_who_see_them(dtype):
             c.check(torch.from_numpy(o), lse, label="the others")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_keys_whose_scores_are_minus_infinity(dtype):
+    """The first 70 keys, prefix and prompt, have none but such scores, and those behind are about -600: weights are relative to
+    what a row has seen.  Rows that see nothing else have no result."""
+    c = Prompts(16, dtype, 4, 2, 64, 16, [40], [90])
+    c.q[:, :, 0] = 8.0
+    c.q[:, :, 1:] *= 0.25
+    c.k[:, :, 0], c.k_pool[:, :, :, 0] = -600.0, -torch.inf
+    c.k[:30, :, 0] = -torch.inf
+    ref, ref_lse = c.reference()
+    seen = np.arange(90) >= 30
+    for algo in _algos(dtype, 64, 16):
+        for splits in (1, 2, 3):
+            out, lse = c.run(algo=algo, num_splits=splits)
+            o = W.widen(out)
+            assert np.isnan(o[~seen]).all()
+            assert np.abs(o[seen] - ref[seen]).max() <= (1e-3 if dtype == "f32" else 2.0 ** -6) * (4 + np.abs(ref[seen]).max())
+            assert np.abs(W.widen(lse)[seen] - ref_lse[seen]).max() <= 600 * 2.0 ** -14
+
+
 def test_largest_scores_and_values():
     """Scores near float32's exponents' middle: weights of one key alone, and sums of the type's largest values."""
     c = Prompts(12, "bf16", 4, 2, 128, 16, [30], [70], scale=50.0)
