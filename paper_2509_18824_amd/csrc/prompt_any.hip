@@ -27,8 +27,8 @@ hipError_t launch_any(const PromptArgs &a, hipStream_t s) {
 }
 
 // out = sum of the parts' results, each scaled by 2^(its largest score - the largest of all), over the like sum of their sums.
-// A thread has eight elements of a row.  The time of a call is that of a few dependent reads, so what there is to do is read
-// (PromptArgs::heads), not found out again: 14 -> 8 us for 512 rows over 32 K in four parts.
+// A thread has eight elements of a row, and four parts of them under way.  The time of a call is that of a few dependent reads, so
+// what there is to do is read (PromptArgs::heads), not found out again: 14 -> 8 us for 64 rows over 8 K in four parts.
 template <typename T>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int bm) {
   const PromptArgs::Head t = a.heads[blockIdx.x];
@@ -39,18 +39,31 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int bm) 
     const size_t at = (size_t)(t.row0 + token) * a.d.num_q_heads + (size_t)h * G + (row - token * G);
     const size_t slot = (((size_t)blockIdx.x * Hkv + h) * a.parts) * bm + r;
     float m = HB_NEG_INF, l = 0.f, whole = 0.f, x[8] = {};
-    for (int p = 0; p < t.parts; ++p) m = fmaxf(m, a.part_ml[(slot + (size_t)p * bm) * 4]);
-    for (int p = 0; p < t.parts; ++p) {
-      const size_t s = slot + (size_t)p * bm;
-      const f32x4 ml = *(const f32x4 *)(a.part_ml + s * 4);
-      float y[8];
-      load8(a.part_o + s * D + d0, y);
-      if (ml[0] == HB_NEG_INF && ml[1] == 0.f) continue;  // sees none of this part's keys
-      const float c = exp2_of(ml[0] - m);
-      l += c * ml[1];
-      whole += c * ml[2];
+    for (int p0 = 0; p0 < t.parts; p0 += 4) {
+      f32x4 ml[4];
+      float y[4][8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] += c * y[e];
+      for (int p = 0; p < 4; ++p) {
+        const size_t s = slot + (size_t)min(p0 + p, t.parts - 1) * bm;
+        ml[p] = *(const f32x4 *)(a.part_ml + s * 4);
+        load8(a.part_o + s * D + d0, y[p]);
+      }
+      const float top = fmaxf(fmaxf(fmaxf(m, ml[0][0]), fmaxf(ml[1][0], ml[2][0])), ml[3][0]);  // (the last one again: no matter)
+      const float alpha = m == top ? 1.f : exp2_of(m - top);
+      m = top;
+      l *= alpha;
+      whole *= alpha;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= alpha;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        if (p0 + p >= t.parts || (ml[p][0] == HB_NEG_INF && ml[p][1] == 0.f)) continue;  // ... or it sees none of this part's keys
+        const float c = exp2_of(ml[p][0] - m);
+        l += c * ml[p][1];
+        whole += c * ml[p][2];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += c * y[p][e];
+      }
     }
     const float inv = 1.f / l;
 #pragma unroll
