@@ -17,10 +17,12 @@
 //             next reads from LDS, laid side by side by hand: left alone, the compiler puts them one behind the other
 //             (8192 rows: 0.62 ms, so 0.50).
 //
-// What bounds it is the matrix cores' rate at the clock that they leave (2.0 of 2.4 GHz under this load).  28 query and 4 kv heads of 128:
+// What bounds it is a SIMD's two kinds of work: of 8192 rows' cycles 53 % have the matrix core busy and 50 % the vector unit (four
+// instructions and an exponential for each matrix instruction; no bank conflicts), at the 1.8 GHz that this load leaves of 2.4.
+// 28 query and 4 kv heads of 128:
 //   one prompt of 8192 rows 479 us, 997 TFLOP/s; of 32768 1106 TFLOP/s (a large bf16 product: 1201 to 1510)
-//   512 rows over 32 K cached 275 us, 859 TFLOP/s: 57 tiles in 4 parts of 256 compute units
-//   8 prompts of 1 to 2048 rows, some behind a cached beginning, 228 us, 836 TFLOP/s
+//   512 rows over 32 K cached 272 us, 878 TFLOP/s: 56 tiles in 4 parts on 256 compute units, and a join of 12 us
+//   8 prompts of 1 to 2048 rows, some behind a cached beginning, 230 us, 830 TFLOP/s
 // Not taken: 64 rows a wavefront, one a SIMD (500 us; 8 ragged prompts 295); tiles of 128 rows by four wavefronts (64 rows alone 9 us
 // instead of 12, but 1024 43 to 52 instead of 36); 512 rows over 32 K in one to three parts (814, 440, 309 us).
 #include <type_traits>
