@@ -685,7 +685,8 @@ int32_t hb_pages_give(int32_t B, int32_t page_size, int32_t max_blocks_per_seq, 
 
 /*
  * Rows of K and V (a prompt's, or any) bit for bit to their slots: row r to pool[slots[r] / page_size][:][slots[r] % page_size][:].
- * A slot outside [0, num_blocks * page_size) has no place and its row is skipped; of two rows with the same slot one wins.
+ * A slot outside [0, num_blocks * page_size) has no place and its row is skipped.  Rows with a place have one each: with the same
+ * slot twice, every 16 bytes of it are one of the two rows'.
  *   k_rows, v_rows  device [n_rows, Hkv, D]     slots  device int32 [n_rows]     pools as in hb_tree_verify_attn
  * Uses desc->{dtype, num_kv_heads, head_dim, page_size, num_blocks}.  Errors: INVALID_ARG, UNSUPPORTED, DEVICE.
  */

@@ -17,8 +17,9 @@
 //             next reads from LDS, laid side by side by hand: left alone, the compiler puts them one behind the other
 //             (8192 rows: 0.62 ms, so 0.50).
 //
-// What bounds it is a SIMD's two kinds of work: of 8192 rows' cycles 53 % have the matrix core busy and 50 % the vector unit (four
-// instructions and an exponential for each matrix instruction; no bank conflicts), at the 1.8 GHz that this load leaves of 2.4.
+// What bounds it is how a SIMD's two wavefronts share it: over 8192 rows the matrix core is busy for 53 % of the cycles, vector
+// instructions are issued in 43 (four and an exponential for each matrix instruction), LDS is busy for 27, without bank conflicts;
+// a wavefront waits for a place to issue in 33 % of its time and for LDS and barriers in 29.  The clock is 1.8 GHz of 2.4 under this load.
 // 28 query and 4 kv heads of 128:
 //   one prompt of 8192 rows 479 us, 997 TFLOP/s; of 32768 1106 TFLOP/s (a large bf16 product: 1201 to 1510)
 //   512 rows over 32 K cached 272 us, 878 TFLOP/s: 56 tiles in 4 parts on 256 compute units, and a join of 12 us

@@ -221,49 +221,70 @@ __device__ __forceinline__ void each_marked(const RulesArgs &a, const Row &r, Ro
 }
 
 // -infinity where the bit of `keep` is not set; and what is no number gives way to it
-__device__ __forceinline__ void keep_of(uint32_t keep, float (&z)[4]) {
+template <int N>
+__device__ __forceinline__ void keep_of(uint32_t keep, float (&z)[N]) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < N; ++e) {
     const uint32_t k = (uint32_t)((int32_t)(keep << (31 - e)) >> 31);
     z[e] = fmaxf(__uint_as_float((__float_as_uint(z[e]) & k) | (0xff800000u & ~k)), -HB_INF);
   }
 }
 
-// Four tokens' logits as they lie in memory; WHOLE: rows are a multiple of four long, and pieces aligned
-template <typename T, bool WHOLE>
+// N tokens' logits as they lie in memory; WHOLE: rows are a multiple of four long, and pieces of four aligned
+template <typename T, bool WHOLE, int N>
 struct Piece {
-  T x[4];
+  T x[N];
 };
 template <>
-struct Piece<float, true> {
+struct Piece<float, true, 4> {
   f32x4 x;
 };
 template <>
-struct Piece<bf16_t, true> {
+struct Piece<bf16_t, true, 4> {
   u32x2 x;
 };
-template <typename T>
-__device__ __forceinline__ void load_piece(const T *p, int n, Piece<T, false> &y) {
+template <>
+struct Piece<bf16_t, true, 8> {
+  u32x2 x[2];
+};
+template <typename T, int N>
+__device__ __forceinline__ void load_piece(const T *p, int n, Piece<T, false, N> &y) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y.x[e] = e < n ? p[e] : T(0);
+  for (int e = 0; e < N; ++e) y.x[e] = e < n ? p[e] : T(0);
 }
-__device__ __forceinline__ void load_piece(const float *p, int, Piece<float, true> &y) { y.x = *(const f32x4 *)p; }
-__device__ __forceinline__ void load_piece(const bf16_t *p, int, Piece<bf16_t, true> &y) { y.x = *(const u32x2 *)p; }
-template <typename T>
-__device__ __forceinline__ void widen(const Piece<T, false> &y, int n, float (&z)[4]) {
+__device__ __forceinline__ void load_piece(const float *p, int, Piece<float, true, 4> &y) { y.x = *(const f32x4 *)p; }
+__device__ __forceinline__ void load_piece(const bf16_t *p, int, Piece<bf16_t, true, 4> &y) { y.x = *(const u32x2 *)p; }
+__device__ __forceinline__ void load_piece(const bf16_t *p, int n, Piece<bf16_t, true, 8> &y) {
+  typedef uint32_t half_aligned __attribute__((ext_vector_type(4), aligned(8)));
+  if (n >= 8) {
+    const half_aligned x = *(const half_aligned *)p;
+    y.x[0] = x.xy;
+    y.x[1] = x.zw;
+  } else {
+    y.x[0] = *(const u32x2 *)p;
+    y.x[1] = (u32x2)0xff80ff80u;  // -infinity
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ void widen(const Piece<T, false, N> &y, int n, float (&z)[N]) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) z[e] = e < n ? load_f32(&y.x[e]) : -HB_INF;
+  for (int e = 0; e < N; ++e) z[e] = e < n ? load_f32(&y.x[e]) : -HB_INF;
 }
-__device__ __forceinline__ void widen(const Piece<float, true> &y, int, float (&z)[4]) {
+__device__ __forceinline__ void widen(const Piece<float, true, 4> &y, int, float (&z)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) z[e] = y.x[e];
 }
-__device__ __forceinline__ void widen(const Piece<bf16_t, true> &y, int, float (&z)[4]) {
+__device__ __forceinline__ void widen_two(uint32_t x, float *z) {
+  z[0] = __uint_as_float(x << 16);
+  z[1] = __uint_as_float(x & 0xffff0000u);
+}
+__device__ __forceinline__ void widen(const Piece<bf16_t, true, 4> &y, int, float (&z)[4]) {
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    z[2 * e] = __uint_as_float(y.x[e] << 16);
-    z[2 * e + 1] = __uint_as_float(y.x[e] & 0xffff0000u);
-  }
+  for (int e = 0; e < 2; ++e) widen_two(y.x[e], z + 2 * e);
+}
+__device__ __forceinline__ void widen(const Piece<bf16_t, true, 8> &y, int, float (&z)[8]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) widen_two(y.x[e / 2][e % 2], z + 2 * e);
 }
 
 // PAST: the caches, which then keep the logits for the second time over them (16 trees of 60 nodes over 152064 tokens: 253 us, else 274)
@@ -291,16 +312,16 @@ __device__ __forceinline__ void store_four(bf16_t *p, int n, const float (&z)[4]
   }
 }
 
-// Tokens v0 .. v1 - 1 four at a time (what a wavefront stores is whole lines then: with eight, in two halves of 16 bytes, half the
-// requests to L2 were for parts of one): f(v, values), those of marked tokens -infinity, or (MARKED) as they are.  The logits
-// of the next turns are asked for before this one's are worked on.
-template <typename T, bool WHOLE, bool MARKED, int kThreads, typename F>
-__device__ __forceinline__ void each_four(const RulesArgs &a, const Row &r, const RowLds<kThreads> &, int t, int v0, int v1, F f) {
-  constexpr int kTurn = kThreads * 4, kDeep = 2;
+// Tokens v0 .. v1 - 1, N at a time: f(v, values), those of marked tokens -infinity, or (MARKED) as they are.  The logits of the next
+// turns are asked for before this one's are worked on.  N is four where something is stored: what a wavefront stores is whole
+// lines then (with eight, in two halves of 16 bytes, half the requests to L2 were for parts of one).
+template <typename T, bool WHOLE, int N, bool MARKED, int kThreads, typename F>
+__device__ __forceinline__ void each_piece(const RulesArgs &a, const Row &r, const RowLds<kThreads> &, int t, int v0, int v1, F f) {
+  constexpr int kTurn = kThreads * N, kDeep = 2;
   const T *row = (const T *)a.logits + (size_t)t * a.V;
-  Piece<T, WHOLE> y[kDeep];
+  Piece<T, WHOLE, N> y[kDeep];
   uint32_t allowed[kDeep];
-  const int first = v0 + (int)threadIdx.x * 4;
+  const int first = v0 + (int)threadIdx.x * N;
   auto ask = [&](int v, int at) {
     if (v >= v1) return;
     load_piece(row + v, a.V - v, y[at]);
@@ -313,9 +334,9 @@ __device__ __forceinline__ void each_four(const RulesArgs &a, const Row &r, cons
     for (int i = 0; i < kDeep; ++i) {
       const int at = v + i * kTurn;
       if (at >= v1) break;
-      float z[4];
+      float z[N];
       widen(y[i], a.V - at, z);
-      const uint32_t bits = allowed[i] >> (at & 4), marked = marked_lds[(at - v0) >> 5] >> ((at - v0) & 31);
+      const uint32_t bits = allowed[i] >> (at & (8 - N)), marked = marked_lds[(at - v0) >> 5] >> ((at - v0) & 31);
       ask(at + kDeep * kTurn, i);
       keep_of(MARKED ? bits | marked : bits & ~marked, z);
       f(at, z);
@@ -329,7 +350,7 @@ __global__ __launch_bounds__(kSplit) void rules_logits_kernel(RulesArgs a) {
   const Row r = row_of<kSplit>(a, t, v0, v1, s);
   if (r.b < 0) return;
   T *out = (T *)a.out + (size_t)t * a.V;
-  each_four<T, WHOLE, true>(a, r, s, t, v0, v1, [&](int v, float (&z)[4]) { store_four<WHOLE>(out + v, a.V - v, z); });
+  each_piece<T, WHOLE, 4, true>(a, r, s, t, v0, v1, [&](int v, float (&z)[4]) { store_four<WHOLE>(out + v, a.V - v, z); });
   // (which may have been written where the logits are: marked ones as they were)
   each_marked<T>(a, r, s, t, v0, v1, false, [&](int v, float z) { store_f32(out + v, z); });
 }
@@ -345,14 +366,15 @@ __device__ __forceinline__ float weight_of(float z, float top, float k) {
   const float d = z == top ? 0.f : z - top;  // also where both are infinite
   return z > -HB_INF ? __builtin_amdgcn_exp2f(d * k) : 0.f;
 }
-// four values' weights.  Plainly they are what they should be for every finite `top` and k > 0: -infinity gives 0.
-__device__ __forceinline__ void weigh(float (&z)[4], float top, float k) {
+// Some values' weights.  Plainly they are what they should be for every finite `top` and k > 0: -infinity gives 0.
+template <int N>
+__device__ __forceinline__ void weigh(float (&z)[N], float top, float k) {
   if (__any(!(top < HB_INF)) || !(k > 0.f)) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = weight_of(z[e], top, k);
+    for (int e = 0; e < N; ++e) z[e] = weight_of(z[e], top, k);
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = __builtin_amdgcn_exp2f((z[e] - top) * k);
+    for (int e = 0; e < N; ++e) z[e] = __builtin_amdgcn_exp2f((z[e] - top) * k);
   }
 }
 __device__ __forceinline__ Stat joined(const Stat x, const Stat y, float k, bool greedy) {
@@ -385,28 +407,32 @@ __device__ __forceinline__ bool greedy_of(const Row &r) { return __builtin_amdgc
 template <typename T, bool WHOLE, int kThreads>
 __device__ __forceinline__ Stat stat_of(const RulesArgs &a, const Row &r, RowLds<kThreads> &s, int t, int v0, int v1, float k) {
   __shared__ Stat waves[kThreads / 64];
+  constexpr int N = sizeof(T) == 2 ? 8 : 4;  // 16 bytes
   const bool greedy = greedy_of(r);
   Stat mine = nothing_of(greedy);
   if (greedy)
-    each_four<T, WHOLE, false>(a, r, s, t, v0, v1, [&](int v, float (&z)[4]) {
+    each_piece<T, WHOLE, N, false>(a, r, s, t, v0, v1, [&](int v, float (&z)[N]) {
       float top = z[0];
 #pragma unroll
-      for (int e = 1; e < 4; ++e) top = fmaxf(top, z[e]);
+      for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
       if (top > mine.top) {
         mine.top = top;
 #pragma unroll
-        for (int e = 3; e >= 0; --e)
+        for (int e = N - 1; e >= 0; --e)
           if (z[e] == top) mine.token = v + e;
       }
     });
   else
-    each_four<T, WHOLE, false>(a, r, s, t, v0, v1, [&](int, float (&z)[4]) {
+    each_piece<T, WHOLE, N, false>(a, r, s, t, v0, v1, [&](int, float (&z)[N]) {
       const float last = mine.top;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) mine.top = fmaxf(mine.top, z[e]);
+      for (int e = 0; e < N; ++e) mine.top = fmaxf(mine.top, z[e]);
       if (__any(last != mine.top)) mine.sum *= weight_of(last, mine.top, k);
       weigh(z, mine.top, k);
-      mine.sum += (z[0] + z[1]) + (z[2] + z[3]);
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < N; e += 4) sum += (z[e] + z[e + 1]) + (z[e + 2] + z[e + 3]);
+      mine.sum += sum;
     });
   each_marked<T>(a, r, s, t, v0, v1, false, [&](int v, float z) {
     if (z > -HB_INF) mine = joined(mine, {z, 1.f, v}, k, greedy);
@@ -423,7 +449,7 @@ __device__ __forceinline__ void probs_of(const RulesArgs &a, const Row &r, RowLd
   float *out = (float *)a.out + (size_t)t * a.V;
   if (!greedy_of(r)) {
     const float scale = all.sum > 0.f ? 1.f / all.sum : 0.f;
-    each_four<T, WHOLE, false>(a, r, s, t, v0, v1, [&](int v, float (&z)[4]) {
+    each_piece<T, WHOLE, 4, false>(a, r, s, t, v0, v1, [&](int v, float (&z)[4]) {
       weigh(z, all.top, k);
 #pragma unroll
       for (int e = 0; e < 4; ++e) z[e] *= scale;
