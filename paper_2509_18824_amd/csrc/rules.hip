@@ -10,9 +10,10 @@
 // share, and make first where they are several) and marks them in a bitmap in LDS.  The row is then gone through without them,
 // four tokens a thread and little to do for each, and they are done behind it, a thread each.  16 trees of 60 nodes over 152064
 // tokens: with the penalties' code at each of a thread's tokens 472 us; with a loop over the marks that a wavefront meets 331
-// (one token in a hundred is marked: nearly every wavefront meets some); so 253, of which 102 are the first time over the logits
-// and 92 the stores by themselves.  What bounds it is the vector work of the two passes.  (A row held in 76 registers a thread
-// between them: 392, with one workgroup a CU; four loads under way a thread instead of two: the same, eight: 355.)
+// (one token in a hundred is marked: nearly every wavefront meets some); so 241.  What bounds it are the bytes past L2: logits and
+// masks from memory (307 MB), the logits again from the last cache, 592 MB of stores, 1.19 GB at 4.9 TB/s, where a copy has 5.1;
+// fewer vector instructions, or more loads under way, change nothing.  (A row held in 76 registers a thread between the passes: 392,
+// with one workgroup a CU.)
 // In float32, in the order that is written above, without contraction: two sides that follow it agree about which z is the
 // largest.
 #include "rules.h"
@@ -287,7 +288,7 @@ __device__ __forceinline__ void widen(const Piece<bf16_t, true, 8> &y, int, floa
   for (int e = 0; e < 4; ++e) widen_two(y.x[e / 2][e % 2], z + 2 * e);
 }
 
-// PAST: the caches, which then keep the logits for the second time over them (16 trees of 60 nodes over 152064 tokens: 253 us, else 274)
+// PAST: the caches, which then keep the logits for the second time over them (16 trees of 60 nodes over 152064 tokens 274 -> 253 us)
 template <bool WHOLE, bool PAST = false>
 __device__ __forceinline__ void store_four(float *p, int n, const float (&z)[4]) {
   const f32x4 x = {z[0], z[1], z[2], z[3]};
