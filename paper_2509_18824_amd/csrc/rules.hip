@@ -12,7 +12,8 @@
 // tokens: with the penalties' code at each of a thread's tokens 472 us; with a loop over the marks that a wavefront meets 331
 // (one token in a hundred is marked: nearly every wavefront meets some); so 241.  What bounds it are the bytes past L2: logits and
 // masks from memory (307 MB), the logits again from the last cache, 592 MB of stores, 1.19 GB at 4.9 TB/s, where a copy has 5.1;
-// fewer vector instructions, or more loads under way, change nothing.  (A row held in 76 registers a thread between the passes: 392,
+// fewer vector instructions, or more loads under way, change nothing.  Biases go to their tokens' places among the marked ones:
+// looked for at each marked token instead, 29 rows of 1148 tokens with up to 242 each took 68 us, so 26.  (A row held in 76 registers a thread between the passes: 392,
 // with one workgroup a CU.)
 // In float32, in the order that is written above, without contraction: two sides that follow it agree about which z is the
 // largest.
@@ -29,7 +30,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kSplit = 256, kStep = kSplit * 8, kMostChunk = 32768, kBiases = 1024;  // threads of a workgroup that has a chunk of a row
+constexpr int kSplit = 256, kStep = kSplit * 8, kMostChunk = 32768;  // threads of a workgroup that has a chunk of a row
 constexpr int kWhole = 1024, kMostWhole = 1 << 18;  // ... that has a row, and tokens of one
 constexpr float kLog2e = 1.4426950408889634f;
 #define HB_INF __builtin_huge_valf()
@@ -48,35 +49,14 @@ extern __shared__ uint32_t marked_lds[];  // a bit for every token of the chunk
 template <int kThreads>
 struct RowLds {
   static constexpr int kSome = 2 * kThreads;
-  int32_t some[kSome];  // marked tokens, so many at a time, and
-  float value[kSome];   // their values
+  uint32_t some[kSome];  // marked tokens, so many at a time (with kBiased, kSeveral: those that have a bias, or several), and
+  float value[kSome];    // their biases, then their values
   int32_t path[64];
-  alignas(16) int32_t bias_id[kBiases];
-  float bias_value[kBiases];
+  int32_t first[kThreads];  // marked tokens of the threads in front of each
   int32_t sums[kThreads / 64];
   int32_t found[2];
 };
-
-// What is done to token v
-template <int kThreads>
-__device__ __forceinline__ void look_up(const RulesArgs &a, const Row &r, const RowLds<kThreads> &s, int v, bool &seen, float &less, float &more) {
-  const int had = r.counts ? r.counts[v] : 0;
-  int c = had & (kPromptFlag - 1);
-  for (int i = 0; i < r.path; ++i) c += s.path[i] == v;
-  seen = c > 0 || (had & kPromptFlag);
-  less = (c > 0 ? r.presence : 0.f) + r.frequency * (float)c;
-  more = 0.f;
-  const int here = min(r.biases, kBiases);
-  for (int i = 0; i < here; i += 4) {  // (the list is filled up with tokens that there are not)
-    const int4 id = *(const int4 *)&s.bias_id[i];
-    if (id.x == v) more += s.bias_value[i];
-    if (id.y == v) more += s.bias_value[i + 1];
-    if (id.z == v) more += s.bias_value[i + 2];
-    if (id.w == v) more += s.bias_value[i + 3];
-  }
-  for (int i = here; i < r.biases; ++i)
-    if (a.bias_id[r.bias0 + i] == v) more += a.bias_value[r.bias0 + i];
-}
+constexpr uint32_t kBiased = 1u << 30, kSeveral = 1u << 31;  // V is at most 2^30
 
 // The row's rules, and the marks of its chunk [v0, v1), which nobody changes behind it.  Every one of kThreads threads calls it.
 template <int kThreads>
@@ -146,17 +126,13 @@ __device__ __forceinline__ Row row_of(const RulesArgs &a, int t, int v0, int v1,
     }
     if (lane == 0) s.found[1] = n;
   }
-  for (int i = tid; i < min((r.biases + 3) & ~3, kBiases); i += kThreads) {
-    s.bias_id[i] = i < r.biases ? a.bias_id[r.bias0 + i] : -1;
-    s.bias_value[i] = i < r.biases ? a.bias_value[r.bias0 + i] : 0.f;
-  }
   __syncthreads();
   r.path = s.found[1];
   auto mark = [&](int v) {
     if (v >= v0 && v < v1) atomicOr(&marked[(v - v0) >> 5], 1u << ((v - v0) & 31));
   };
   if (tid < r.path) mark(s.path[tid]);
-  for (int i = tid; i < r.biases; i += kThreads) mark(i < kBiases ? s.bias_id[i] : a.bias_id[r.bias0 + i]);
+  for (int i = tid; i < r.biases; i += kThreads) mark(a.bias_id[r.bias0 + i]);
   if (r.counts && !made) {
     if (a.V % 4 == 0) {
 #pragma unroll 4
@@ -182,7 +158,7 @@ __device__ __forceinline__ Row row_of(const RulesArgs &a, int t, int v0, int v1,
     if (w < tid >> 6) upto += s.sums[w];
     r.marks += s.sums[w];
   }
-  r.first = upto - mine;
+  r.first = s.first[tid] = upto - mine;
   return r;
 }
 
@@ -194,7 +170,7 @@ __device__ __forceinline__ void each_marked(const RulesArgs &a, const Row &r, Ro
   const int words = (v1 - v0 + 31) / 32;
   if (again && r.marks <= kSome) {
     __syncthreads();
-    for (int i = threadIdx.x; i < r.marks; i += kThreads) f(s.some[i], s.value[i]);
+    for (int i = threadIdx.x; i < r.marks; i += kThreads) f((int)s.some[i], s.value[i]);
     return;
   }
   for (int from = 0; from < r.marks; from += kSome) {
@@ -204,13 +180,35 @@ __device__ __forceinline__ void each_marked(const RulesArgs &a, const Row &r, Ro
       for (uint32_t m = marked_lds[i]; m; m &= m - 1, ++at)
         if (at >= 0 && at < kSome) s.some[at] = v0 + 32 * i + __ffs(m) - 1;
     __syncthreads();
+    // each bias to its token's place among the marks: those of the threads in front, of this thread's words in front, of the word
+    for (int i = threadIdx.x; i < r.biases; i += kThreads) {
+      const int v = a.bias_id[r.bias0 + i];
+      if (v < v0 || v >= v1) continue;
+      const int at_v = v - v0, word = at_v >> 5, owner = word % kThreads;
+      int place = s.first[owner] - from + __popc(marked_lds[word] & ((1u << (at_v & 31)) - 1));
+      for (int x = owner; x < word; x += kThreads) place += __popc(marked_lds[x]);
+      if (place < 0 || place >= kSome) continue;
+      if (atomicOr(&s.some[place], kBiased) & kBiased) atomicOr(&s.some[place], kSeveral);
+      s.value[place] = a.bias_value[r.bias0 + i];
+    }
+    if (r.biases > 0) __syncthreads();
     for (int i = threadIdx.x; i < min(r.marks - from, kSome); i += kThreads) {
-      const int v = s.some[i];
+      const uint32_t found = s.some[i];
+      const int v = (int)(found & (kBiased - 1));
+      s.some[i] = (uint32_t)v;
       float z = load_f32((const T *)a.logits + (size_t)t * a.V + v);
       const uint32_t bits = r.mask ? r.mask[v >> 3] : 0xffu;
-      bool seen;
-      float less, more;
-      look_up(a, r, s, v, seen, less, more);
+      const int had = r.counts ? r.counts[v] : 0;
+      int c = had & (kPromptFlag - 1);
+      for (int p = 0; p < r.path; ++p) c += s.path[p] == v;
+      const bool seen = c > 0 || (had & kPromptFlag);
+      const float less = (c > 0 ? r.presence : 0.f) + r.frequency * (float)c;
+      float more = found & kBiased ? s.value[i] : 0.f;
+      if (found & kSeveral) {  // in their order
+        more = 0.f;
+        for (int x = 0; x < r.biases; ++x)
+          if (a.bias_id[r.bias0 + x] == v) more += a.bias_value[r.bias0 + x];
+      }
       if (seen) z = z > 0.f ? z / r.repetition : z * r.repetition;
       z = z - less;
       z = z + more;

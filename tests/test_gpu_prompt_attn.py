@@ -56,6 +56,17 @@ def test_one_token_over_a_long_prefix(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [8, 64, 72, 128, 136, 256])
+def test_many_parts(dtype, D):
+    """More parts than a thread of the join has under way, and than its lanes have groups; some rows see nothing of some."""
+    c = Prompts(21, dtype, 6, 2, D, 16, [5000, 30, 4700], [3, 40, 1])
+    for algo in _algos(dtype, D, 16):
+        for splits in (18, 70):
+            out, lse = c.run(algo=algo, num_splits=splits)
+            c.check(out, lse)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_many_sequences(dtype):
     """More of them than a wavefront has lanes, most of one row or none."""
     rng = np.random.default_rng(8)
