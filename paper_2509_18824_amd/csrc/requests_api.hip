@@ -75,10 +75,12 @@ static int32_t make_prompt_plan(const hb_attn_desc *d, PromptPlan *p) {
   p->tiles = (int32_t)tiles;
   int64_t parts = d->num_splits;
   if (parts == 0) {
-    parts = tiles > 0 ? 2 * p->units / (tiles * d->num_kv_heads) : 1;  // more find nothing to do, at some cost
-    // The float32 kernel's tiles are short, and a join costs as much as two or three of them: 2 prompts of 200 to 256 rows 11.7 us whole, 14.2 cut;
-    // one of 512 18.1 and 20.8; one row over 512 keys 20.7 and 14.9.
-    if (!p->mfma && (parts < 8 || span <= 512)) parts = 1;
+    // More find nothing to do, at some cost: 64 sequences of a token over 8 K whole 198 us, in at most 3, 7, 15 parts 267, 356, 530
+    parts = tiles > 0 ? 2 * p->units / (tiles * d->num_kv_heads) : 1;
+    // A join costs 2 to 4 us, as much as a few tiles.  bf16, whole and cut: 4 prompts of 64 rows over 256 positions 20.3 and 24.9,
+    // one of 512 24.4 and 27.2; one of 256 over 512 30.7 and 29.3, over 768 37.8 and 31.9.  Float32: 2 prompts of 200 to 256 rows 11.7 and
+    // 14.2, one of 512 18.1 and 20.8; one row over 512 20.7 and 14.9.
+    if (p->mfma ? span <= 768 : parts < 8 || span <= 512) parts = 1;
   }
   if (parts > span / least) parts = span / least;
   if (parts > 256) parts = 256;

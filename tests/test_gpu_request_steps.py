@@ -101,6 +101,31 @@ def test_prompts_in_parts_against_the_oracle(S, whole):
     assert pages.length.tolist() == [65, 30, 17] and pages.pages.tolist() == [5, 2, 2] and pages.free_count.tolist() == [blocks - 9]
 
 
+def test_a_prompt_that_gets_no_pages_waits(S):
+    """Of three prompts the second is refused: it has no first token and no rows in the cache, the others are as if alone, and it goes on
+    when another's pages are given back."""
+    rng, model, B, T, blocks = np.random.default_rng(13), Model(2), 3, 160, 6
+    pages, pools = S.PagePool(B, PAGE, 12, blocks, T), None
+    pools = model.pools(blocks)
+    stack = _stack(S, model, pages, pools, B, T, 12, blocks)
+    prompts = [rng.integers(0, V, n) for n in (40, 70, 0)]
+    offset = _load(stack, model, prompts)
+    stack.run()
+    assert pages.granted.tolist() == [1, 0, 1] and pages.length.tolist() == [40, 0, 0] and stack.first_ids.tolist()[1:] == [-1, -1]
+    assert (pages.slots[40:].cpu() == -1).all() and pages.free_count.item() == 3
+    _near(wide(stack.final_hidden)[:40], model.hidden_ref(model.embedding[prompts[0]]))
+    pages.length[0] = 0
+    pages.give(pages.length)
+    assert pages.free_count.item() == blocks
+    _load(stack, model, [prompts[0][:0], prompts[1], prompts[0][:0]])
+    stack.run()
+    assert pages.granted.tolist() == [1, 1, 1] and pages.length.tolist() == [0, 70, 0]
+    ref = model.hidden_ref(model.embedding[prompts[1]])
+    _near(wide(stack.final_hidden)[:70], ref)
+    logits = wide(stack.final_hidden)[69] @ wide(model.lm).T
+    assert logits[stack.first_ids[1].item()] >= logits.max() - 1e-4 * np.abs(logits).max()
+
+
 def test_a_prompt_and_then_verification_steps_over_its_cache(S):
     """Prompt, tree, prompt again: what a verification step sees of a prompt is what the prompt's own rows saw.  The nodes of a chain
     have the hidden states of the prompt that goes on with them (both within 1e-2 of the exact ones, two layers of bf16), the
