@@ -327,3 +327,35 @@ def test_sampled_steps_from_a_hip_graph(S):
         torch.cuda.synchronize()
         for a, b in zip(eager, outs):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_calls_on_two_streams_at_once(S):
+    """Every call beside another of its kind, each with buffers of its own, handed the stream or found on the current one."""
+    import paper_2509_18824_amd as hb
+    from prompts import Prompts
+    from test_gpu_requests import Rules, _pages, _take
+    cases = [Prompts(31, "bf16", 8, 2, 128, 16, [900, 40], [200, 33]), Prompts(32, "f32", 4, 2, 64, 16, [700, 3], [50, 90])]
+    rules = [Rules(33, "bf16", [60, 60, 40], 5000, 9, 5), Rules(34, "f32", [3, 8], 30000, 700, 5)]
+    want = [(c.run(), r.run(), _take(_pages(9 + i, 12, 16, 90, 300, 0, 2))) for i, (c, r) in enumerate(zip(cases, rules))]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(4):
+        made = []
+        for i, (c, r, stream) in enumerate(zip(cases, rules, streams)):
+            with torch.cuda.stream(stream):
+                made.append((c.run(), r.run(), _take(_pages(9 + i, 12, 16, 90, 300, 0, 2))))
+        torch.cuda.synchronize()
+        for w, m in zip(want, made):
+            for a, b in zip((*w[0], *w[1], *w[2].values()), (*m[0], *m[1], *m[2].values())):
+                assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    # the stream as an argument: behind what fills the rows there, not behind the current stream
+    k = torch.zeros((64, 4, 128), dtype=torch.bfloat16, device="cuda")
+    pools = [torch.zeros((8, 4, 16, 128), dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    slots = i32(np.arange(64))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(streams[0]):
+        for _ in range(50):
+            k.add_(1.0)
+    hb.hb_kv_append(S.make_desc("bf16", 1, 4, 4, 128, 16, 1, 8, 0, 1, 1.0), k, k, slots, *pools, stream=streams[0])
+    torch.cuda.synchronize()
+    assert (pools[0][:4] == 50.0).all() and (pools[1][:4] == 50.0).all() and (pools[0][4:] == 0).all()

@@ -175,9 +175,9 @@ def test_rules_against_the_oracle(dtype, nodes, V, biases, masks):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("nodes,V,biases,masks,had", [([60, 60, 60], 1000, 5, 7, 0.1), ([64, 0, 64, 33], 9001, 1100, 3, 0.5), ([1] * 130, 4000, 3, 5, 0.9),
-                                                      ([43, 43, 43], 30000, 0, 0, 0.2), ([50, 50, 50], 20004, 2, 4, 0.0)])
+                                                      ([43, 43, 43], 30000, 0, 0, 0.2), ([50, 50, 50], 20004, 2, 4, 0.0), ([44, 43, 43], 262148, 2, 1, 0.01)])
 def test_rules_of_many_rows(dtype, nodes, V, biases, masks, had):
-    """A workgroup a row: counts of a few tokens and of nearly all, shared by a tree's rows or not."""
+    """A workgroup a row: counts of a few tokens and of nearly all, shared by a tree's rows or not; rows that are too long for one."""
     c = Rules(V + len(nodes) + 1, dtype, nodes, V, biases, masks)
     rng = np.random.default_rng(V)
     c.counts = np.where(rng.random(c.counts.shape) < had, rng.integers(1, 4, c.counts.shape), 0) + (rng.random(c.counts.shape) < had / 2) * (1 << 30)
