@@ -8,10 +8,12 @@
 //   O^T = V^T P^T   16x16x4: A = 16 of D x 4 keys, B = 4 keys x 16 rows
 // The accumulator of lane (j, g), j = lane % 16, g = lane / 16, holds row j's scores for keys 4g + r, r = 0..3: what the
 // r-th instruction of the second product wants in that lane when its four keys are r, 4 + r, 8 + r, 12 + r.
-// A tile of 16 x 64 x 128 is 64 matrix instructions of 32 cycles for each wavefront, 1 us; it takes 2 with one workgroup on a CU (the
-// softmax between the products waits for lanes and LDS) and 1.2 with two.  2 prompts of 200 to 256 rows, 4 heads: 11.7 us; one
-// of 2048 rows 63, of 8192 500 (137 TFLOP/s of the 153 that a large float32 product has).  With sixteen rows
-// for each wavefront, which share the keys, these are 20.3 (four times fewer workgroups, and a join of parts) and 72.
+// What bounds it: for heads of 64 a tile's products are 32 matrix instructions of 32 clocks for each wavefront, 0.5 us; the tile takes 2
+// alone on a CU (pages, keys, LDS and the softmax between the products, one behind the other), and several workgroups on a CU
+// fill each other's gaps, up to what L2 gives: every 16 rows bring all keys.  4 heads of 64 on one of keys: 2 prompts of 200 to 256
+// rows 11.6 us; one of 2048 rows 65, of 8192 510 (68 TFLOP/s of the 153 that a large float32 product has).  With sixteen rows for each
+// wavefront, which share the keys, the first two are 20.3 (four times fewer workgroups, and a join of parts) and 72.  Page ids asked for a
+// tile ahead: one row over 16 K whole 533 -> 441 us, but the prompts 12.8 and 70, and 8192 rows with heads of 128 1056 -> 1701.
 // Softmax is online per row in base 2.  Rows of K and V are four floats apart from a multiple of 64 in LDS: no operand read
 // has a bank conflict.  A head dimension between the sizes built here is filled up with zeros.
 #pragma once
