@@ -575,7 +575,9 @@ hipError_t go_logits(const RulesArgs &a, hipStream_t s) {
 // workgroups that share a row, and their chunks of it
 static int32_t split(int32_t rows, int32_t V, int32_t *chunk) {
   const int64_t most = ((int64_t)V + kStep - 1) / kStep;
-  int64_t parts = rows > 0 ? (4096 + rows - 1) / rows : 1;
+  // Some 1024 workgroups: what each does before it reads its chunk is as much as 2000 tokens of it.  152064 tokens, with 256, 512, 1024, 2048,
+  // 4096: 42 rows of 7 sequences 49, 38, 34, 35, 44 us; 64 rows 61, 47, 41, 42, 46; their logits alone 33, 27, 24, 24, 26; 8 rows 20, 18, 18, 18, 18
+  int64_t parts = rows > 0 ? (1024 + rows - 1) / rows : 1;
   parts = parts < 1 ? 1 : parts > most ? most : parts;
   int64_t len = (((int64_t)V + parts - 1) / parts + kStep - 1) / kStep * kStep;
   if (len > kMostChunk) len = kMostChunk;
