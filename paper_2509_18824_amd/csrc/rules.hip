@@ -587,7 +587,8 @@ static int32_t split(int32_t rows, int32_t V, int32_t *chunk) {
 
 bool rules_marks(int32_t B, int32_t T) { return T >= 4 * (int64_t)B; }
 
-// 0: a workgroup has a row for itself
+// 0: a workgroup has a row for itself.  152064 tokens, a workgroup and several: 90 rows 54 and 48 us, 120 rows 55 to 63 and 57 to 61, 160 rows 59 to 66
+// and 69 to 77, 480 rows 114 and 197
 int32_t rules_parts(int32_t rows, int32_t V, int32_t *chunk) {
   return rows >= 128 && V <= kMostWhole ? 0 : split(rows, V, chunk);
 }
