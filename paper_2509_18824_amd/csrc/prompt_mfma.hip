@@ -87,7 +87,7 @@ struct Shape {
   static constexpr int kSteps = D / 16, kSlabs = D / 32, kBlocks = KT / 32;
   // tiles that have landed beside the one in work when its last block begins; tiles that may still be under way then
   static constexpr int kAhead = kBlocks == 1 ? 3 : 2, kLate = NS - 1 - kAhead;
-  static constexpr size_t kLds = (size_t)NS * kStage;
+  static constexpr size_t kLds = (size_t)NS * kStage + 4 * NW;  // and a word for each wavefront's rows
   static_assert(KT == 32 || KT == 64, "blocks of 32 keys, one or two a tile");
   static_assert(NW * kKeysPerLoad % 16 == 0, "a wavefront's loads lie sixteens apart");
   static_assert(kLoads % NW == 0 && kLate >= 0 && kLds <= 160 * 1024, "a tile's loads are dealt evenly");
@@ -240,8 +240,13 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, i
   // divided by; and as they are in float32, for the log-sum-exp
   float ref, l, le;
   const float c1 = a.d.softmax_scale * kLog2e;
+  // A workgroup does its part up to three times, see below; in the third, rows whose bits are set here in a way of their own.  (In
+  // registers, this and what it needs cost the loop some that it does not have.)
+  uint32_t *const anew = (uint32_t *)(smem + (size_t)NS * S::kStage) + wave;
+  int pass = 0;
 #pragma unroll 1
-  for (int careful = 0;; careful = 1) {
+  for (;; ++pass) {
+  const bool careful = pass > 0;
   ref = 0.f;
   const float most = careful ? -1.f : kMost;  // careful: every step looks
 
@@ -290,11 +295,14 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, i
       asm volatile("" ::: "memory");
       const float mx = half_max(max16(x)) * c1;  // c1 > 0
       // (a row's own weights decide, not those of the others in the wavefront)
-      // nothing: no score so far that was more than -infinity, or none that is not lost against the reference of such a beginning
-      const bool nothing = first || (careful && half_sum(l) == 0.f);
-      const bool grow = nothing ? mx > HB_NEG_INF : half_max(part.rounded) > kMost && mx > ref;
-      const float alpha = grow && !nothing ? __builtin_amdgcn_exp2f(ref - mx) : 1.f;
-      ref = grow ? mx : ref;
+      const bool mine = pass == 2 && (*anew >> j & 1);
+      // a row of `anew`: 2^raise is more than twice the keys
+      const float raise = (float)(33 - __builtin_clz(end - begin)), so_far = half_sum(l), heaviest = half_max(part.rounded), to = mine ? mx + raise : mx;
+      // nothing: no score so far that was more than -infinity
+      const bool nothing = first || (mine && so_far == 0.f);
+      const bool grow = nothing ? mx > HB_NEG_INF : (mine || heaviest > kMost) && to > ref;
+      const float alpha = grow && !nothing ? __builtin_amdgcn_exp2f(ref - to) : 1.f;
+      ref = grow ? to : ref;
       if (first) {  // what the sums hold so far is nothing
         l = le = 0.f;
 #pragma unroll
@@ -424,24 +432,15 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, i
 
   // Keys that a row does not see have weight 0 in the products, and 0 times a value that is not finite is no number.  Where
   // that, or anything else, has made results that are not finite, or left a row that sees keys without weights (its first
-  // block's scores were all -infinity, and those behind are far below 0), the workgroup does its part once more, `careful`: such
-  // values of keys that some row does not see are zeros in LDS, and are added here to the rows that see them, and a row's reference
-  // is made when it has a score.  All others get the bits that they had.
-  if (careful) {
-    for (int kk = max(begin, all_see + 1); kk < end; ++kk) {  // a row of the prompt: the prefix is seen by all
-      const bf16_t *vs = vr + ((size_t)(w.row0 + kk - P) * Hkv + h) * D;
-      if (kk <= sees)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float y = bf16_to_f32(vs[32 * dt + 8 * (r >> 2) + 4 * hf + (r & 3)]);
-            if (!(fabsf(y) < __builtin_huge_valf())) o[dt][r] += y;
-          }
-    }
-    break;
-  }
-  float none = half_sum(l) == 0.f && sees >= begin ? __builtin_nanf("") : 0.f;  // 0, or no number
+  // block's scores were all -infinity, and those behind are far below 0), the workgroup does its part once
+  // more, `careful`: such values of keys that some row does not see are zeros in LDS.  What is so now is so by what a row sees.  Where
+  // there are such rows still (weights of up to 256, or many, times values near float32's largest; no reference; a value that is not
+  // finite), it does its part a third time, in which a row that was such has its reference when it has a score, and `raise`
+  // above its largest score: its weights' sum is at most one, and a sum of them times finite values finite.  All others get the bits
+  // that they had each time.
+  if (pass == 2) break;
+  // (a lane's; 0, or no number)
+  float none = half_sum(l) == 0.f && sees >= begin ? __builtin_nanf("") : 0.f;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -453,8 +452,24 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, i
   if (!no_rows && my_tiles > 0 && none != none) *(int *)smem = 1;
   __syncthreads();
   if (*(int *)smem == 0) break;
+  if (careful) {
+    const unsigned long long lanes = __ballot(none != none);
+    *anew = (uint32_t)lanes | (uint32_t)(lanes >> 32);  // two lanes share a row
+  }
   __syncthreads();
-  }  // careful
+  }
+  if (pass > 0)  // values that were left out, to the rows that see them
+    for (int kk = max(begin, all_see + 1); kk < end; ++kk) {  // a row of the prompt: the prefix is seen by all
+      const bf16_t *vs = vr + ((size_t)(w.row0 + kk - P) * Hkv + h) * D;
+      if (kk <= sees)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float y = bf16_to_f32(vs[32 * dt + 8 * (r >> 2) + 4 * hf + (r & 3)]);
+            if (!(fabsf(y) < __builtin_huge_valf())) o[dt][r] += y;
+          }
+    }
 
   // ---- results ------------------------------------------------------------------------------------------------------
   // (the arguments are read again, so that the loop need not keep them in its registers)

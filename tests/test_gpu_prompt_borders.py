@@ -1,0 +1,80 @@
+"""hb_prompt_attn where weights and values come near the ends of float32: results that are finite are found, and rows beside them
+keep their bits."""
+import numpy as np
+import pytest
+import torch
+
+import workloads as W
+from prompts import Prompts
+from test_gpu_prompt_attn import _algos
+
+pytestmark = pytest.mark.gpu
+
+
+def _along_one_dimension(c, scores):
+    """Every row's natural score of prefix position p is scores[p], of prompt row i scores[len + i] (one sequence)."""
+    c.scale = 0.125
+    c.q[:], c.k[:] = 0, 0
+    c.q[:, :, 0] = 8.0
+    n = c.lens[0]
+    for p in range(n):
+        c.k_pool[c.table[0, p // c.page], :, p % c.page] = 0
+        c.k_pool[c.table[0, p // c.page], :, p % c.page, 0] = scores[p]
+    c.k[:, :, 0] = torch.tensor(scores[n:], dtype=c.tdtype)[:, None]
+
+
+def _value(c, p, x):
+    """The values of position p (prefix, then prompt rows)."""
+    n = c.lens[0]
+    if p < n:
+        c.v_pool[c.table[0, p // c.page], :, p % c.page] = x
+    else:
+        c.v[p - n] = x
+
+
+def _large(D, key, score, sizes):
+    """Rows behind ``key`` see a value of ``sizes`` (one a dimension, over and over) whose score is the only one above 0."""
+    def make(dtype):
+        c = Prompts(41, dtype, 4, 2, D, 16, [70], [300])
+        scores = [0.0] * 370
+        scores[key] = score
+        _along_one_dimension(c, scores)
+        _value(c, key, torch.tensor(np.resize(sizes, D), dtype=c.tdtype))
+        return c
+    return make
+
+
+# A key of a later block whose score is 7 to 8 in base 2 above the first one's: it takes a quarter to two thirds of a row
+CASES = {
+    "prefix, 64": _large(64, 40, 4.84375, [3.0e38, -3.0e38, 1.0, 1e-3]),
+    "prefix, 128": _large(128, 66, 5.5, [-3.0e38, 2.0, 3.0e38]),
+    "prompt, 64": _large(64, 150, 5.5, [3.0e38]),
+    "prompt, 128": _large(128, 200, 4.84375, [2.0e36, -5.0, 1e37]),
+}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", CASES)
+def test_a_large_value_with_a_weight_above_the_reference(name, dtype):
+    c = CASES[name](dtype)
+    ref = c.reference()
+    assert np.isfinite(ref[0]).all() and np.abs(ref[0]).max() > 1e35
+    for algo in _algos(dtype, c.D, 16):
+        for splits in (1, 2, 5):
+            out, lse = c.run(algo=algo, num_splits=splits)
+            _within(c, out, lse, ref, f"{name} {algo} {splits}")
+
+
+def _within(c, out, lse, ref, label):
+    """As Prompts.check, dimension by dimension, where values differ by forty orders of magnitude.
+    Scores here are exact: one product each, of numbers of a few bits.  A weight is off by two roundings of its exponent's argument
+    (of at most 16: 2^-20 each) and one of its own, 2^-24; in bf16 by 2^-8 / 2, in the product and the sum, which each takes for
+    itself; n of them are added with 2^-24 of the mass each."""
+    mass, _ = c.reference(v=np.abs(W.widen(c.v)), v_pool=np.abs(W.widen(c.v_pool)))
+    n = c.lens[0] + c.rows[0]
+    half = 2.0 ** -24 if c.dtype == "f32" else 2.0 ** -8
+    tol = (2 * 3 * 2.0 ** -20 + (n + 16) * 2.0 ** -24) * mass + (half if c.dtype == "bf16" else 0) * mass + 2 * half * np.abs(ref[0]) + 1e-30
+    got = W.widen(out)
+    assert np.isfinite(got).all(), (label, np.argwhere(~np.isfinite(got))[:3])
+    assert (np.abs(got - ref[0]) <= tol).all(), (label, (np.abs(got - ref[0]) / tol).max())
+    assert np.abs(W.widen(lse) - ref[1]).max() <= 3 * 2.0 ** -20 + (n + 16) * 2.0 ** -24 + 2.0 ** -22 * np.abs(ref[1]).max(), label
