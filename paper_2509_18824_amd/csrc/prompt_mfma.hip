@@ -431,8 +431,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, i
   for (int i = my_tiles; i < n_tiles; ++i) turn(i);
 
   // Keys that a row does not see have weight 0 in the products, and 0 times a value that is not finite is no number.  Where
-  // that, or anything else, has made results that are not finite, or left a row that sees keys without weights (its first
-  // block's scores were all -infinity, and those behind are far below 0), the workgroup does its part once
+  // that, or anything else, has made results that are not finite, or a row that sees keys has next to no weights (a row with a
+  // reference has one of 1; its first block's scores were all -infinity, and those behind are below 0), the workgroup does its part once
   // more, `careful`: such values of keys that some row does not see are zeros in LDS.  What is so now is so by what a row sees.  Where
   // there are such rows still (weights of up to 256, or many, times values near float32's largest; no reference; a value that is not
   // finite), it does its part a third time, in which a row that was such has its reference when it has a score, and `raise`
@@ -440,7 +440,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_mfma_kernel(PromptArgs a, i
   // that they had each time.
   if (pass == 2) break;
   // (a lane's; 0, or no number)
-  float none = half_sum(l) == 0.f && sees >= begin ? __builtin_nanf("") : 0.f;
+  float none = !(half_sum(l) >= 0.5f) && sees >= begin ? __builtin_nanf("") : 0.f;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll

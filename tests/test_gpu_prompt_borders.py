@@ -78,3 +78,25 @@ def _within(c, out, lse, ref, label):
     assert np.isfinite(got).all(), (label, np.argwhere(~np.isfinite(got))[:3])
     assert (np.abs(got - ref[0]) <= tol).all(), (label, (np.abs(got - ref[0]) / tol).max())
     assert np.abs(W.widen(lse) - ref[1]).max() <= 3 * 2.0 ** -20 + (n + 16) * 2.0 ** -24 + 2.0 ** -22 * np.abs(ref[1]).max(), label
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("low", [-86.0, -87.5, -89.0, -95.0, -104.0])
+def test_small_scores_behind_a_block_of_none(dtype, low):
+    """The first 70 keys have scores of -infinity, those behind lie where 2^x leaves float32's normal numbers, some on either side."""
+    c = Prompts(44, dtype, 4, 2, 64, 16, [40], [160])
+    scores = [-float("inf")] * 70 + [low - (p * 7 % 5) * 0.5 for p in range(130)]
+    _along_one_dimension(c, [max(s, -1e30) for s in scores])
+    c.k[:30, :, 0], c.k_pool[:, :, :, 0] = -torch.inf, -torch.inf
+    c.k[:30, :, 1:], c.q[:, :, 1:] = 0, 0
+    ref, ref_lse = c.reference()
+    seen = np.arange(160) >= 30
+    # scores are exact; the argument of an exponential is one of (score - reference), off by 2^-17 of scores of up to 128 in float32
+    tol = (2.0 ** -14 if dtype == "f32" else 2.0 ** -7) * (np.abs(ref[seen]).max() + 4)
+    for algo in _algos(dtype, 64, 16):
+        for splits in (1, 2, 3):
+            out, lse = c.run(algo=algo, num_splits=splits)
+            o = W.widen(out)
+            assert np.isnan(o[~seen]).all()
+            assert np.abs(o[seen] - ref[seen]).max() <= tol, (algo, splits, np.abs(o[seen] - ref[seen]).max())
+            assert np.abs(W.widen(lse)[seen] - ref_lse[seen]).max() <= 1e-4
