@@ -704,7 +704,7 @@ int32_t hb_kv_append(const hb_attn_desc *desc, int32_t n_rows, const void *k_row
  * max_nodes_per_tree is not read.  num_splits is the most parts that a row's keys are cut into (0: the library's choice, from
  * the lengths); max_prefix_len_hint sizes workspace and launch and no more: a longer prefix is taken whole.
  * What a row does not see has no influence on it, whatever bits it holds: later rows, slots behind the prefix, other sequences.
- * On the matrix cores finite values with finite scores have a finite result, up to the type's largest.
+ * Finite values with finite scores have a finite result, up to the type's largest.
  * Accumulation is float32; on the matrix cores in bf16 a softmax weight is rounded to bf16 (by 2^-8 of itself at most) for its
  * product with a value and for the sum that results are divided by, not for lse.  bf16 results are rounded once at the end.
  * out, lse and workspace overlap neither each other nor what is read.

@@ -88,6 +88,7 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
   constexpr int kKeys = kAnyKeys, kRow = DP + 4, kTiles = DP / 16, kSteps = DP / 4, kPieces = DP / 8, kAsks = kKeys * kPieces / 256;
   float *lk = lds, *lv = lds + kKeys * kRow;
   int &bad = *(int *)(lds + 2 * kKeys * kRow);  // a value of this tile's is left out, see below
+  int &anew = *(int *)(lds + 2 * kKeys * kRow + 1);  // rows (a bit each) that are done once more, see below
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, j = lane & 15, kg = lane >> 4;
   const int G = a.d.num_q_heads / a.d.num_kv_heads, D = a.d.head_dim, Hkv = a.d.num_kv_heads;
   const int own = wave * 16;  // this wavefront's first key of a tile
@@ -103,9 +104,7 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) qf[s] = there && 4 * s + kg < D ? load_f32((const T *)a.q + at * D + 4 * s + kg) : 0.f;
   f32x4 o[kTiles];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-  float m = HB_NEG_INF, l = 0.f;
+  float m, l;
   const float c1 = a.d.softmax_scale * kLog2e;
 
   // the next tile is on its way to registers while this one is worked on
@@ -136,8 +135,19 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
       }
     }
   };
-  ask(w.begin);
 
+  // Weights of at most 1, times values near float32's largest, may have a sum that is beyond it where their mean is not.  Where
+  // a wavefront's results of a row are not finite, the tile is done once more: such a row's weights are 2^raise times smaller
+  // then, so that their sum is a half at most; the others are as they were.  (A value that is not finite comes here for nothing.)
+  if (tid == 0) anew = 0;
+  float raise = 0.f, smaller = 1.f;
+  for (int again = 0;; ++again) {
+  ask(w.begin);
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  m = HB_NEG_INF;
+  l = 0.f;
+#pragma unroll 1
   for (int k0 = w.begin; k0 < w.end; k0 += kKeys) {
     __syncthreads();
     if (tid == 0) bad = 0;
@@ -188,7 +198,7 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
     for (int t = 0; t < kTiles; ++t) o[t] *= alpha;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const float p = exp2_of(sc[r] - ref);
+      const float p = exp2_of(sc[r] - ref) * smaller;
       l += p;
       const float *vr = lv + (own + 4 * kg + r) * kRow + j;
 #pragma unroll
@@ -210,15 +220,34 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
     }
   }
 
+  if (again) {
+    __syncthreads();
+    break;
+  }
+  float none = 0.f;  // or no number
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) none = fmaf(o[t][r], 0.f, none);
+  const unsigned long long lanes = __ballot(there && none != none);  // four lanes share a row
+  if (lanes && lane == 0) atomicOr(&anew, (int)((lanes | lanes >> 16 | lanes >> 32 | lanes >> 48) & 0xffff));
+  __syncthreads();
+  if (anew == 0) break;
+  if (anew >> j & 1) {
+    const int more = 33 - __builtin_clz(w.end - w.begin);  // 2^more is more than twice the keys
+    raise = (float)more;
+    smaller = __uint_as_float((uint32_t)(127 - more) << 23);
+  }
+  }
+
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
   // one result of the wavefronts': through LDS, where the keys were
   float *lo = lds, *ml = lds + 64 * kRow;  // [wavefront][row]
-  __syncthreads();
 #pragma unroll
   for (int dt = 0; dt < kTiles; ++dt) *(f32x4 *)(lo + (wave * 16 + j) * kRow + 16 * dt + 4 * kg) = o[dt];
   if (kg == 0) {
-    ml[2 * (wave * 16 + j)] = m;
+    ml[2 * (wave * 16 + j)] = m + raise;
     ml[2 * (wave * 16 + j) + 1] = l;
   }
   __syncthreads();
@@ -235,13 +264,14 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
   const int mine = first + r, t2 = mine / G;
   if ((int64_t)mine >= (int64_t)w.n * G) return;
   const size_t to = (size_t)(w.row0 + t2) * a.d.num_q_heads + (size_t)h * G + (mine - t2 * G);
-  const float inv = w.parts == 1 ? 1.f / sum : 1.f;
+  // four results that are finite each: quarters of them, and of what divides them
+  const float inv = w.parts == 1 ? 1.f / (0.25f * sum) : 1.f;
   for (int d0 = 8 * of; d0 < D; d0 += 128) {
     float x[8] = {};
 #pragma unroll
     for (int v = 0; v < 4; ++v)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] += scale[v] * lo[(v * 16 + r) * kRow + d0 + e];
+      for (int e = 0; e < 8; ++e) x[e] += 0.25f * scale[v] * lo[(v * 16 + r) * kRow + d0 + e];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= inv;
     if (w.parts == 1)
@@ -249,7 +279,7 @@ __device__ __forceinline__ void prompt_any_rows(const PromptArgs &a, const Promp
     else
       store8(a.part_o + (slot0 + r) * D + d0, x);
   }
-  if (of == 0 && w.parts > 1) *(f32x4 *)(a.part_ml + (slot0 + r) * 4) = (f32x4){most, sum, sum, 0.f};
+  if (of == 0 && w.parts > 1) *(f32x4 *)(a.part_ml + (slot0 + r) * 4) = (f32x4){most, 0.25f * sum, sum, 0.f};
   if (of == 0 && w.parts == 1 && a.lse) a.lse[to] = (most + log2f(sum)) * kLn2;
 }
 

@@ -44,6 +44,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int bm) 
     const int row = t.first + r, token = row / G;
     const size_t at = (size_t)(t.row0 + token) * a.d.num_q_heads + (size_t)h * G + (row - token * G);
     const size_t slot = (((size_t)blockIdx.x * Hkv + h) * a.parts) * bm + r;
+    constexpr float kShare = 1.f / 512;  // 256 results at most that are finite each: their sum is
     float m = HB_NEG_INF, l = 0.f, whole = 0.f, x[8] = {};
     for (int p0 = group; p0 < t.parts; p0 += 4 * groups) {
       f32x4 ml[4];
@@ -65,10 +66,10 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int bm) 
       for (int p = 0; p < 4; ++p) {
         if (p0 + p * groups >= t.parts || (ml[p][0] == HB_NEG_INF && ml[p][1] == 0.f)) continue;  // ... or it sees none of this part's keys
         const float c = exp2_of(ml[p][0] - m);
-        l += c * ml[p][1];
+        l += kShare * c * ml[p][1];
         whole += c * ml[p][2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += c * y[p][e];
+        for (int e = 0; e < 8; ++e) x[e] += kShare * c * y[p][e];
       }
     }
     if (MANY) {

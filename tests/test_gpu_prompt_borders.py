@@ -100,3 +100,51 @@ def test_small_scores_behind_a_block_of_none(dtype, low):
             assert np.isnan(o[~seen]).all()
             assert np.abs(o[seen] - ref[seen]).max() <= tol, (algo, splits, np.abs(o[seen] - ref[seen]).max())
             assert np.abs(W.widen(lse)[seen] - ref_lse[seen]).max() <= 1e-4
+
+
+@pytest.mark.parametrize("dtype,largest", [("f32", 3.0e38), ("bf16", 3.3895313892515355e38)])
+@pytest.mark.parametrize("D", [64, 72, 128])
+def test_all_values_are_the_types_largest(dtype, largest, D):
+    """A mean of such values is such a value, with other signs in every dimension, whole and in parts."""
+    c = Prompts(42, dtype, 4, 2, D, 16, [90], [200])
+    sign = torch.where(torch.arange(D) % 3 == 0, -1.0, 1.0)
+    for p in range(290):
+        _value(c, p, (largest * sign).to(c.tdtype))
+    for algo in _algos(dtype, D, 16):
+        for splits in (1, 2, 4):
+            out, _ = c.run(algo=algo, num_splits=splits)
+            # weights of 290 keys and their sum: (290 + 16) 2^-24 twice; in bf16 less than the half step that they are rounded to
+            far = np.abs(W.widen(out) / (largest * sign.double().numpy()) - 1)
+            assert far.max() <= (2 * 306 * 2.0 ** -24 if dtype == "f32" else 0), (algo, splits, far.max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_do_not_see_a_large_value_keep_their_bits(dtype):
+    """The same workgroup has rows whose sums overflow at first and rows whose do not."""
+    c = Prompts(43, dtype, 4, 2, 64, 16, [20], [120], sharp=2.0)
+    for algo in _algos(dtype, 64, 16):
+        for splits in (1, 3):
+            want, want_lse = c.run(algo=algo, num_splits=splits)
+            d = c.device()
+            d["v"][50:] = 3.3e38
+            d["v"][90, 0, 3] = torch.inf
+            got, got_lse = c.run(dev=d, algo=algo, num_splits=splits)
+            assert torch.equal(got[:50], want[:50]) and torch.equal(got_lse[:50], want_lse[:50])
+            assert torch.equal(got_lse[:50], want_lse[:50]) and torch.isfinite(got[50:90].float()).all()
+            assert (got[90:, :2, 3] == torch.inf).all() and torch.isfinite(got[90:, 2:].float()).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 136])
+def test_many_parts_of_large_values(dtype, D):
+    """More parts than a thread of the join has, each with a finite result of its own near the type's largest, whose sum is beyond it."""
+    c = Prompts(45, dtype, 4, 2, D, 16, [5000], [3])
+    for p in range(5003):
+        _value(c, p, 3.0e38)
+    exact = float(torch.tensor(3.0e38, dtype=c.tdtype).double())
+    for algo in _algos(dtype, D, 16):
+        for splits in (0, 18, 70):
+            out, _ = c.run(algo=algo, num_splits=splits)
+            far = np.abs(W.widen(out) / exact - 1)
+            # sums of 5003 weights and as many products, 2^-24 each at most
+            assert far.max() <= (2 * 5100 * 2.0 ** -24 if dtype == "f32" else 2.0 ** -8), (algo, splits, far.max())
