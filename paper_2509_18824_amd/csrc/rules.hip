@@ -355,25 +355,26 @@ __global__ __launch_bounds__(kSplit) void rules_logits_kernel(RulesArgs a) {
 }
 
 // What is known of some tokens of a row: of a greedy one (k = 0) the largest value and the lowest token that has it; of the
-// others the largest value, or the lowest that there is, and the sum of 2^((z - largest) k), 0 where nothing is left
+// others the largest value, or the lowest that there is, and the sum of 2^((z - largest) / 2 * k), 0 where nothing is left
 struct Stat {
   float top, sum;
   int token;
 };
 constexpr float kLowest = -3.402823466e38f;
+// Half the difference, which float32 has for all finite values (and no further rounding); k is more than 0, so that what is infinite stays so.
 __device__ __forceinline__ float weight_of(float z, float top, float k) {
-  const float d = z == top ? 0.f : z - top;  // also where both are infinite
-  return z > -HB_INF ? __builtin_amdgcn_exp2f(d * k) : 0.f;
+  const float d = z == top ? 0.f : fmaf(z, 0.5f, -0.5f * top);  // also where both are infinite
+  return __builtin_amdgcn_exp2f(d * k);
 }
-// Some values' weights.  Plainly they are what they should be for every finite `top` and k > 0: -infinity gives 0.
+// Some values' weights.  Plainly they are what they should be for every finite `top`: -infinity gives 0.
 template <int N>
 __device__ __forceinline__ void weigh(float (&z)[N], float top, float k) {
-  if (__any(!(top < HB_INF)) || !(k > 0.f)) {
+  if (__any(!(top < HB_INF))) {
 #pragma unroll
     for (int e = 0; e < N; ++e) z[e] = weight_of(z[e], top, k);
   } else {
 #pragma unroll
-    for (int e = 0; e < N; ++e) z[e] = __builtin_amdgcn_exp2f((z[e] - top) * k);
+    for (int e = 0; e < N; ++e) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], 0.5f, -0.5f * top) * k);
   }
 }
 __device__ __forceinline__ Stat joined(const Stat x, const Stat y, float k, bool greedy) {
@@ -395,9 +396,9 @@ __device__ __forceinline__ Stat joined_lanes(Stat x, float k, bool greedy) {
   return x;
 }
 __device__ __forceinline__ Stat nothing_of(bool greedy) { return {greedy ? -HB_INF : kLowest, 0.f, 0x7fffffff}; }
-// (the same in every lane, and known to be)
+// (the same in every lane, and known to be.  An infinite temperature has a slope that leaves finite values alike to 2^-21.)
 __device__ __forceinline__ float slope_of(const Row &r) {
-  const float k = fminf(kLog2e / r.temperature, 3e38f);
+  const float k = fminf(fmaxf(2.f * (kLog2e / r.temperature), 1e-45f), 3e38f);
   return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(r.temperature > 0.f ? k : 0.f)));
 }
 __device__ __forceinline__ bool greedy_of(const Row &r) { return __builtin_amdgcn_readfirstlane(!(r.temperature > 0.f)); }
