@@ -723,7 +723,7 @@ size_t hb_prompt_attn_workspace_bytes(const hb_attn_desc *desc);
  *          (the root is the pending committed token, which counts holds already)
  *   z      = logit; if c > 0 or the token is in the prompt: z / repetition where z > 0, z * repetition elsewhere
  *   z      = z - (presence * [c > 0] + frequency * c) + bias;  -infinity where the mask forbids the token or z is no number
- * in float32, operation by operation as written.
+ * in float32, operation by operation as written; a token with c = 0 has no penalty of the two, whatever they are.
  * hb_rules_logits: out = z, in the type of the logits (which out may be, all of it, and must not overlap otherwise).
  * hb_rules_probs:  probs = exp((z - max z) / temperature) / sum, what hb_tree_accept_sample takes; temperature 0 (or less, or
  *   no number): 1 at the largest z, the lowest token among equals, which makes that call's rule the greedy one.  Infinite z

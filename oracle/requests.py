@@ -92,7 +92,7 @@ def rules_logits_ref(logits, node_offset, parent, draft_ids, counts, rules, bias
             with np.errstate(invalid="ignore"):
                 z = logits[t].copy()
                 z = np.where(seen, np.where(z > 0, z / repetition, z * repetition), z)
-                z = z - (presence * (c > 0) + frequency * c)
+                z = z - np.where(c > 0, presence + frequency * c, 0.0)
                 for token, value in (biases[b] if biases else []):
                     z[token] += value
             z[np.isnan(z)] = -np.inf

@@ -202,7 +202,7 @@ __device__ __forceinline__ void each_marked(const RulesArgs &a, const Row &r, Ro
       int c = had & (kPromptFlag - 1);
       for (int p = 0; p < r.path; ++p) c += s.path[p] == v;
       const bool seen = c > 0 || (had & kPromptFlag);
-      const float less = (c > 0 ? r.presence : 0.f) + r.frequency * (float)c;
+      const float less = c > 0 ? r.presence + r.frequency * (float)c : 0.f;  // (an infinite penalty times none is none)
       float more = found & kBiased ? s.value[i] : 0.f;
       if (found & kSeveral) {  // in their order
         more = 0.f;

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import workloads as W
+from oracle import rules_probs_ref
 from test_gpu_requests import Rules
 
 pytestmark = pytest.mark.gpu
@@ -46,3 +47,24 @@ def test_no_temperature_is_too_high_for_infinities(dtype, rows, V):
         want /= want.sum()
         # (z - max) / T of at most 6, in float32 with a factor of 2^-126 and less: 2^-20; a sum of V numbers
         assert (np.abs(p[t] - want) <= 1e-4 * want + 1e-37).all(), (t, np.abs(p[t] - want).max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(4, 700), (130, 700)])
+def test_tokens_that_were_never_there_have_no_penalty(dtype, rows, V):
+    """Penalties that are infinite, or no numbers, fall on what a request has had and on nothing else."""
+    inf, nan = float("inf"), float("nan")
+    c = Rules(52, dtype, [1] * rows, V, 0, 0, temps=(1.0,), path=False)
+    c.rules[:, 1:] = np.resize([[1, 0, inf], [1, inf, 0], [1, 0, nan], [1, 0.5, 0.25]], (rows, 3))
+    c.counts[:] = 0
+    c.counts[:, 20], c.counts[:, 21] = 3, 1 << 30
+    c.biases = [[(21, 1.5), (30, 2.0), (31, -1.0)] for _ in range(rows)]
+    z, p = c.run()
+    z, x = W.widen(z), W.widen(c.logits)
+    half = 2.0 ** -23 if dtype == "f32" else 2.0 ** -8  # one rounding of the sum, and one of the type
+    for token, more in ((21, 1.5), (30, 2.0), (31, -1.0), (40, 0.0)):
+        assert (np.abs(z[:, token] - x[:, token] - more) <= half * (np.abs(x[:, token]) + 2)).all(), token
+    for t in range(rows):
+        assert z[t, 20] == -inf if t % 4 < 3 else np.abs(z[t, 20] - (x[t, 20] - 1.25)) <= half * 10
+    want = rules_probs_ref(z, np.arange(rows + 1), c.rules)
+    assert dtype != "f32" or (np.abs(W.widen(p) - want) <= 1e-5 * want + 1e-37).all()
