@@ -667,6 +667,8 @@ size_t hb_kv4_evict_workspace_bytes(const hb_attn_desc *desc, int32_t budget);
  *   block_table  device int32 [B, max_blocks_per_seq]                    slots       device int32 [n_rows]
  *   free_pages   device int32 [num_blocks], free_count, free_left  device int32 [1]
  * slots, new_len and granted may be NULL.  Rows behind the last sequence and all other entries stay as they are.
+ * Offsets that fall, are negative or, where there are slots, lie beyond n_rows are those of a sequence that is not served and
+ * stands in nobody's way.  Without slots n_rows is not looked at.
  * hb_pages_give: the pages behind a sequence's first keep_len[b] positions go back: entries ceil(keep_len[b] / page_size) to
  * pages[b] - 1, the c-th of m in all to free_pages[free_count + m - 1 - c], so that giving what was just taken restores the
  * list; pages_out[b] = the pages it keeps, free_now = free_count + m.  keep_len 0: all of them.  block_table is not written.

@@ -672,7 +672,7 @@ def hb_pages_take(page_size: int, reserve: int, prefix_len, row_offset, pages, f
                   pages_out, granted, free_left, stream=None) -> None:
     """``block_table`` [B, max_blocks]; ``free_pages`` [num_blocks]; ``slots`` [n_rows], or None."""
     B, max_blocks = block_table.shape
-    n_rows = slots.numel() if slots is not None else 2 ** 31 - 1  # without slots, offsets are not bounded by them
+    n_rows = slots.numel() if slots is not None else 0
     _check(lib.hb_pages_take(B, page_size, max_blocks, free_pages.numel(), n_rows, reserve, _ints(prefix_len, B), _ints(row_offset, B + 1),
                              _ints(pages, B), _ints(free_pages, 0), _ints(free_count, 1), _ints(block_table, 0), _ints(slots, 0),
                              _ints(new_len, B), _ints(pages_out, B), _ints(granted, B), _ints(free_left, 1), _stream(stream)))

@@ -23,10 +23,11 @@ __device__ __forceinline__ Taken wanted(const PagesArgs &a, int b) {
   const int32_t len = a.len[b], have = a.have[b];
   t.len = len < 0 ? 0 : len > cap ? cap : len;
   t.have = have < 0 ? 0 : have > a.max_blocks ? a.max_blocks : have;
-  int64_t r0 = a.row_offset[b], r1 = a.row_offset[b + 1];
-  t.rows = r0 < 0 || r1 < r0 || r1 > a.n_rows ? 0 : r1 - r0;
+  const int64_t r0 = a.row_offset[b], r1 = a.row_offset[b + 1];
+  const bool there = r0 >= 0 && r1 >= r0 && (!a.slots || r1 <= a.n_rows);  // its rows have slots
+  t.rows = there ? r1 - r0 : 0;
   t.want = (t.len + t.rows + a.reserve + a.page - 1) / a.page;
-  t.fits = t.want <= a.max_blocks;
+  t.fits = there && t.want <= a.max_blocks;
   t.need = t.fits && t.want > t.have ? t.want - t.have : 0;
   return t;
 }
@@ -158,20 +159,21 @@ __global__ __launch_bounds__(256) void kv_append_kernel(int n, int Hkv, int page
   }
 }
 
-unsigned shares(const PagesArgs &a, int64_t items) {
-  const int64_t y = (items / (a.batch > 0 ? a.batch : 1) + 1023) / 1024;
+// workgroups of a sequence, of which each writes some thousand items
+unsigned shares(int64_t items) {
+  const int64_t y = (items + 1023) / 1024;
   return (unsigned)(y < 1 ? 1 : y > 64 ? 64 : y);
 }
 
 }  // namespace
 
 hipError_t launch_pages_take(const PagesArgs &a, hipStream_t s) {
-  pages_take_kernel<<<dim3(a.batch, shares(a, a.n_rows)), 256, 0, s>>>(a);
+  pages_take_kernel<<<dim3(a.batch, shares(a.slots ? a.n_rows / a.batch : a.max_blocks)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_give(const PagesArgs &a, hipStream_t s) {
-  pages_give_kernel<<<dim3(a.batch, shares(a, a.num_blocks)), 256, 0, s>>>(a);
+  pages_give_kernel<<<dim3(a.batch, shares(a.num_blocks / a.batch)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

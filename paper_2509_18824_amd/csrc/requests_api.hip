@@ -159,7 +159,7 @@ int32_t hb_pages_take(int32_t B, int32_t page_size, int32_t max_blocks_per_seq, 
       if ((rc = check_apart(names[i], out[i], {out[k]}))) return rc;
   }
   PagesArgs a = {B, page_size, max_blocks_per_seq, num_blocks, n_rows, reserve, prefix_len, row_offset, pages, free_pages, free_count,
-                 block_table, nullptr, n_rows ? slots : nullptr, new_len, pages_out, granted, free_left};
+                 block_table, nullptr, slots, new_len, pages_out, granted, free_left};
   HB_HIP_TRY(launch_pages_take(a, (hipStream_t)stream));
   return HB_OK;
 }

@@ -1,11 +1,13 @@
 """Pages and sampling rules on the GPU at the borders of what the calls take."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
 
 import workloads as W
-from oracle import rules_probs_ref
-from test_gpu_requests import Rules
+from oracle import pages_take_ref, rules_probs_ref
+from test_gpu_requests import Rules, _pages, _take
 
 pytestmark = pytest.mark.gpu
 i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
@@ -68,3 +70,54 @@ def test_tokens_that_were_never_there_have_no_penalty(dtype, rows, V):
         assert z[t, 20] == -inf if t % 4 < 3 else np.abs(z[t, 20] - (x[t, 20] - 1.25)) <= half * 10
     want = rules_probs_ref(z, np.arange(rows + 1), c.rules)
     assert dtype != "f32" or (np.abs(W.widen(p) - want) <= 1e-5 * want + 1e-37).all()
+
+
+def test_rows_that_the_slots_cannot_hold_are_not_served():
+    """Offsets beyond the rows, or falling: such a sequence keeps what it has, and bars nobody."""
+    import paper_2509_18824_amd as hb
+    lens, have, blocks = [5, 0, 17, 3], [1, 0, 2, 1], 30
+    table = np.full((4, 8), -1)
+    table[0, 0], table[2, :2], table[3, 0] = 20, [21, 22], 23
+    for offset, bad in (([0, 4, 4, 30, 33], (2, 3)), ([0, 20, 10, 12, 14], (1,)), ([-2, 3, 5, 7, 9], (0,))):
+        got = dict(table=i32(table), slots=i32([-2] * 25), new_len=i32([-9] * 4), have=i32([-9] * 4), granted=i32([-9] * 4), left=i32([-9]))
+        hb.hb_pages_take(16, 3, i32(lens), i32(offset), i32(have), i32(list(range(20)) + [-1] * 10), i32([20]), got["table"], got["slots"],
+                         got["new_len"], got["have"], got["granted"], got["left"])
+        rows = np.diff(offset)
+        for b in range(4):
+            if b in bad:
+                assert got["granted"][b] == 0 and got["new_len"][b] == lens[b] and got["have"][b] == have[b]
+                assert np.array_equal(got["table"][b].cpu().numpy(), table[b])
+            else:
+                assert got["granted"][b] == 1 and got["new_len"][b] == lens[b] + rows[b]
+                assert got["have"][b] == max(have[b], -(-(lens[b] + rows[b] + 3) // 16))
+                assert (got["slots"][offset[b]:offset[b + 1]] >= 0).all()
+        assert got["left"] == 20 - int((got["have"].cpu() - torch.tensor(have)).sum())
+
+
+def test_pages_without_slots_by_the_c_call():
+    """Without slots no number of rows bounds the offsets."""
+    import paper_2509_18824_amd as hb
+    c = _pages(3, 20, 16, 50, 60, 0, 2)
+    want = _take(c)
+    got = dict(table=i32(c["table"]), new_len=i32([-9] * 20), have=i32([-9] * 20), granted=i32([-9] * 20), left=i32([-9]))
+    lens, offset, have, free, count = i32(c["lens"]), i32(c["offset"]), i32(c["have"]), i32(c["free"]), i32([c["n_free"]])
+    at = lambda t: C.c_void_p(t.data_ptr())
+    stream = C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert hb.lib.hb_pages_take(20, 16, c["max_blocks"], c["blocks"], 0, 2, at(lens), at(offset), at(have), at(free), at(count), at(got["table"]), None,
+                                at(got["new_len"]), at(got["have"]), at(got["granted"]), at(got["left"]), stream) == 0
+    torch.cuda.synchronize()
+    for name in got:
+        assert torch.equal(got[name], want[name]), name
+
+
+def test_tables_of_many_entries_without_slots():
+    """A row of pages longer than a workgroup has threads, and several of them."""
+    import paper_2509_18824_amd as hb
+    B, page, n = 3, 1, 5000
+    blocks = B * n + 9
+    table, have, left = i32(np.full((B, n + 3), -1)), i32([0] * B), i32([0])
+    free = np.random.default_rng(5).permutation(blocks)
+    hb.hb_pages_take(page, 0, i32([0] * B), i32(np.arange(B + 1) * n), i32([0] * B), i32(free), i32([blocks]), table, None, None, have, None, left)
+    want, _, _, kept, _, rest = pages_take_ref(page, n + 3, blocks, 0, [0] * B, np.arange(B + 1) * n, [0] * B, free, np.full((B, n + 3), -1),
+                                               np.zeros(B * n, int))
+    assert np.array_equal(table.cpu().numpy(), want) and have.tolist() == kept.tolist() and left.tolist() == [rest]
