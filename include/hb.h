@@ -666,6 +666,8 @@ size_t hb_kv4_evict_workspace_bytes(const hb_attn_desc *desc, int32_t budget);
  *   prefix_len, pages, new_len, pages_out, granted  device int32 [B]     row_offset  device int32 [B+1]
  *   block_table  device int32 [B, max_blocks_per_seq]                    slots       device int32 [n_rows]
  *   free_pages   device int32 [num_blocks], free_count, free_left  device int32 [1]
+ * A negative prefix_len is an empty place of the batch: nobody is there to be served (granted 0), and nobody waits for it.  (A length of
+ * 0 is a request's that has no positions yet, and reserve asks pages for it.)
  * slots, new_len and granted may be NULL.  Rows behind the last sequence and all other entries stay as they are.
  * Offsets that fall, are negative or, where there are slots, lie beyond n_rows are those of a sequence that is not served and
  * stands in nobody's way.  Without slots n_rows is not looked at.

@@ -14,20 +14,20 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct Taken {
-  int64_t len, rows, want, have, need;  // positions, new rows, pages wanted, pages there, pages to take
+  int64_t len, rows, want, have, need;  // positions (negative: an empty place), new rows, pages wanted, pages there, pages to take
   bool fits;
 };
 __device__ __forceinline__ Taken wanted(const PagesArgs &a, int b) {
   Taken t;
   const int64_t cap = (int64_t)a.max_blocks * a.page;
   const int32_t len = a.len[b], have = a.have[b];
-  t.len = len < 0 ? 0 : len > cap ? cap : len;
+  t.len = len > cap ? cap : len;
   t.have = have < 0 ? 0 : have > a.max_blocks ? a.max_blocks : have;
   const int64_t r0 = a.row_offset[b], r1 = a.row_offset[b + 1];
-  const bool there = r0 >= 0 && r1 >= r0 && (!a.slots || r1 <= a.n_rows);  // its rows have slots
-  t.rows = there ? r1 - r0 : 0;
+  const bool hold = r0 >= 0 && r1 >= r0 && (!a.slots || r1 <= a.n_rows);  // the slots hold its rows
+  t.rows = hold ? r1 - r0 : 0;
   t.want = (t.len + t.rows + a.reserve + a.page - 1) / a.page;
-  t.fits = there && t.want <= a.max_blocks;
+  t.fits = hold && len >= 0 && t.want <= a.max_blocks;
   t.need = t.fits && t.want > t.have ? t.want - t.have : 0;
   return t;
 }

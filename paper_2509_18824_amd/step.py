@@ -242,8 +242,10 @@ class PagePool:
     ``take`` gives pages to sequences that get ``row_offset[b+1] - row_offset[b]`` new positions (and ``reserve`` more, for a tree's
     accepted nodes) and says where the new rows go; ``length`` is advanced by ``advance``, when they are there.  A sequence that is not
     ``granted`` keeps its length, and its rows' slots are -1, which the append passes over.  ``give`` takes back what is behind
-    ``keep_len`` positions (all: 0); a sequence that ends has ``length`` set to 0 as well.  Nothing is synchronised or allocated, so a HIP
-    graph can hold it all."""
+    ``keep_len`` positions (all: 0).  A sequence that ends has ``length`` set to -1 as well, an empty place, which takes no pages (0 is a
+    sequence that has no positions yet: it is given those that ``reserve`` asks for); the next request there begins with 0.  A verification
+    step's ``new_len`` is 0 for an empty place, which has to stay one.  Nothing is synchronised or allocated, so a HIP graph can hold it
+    all."""
 
     def __init__(self, B: int, page: int, max_blocks: int, num_blocks: int, max_rows: int, reserve: int = 0, device="cuda"):
         i32 = lambda n, value=0: torch.full((n,), value, dtype=torch.int32, device=device)

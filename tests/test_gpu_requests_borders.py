@@ -121,3 +121,54 @@ def test_tables_of_many_entries_without_slots():
     want, _, _, kept, _, rest = pages_take_ref(page, n + 3, blocks, 0, [0] * B, np.arange(B + 1) * n, [0] * B, free, np.full((B, n + 3), -1),
                                                np.zeros(B * n, int))
     assert np.array_equal(table.cpu().numpy(), want) and have.tolist() == kept.tolist() and left.tolist() == [rest]
+
+
+@pytest.mark.parametrize("short", [False, True])
+def test_empty_places_take_no_pages(short):
+    """A negative length: nobody is there, nothing is reserved, and nobody behind waits for it."""
+    import paper_2509_18824_amd as hb
+    B, page, reserve, max_blocks, blocks = 6, 16, 8, 5, 40
+    lens, rows, have = np.array([-1, 20, -1, 0, -7, 3]), np.array([0, 5, 0, 30, 4, 2]), np.array([0, 2, 1, 0, 0, 1])
+    offset = np.concatenate([[0], np.cumsum(rows)])
+    table = np.full((B, max_blocks), -1)
+    table[1, :2], table[2, 0], table[5, 0] = [30, 31], 32, 33
+    there = lens >= 0
+    free = list(range(3 if short else 20))
+    got = dict(table=i32(table), slots=i32([-2] * int(offset[-1])), new_len=i32([-9] * B), have=i32([-9] * B), granted=i32([-9] * B), left=i32([-9]))
+    hb.hb_pages_take(page, reserve, i32(lens), i32(offset), i32(have), i32(free + [-1] * (blocks - len(free))), i32([len(free)]), got["table"], got["slots"],
+                     got["new_len"], got["have"], got["granted"], got["left"])
+    # as if they were not in the batch
+    want_table, want_slots = table.copy(), np.full(offset[-1], -1)
+    packed = np.concatenate([[0], np.cumsum(rows[there])])
+    t, s, n, h, g, left = pages_take_ref(page, max_blocks, blocks, reserve, lens[there], packed, have[there], free, table[there], np.full(packed[-1], -2))
+    want_table[there] = t
+    want_slots[np.repeat(there, rows)] = s
+    assert np.array_equal(got["table"].cpu().numpy(), want_table) and np.array_equal(got["slots"].cpu().numpy(), want_slots)
+    for name, x, empty in (("new_len", n, lens), ("have", h, have), ("granted", g, 0 * lens)):
+        want = np.array(empty)
+        want[there] = x
+        assert got[name].tolist() == want.tolist(), name
+    assert got["left"].tolist() == [left]
+
+
+def test_a_place_that_a_request_has_left():
+    """Its pages are the others' until somebody comes, also where pages run short."""
+    import paper_2509_18824_amd.step as S
+    pages = S.PagePool(3, 16, 6, 7, 64, reserve=8)
+    step = lambda *rows: (pages.take(i32(np.concatenate([[0], np.cumsum(rows)]))), pages.advance())
+    step(30, 20, 1)
+    assert pages.pages.tolist() == [3, 2, 1] and pages.free_count.tolist() == [1]
+    pages.length[0] = -1
+    pages.give(pages.length)
+    for _ in range(2):
+        step(0, 1, 1)
+        assert pages.pages.tolist() == [0, 2, 1] and pages.free_count.tolist() == [4] and pages.length[0] == -1
+    step(0, 60, 1)
+    assert pages.granted.tolist() == [0, 1, 1] and pages.pages.tolist() == [0, 6, 1] and pages.free_count.tolist() == [0]
+    step(0, 0, 12)  # no page is left: the last one waits for those of sequence 1, not for the empty place
+    assert pages.granted.tolist() == [0, 1, 0] and pages.length.tolist() == [-1, 82, 4]
+    pages.length[1] = -1
+    pages.give(pages.length)
+    pages.length[0] = 0
+    step(40, 0, 12)
+    assert pages.granted.tolist() == [1, 0, 1] and pages.length.tolist() == [40, -1, 16] and pages.pages.tolist() == [3, 0, 2]
