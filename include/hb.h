@@ -691,7 +691,8 @@ int32_t hb_pages_give(int32_t B, int32_t page_size, int32_t max_blocks_per_seq, 
  * Rows of K and V (a prompt's, or any) bit for bit to their slots: row r to pool[slots[r] / page_size][:][slots[r] % page_size][:].
  * A slot outside [0, num_blocks * page_size) has no place and its row is skipped.  Rows with a place have one each: with the same
  * slot twice, every 16 bytes of it are one of the two rows'.
- *   k_rows, v_rows  device [n_rows, Hkv, D]     slots  device int32 [n_rows]     pools as in hb_tree_verify_attn
+ *   k_rows, v_rows  device [n_rows, Hkv, D]     slots  device int32 [n_rows]     pools as in hb_tree_verify_attn, which overlap
+ *                                                                                neither each other nor what is read
  * Uses desc->{dtype, num_kv_heads, head_dim, page_size, num_blocks}.  Errors: INVALID_ARG, UNSUPPORTED, DEVICE.
  */
 int32_t hb_kv_append(const hb_attn_desc *desc, int32_t n_rows, const void *k_rows, const void *v_rows, const int32_t *slots, void *k_pool,
@@ -711,7 +712,7 @@ int32_t hb_kv_append(const hb_attn_desc *desc, int32_t n_rows, const void *k_row
  * Finite values with finite scores have a finite result, up to the type's largest.
  * Accumulation is float32; on the matrix cores in bf16 a softmax weight is rounded to bf16 (by 2^-8 of itself at most) for its
  * product with a value and for the sum that results are divided by, not for lse.  bf16 results are rounded once at the end.
- * out, lse and workspace overlap neither each other nor what is read.
+ * out, lse and workspace overlap neither each other nor what is read, the whole pools among it.
  * Errors: INVALID_ARG, UNSUPPORTED (dtype, D; total_nodes * Hq beyond 2^30; HB_ATTN_MFMA on a shape it cannot take),
  * WORKSPACE, DEVICE.  batch == 0 or total_nodes == 0 is a successful no-op.
  */
@@ -746,7 +747,7 @@ size_t hb_prompt_attn_workspace_bytes(const hb_attn_desc *desc);
  *   mask_row     device int32 [T]: the mask of each row, outside [0, num_masks): none; or NULL: row t's is mask t
  *   workspace    device, hb_rules_probs_workspace_bytes(T, V) bytes, 16-byte aligned, overwritten; may be NULL when that is 0
  *   tokens       device int32 [n]; row_offset device int32 [B+1], or NULL: n / B of every sequence (out_tokens [B, max_path])
- * logits, out, probs, counts, rules and mask are 16-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED (dtype,
+ * logits, out, probs, counts, rules and mask are 16-byte aligned; what a call writes overlaps nothing else of it, but out logits.  Errors: INVALID_ARG, UNSUPPORTED (dtype,
  * max_nodes_per_tree > 64, V > 2^30), WORKSPACE, DEVICE.  T == 0 or B == 0 is a no-op.
  */
 int32_t hb_rules_count(int32_t B, int32_t V, int32_t n, const int32_t *row_offset_or_null, const int32_t *tokens, int32_t prompt,

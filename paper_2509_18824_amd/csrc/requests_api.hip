@@ -15,7 +15,13 @@ struct Span {
   const void *at;
   int64_t bytes;
 };
-static int32_t check_apart(const char *name, Span out, std::initializer_list<Span> in) {
+// a pool's bytes, and no more than an address space has
+static int64_t pool_bytes(const hb_attn_desc &d) {
+  const double n = (double)d.num_blocks * d.page_size * d.num_kv_heads * d.head_dim * (d.dtype == HB_F32 ? 4 : 2);
+  return n < 1e18 ? (int64_t)n : (int64_t)1e18;
+}
+template <typename List = std::initializer_list<Span>>
+static int32_t check_apart(const char *name, Span out, const List &in) {
   for (const Span &x : in) {
     const uintptr_t o = (uintptr_t)out.at, i = (uintptr_t)x.at;
     if (o && i && out.bytes > 0 && x.bytes > 0 && o < i + (uint64_t)x.bytes && i < o + (uint64_t)out.bytes)
@@ -108,6 +114,14 @@ struct RulesCall {
   const int32_t *mask_row;
 };
 
+// What a call with sampling rules writes, apart from what it reads beside the logits
+static int32_t check_rules_apart(const char *name, Span out, int32_t B, int32_t T, int32_t V, const RulesCall &r) {
+  const int64_t b = B, t = T, n = r.n_bias, words = ((int64_t)V + 31) / 32;
+  return check_apart(name, out, {{r.node_offset, 4 * b + 4}, {r.parent, 4 * t}, {r.draft_ids, 4 * t}, {r.counts, 4 * b * V}, {r.rules, 16 * b},
+                                 {n ? r.bias_offset : nullptr, 4 * b + 4}, {r.bias_id, 4 * n}, {r.bias_value, 4 * n},
+                                 {r.mask, 4 * words * r.num_masks}, {r.mask_row, 4 * t}});
+}
+
 static int32_t check_rules(int32_t dtype, int32_t B, int32_t max_nodes, int32_t T, int32_t V, const void *logits, const RulesCall &r,
                            const void *out, RulesArgs *a) {
   if (dtype != HB_F32 && dtype != HB_BF16) return fail(HB_ERR_UNSUPPORTED, "dtype %d: only HB_F32 and HB_BF16 are supported", dtype);
@@ -197,6 +211,9 @@ int32_t hb_kv_append(const hb_attn_desc *desc, int32_t n_rows, const void *k_row
   if (!k_rows || !v_rows || !slots || !k_pool || !v_pool) return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
   if (misaligned(k_rows, 16) || misaligned(v_rows, 16) || misaligned(k_pool, 16) || misaligned(v_pool, 16))
     return fail(HB_ERR_INVALID_ARG, "rows and pools must be 16-byte aligned");
+  const int64_t bytes = (int64_t)n_rows * desc->num_kv_heads * desc->head_dim * (desc->dtype == HB_F32 ? 4 : 2);
+  const Span k = {k_pool, pool_bytes(*desc)}, v = {v_pool, k.bytes}, kr = {k_rows, bytes}, vr = {v_rows, bytes}, s = {slots, (int64_t)n_rows * 4};
+  if ((rc = check_apart("k_pool", k, {v, kr, vr, s})) || (rc = check_apart("v_pool", v, {kr, vr, s}))) return rc;
   HB_HIP_TRY(launch_kv_append(*desc, n_rows, k_rows, v_rows, slots, k_pool, v_pool, (hipStream_t)stream));
   return HB_OK;
 }
@@ -229,6 +246,12 @@ int32_t hb_prompt_attn(const hb_attn_desc *desc, const void *q, const void *k_ro
     if (misaligned(workspace, 256)) return fail(HB_ERR_WORKSPACE, "workspace must be 256-byte aligned");
     if ((rc = check_apart("workspace", {workspace, (int64_t)p.bytes}, {in[0], in[1], in[2], o, l}))) return rc;
   }
+  const int64_t B = desc->batch, pool = prefix_len ? pool_bytes(*desc) : 0;
+  const Span cache[] = {{k_pool, pool}, {v_pool, pool}, {block_table, prefix_len ? B * desc->max_blocks_per_seq * 4 : 0}, {prefix_len, 4 * B},
+                        {row_offset, 4 * B + 4}};
+  if ((rc = check_apart("out", o, cache)) || (rc = check_apart("lse", l, cache)) ||
+      (p.bytes && (rc = check_apart("workspace", {workspace, (int64_t)p.bytes}, cache))))
+    return rc;
   PromptArgs a = {*desc, q, k_rows, v_rows, k_pool, v_pool, block_table, prefix_len, row_offset, out, lse,
                   p.bytes ? (float *)workspace : nullptr, p.bytes ? (float *)((char *)workspace + p.ml_offset) : nullptr,
                   p.bytes ? (PromptArgs::Head *)((char *)workspace + p.heads_offset) : nullptr, p.tiles, p.parts, p.units};
@@ -246,6 +269,8 @@ int32_t hb_rules_count(int32_t B, int32_t V, int32_t n, const int32_t *row_offse
   if (B == 0 || n == 0) return HB_OK;
   if (!tokens || !counts) return fail(HB_ERR_INVALID_ARG, "a required device pointer is NULL");
   if (!row_offset && n % B) return fail(HB_ERR_INVALID_ARG, "without row_offset every sequence has as many tokens: %d of %d", n, B);
+  int32_t rc;
+  if ((rc = check_apart("counts", {counts, (int64_t)B * V * 4}, {{tokens, (int64_t)n * 4}, {row_offset, (int64_t)B * 4 + 4}}))) return rc;
   HB_HIP_TRY(launch_rules_count(B, V, n, row_offset, tokens, prompt, counts, (hipStream_t)stream));
   return HB_OK;
 }
@@ -255,12 +280,12 @@ int32_t hb_rules_logits(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, in
                         const float *rules, const int32_t *bias_offset, int32_t n_bias, const int32_t *bias_id, const float *bias_value,
                         int32_t num_masks, const uint32_t *mask, const int32_t *mask_row, void *out, void *stream) {
   RulesArgs a;
-  int32_t rc = check_rules(dtype, B, max_nodes_per_tree, T, V, logits,
-                           {node_offset, parent, draft_ids, counts, rules, bias_offset, n_bias, bias_id, bias_value, num_masks, mask, mask_row},
-                           out, &a);
+  const RulesCall r = {node_offset, parent, draft_ids, counts, rules, bias_offset, n_bias, bias_id, bias_value, num_masks, mask, mask_row};
+  int32_t rc = check_rules(dtype, B, max_nodes_per_tree, T, V, logits, r, out, &a);
   if (rc || T == 0 || B == 0) return rc;
   const int64_t bytes = (int64_t)T * V * (dtype == HB_F32 ? 4 : 2);
   if (out != logits && (rc = check_apart("out", {out, bytes}, {{logits, bytes}}))) return rc;
+  if ((rc = check_rules_apart("out", {out, bytes}, B, T, V, r))) return rc;
   HB_HIP_TRY(launch_rules_logits(a, (hipStream_t)stream));
   return HB_OK;
 }
@@ -279,9 +304,8 @@ int32_t hb_rules_probs(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, int
                        int32_t num_masks, const uint32_t *mask, const int32_t *mask_row, float *probs, void *workspace,
                        size_t workspace_bytes, void *stream) {
   RulesArgs a;
-  int32_t rc = check_rules(dtype, B, max_nodes_per_tree, T, V, logits,
-                           {node_offset, parent, draft_ids, counts, rules, bias_offset, n_bias, bias_id, bias_value, num_masks, mask, mask_row},
-                           probs, &a);
+  const RulesCall r = {node_offset, parent, draft_ids, counts, rules, bias_offset, n_bias, bias_id, bias_value, num_masks, mask, mask_row};
+  int32_t rc = check_rules(dtype, B, max_nodes_per_tree, T, V, logits, r, probs, &a);
   if (rc || T == 0 || B == 0) return rc;
   const size_t need = hb_rules_probs_workspace_bytes(T, V);
   if (need && (!workspace || workspace_bytes < need))
@@ -290,6 +314,8 @@ int32_t hb_rules_probs(int32_t dtype, int32_t B, int32_t max_nodes_per_tree, int
   const int64_t el = dtype == HB_F32 ? 4 : 2;
   const Span in = {logits, (int64_t)T * V * el}, o = {probs, (int64_t)T * V * 4};
   if ((rc = check_apart("probs", o, {in})) || (need && (rc = check_apart("workspace", {workspace, (int64_t)need}, {in, o})))) return rc;
+  if ((rc = check_rules_apart("probs", o, B, T, V, r)) || (need && (rc = check_rules_apart("workspace", {workspace, (int64_t)need}, B, T, V, r))))
+    return rc;
   int32_t chunk;
   if (rules_parts(T, V, &chunk))
     a.stats = (float *)workspace;
