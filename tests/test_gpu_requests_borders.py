@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import workloads as W
-from oracle import pages_take_ref, rules_probs_ref
+from oracle import pages_take_ref, rules_probs_ref, tree_accept_sample_ref
 from test_gpu_requests import Rules, _pages, _take
 
 pytestmark = pytest.mark.gpu
@@ -71,6 +71,8 @@ def test_tokens_that_were_never_there_have_no_penalty(dtype, rows, V):
     want = rules_probs_ref(z, np.arange(rows + 1), c.rules)
     assert dtype != "f32" or (np.abs(W.widen(p) - want) <= 1e-5 * want + 1e-37).all()
 
+
+# ---- pages ------------------------------------------------------------------------------------------
 
 def test_rows_that_the_slots_cannot_hold_are_not_served():
     """Offsets beyond the rows, or falling: such a sequence keeps what it has, and bars nobody."""
@@ -172,3 +174,65 @@ def test_a_place_that_a_request_has_left():
     pages.length[0] = 0
     step(40, 0, 12)
     assert pages.granted.tolist() == [1, 0, 1] and pages.length.tolist() == [40, -1, 16] and pages.pages.tolist() == [3, 0, 2]
+
+
+# ---- in place ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nodes,V,biases,masks", [([8], 1000, 3, 5), ([60, 0, 1], 1001, 40, 9), ([3, 2], 33, 5, 2), ([5, 9], 40000, 1500, 3),
+                                                  ([1, 1], 100003, 7, 1), ([1] * 130, 4001, 3, 5), ([7], 9000, 900, 0)])
+def test_rules_in_place(dtype, nodes, V, biases, masks):
+    """Logits over themselves, with counts, paths, biases and masks: the bits of the call beside it."""
+    import paper_2509_18824_amd as hb
+    c = Rules(61 + V, dtype, nodes, V, biases, masks)
+    c.logits[0, ::3] = float("nan")
+    c.counts[:, :40] = 1
+    z, _ = c.run()
+    x = c.logits.cuda()
+    hb.hb_rules_logits(x, max(nodes), *c.args(), x)
+    assert torch.equal(x.view(torch.int32 if dtype == "f32" else torch.int16), z.view(torch.int32 if dtype == "f32" else torch.int16))
+
+
+# ---- a sampled step ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("seed", range(4))
+def test_every_token_of_a_sampled_step(seed):
+    """Drafts drawn from what the target thinks, so that many are accepted; a sequence whose grammar leaves nothing.  Acceptance is in exact
+    integers: of the step's own probabilities the oracle makes the same paths, tokens and last tokens, and these are counted."""
+    import paper_2509_18824_amd.step as S
+    from test_gpu_request_steps import _sampled
+    inp, step, rng, vocab = _sampled(S, 70 + seed)
+    off, parent = inp.node_offset.numpy(), inp.parent.numpy()
+    r = step.rules
+    r.mask[4].zero_()
+    r.mask_row[off[1]:off[2]] = 4
+    r.rules[:, 0] = torch.tensor(np.resize([1.5, 0.0, 2.5], inp.B), dtype=torch.float32)
+    had = r.counts.clone()
+    pools = [p.clone() for p in (step.dev.k_pool, step.dev.v_pool)]
+    step.run()
+    p = step.probs.double().cpu().numpy()
+    draft = step.draft_ids.cpu().numpy().copy()
+    q = np.full((inp.total_nodes, vocab), 1.0 / vocab)
+    for b in range(inp.B):
+        for n in range(off[b], off[b + 1]):
+            q[n] = 0.9 * p[n] / max(p[n].sum(), 1e-30) + 0.1 / vocab
+            if n > off[b]:
+                draft[n] = rng.choice(vocab, p=q[off[b] + parent[n]] / q[off[b] + parent[n]].sum())
+    step.draft_ids.copy_(torch.from_numpy(draft))
+    step.q_draft.copy_(torch.from_numpy(q.astype(np.float32)))
+    r.counts.copy_(had)
+    step.dev.k_pool.copy_(pools[0])
+    step.dev.v_pool.copy_(pools[1])
+    step.run()
+    got = step.probs.cpu().numpy()
+    u = lambda t: t.cpu().numpy().view(np.uint32)
+    want = tree_accept_sample_ref(off, parent, draft, got, step.q_draft.cpu().numpy(), u(step.u_accept), u(step.u_bonus), inp.max_path)
+    for name, x in zip(("accept_len", "accept_path", "out_tokens", "bonus"), want):
+        assert np.array_equal(getattr(step, name).cpu().numpy(), x), name
+    alen, _, tokens, bonus = want
+    assert alen.max() >= 3 and alen[1] == 1 and bonus[1] == -1 and not got[off[1]:off[2]].any()
+    for b in range(inp.B):
+        assert tokens[b, alen[b] - 1] == bonus[b]  # -1 where a mask has left nothing
+        for t in tokens[b][tokens[b] >= 0]:
+            had[b, t] += 1
+    assert torch.equal(had, r.counts)
