@@ -732,7 +732,7 @@ size_t hb_prompt_attn_workspace_bytes(const hb_attn_desc *desc);
  * hb_rules_logits: out = z, in the type of the logits (which out may be, all of it, and must not overlap otherwise).
  * hb_rules_probs:  probs = exp((z - max z) / temperature) / sum, what hb_tree_accept_sample takes; temperature 0 (or less, or
  *   no number): 1 at the largest z, the lowest token among equals, which makes that call's rule the greedy one.  Infinite z
- *   share the whole.  A row that the rules leave nothing of is zero.
+ *   share the whole.  A row that the rules leave nothing of is zero.  Top-k, top-p and min-p are not among the rules.
  * hb_rules_count: tokens into counts: each adds 1 to its sequence's entry, or with prompt = 1 marks it as one of the prompt's
  *   (2^30).  Tokens outside [0, V) are skipped, so out_tokens of an acceptance is counted as it is.
  *

@@ -569,8 +569,10 @@ class PromptLayerStack:
     """Buffers and call chain that take prompts, whole or in parts, through ``n_layers`` decoder layers (those of
     ``VerifyLayerStack``, with the same weights): pages for the new rows, then in each layer the rows' attention over what the cache
     holds and over each other, and their append; at the end each sequence's last row through the LM head.  ``first_ids[b]`` is the token
-    that follows the rows (-1: sequence b had none, or no pages).  ``desc`` is a batch of at most ``desc.total_nodes`` rows; ``row_offset`` may say
-    fewer.  Pools and pages are those that the verification steps go on with.  ``run`` only enqueues kernels."""
+    that follows the rows by the largest logit, whatever rules the request has (-1: sequence b had none, or no pages); with rules, its
+    row of ``final_hidden`` goes through the LM head's projection and ``rules_probs`` instead.  ``desc`` is a batch of at most
+    ``desc.total_nodes`` rows; ``row_offset`` may say fewer.  Pools and pages are those that the verification steps go on with.  ``run`` only
+    enqueues kernels."""
 
     def __init__(self, desc: hb.AttnDesc, pages: PagePool, pools, w_qkv, w_o, lm_weight, row_offset, hidden0: torch.Tensor,
                  theta: float = 1e6, mlp=None):

@@ -89,7 +89,8 @@ def test_small_scores_behind_a_block_of_none(dtype, low):
     _along_one_dimension(c, [max(s, -1e30) for s in scores])
     c.k[:30, :, 0], c.k_pool[:, :, :, 0] = -torch.inf, -torch.inf
     c.k[:30, :, 1:], c.q[:, :, 1:] = 0, 0
-    ref, ref_lse = c.reference()
+    with np.errstate(invalid="ignore", divide="ignore"):  # rows that see no other score have no result
+        ref, ref_lse = c.reference()
     seen = np.arange(160) >= 30
     # scores are exact; the argument of an exponential is one of (score - reference), off by 2^-17 of scores of up to 128 in float32
     tol = (2.0 ** -14 if dtype == "f32" else 2.0 ** -7) * (np.abs(ref[seen]).max() + 4)
